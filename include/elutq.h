@@ -385,6 +385,53 @@ int elutq_hlq_fit(const void* W, int q, int G, int N, int K, int t_max, uint8_t*
                   void* offsets, double* err_trace, void* stream);
 
 /*
+ * Microscaled 4-bit floating point, the 4-bit format that the tensor cores multiply natively (no counterpart in the
+ * paper: for the layers of a model that are kept at 4 bits beside HLQ ones, and for mixtures of experts).
+ *
+ * A matrix [rows][K] is stored as
+ *   codes   uint8 [rows][K/2]: E2M1 values 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign bit, two to a byte, the even column in
+ *           the low half
+ *   scales  uint8 [rows][K/B], one per B consecutive columns:
+ *           ELUTQ_MX4_MXFP4  B = 32, E8M0: 2^(byte - 127), 255 = NaN
+ *           ELUTQ_MX4_NVFP4  B = 16, E4M3 without a sign, 127 = NaN; one fp32 factor for the whole matrix on top, which the
+ *                            caller keeps (prescale when quantising, alpha afterwards)
+ * both dense and row-major, K a multiple of 32, any number of rows.  `codes` must be 16-byte aligned.  All pointers are
+ * device memory; nothing is allocated, nothing is synchronised, every call can be captured into a graph.
+ */
+#define ELUTQ_MX4_MXFP4 0
+#define ELUTQ_MX4_NVFP4 1
+
+#define ELUTQ_TYPE_F16  0
+#define ELUTQ_TYPE_BF16 1
+#define ELUTQ_TYPE_F32  2
+
+#define ELUTQ_MX4_FLAG_SWIGLU 0x1u /* a row of X holds 2 K values [g | u]; silu(g) * u, formed in fp32, is quantised */
+
+/* Sizes in bytes of the codes and the scales of a matrix.  Pure function, no CUDA call. */
+int elutq_mx4_bytes(int format, int rows, int K, size_t* code_bytes, size_t* scale_bytes);
+
+/*
+ * Dense values to codes and scales.
+ *   X         device, x_rows rows that start `ld` elements apart (ld >= K, 2 K with the SwiGLU flag), elements of x_type
+ *             (ELUTQ_TYPE_); 16-byte aligned, ld a multiple of 16 bytes
+ *   prescale  NULL, or device float [1]: values are multiplied by it (in fp32) first
+ *   index     NULL: row r of the result is row r of X.  Otherwise device int [rows]: row index[r] / index_div of X (rows
+ *             sorted by expert from (token, choice) pairs); an index outside [0, x_rows * index_div) gives a row of zeros
+ *   n_rows    NULL, or device int [1]: rows from *n_rows on are left as they were
+ *   codes, scales  written
+ * A block's scale: with amax its largest magnitude, MXFP4 2^(floor(log2 amax) - 2), at least 2^-127; NVFP4 E4M3 of
+ * amax / 6 (rounded to fp32, then to the nearest E4M3 value, 448 at most).  A code is the E2M1 value nearest to the exact value / scale,
+ * ties to the even code, 6 at most.  A block that holds an infinity or a NaN gets the scale NaN and codes 0.
+ */
+int elutq_mx4_quantize(const void* X, int x_type, int x_rows, long long ld, int rows, int K, int format, unsigned flags,
+                       const float* prescale, const int* index, int index_div, const int* n_rows, void* codes, void* scales,
+                       void* stream);
+
+/* Y[rows][K] (y_type, dense, 16-byte aligned) = alpha * code * scale.  alpha: NULL (1), or device float [1]. */
+int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K, int format, const float* alpha, void* Y,
+                         int y_type, void* stream);
+
+/*
  * Device-side status of the library-owned scratch of `stream` (synchronises the stream).
  * *status is 0 unless a kernel gave up on a bounded wait (then a non-zero code that stays set
  * until elutq_release_scratch).  Kernels never spin without a limit.  While it is set, the finalize kernels

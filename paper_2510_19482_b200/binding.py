@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_int, c_size_t, c_uint, c_ulonglong, c_void_p
+from ctypes import c_char_p, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -22,6 +22,10 @@ FLAG_TABLE_I8 = 0x200
 
 # elutq_gemm_kernel
 KERNEL_DECODE, KERNEL_LOOK_UP, KERNEL_FRAGMENT, KERNEL_TENSOR_MEMORY, KERNEL_SHARED_MEMORY = range(5)
+
+MX4_MXFP4, MX4_NVFP4 = 0, 1
+MX4_FLAG_SWIGLU = 0x1
+TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
 
 
 class GemvCall(ctypes.Structure):
@@ -60,6 +64,9 @@ _SIGNATURES = {
     "elutq_takes_tensor_path": (c_int, [c_int, c_int, c_int, c_int, c_uint]),
     "elutq_gemm_kernel": (c_int, [c_int, c_int, c_int, c_int, c_int, c_uint]),
     "elutq_hlq_fit": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "elutq_mx4_bytes": (c_int, [c_int, c_int, c_int, ctypes.POINTER(c_size_t), ctypes.POINTER(c_size_t)]),
+    "elutq_mx4_quantize": (c_int, [c_void_p, c_int, c_int, c_longlong, c_int, c_int, c_int, c_uint, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "elutq_mx4_dequantize": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p]),
     "elutq_chain_plan_bytes": (c_int, [ctypes.POINTER(GemvCall), c_int, ctypes.POINTER(c_size_t)]),
     "elutq_chain_plan": (c_int, [ctypes.POINTER(GemvCall), c_int, c_void_p, c_size_t, c_void_p]),
     "elutq_chain_run": (c_int, [c_void_p, c_int, c_void_p]),
@@ -233,6 +240,44 @@ def elutq_hlq_fit(W, q: int, G: int, t_max: int = 10, trace: bool = False, strea
     _check(lib().elutq_hlq_fit(_ptr(W), q, G, N, K, t_max, _ptr(planes), _ptr(scales), _ptr(offsets),
                                _ptr(tr) if trace else None, _stream(stream)), "elutq_hlq_fit")
     return (planes, scales, offsets, tr) if trace else (planes, scales, offsets)
+
+
+_TYPES = None
+
+
+def _type(t) -> int:
+    """ELUTQ_TYPE_ of a tensor (-1: none, which the library refuses)."""
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_F32}
+    return _TYPES.get(t.dtype, -1)
+
+
+def elutq_mx4_bytes(fmt: int, rows: int, K: int):
+    """(bytes of the codes, bytes of the scales) of a matrix."""
+    codes, scales = c_size_t(0), c_size_t(0)
+    _check(lib().elutq_mx4_bytes(fmt, rows, K, ctypes.byref(codes), ctypes.byref(scales)), "elutq_mx4_bytes")
+    return codes.value, scales.value
+
+
+def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, flags: int = 0, prescale=None, index=None, index_div: int = 1,
+                       n_rows=None, stream=None):
+    """X fp16, bf16 or fp32 [x_rows, K] (or [x_rows, 2 K], SwiGLU), unit stride along a row -> (codes uint8 [rows, K/2], scales uint8 [rows, K/B])."""
+    import torch
+    if codes is None:
+        codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=X.device)
+    if scales is None:
+        scales = torch.empty((rows, K // (32 if fmt == MX4_MXFP4 else 16)), dtype=torch.uint8, device=X.device)
+    if X.dim() != 2 or X.stride(1) != 1:
+        raise ElutqError(-2, "elutq_mx4_quantize")
+    _check(lib().elutq_mx4_quantize(_ptr(X), _type(X), X.shape[0], X.stride(0), rows, K, fmt, flags, _ptr(prescale), _ptr(index), index_div,
+                                    _ptr(n_rows), _ptr(codes), _ptr(scales), _stream(stream)), "elutq_mx4_quantize")
+    return codes, scales
+
+
+def elutq_mx4_dequantize(codes, scales, Y, rows: int, K: int, fmt: int, alpha=None, stream=None) -> None:
+    _check(lib().elutq_mx4_dequantize(_ptr(codes), _ptr(scales), rows, K, fmt, _ptr(alpha), _ptr(Y), _type(Y), _stream(stream)), "elutq_mx4_dequantize")
 
 
 def elutq_device_status(stream=None) -> int:

@@ -1,0 +1,362 @@
+// Microscaled 4-bit floating point: dense values to codes and block scales, and back.
+//
+// A block is 32 (MXFP4) or 16 (NVFP4) consecutive columns of a row.  With amax its largest magnitude:
+//
+//   MXFP4   scale 2^e, e = floor(log2(amax)) - 2 (the exponent field of amax less that of 6), not below 2^-127.  Dividing by it
+//           is exact, so a code is one rounding of the value.  Values above 6 scales (amax / 2^e is below 8) become 6.
+//   NVFP4   scale E4M3(amax / 6), the quotient rounded to fp32 first; 448 at most, 0 where amax is below 6 * 2^-10 (all codes are 0 then)
+//   code    the E2M1 value nearest to value / scale, ties to the even code, 6 at most, with the value's sign
+//
+// NVFP4's quotient: a code has to be that of the exact value / scale, and a value half-way between two codes is common (a scale has
+// four significant bits, a half-way point three).  r = 1 / s rounded to nearest, q = y r and one correction by the remainder
+// y - q s (exact in a fused multiply-add) give the quotient rounded to nearest: a true tie is hit exactly, and
+// for 16-bit inputs nothing else rounds onto a half-way point (y and the point times s have at most 11 bits between them).  For
+// 24-bit values something can: by the remainder's sign the quotient is then rounded to odd (cut off, and the last bit set if anything
+// was left), which no half-way point is.
+//
+// Bound: HBM.  A thread takes 16 columns (one load of 32 bytes for 16-bit inputs, one block of NVFP4, half a block of MXFP4, whose
+// amax it shares with its neighbour) and stores 8 bytes of codes; 32 bytes a thread in flight are 64 KB an SM.
+#include <cuda_bf16.h>
+
+#include "mx4.cuh"
+
+namespace elutq {
+
+namespace {
+
+constexpr int kChunk = 16;                 // columns of a thread
+
+struct QuantArgs {
+    const void* X;
+    long long ld;              // elements between rows of X
+    const float* prescale;     // null: 1
+    const int* index;          // null: row r of X; otherwise row index[r] / div (none: zeros)
+    const int* n_rows;         // null: all
+    uint2* codes;
+    uint8_t* scales;
+    int row0, rows, K;         // this launch: rows [row0, row0 + rows)
+    long long x_rows;          // rows of X, times div
+    Div per_row, div;          // chunks of a row; the index's divisor
+    int wide;                  // rows of X start on 32 bytes
+};
+
+// 32 bytes at p, 32-byte aligned with WIDE and 16-byte aligned otherwise
+template <bool WIDE>
+__device__ __forceinline__ void load32(uint32_t (&v)[8], const void* p) {
+    if constexpr (WIDE) {
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
+    } else {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+}
+
+// 16 values as fp32
+template <int TYPE, bool WIDE>
+__device__ __forceinline__ void load_chunk(float (&y)[kChunk], const void* X, long long at) {
+    uint32_t v[8];
+    if constexpr (TYPE == ELUTQ_TYPE_F32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load32<WIDE>(v, reinterpret_cast<const float*>(X) + at + 8 * h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[8 * h + i] = __uint_as_float(v[i]);
+        }
+    } else {
+        load32<WIDE>(v, reinterpret_cast<const uint16_t*>(X) + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (TYPE == ELUTQ_TYPE_F16) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+                y[2 * i] = f.x;
+                y[2 * i + 1] = f.y;
+            } else {
+                y[2 * i] = __uint_as_float(v[i] << 16);
+                y[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+            }
+        }
+    }
+}
+
+// Eight values (already divided by their scale) as a word of codes, the first in the lowest bits
+__device__ __forceinline__ uint32_t codes_of(const float* v) {
+    uint32_t d;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return d;
+}
+__device__ __forceinline__ float e4m3_value(uint32_t byte) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)byte));
+    return __half2float(__ushort_as_half((uint16_t)h));
+}
+// FULL: values of up to 24 bits; otherwise of up to 11
+template <bool FULL>
+__device__ __forceinline__ float quotient(float y, float s, float r) {
+    float q = y * r;
+    q = fmaf(fmaf(-q, s, y), r, q);
+    if constexpr (FULL) {
+        const float rest = fmaf(-q, s, y);
+        const int below = (__float_as_int(rest) ^ __float_as_int(q)) < 0 ? 1 : 0;      // the exact quotient's magnitude is below |q|
+        if (rest != 0.0f && q != 0.0f) q = __int_as_float((__float_as_int(q) - below) | 1);
+    }
+    return copysignf(q, y);                    // (the correction makes +0 of -0)
+}
+
+template <int FMT, int TYPE, bool SWIGLU, bool WIDE>
+__device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int chunk) {
+    float y[kChunk];
+    long long src = row;
+    bool some = true;
+    if (a.index != nullptr) {
+        const int i = __ldg(a.index + row);
+        some = i >= 0 && i < a.x_rows;
+        src = some ? a.div.of(i) : 0;
+    }
+    if (some) {
+        const long long at = src * a.ld + (long long)chunk * kChunk;
+        load_chunk<TYPE, WIDE>(y, a.X, at);
+        if constexpr (SWIGLU) {
+            float u[kChunk];
+            load_chunk<TYPE, WIDE>(u, a.X, at + a.K);
+            // silu(g) u in fp32 (a few units in the last place)
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) y[i] = __fdividef(y[i], 1.0f + expf(-y[i])) * u[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) y[i] = 0.0f;
+    }
+    if (a.prescale != nullptr) {
+        const float p = __ldg(a.prescale);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) y[i] *= p;
+    }
+    // the largest magnitude as an integer: infinity and NaN are above every number
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const bool bad = top >= 0x7f800000u;
+
+    uint32_t byte;
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
+        const int e = max((int)(top >> 23) - 2, 0);
+        byte = bad ? 255u : (uint32_t)e;
+        const float f = __uint_as_float((uint32_t)(254 - min(e, 252)) << 23);            // 2^(127 - e)
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) y[i] *= f;
+    } else {
+        uint16_t two;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(__fdiv_rn(__uint_as_float(top), 6.0f)));
+        byte = bad ? 127u : (uint32_t)two & 0xffu;
+        const float s = e4m3_value(byte), r = byte == 0u ? 0.0f : __frcp_rn(s);
+        const bool full = TYPE == ELUTQ_TYPE_F32 || SWIGLU || a.prescale != nullptr;
+        if (full) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) y[i] = quotient<true>(y[i], s, r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) y[i] = quotient<false>(y[i], s, r);
+        }
+    }
+    uint2 codes = make_uint2(codes_of(y), codes_of(y + 8));
+    if (bad) codes = make_uint2(0u, 0u);
+    const long long at = (long long)row * a.per_row.d + chunk;
+    a.codes[at] = codes;
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
+        if ((chunk & 1) == 0) a.scales[at >> 1] = (uint8_t)byte;
+    } else {
+        a.scales[at] = (uint8_t)byte;
+    }
+}
+
+// A thread per chunk of 16 columns.  A row has an even number of chunks, so the two halves of a block of 32 are neighbouring lanes and
+// leave together.
+template <int FMT, int TYPE, bool SWIGLU>
+__global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantArgs a) {
+    const unsigned id = blockIdx.x * blockDim.x + threadIdx.x;
+    const int local = a.per_row.of((int)id), chunk = (int)id - local * a.per_row.d, row = a.row0 + local;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int limit = a.n_rows != nullptr ? min(__ldg(a.n_rows), a.row0 + a.rows) : a.row0 + a.rows;
+    const bool mine = row < limit;
+    if (!__any_sync(0xffffffffu, mine)) return;
+    // lanes without work run on the last row that has some (the shuffle wants whole warps): the same bytes are stored twice
+    const int r = mine ? row : limit - 1;
+    if (a.wide) quantise_chunk<FMT, TYPE, SWIGLU, true>(a, r, chunk);
+    else quantise_chunk<FMT, TYPE, SWIGLU, false>(a, r, chunk);
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_chunk(void* Y, long long at, const float (&v)[kChunk]) {
+    uint32_t w[TYPE == ELUTQ_TYPE_F32 ? 16 : 8];
+#pragma unroll
+    for (int i = 0; i < kChunk / 2; ++i) {
+        if constexpr (TYPE == ELUTQ_TYPE_F32) {
+            w[2 * i] = __float_as_uint(v[2 * i]);
+            w[2 * i + 1] = __float_as_uint(v[2 * i + 1]);
+        } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    constexpr int N4 = TYPE == ELUTQ_TYPE_F32 ? 4 : 2;
+    uint4* p = reinterpret_cast<uint4*>(Y) + at * N4;
+#pragma unroll
+    for (int i = 0; i < N4; ++i) p[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
+// value = alpha * code * scale: the product of code and scale is exact in fp32 (two and four significant bits), alpha's is
+// rounded to fp32 and the result once more to its type.
+template <int FMT, int TYPE>
+__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ alpha,
+                                                             void* Y, long long chunks) {
+    const long long at = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (at >= chunks) return;
+    const uint2 c = __ldg(codes + at);
+    const uint32_t byte = __ldg(scales + (FMT == ELUTQ_MX4_MXFP4 ? at >> 1 : at));
+    float s;
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) s = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+    else s = e4m3_value(byte);
+    const float f = alpha != nullptr ? __ldg(alpha) : 1.0f;
+    float v[kChunk];
+#pragma unroll
+    for (int i = 0; i < kChunk / 2; ++i) {
+        const uint32_t b = ((i < 4 ? c.x : c.y) >> (8 * (i & 3))) & 0xffu;
+        uint32_t h;
+        asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "h"((uint16_t)b));
+        const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        v[2 * i] = two.x * s * f;
+        v[2 * i + 1] = two.y * s * f;
+    }
+    store_chunk<TYPE>(Y, at, v);
+}
+
+// Few chunks: small blocks, so that more SMs have some.  (8 x 4096: 32 blocks of 64 instead of 8 of 256.)
+inline unsigned threads_for(long long chunks, int num_sms) { return chunks < 256LL * num_sms ? 64u : 256u; }
+
+template <class K, class... A>
+int launch(K kernel, long long chunks, cudaStream_t stream, const A&... args) {
+    const unsigned threads = threads_for(chunks, device_sm_count());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((chunks + threads - 1) / threads));
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e == cudaSuccess) count_launch(1);
+    return (int)e;
+}
+
+template <int FMT, int TYPE>
+int launch_quantize(const QuantArgs& a, long long chunks, bool swiglu, cudaStream_t stream) {
+    return swiglu ? launch(mx4_quantize_kernel<FMT, TYPE, true>, chunks, stream, a) : launch(mx4_quantize_kernel<FMT, TYPE, false>, chunks, stream, a);
+}
+
+}  // namespace
+
+}  // namespace elutq
+
+using namespace elutq;
+
+extern "C" int elutq_mx4_bytes(int format, int rows, int K, size_t* code_bytes, size_t* scale_bytes) {
+    if (!code_bytes || !scale_bytes) return ELUTQ_ERR_INVALID_ARG;
+    const int st = mx4_check(format, rows, K);
+    if (st != ELUTQ_OK) return st;
+    *code_bytes = (size_t)rows * (K / 2);
+    *scale_bytes = (size_t)rows * (K / mx4_block(format));
+    return ELUTQ_OK;
+}
+
+extern "C" int elutq_mx4_quantize(const void* X, int x_type, int x_rows, long long ld, int rows, int K, int format, unsigned flags,
+                                  const float* prescale, const int* index, int index_div, const int* n_rows, void* codes, void* scales,
+                                  void* stream) {
+    if (!X || !codes || !scales) return ELUTQ_ERR_INVALID_ARG;
+    if (x_type < ELUTQ_TYPE_F16 || x_type > ELUTQ_TYPE_F32 || (flags & ~ELUTQ_MX4_FLAG_SWIGLU)) return ELUTQ_ERR_INVALID_ARG;
+    const int st = mx4_check(format, rows, K);
+    if (st != ELUTQ_OK) return st;
+    if (x_rows <= 0 || (index != nullptr && index_div < 1)) return ELUTQ_ERR_INVALID_ARG;
+    const bool swiglu = (flags & ELUTQ_MX4_FLAG_SWIGLU) != 0;
+    if (ld < (swiglu ? 2LL : 1LL) * K || (index == nullptr && x_rows < rows)) return ELUTQ_ERR_SHAPE;
+    const long long size = x_type == ELUTQ_TYPE_F32 ? 4 : 2;
+    if (!mx4_aligned(X, 16) || (ld * size) % 16 != 0 || !mx4_aligned(codes, 16) || !mx4_aligned(prescale, 4) || !mx4_aligned(index, 4) || !mx4_aligned(n_rows, 4))
+        return ELUTQ_ERR_ALIGN;
+    QuantArgs a;
+    a.X = X;
+    a.ld = ld;
+    a.prescale = prescale;
+    a.index = index;
+    a.n_rows = n_rows;
+    a.codes = reinterpret_cast<uint2*>(codes);
+    a.scales = reinterpret_cast<uint8_t*>(scales);
+    a.K = K;
+    a.x_rows = (long long)x_rows * (index != nullptr ? index_div : 1);
+    a.per_row.set(K / kChunk);
+    a.div.set(index != nullptr ? index_div : 1);
+    a.wide = mx4_aligned(X, 32) && (ld * size) % 32 == 0;
+    // thread numbers stay below 2^31, the last block's idle ones too
+    const int most = (0x7fffffff - 256) / a.per_row.d;
+    for (int r = 0; r < rows; r += a.rows) {
+        a.row0 = r;
+        a.rows = rows - r < most ? rows - r : most;
+        const long long chunks = (long long)a.rows * a.per_row.d;
+        int ce;
+        if (format == ELUTQ_MX4_MXFP4)
+            ce = x_type == ELUTQ_TYPE_F16 ? launch_quantize<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_F16>(a, chunks, swiglu, (cudaStream_t)stream)
+                 : x_type == ELUTQ_TYPE_BF16 ? launch_quantize<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_BF16>(a, chunks, swiglu, (cudaStream_t)stream)
+                                             : launch_quantize<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_F32>(a, chunks, swiglu, (cudaStream_t)stream);
+        else
+            ce = x_type == ELUTQ_TYPE_F16 ? launch_quantize<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_F16>(a, chunks, swiglu, (cudaStream_t)stream)
+                 : x_type == ELUTQ_TYPE_BF16 ? launch_quantize<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_BF16>(a, chunks, swiglu, (cudaStream_t)stream)
+                                             : launch_quantize<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_F32>(a, chunks, swiglu, (cudaStream_t)stream);
+        if (ce != 0) {
+            note_cuda_error(ce);
+            return ELUTQ_ERR_CUDA;
+        }
+    }
+    return ELUTQ_OK;
+}
+
+extern "C" int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K, int format, const float* alpha, void* Y, int y_type, void* stream) {
+    if (!codes || !scales || !Y) return ELUTQ_ERR_INVALID_ARG;
+    if (y_type < ELUTQ_TYPE_F16 || y_type > ELUTQ_TYPE_F32) return ELUTQ_ERR_INVALID_ARG;
+    const int st = mx4_check(format, rows, K);
+    if (st != ELUTQ_OK) return st;
+    if (!mx4_aligned(codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
+    const long long chunks = (long long)rows * (K / kChunk);
+    if (chunks > 64LL * 0x7fffffffLL) return ELUTQ_ERR_SHAPE;                 // (blocks of a launch)
+    const uint2* c = reinterpret_cast<const uint2*>(codes);
+    const uint8_t* s = reinterpret_cast<const uint8_t*>(scales);
+    int ce = 0;
+    auto go = [&](auto kernel) { ce = launch(kernel, chunks, (cudaStream_t)stream, c, s, alpha, Y, chunks); };
+    if (format == ELUTQ_MX4_MXFP4) {
+        if (y_type == ELUTQ_TYPE_F16) go(mx4_dequantize_kernel<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_F16>);
+        else if (y_type == ELUTQ_TYPE_BF16) go(mx4_dequantize_kernel<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_BF16>);
+        else go(mx4_dequantize_kernel<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_F32>);
+    } else {
+        if (y_type == ELUTQ_TYPE_F16) go(mx4_dequantize_kernel<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_F16>);
+        else if (y_type == ELUTQ_TYPE_BF16) go(mx4_dequantize_kernel<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_BF16>);
+        else go(mx4_dequantize_kernel<ELUTQ_MX4_NVFP4, ELUTQ_TYPE_F32>);
+    }
+    if (ce != 0) {
+        note_cuda_error(ce);
+        return ELUTQ_ERR_CUDA;
+    }
+    return ELUTQ_OK;
+}
