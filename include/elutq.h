@@ -432,6 +432,31 @@ int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K,
                          int y_type, void* stream);
 
 /*
+ * Y[M][N] (y_type, dense, 16-byte aligned) = alpha * X[M][K] * W[N][K]^T of two matrices in the same format.  Products are exact, sums
+ * are fp32 in the tensor core's order, the result is multiplied by alpha (NULL: 1, or device float [1]) in fp32 and
+ * rounded once to y_type.  A row whose scales or values are NaN gives NaN.  Any M and N up to 2^30.
+ */
+int elutq_mx4_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y, int y_type,
+                   int M, int N, int K, int format, const float* alpha, void* stream);
+
+/*
+ * The same with a matrix of weights per group (expert): rows offsets[e] .. offsets[e+1] - 1 of X times W_e[N][K]^T, times alpha[e].
+ *   w_codes, w_scales  E matrices of N rows, one behind the other; E at most 1024, E * N below 2^30
+ *   offsets            device int [E + 1], ascending, in [0, M]; the host does not read it.  A group may be empty.  Rows of Y in
+ *                      front of offsets[0] and from offsets[E] on are left as they were.  (Borders out of order or out of
+ *                      range are cut to what is left of [0, M]: nothing outside is touched, and no row is written twice.)
+ *   alpha              NULL (1), or device float [E]
+ */
+int elutq_mx4_gemm_grouped(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const int* offsets,
+                           void* Y, int y_type, int M, int N, int K, int E, int format, const float* alpha, void* stream);
+
+/* Test entry for the bounded waits of the two products: the call is launched with its loads left out and the poll limit
+ * `wait_limit`, so that every role gives up and the kernel returns; elutq_device_status then reads ELUTQ_DEVICE_WAIT_EXPIRED on any
+ * stream of the device until elutq_release_scratch.  Y receives undefined values. */
+int elutq_mx4_test_wait_expiry(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y,
+                               int y_type, int M, int N, int K, int format, unsigned wait_limit, void* stream);
+
+/*
  * Device-side status of the library-owned scratch of `stream` (synchronises the stream).
  * *status is 0 unless a kernel gave up on a bounded wait (then a non-zero code that stays set
  * until elutq_release_scratch).  Kernels never spin without a limit.  While it is set, the finalize kernels

@@ -67,6 +67,9 @@ _SIGNATURES = {
     "elutq_mx4_bytes": (c_int, [c_int, c_int, c_int, ctypes.POINTER(c_size_t), ctypes.POINTER(c_size_t)]),
     "elutq_mx4_quantize": (c_int, [c_void_p, c_int, c_int, c_longlong, c_int, c_int, c_int, c_uint, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "elutq_mx4_dequantize": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p]),
+    "elutq_mx4_gemm": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p]),
+    "elutq_mx4_gemm_grouped": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p]),
+    "elutq_mx4_test_wait_expiry": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_uint, c_void_p]),
     "elutq_chain_plan_bytes": (c_int, [ctypes.POINTER(GemvCall), c_int, ctypes.POINTER(c_size_t)]),
     "elutq_chain_plan": (c_int, [ctypes.POINTER(GemvCall), c_int, c_void_p, c_size_t, c_void_p]),
     "elutq_chain_run": (c_int, [c_void_p, c_int, c_void_p]),
@@ -278,6 +281,21 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
 
 def elutq_mx4_dequantize(codes, scales, Y, rows: int, K: int, fmt: int, alpha=None, stream=None) -> None:
     _check(lib().elutq_mx4_dequantize(_ptr(codes), _ptr(scales), rows, K, fmt, _ptr(alpha), _ptr(Y), _type(Y), _stream(stream)), "elutq_mx4_dequantize")
+
+
+def elutq_mx4_gemm(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, alpha=None, stream=None) -> None:
+    _check(lib().elutq_mx4_gemm(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(Y), _type(Y), M, N, K, fmt, _ptr(alpha),
+                                _stream(stream)), "elutq_mx4_gemm")
+
+
+def elutq_mx4_gemm_grouped(x_codes, x_scales, w_codes, w_scales, offsets, Y, M: int, N: int, K: int, E: int, fmt: int, alpha=None, stream=None) -> None:
+    _check(lib().elutq_mx4_gemm_grouped(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(offsets), _ptr(Y), _type(Y), M, N, K, E, fmt,
+                                        _ptr(alpha), _stream(stream)), "elutq_mx4_gemm_grouped")
+
+
+def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, wait_limit: int, stream=None) -> None:
+    _check(lib().elutq_mx4_test_wait_expiry(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(Y), _type(Y), M, N, K, fmt, wait_limit,
+                                            _stream(stream)), "elutq_mx4_test_wait_expiry")
 
 
 def elutq_device_status(stream=None) -> int:

@@ -10,6 +10,7 @@
 #include <utility>
 
 #include "common.cuh"
+#include "mx4.cuh"
 
 namespace elutq {
 
@@ -471,8 +472,11 @@ int elutq_device_status(void* stream, int* status) {
     *status = 0;
     e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e);
-    if (!ptr) return ELUTQ_OK;
     unsigned word = 0;
+    e = (cudaError_t)mx4_status(&word);
+    if (e != cudaSuccess) return cuda_fail(e);
+    *status = (int)word;
+    if (!ptr || word != 0) return ELUTQ_OK;
     e = cudaMemcpy(&word, ptr, sizeof(word), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(e);
     *status = (int)word;
@@ -494,6 +498,8 @@ int elutq_release_scratch(void) {
         if (e != cudaSuccess && first == cudaSuccess) first = e;
     }
     g_parked.clear();
+    const cudaError_t e = (cudaError_t)mx4_clear_status();
+    if (e != cudaSuccess && first == cudaSuccess) first = e;
     if (first != cudaSuccess) return cuda_fail(first);
     return ELUTQ_OK;
 }

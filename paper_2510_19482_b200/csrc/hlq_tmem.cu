@@ -30,12 +30,11 @@
 //
 // Every wait is bounded; a thread whose wait runs out raises the status word and a CTA-wide flag that ends the other
 // roles' waits; copies and MMAs in flight are waited for (bounded), tensor memory is freed, the kernel returns.
-#include <cuda.h>
-
 #include <initializer_list>
 #include <mutex>
 
 #include "common.cuh"
+#include "tensor_map.cuh"
 
 namespace elutq {
 
@@ -816,22 +815,6 @@ __global__ void __launch_bounds__(256) hlq_tmem_finalize_kernel(const TmemArgs a
         if (m0 + i < m_end) store_out(a.g, (size_t)(m0 + i) * a.g.N + n, acc[i]);
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encode_fn() {
-    static const EncodeFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-            r != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    return fn;
-}
-
 // How the steps of a call are dealt to the SMs: equal shares of all steps, which leaves tiles to be added up from parts; whole tiles,
 // which leaves SMs idle; or each tile's K over a cluster of CTAs, which add up through their shared memory.  In us: a step takes
 // c when the other SMs do not fight for the L2, 10 % more when all do, the parts 5 (a second kernel 8) and their fp32 bytes at 2.2 TB/s, a cluster's
@@ -934,7 +917,7 @@ int launch_tmem_q(const GemmArgs& g, int num_sms, cudaStream_t stream) {
         if (a.xs > kMaxX) a.xs = kMaxX;
     };
 
-    EncodeFn enc = encode_fn();
+    EncodeTiledFn enc = encode_tiled_fn();
     if (!enc) return (int)cudaErrorNotSupported;
     CUtensorMap map;
     const cuuint64_t dims[2] = {(cuuint64_t)g.K, (cuuint64_t)g.M}, strides[1] = {(cuuint64_t)g.K * 2};
@@ -1032,6 +1015,18 @@ const int (&cluster_table())[kMaxSplit + 1] {
 }
 
 }  // namespace
+
+EncodeTiledFn encode_tiled_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
 
 int resident_clusters(int size) { return cluster_table()[size]; }
 

@@ -18,4 +18,8 @@ inline int mx4_check(int format, int rows, int K) {
 }
 inline bool mx4_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// The status word of the current device's 4-bit products (mx4_gemm.cu): a cudaError_t value each.
+int mx4_status(unsigned* word);
+int mx4_clear_status();
+
 }  // namespace elutq

@@ -1,0 +1,728 @@
+// Products of microscaled 4-bit matrices, dense and grouped by expert, on tcgen05.mma with block scales.
+//
+//   Y[t][n] = alpha_e * sum_k X[t][k] W_e[n][k],  rows t of group e (one group: a dense product)
+//
+// The tensor core takes both operands as codes and multiplies every product of two blocks by their two scales; sums are fp32.
+//
+//   tile       128 weight rows (256 by a pair of CTAs) x up to 256 tokens.  Weight rows are the MMA's M, lanes of tensor memory; tokens its
+//              N, columns of tensor memory, 8 at least: a decoding batch wastes nothing but padding to 8, and a group's rest is as wide as it is.
+//   K          in steps of 256: 128 bytes of codes a row, one 128-byte swizzle atom wide, brought by TMA into a ring of stages.
+//   scales     are row-major, while the tensor core wants, per 128 rows and 4 scales, 512 bytes with row r's four at
+//              16 (r mod 32) + 4 (r / 32).  A warp per 128 rows holds rows l, l + 32, l + 64, l + 96 in lane l, loads two steps' scales of
+//              a row at a time, a pair of steps ahead, and stores the four rows' words side by side (16 bytes, no conflicts).  The MMA warp copies
+//              them to tensor memory (tcgen05.cp) in front of the step's MMAs; copies and MMAs of one thread run in order.
+//   sums       two accumulators; the epilogue warps empty one while the next tile fills the other.  256 tokens leave no room for two beside the
+//              scales: they overlap by 48 columns, which the epilogue empties first.
+//   few tiles  a cluster of CTAs shares a tile's K; the parts meet in shared memory, each CTA adds up its share of the tokens in the
+//              cluster's order and stores them.
+//   tail       K: TMA fills codes with zeros, the scale warps scales.  Rows behind the last one of the matrix or the group: whatever is
+//              there; a row of one operand only reaches its own row or column of the sums, and those are not stored.
+//
+// Every wait is bounded: the thread whose wait runs out raises the device's status word, and all roles leave their loops.
+#include <cuda_bf16.h>
+
+#include "mx4.cuh"
+#include "tensor_map.cuh"
+
+namespace elutq {
+
+namespace {
+
+constexpr int kTileW = 128;                // weight rows of a CTA
+constexpr int kMaxTokens = 256;            // tokens of a tile
+constexpr int kStepBytes = 128;            // codes of a row in a step: 256 k
+constexpr int kMaxStages = 10;
+constexpr int kMaxSplit = 8;
+constexpr int kMaxSplitTokens = 64;
+constexpr int kMaxGroups = 1024;
+constexpr int kAcc1 = 208, kScaleCols = 464;     // second accumulator; scales (48 columns)
+constexpr int kSmem = 232448;
+constexpr uint32_t kWaitLimit = 1u << 22;
+
+__device__ unsigned g_status;              // 0, or what a launch on this device gave up on
+
+struct Mx4Args {
+    const uint8_t *x_scales, *w_scales;
+    const float* alpha;
+    const int* offsets;        // null: one group of all rows
+    void* Y;
+    int y_type;
+    int M, N, K, E;
+    int sk;                    // scale bytes of a row
+    int tokens;                // tokens of a tile at most
+    int w_tiles;               // of a group
+    int steps;                 // of the whole K
+    int split;                 // CTAs that share a tile's K
+    int stages;
+    int x_box;                 // rows of one X load
+    int x_vec, w_vec;          // bytes of one load of scales
+    int test;                  // 1: no load is issued
+    uint32_t wait_limit;
+};
+
+enum { kBarFull = 0, kBarScales = kBarFull + kMaxStages, kBarEmpty = kBarScales + kMaxStages, kBarAccFull = kBarEmpty + kMaxStages, kBarAccFree = kBarAccFull + 2,
+       kBarPartsFull = kBarAccFree + 2, kBarPartsFree, kBarDrain, kNumBars };
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {       // bar: a shared::cluster address
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+template <bool CLUSTER>
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    if constexpr (CLUSTER)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// By a whole warp, with one answer for it: false once anything in the CTA has given up.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t limit) {
+    bool ok = false, over = false;
+    for (uint32_t i = 0; i < limit && !ok && !over; ++i) {
+        ok = try_wait<CLUSTER>(bar, parity);
+        over = !ok && (i & 15u) == 15u && *gave_up;
+    }
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if (!ok && !over) {
+        *gave_up = 1;
+        atomicExch(&g_status, kStatusWaitExpired);
+    }
+    __syncwarp();
+    return false;
+}
+// Whether `ok` holds in all epilogue warps (which pass their barrier).
+__device__ __forceinline__ bool epilogue_agrees(bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)ok) : "memory");
+    return all != 0;
+}
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// K-major, 128-byte swizzle, 1024 bytes per 8 rows
+__device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// 32 rows of 16 bytes, no swizzle: 128 bytes per 8 rows
+__device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1 << 46);
+}
+template <int CG>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+    if constexpr (CG == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+}
+template <int FMT, int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    if constexpr (FMT == ELUTQ_MX4_MXFP4 && CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
+    else if constexpr (FMT == ELUTQ_MX4_MXFP4)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::mxf4.block_scale.block32 [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
+    else if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.block16 [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.block16 [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sa), "r"(sb) : "memory");
+}
+// One arrival on `bar` (of both CTAs of a pair) once all MMAs and copies issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16]) {     // names the registers: nothing may use them earlier
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+
+// A ring's stage and the parity of its use
+struct Ring {
+    int len, i = 0;
+    uint32_t phase = 0;
+    __device__ explicit Ring(int n) : len(n) {}
+    __device__ void next() {
+        if (++i == len) { i = 0; phase ^= 1u; }
+    }
+};
+
+// The scales of one row: two steps, WORDS words (4 MXFP4 or 8 NVFP4).  Bytes behind the row's end are 0.
+template <int WORDS>
+__device__ __forceinline__ void load_scales(uint32_t (&w)[WORDS], const uint8_t* row, int at, int end, int vec) {
+    if (vec == 16) {
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (at + 4 * i < end) v = __ldg(reinterpret_cast<const uint4*>(row + at + 4 * i));
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    } else if (vec == 4) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = at + 4 * i < end ? __ldg(reinterpret_cast<const uint32_t*>(row + at + 4 * i)) : 0u;
+    } else if (vec == 2) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const int p = at + 4 * i;
+            const uint32_t lo = p < end ? __ldg(reinterpret_cast<const uint16_t*>(row + p)) : 0u;
+            const uint32_t hi = p + 2 < end ? __ldg(reinterpret_cast<const uint16_t*>(row + p + 2)) : 0u;
+            w[i] = lo | hi << 16;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            uint32_t v = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (at + 4 * i + b < end) v |= (uint32_t)__ldg(row + at + 4 * i + b) << (8 * b);
+            w[i] = v;
+        }
+    }
+}
+
+struct Tile {
+    int e, n0, t0, count;      // group, first weight row in it, first token, tokens
+};
+
+// Where the groups' tiles begin in the list of all tiles: starts[E + 1], then the first row [E] and the number of rows [E] of each group.
+// Borders out of order or out of range are cut to what is left of [0, M).
+__device__ __forceinline__ void list_groups(const Mx4Args& a, int* table) {
+    int* starts = table;
+    int* first = table + a.E + 1;
+    int* rows = first + a.E;
+    const int lane = threadIdx.x & 31;
+    int tiles = 0, border = 0;                  // of the groups before this turn
+    for (int e0 = 0; e0 < a.E; e0 += 32) {
+        const int e = e0 + lane;
+        int lo = 0, hi = 0;
+        if (e < a.E) {
+            lo = min(max(__ldg(a.offsets + e), 0), a.M);
+            hi = min(max(__ldg(a.offsets + e + 1), lo), a.M);
+        }
+        int most = hi;                          // the largest border so far
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, most, o);
+            if (lane >= o) most = max(most, v);
+        }
+        most = max(most, border);
+        int before = __shfl_up_sync(0xffffffffu, most, 1);
+        if (lane == 0) before = border;
+        lo = max(lo, before);
+        const int n = max(hi - lo, 0);
+        const int mine = (n + a.tokens - 1) / a.tokens * a.w_tiles;
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (e < a.E) {
+            starts[e] = tiles + sum - mine;
+            first[e] = lo;
+            rows[e] = n;
+        }
+        tiles += __shfl_sync(0xffffffffu, sum, 31);
+        border = __shfl_sync(0xffffffffu, most, 31);
+    }
+    if (lane == 0) starts[a.E] = tiles;
+}
+
+// A group's rows are cut into as many tiles as they need, of nearly equal height (multiples of 8).  The token tiles of one block of
+// weights are neighbours in the list: they run at the same time and read the weights from L2.
+template <int CG>
+__device__ __forceinline__ Tile tile_at(const Mx4Args& a, const int* table, int i) {
+    Tile t;
+    int rows = a.M, local = i;
+    t.e = 0;
+    t.t0 = 0;
+    if (a.offsets != nullptr) {
+        int lo = 0, hi = a.E;                   // starts[lo] <= i < starts[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (table[mid] <= i) lo = mid;
+            else hi = mid;
+        }
+        t.e = lo;
+        local = i - table[lo];
+        t.t0 = table[a.E + 1 + lo];
+        rows = table[2 * a.E + 1 + lo];
+    }
+    const int n = (rows + a.tokens - 1) / a.tokens;
+    const int height = ((rows + n - 1) / n + 7) / 8 * 8;
+    const int w = local / n, p = local - w * n;
+    t.n0 = w * (CG * kTileW);
+    t.t0 += p * height;
+    t.count = min(height, rows - p * height);
+    return t;
+}
+
+__device__ __forceinline__ void store_y(const Mx4Args& a, long long at, float v) {
+    if (a.y_type == ELUTQ_TYPE_F16) reinterpret_cast<__half*>(a.Y)[at] = __float2half_rn(v);
+    else if (a.y_type == ELUTQ_TYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.Y)[at] = __float2bfloat16_rn(v);
+    else reinterpret_cast<float*>(a.Y)[at] = v;
+}
+
+// Warps: 0 loads codes, 1 issues MMAs, 2 weights' scales, 3 (and 8: tokens 128 to 255) activations' scales, 4 to 7 epilogue.
+template <int FMT, int CG>
+__global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
+    constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
+    constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int blocks = (a.tokens + 127) / 128;                    // of 128 tokens
+    const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
+    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + blocks) * CH * 512;
+    uint8_t* sW = smem;
+    uint8_t* sX = sW + a.stages * w_bytes;
+    uint8_t* sS = sX + a.stages * x_bytes;
+    float* parts = reinterpret_cast<float*>(sS + a.stages * s_bytes);                 // [tokens][128], clusters only
+    uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(parts) + (a.split > 1 ? a.tokens * kTileW * 4 : 0));
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+    volatile uint32_t* gave_up = tmem_slot + 1;
+    int* table = reinterpret_cast<int*>(tmem_slot + 2);
+    const uint32_t bar0 = smem_u32(bars);
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    uint32_t rank = 0;                                            // in the cluster
+    if (CG == 2 || a.split > 1) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const bool leader = CG == 1 || rank == 0;
+
+    if (warp == 1) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(tmem_slot)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(tmem_slot)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    if (threadIdx.x == 0) {
+        auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
+        for (int i = 0; i < a.stages; ++i) {
+            init(kBarFull + i, 1);
+            init(kBarScales + i, CG * (1 + blocks));
+            init(kBarEmpty + i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            init(kBarAccFull + i, 1);
+            init(kBarAccFree + i, CG * 4);
+        }
+        init(kBarPartsFull, a.split);
+        init(kBarPartsFree, a.split);
+        init(kBarDrain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gave_up = 0;
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&x_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" :: "l"(&w_map) : "memory");
+    }
+    __syncwarp();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (a.offsets != nullptr && warp == 0) list_groups(a, table);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2 || a.split > 1) cluster_barrier();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
+
+    const int team = CG == 2 ? 2 : a.split;                       // CTAs that work on one tile
+    const int first = blockIdx.x / team, stride = gridDim.x / team;
+    const int tiles = a.offsets != nullptr ? table[a.E] : a.w_tiles * ((a.M + a.tokens - 1) / a.tokens);
+    // this CTA's steps, in pairs
+    const int pairs = (a.steps + 1) / 2;
+    const int step0 = CG == 2 ? 0 : 2 * (int)((long long)pairs * rank / a.split);
+    const int step1 = CG == 2 ? a.steps : min(a.steps, 2 * (int)((long long)pairs * (rank + 1) / a.split));
+    const uint32_t limit = a.wait_limit;
+
+    if (warp == 0) {
+        Ring r(a.stages);
+        int issued = 0;
+        bool ok = true;
+        for (int i = first; i < tiles && ok; i += stride) {
+            const Tile t = tile_at<CG>(a, table, i);
+            const int per_cta = CG == 2 ? (t.count + 15) / 16 * 8 : (t.count + 7) / 8 * 8;
+            const int boxes = (per_cta + a.x_box - 1) / a.x_box;
+            const int w_row = t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0), x_row = t.t0 + (CG == 2 ? (int)rank * per_cta : 0);
+            const uint32_t bytes = CG * (w_bytes + boxes * a.x_box * kStepBytes);
+            for (int s = step0; s < step1; ++s) {
+                ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                if (!ok) break;
+                if (elect_one() && !a.test) {
+                    const uint32_t full = CG == 2 ? at_rank(bar(kBarFull + r.i), 0) : bar(kBarFull + r.i);
+                    if (leader) expect(bar(kBarFull + r.i), bytes);
+                    tma_load<CG>(smem_u32(sW + r.i * w_bytes), &w_map, s * kStepBytes, w_row, full);
+                    for (int b = 0; b < boxes; ++b)
+                        tma_load<CG>(smem_u32(sX + r.i * x_bytes + b * a.x_box * kStepBytes), &x_map, s * kStepBytes, x_row + b * a.x_box, full);
+                }
+                __syncwarp();
+                ++issued;
+                r.next();
+            }
+        }
+        // a wait ran out: copies in flight still land (each stage's last ones), in front of the CTA's end
+        if (!ok && leader && !a.test) {
+            for (int j = 0; j < min(issued, a.stages); ++j) {
+                if (r.i == 0) r.phase ^= 1u;
+                r.i = r.i == 0 ? a.stages - 1 : r.i - 1;
+                for (uint32_t n = 0; n < limit && !try_wait<false>(bar(kBarFull + r.i), r.phase); ++n) {}
+            }
+        }
+    } else if (warp == 1 && leader) {
+        Ring r(a.stages);
+        const bool overlap = a.tokens > kAcc1;
+        int n = 0;
+        bool ok = true;
+        for (int i = first; i < tiles && ok; i += stride, ++n) {
+            const Tile t = tile_at<CG>(a, table, i);
+            const int b = n & 1, use = n >> 1;
+            if (overlap) ok = n == 0 || wait<CG == 2>(bar(kBarAccFree + b), (uint32_t)(b == 1 ? use : use - 1) & 1u, gave_up, limit);
+            else ok = wait<CG == 2>(bar(kBarAccFree + b), ((uint32_t)use & 1u) ^ 1u, gave_up, limit);
+            if (!ok) break;
+            const int cols = CG == 2 ? (t.count + 15) / 16 * 16 : (t.count + 7) / 8 * 8;
+            const uint32_t idesc = 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (FMT == ELUTQ_MX4_MXFP4 ? 1u << 23 : 0u) | (uint32_t)(CG * kTileW >> 4) << 24;
+            const uint32_t acc = tmem + (b ? kAcc1 : 0), sa = tmem + kScaleCols, sb = sa + 4 * CH;
+            for (int s = step0; s < step1; ++s) {
+                ok = wait<CG == 2>(bar(kBarFull + r.i), r.phase, gave_up, limit) && wait<CG == 2>(bar(kBarScales + r.i), r.phase, gave_up, limit);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint64_t da = operand_desc(smem_u32(sW + r.i * w_bytes)), db = operand_desc(smem_u32(sX + r.i * x_bytes));
+                const uint32_t ss = smem_u32(sS + r.i * s_bytes);
+                const int parts64 = min(4, (a.K - s * 256 + 63) / 64);
+                if (elect_one()) {
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        copy_scales<CG>(sa + 4 * c, scales_desc(ss + c * 512));
+                        for (int h = 0; h < blocks; ++h) copy_scales<CG>(sb + 4 * (c * blocks + h), scales_desc(ss + (CH + c * blocks + h) * 512));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j < parts64) {
+                            const int c = j / SUB;
+                            const uint32_t id = (uint32_t)(j % SUB) * 2u;             // which of the group's scales
+                            mma<FMT, CG>(acc, da + 2 * j, db + 2 * j, idesc | id << 29 | id << 4, sa + 4 * c, sb + 4 * c * blocks, s > step0 || j > 0);
+                        }
+                    }
+                    commit<CG>(bar(kBarEmpty + r.i));
+                    if (s == step1 - 1) commit<CG>(bar(kBarAccFull + b));
+                }
+                __syncwarp();
+                r.next();
+            }
+        }
+        if (!ok) {                             // what has been issued ends in front of the tensor memory's release
+            if (elect_one()) commit<CG>(bar(kBarDrain));
+            __syncwarp();
+            for (uint32_t k = 0; k < limit && !try_wait<false>(bar(kBarDrain), 0u); ++k) {}
+        }
+    } else if (warp == 2 || warp == 3 || warp == 8) {
+        const int block = warp == 2 ? 0 : warp == 3 ? 1 : 2;      // weights, tokens 0 to 127, 128 to 255
+        if (block <= blocks) {
+            constexpr int WORDS = 2 * CH;
+            Ring r(a.stages);
+            const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
+            const int vec = block == 0 ? a.w_vec : a.x_vec;
+            const long long last = block == 0 ? (long long)a.E * a.N - 1 : a.M - 1;
+            bool ok = true;
+            for (int i = first; i < tiles && ok; i += stride) {
+                const Tile t = tile_at<CG>(a, table, i);
+                const long long row0 = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
+                const uint8_t* rows[4];
+                uint32_t w[4][WORDS];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    rows[q] = base + min(row0 + lane + 32 * q, last) * a.sk;
+                    load_scales<WORDS>(w[q], rows[q], step0 * 4 * CH, a.sk, vec);
+                }
+                for (int s = step0; s < step1 && ok; s += 2) {
+                    uint32_t ahead[4][WORDS] = {};
+                    if (s + 2 < step1) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) load_scales<WORDS>(ahead[q], rows[q], (s + 2) * 4 * CH, a.sk, vec);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (s + h < step1 && ok) {
+                            ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                            if (ok) {
+                                uint8_t* to = sS + r.i * s_bytes + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
+                                const int pitch = block == 0 ? 512 : blocks * 512;
+#pragma unroll
+                                for (int c = 0; c < CH; ++c)
+                                    *reinterpret_cast<uint4*>(to + c * pitch) = make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                __syncwarp();
+                                if (lane == 0) {
+                                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
+                                    else arrive(bar(kBarScales + r.i));
+                                }
+                                __syncwarp();
+                                r.next();
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < WORDS; ++k) w[q][k] = ahead[q][k];
+                }
+            }
+        }
+    } else if (warp >= 4 && warp < 8) {
+        const int quarter = warp & 3;                             // lanes of tensor memory
+        const bool overlap = a.tokens > kAcc1;
+        int n = 0;
+        bool ok = true;
+        for (int i = first; i < tiles && ok; i += stride, ++n) {
+            const Tile t = tile_at<CG>(a, table, i);
+            const int b = n & 1, use = n >> 1;
+            ok = wait<CG == 2>(bar(kBarAccFull + b), (uint32_t)use & 1u, gave_up, limit);
+            if (a.split > 1) ok = epilogue_agrees(ok && wait<true>(bar(kBarPartsFree), ((uint32_t)n & 1u) ^ 1u, gave_up, limit));
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + (b ? kAcc1 : 0) + ((uint32_t)(quarter * 32) << 16);
+            const float alpha = a.alpha != nullptr ? __ldg(a.alpha + t.e) : 1.0f;
+            const int row = quarter * 32 + lane, col = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + row;
+            auto release = [&](int which) {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarAccFree + which), 0));
+                    else arrive(bar(kBarAccFree + which));
+                }
+                __syncwarp();
+            };
+            if (a.split > 1) {
+                for (int c0 = 0; c0 < t.count; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(v, acc + c0);
+                    tmem_ld_wait(v);
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        if (c0 + c < t.count) parts[(c0 + c) * kTileW + row] = __uint_as_float(v[c]);
+                }
+                release(b);
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (threadIdx.x - 128u < (unsigned)a.split) arrive_cluster(at_rank(bar(kBarPartsFull), threadIdx.x - 128u));
+                __syncwarp();
+                ok = wait<true>(bar(kBarPartsFull), (uint32_t)n & 1u, gave_up, limit);
+                if (ok) {
+                    for (int c = (int)rank; c < t.count; c += a.split) {
+                        float sum = 0.0f;
+                        for (int s = 0; s < a.split; ++s) sum += ld_cluster_f32(parts + c * kTileW + row, (unsigned)s);
+                        if (col < a.N) store_y(a, (long long)(t.t0 + c) * a.N + col, sum * alpha);
+                    }
+                }
+                ok = epilogue_agrees(ok);
+                if (threadIdx.x - 128u < (unsigned)a.split) arrive_cluster(at_rank(bar(kBarPartsFree), threadIdx.x - 128u));
+                __syncwarp();
+                continue;
+            }
+            // overlapping accumulators: the 48 columns that both have first, then the other one may be filled
+            const int shared = (kMaxTokens - kAcc1) / 16, turns = overlap ? kMaxTokens / 16 : (t.count + 15) / 16;
+            for (int k = 0; k < turns; ++k) {
+                const int g = !overlap || b == 1 ? k : k < shared ? kAcc1 / 16 + k : k - shared;
+                const int c0 = 16 * g;
+                if (c0 < t.count) {
+                    uint32_t v[16];
+                    tmem_ld16(v, acc + c0);
+                    tmem_ld_wait(v);
+                    if (col < a.N) {
+                        const long long at = (long long)(t.t0 + c0) * a.N + col;
+#pragma unroll
+                        for (int c = 0; c < 16; ++c)
+                            if (c0 + c < t.count) store_y(a, at + (long long)c * a.N, __uint_as_float(v[c]) * alpha);
+                    }
+                    __syncwarp();
+                }
+                if (overlap && k == shared - 1) release(b ^ 1);
+            }
+            if (!overlap) release(b);
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2 || a.split > 1) cluster_barrier();                // no CTA leaves while another reads its memory or arrives on its barriers
+    if (warp == 1) {
+        if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+    }
+}
+
+struct Plan { int cg, tokens, x_box, split, stages, grid; size_t smem; };
+
+constexpr int kFixed = kNumBars * 8 + 16;
+
+// Ring length and shared memory of a plan whose other fields are set; false if fewer than two stages fit.
+bool fill_plan(Plan& p, int format, int E, bool grouped) {
+    const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4;
+    const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024 + (1 + (p.tokens + 127) / 128) * ch * 512;
+    const int fixed = kFixed + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
+    p.stages = (kSmem - fixed) / stage;
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    p.smem = (size_t)p.stages * stage + fixed;
+    return p.stages >= 2;
+}
+
+Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms) {
+    Plan p = {};
+    const int units = (K + 511) / 512;
+    p.cg = 1;
+    p.split = 1;
+    // rows of a tile: all of a small batch, even shares of a large one; a group's are not known here
+    const int per = grouped ? (M + E - 1) / E * 2 : M;
+    const int n = (per + kMaxTokens - 1) / kMaxTokens;
+    p.tokens = ((per + n - 1) / n + 7) / 8 * 8;
+    if (p.tokens > 32) p.tokens = (p.tokens + 31) / 32 * 32;
+    p.x_box = grouped ? (p.tokens > 32 ? 32 : p.tokens) : p.tokens;
+    const long long most = grouped ? (long long)((N + kTileW - 1) / kTileW) * ((M + p.tokens - 1) / p.tokens + (E < M ? E : M))
+                                   : (long long)((N + kTileW - 1) / kTileW) * n;
+    if (p.tokens <= kMaxSplitTokens)
+        while (p.split < kMaxSplit && most * p.split * 2 <= num_sms && p.split * 2 <= units) p.split *= 2;
+    fill_plan(p, format, E, grouped);
+    const long long teams = num_sms / p.split;
+    p.grid = (int)(most < teams ? most : teams) * p.split;
+    return p;
+}
+
+int vec_of(const void* base, int row) {
+    const uintptr_t v = reinterpret_cast<uintptr_t>(base) | (uintptr_t)row;
+    return v % 16 == 0 ? 16 : v % 4 == 0 ? 4 : v % 2 == 0 ? 2 : 1;
+}
+
+int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int box) {
+    const EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return (int)cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)K / 2, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)K / 2};
+    const cuuint32_t sizes[2] = {kStepBytes, (cuuint32_t)box}, elem[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, sizes, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? 0 : (int)cudaErrorInvalidValue;
+}
+
+template <int FMT, int CG>
+int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
+    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return (int)e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.grid);
+    cfg.blockDim = dim3(p.tokens > 128 ? 288u : 256u);
+    cfg.dynamicSmemBytes = p.smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)(CG == 2 ? 2 : p.split);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CG == 2 || p.split > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<FMT, CG>, xm, wm, a);
+    if (e == cudaSuccess) count_launch(1);
+    return (int)e;
+}
+
+int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const int* offsets, void* Y, int y_type,
+            int M, int N, int K, int E, int format, const float* alpha, uint32_t test_limit, void* stream) {
+    if (!x_codes || !x_scales || !w_codes || !w_scales || !Y) return ELUTQ_ERR_INVALID_ARG;
+    if (N <= 0 || E <= 0 || y_type < ELUTQ_TYPE_F16 || y_type > ELUTQ_TYPE_F32) return ELUTQ_ERR_INVALID_ARG;
+    const int st = mx4_check(format, M, K);
+    if (st != ELUTQ_OK) return st;
+    if (E > kMaxGroups) return ELUTQ_ERR_UNSUPPORTED;
+    if (M > 0x3fffffff || (long long)E * N > 0x3fffffffLL) return ELUTQ_ERR_SHAPE;           // rows are 32-bit coordinates
+    if (!mx4_aligned(x_codes, 16) || !mx4_aligned(w_codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(offsets, 4) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
+    const bool grouped = offsets != nullptr;
+    const Plan p = plan_for(M, N, K, E, format, grouped, device_sm_count());
+    Mx4Args a;
+    a.x_scales = reinterpret_cast<const uint8_t*>(x_scales);
+    a.w_scales = reinterpret_cast<const uint8_t*>(w_scales);
+    a.alpha = alpha;
+    a.offsets = offsets;
+    a.Y = Y;
+    a.y_type = y_type;
+    a.M = M; a.N = N; a.K = K; a.E = E;
+    a.sk = K / mx4_block(format);
+    a.tokens = p.tokens;
+    a.w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
+    a.steps = (K + 255) / 256;
+    a.split = p.split;
+    a.stages = p.stages;
+    a.x_box = p.x_box;
+    a.x_vec = vec_of(x_scales, a.sk);
+    a.w_vec = vec_of(w_scales, a.sk);
+    a.test = test_limit != 0;
+    a.wait_limit = test_limit != 0 ? test_limit : kWaitLimit;
+    CUtensorMap xm, wm;
+    int ce = tensor_map(&xm, x_codes, M, K, p.x_box);
+    if (ce == 0) ce = tensor_map(&wm, w_codes, (long long)E * N, K, kTileW);
+    if (ce == 0)
+        ce = format == ELUTQ_MX4_MXFP4 ? (p.cg == 2 ? launch_mx4<ELUTQ_MX4_MXFP4, 2>(p, xm, wm, a, (cudaStream_t)stream) : launch_mx4<ELUTQ_MX4_MXFP4, 1>(p, xm, wm, a, (cudaStream_t)stream))
+                                       : (p.cg == 2 ? launch_mx4<ELUTQ_MX4_NVFP4, 2>(p, xm, wm, a, (cudaStream_t)stream) : launch_mx4<ELUTQ_MX4_NVFP4, 1>(p, xm, wm, a, (cudaStream_t)stream));
+    if (ce == 0) return ELUTQ_OK;
+    note_cuda_error(ce);
+    return ELUTQ_ERR_CUDA;
+}
+
+}  // namespace
+
+int mx4_status(unsigned* word) { return (int)cudaMemcpyFromSymbol(word, g_status, sizeof(*word)); }
+int mx4_clear_status() {
+    const unsigned zero = 0;
+    return (int)cudaMemcpyToSymbol(g_status, &zero, sizeof(zero));
+}
+
+}  // namespace elutq
+
+using namespace elutq;
+
+extern "C" int elutq_mx4_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y, int y_type,
+                              int M, int N, int K, int format, const float* alpha, void* stream) {
+    return run_mx4(x_codes, x_scales, w_codes, w_scales, nullptr, Y, y_type, M, N, K, 1, format, alpha, 0, stream);
+}
+
+extern "C" int elutq_mx4_gemm_grouped(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const int* offsets,
+                                      void* Y, int y_type, int M, int N, int K, int E, int format, const float* alpha, void* stream) {
+    if (!offsets) return ELUTQ_ERR_INVALID_ARG;
+    return run_mx4(x_codes, x_scales, w_codes, w_scales, offsets, Y, y_type, M, N, K, E, format, alpha, 0, stream);
+}
+
+extern "C" int elutq_mx4_test_wait_expiry(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y, int y_type,
+                                          int M, int N, int K, int format, unsigned wait_limit, void* stream) {
+    if (wait_limit == 0) return ELUTQ_ERR_INVALID_ARG;
+    return run_mx4(x_codes, x_scales, w_codes, w_scales, nullptr, Y, y_type, M, N, K, 1, format, nullptr, wait_limit, stream);
+}

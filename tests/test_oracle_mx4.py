@@ -86,6 +86,28 @@ def test_refusals_of_the_conversions():
     assert elutq.elutq_launch_count() == before
 
 
+def test_refusals_of_the_products():
+    L = elutq.lib()
+    before = elutq.elutq_launch_count()
+
+    def gemm(xc=16, xs=16, wc=16, ws=16, Y=16, y_type=0, M=4, N=4, K=64, fmt=0, alpha=None):
+        return L.elutq_mx4_gemm(xc, xs, wc, ws, Y, y_type, M, N, K, fmt, alpha, None)
+
+    def grouped(offsets=16, M=4, N=4, K=64, E=2, fmt=0, alpha=None):
+        return L.elutq_mx4_gemm_grouped(16, 16, 16, 16, offsets, 16, 0, M, N, K, E, fmt, alpha, None)
+
+    for name in ("xc", "xs", "wc", "ws", "Y"):
+        assert gemm(**{name: None}) == -1
+    for name in ("M", "N", "K"):
+        assert gemm(**{name: 0}) == gemm(**{name: -1}) == grouped(**{name: 0}) == -1
+    assert gemm(y_type=3) == gemm(fmt=2) == grouped(offsets=None) == grouped(E=0) == -1
+    assert gemm(K=48) == gemm(M=1 << 30) == gemm(N=1 << 30) == grouped(N=1 << 29, E=2) == grouped(K=40) == -2
+    assert gemm(xc=8) == gemm(wc=24) == gemm(Y=8) == gemm(alpha=2) == grouped(offsets=18) == grouped(alpha=6) == -3
+    assert grouped(E=1025) == -5
+    assert L.elutq_mx4_test_wait_expiry(16, 16, 16, 16, 16, 0, 4, 4, 64, 0, 0, None) == -1
+    assert elutq.elutq_launch_count() == before
+
+
 def test_the_binding_refuses_what_it_cannot_marshal():
     with pytest.raises(elutq.ElutqError):
         elutq.elutq_mx4_quantize(torch.zeros((4, 64), dtype=torch.float64), 4, 64, 0, stream=0)
