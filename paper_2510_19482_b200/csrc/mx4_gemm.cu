@@ -232,7 +232,7 @@ __device__ __forceinline__ void list_groups(const Mx4Args& a, int* table) {
         int lo = 0, hi = 0;
         if (e < a.E) {
             lo = min(max(__ldg(a.offsets + e), 0), a.M);
-            hi = min(max(__ldg(a.offsets + e + 1), lo), a.M);
+            hi = min(max(__ldg(a.offsets + e + 1), 0), a.M);
         }
         int most = hi;                          // the largest border so far
 #pragma unroll
