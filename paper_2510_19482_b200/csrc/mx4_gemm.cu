@@ -9,7 +9,7 @@
 //   K          in steps of 256: 128 bytes of codes a row, one 128-byte swizzle atom wide, brought by TMA into a ring of stages.
 //   scales     are row-major, while the tensor core wants, per 128 rows and 4 scales, 512 bytes with row r's four at
 //              16 (r mod 32) + 4 (r / 32).  A warp per 128 rows holds rows l, l + 32, l + 64, l + 96 in lane l, loads two steps' scales of
-//              a row at a time, a pair of steps ahead, and stores the four rows' words side by side (16 bytes, no conflicts).  The MMA warp copies
+//              a row at a time, some pairs ahead (across tiles), and stores the four rows' words side by side (16 bytes, no conflicts).  The MMA warp copies
 //              them to tensor memory (tcgen05.cp) in front of the step's MMAs; copies and MMAs of one thread run in order.
 //   sums       two accumulators; the epilogue warps empty one while the next tile fills the other.  256 tokens leave no room for two beside the
 //              scales: they overlap by 48 columns, which the epilogue empties first.
@@ -298,15 +298,14 @@ __device__ __forceinline__ void store_y(const Mx4Args& a, long long at, float v)
     else reinterpret_cast<float*>(a.Y)[at] = v;
 }
 
-// Warps: 0 loads codes, 1 issues MMAs, 2 weights' scales, 3 (and 8: tokens 128 to 255) activations' scales, 4 to 7 epilogue.
-template <int FMT, int CG>
+// NB: blocks of 128 tokens in a tile at most.  Warps: 0 loads codes, 1 issues MMAs, 2 weights' scales, 3 (and 8: tokens 128 to 255) activations' scales, 4 to 7 epilogue.
+template <int FMT, int CG, int NB>
 __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
     constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
-    const int blocks = (a.tokens + 127) / 128;                    // of 128 tokens
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
-    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + blocks) * CH * 512;
+    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + NB) * CH * 512;
     uint8_t* sW = smem;
     uint8_t* sX = sW + a.stages * w_bytes;
     uint8_t* sS = sX + a.stages * x_bytes;
@@ -335,7 +334,7 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
         auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
         for (int i = 0; i < a.stages; ++i) {
             init(kBarFull + i, 1);
-            init(kBarScales + i, CG * (1 + blocks));
+            init(kBarScales + i, CG * (1 + NB));
             init(kBarEmpty + i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -427,15 +426,23 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
 #pragma unroll
                     for (int c = 0; c < CH; ++c) {
                         copy_scales<CG>(sa + 4 * c, scales_desc(ss + c * 512));
-                        for (int h = 0; h < blocks; ++h) copy_scales<CG>(sb + 4 * (c * blocks + h), scales_desc(ss + (CH + c * blocks + h) * 512));
-                    }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (j < parts64) {
-                            const int c = j / SUB;
-                            const uint32_t id = (uint32_t)(j % SUB) * 2u;             // which of the group's scales
-                            mma<FMT, CG>(acc, da + 2 * j, db + 2 * j, idesc | id << 29 | id << 4, sa + 4 * c, sb + 4 * c * blocks, s > step0 || j > 0);
-                        }
+                        for (int h = 0; h < NB; ++h) copy_scales<CG>(sb + 4 * (c * NB + h), scales_desc(ss + (CH + c * NB + h) * 512));
+                    }
+                    // (no condition around a whole step's MMAs: each costs their issue)
+                    auto step_mma = [&](int j, uint32_t accumulate) {
+                        const int c = j / SUB;
+                        const uint32_t id = (uint32_t)(j % SUB) * 2u;             // which of the group's scales
+                        mma<FMT, CG>(acc, da + 2 * j, db + 2 * j, idesc | id << 29 | id << 4, sa + 4 * c, sb + 4 * c * NB, accumulate);
+                    };
+                    step_mma(0, s > step0);
+                    if (parts64 == 4) {
+                        step_mma(1, 1);
+                        step_mma(2, 1);
+                        step_mma(3, 1);
+                    } else {
+                        if (parts64 > 1) step_mma(1, 1);
+                        if (parts64 > 2) step_mma(2, 1);
                     }
                     commit<CG>(bar(kBarEmpty + r.i));
                     if (s == step1 - 1) commit<CG>(bar(kBarAccFull + b));
@@ -451,54 +458,71 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
         }
     } else if (warp == 2 || warp == 3 || warp == 8) {
         const int block = warp == 2 ? 0 : warp == 3 ? 1 : 2;      // weights, tokens 0 to 127, 128 to 255
-        if (block <= blocks) {
-            constexpr int WORDS = 2 * CH;
+        if (block <= NB) {
+            constexpr int WORDS = 2 * CH, AHEAD = FMT == ELUTQ_MX4_MXFP4 ? 4 : 3;      // pairs of steps in flight
             Ring r(a.stages);
             const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
             const int vec = block == 0 ? a.w_vec : a.x_vec;
             const long long last = block == 0 ? (long long)a.E * a.N - 1 : a.M - 1;
-            bool ok = true;
-            for (int i = first; i < tiles && ok; i += stride) {
-                const Tile t = tile_at<CG>(a, table, i);
+            uint8_t* to = sS + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
+            const int pitch = block == 0 ? 512 : NB * 512;
+            const uint8_t* rows[4];
+            uint32_t w[AHEAD][4][WORDS];
+            int load_i = first, load_s = step0;                   // the next pair to load
+            auto aim = [&] {
+                if (load_i >= tiles) return;
+                const Tile t = tile_at<CG>(a, table, load_i);
                 const long long row0 = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
-                const uint8_t* rows[4];
-                uint32_t w[4][WORDS];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    rows[q] = base + min(row0 + lane + 32 * q, last) * a.sk;
-                    load_scales<WORDS>(w[q], rows[q], step0 * 4 * CH, a.sk, vec);
+                for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, last) * a.sk;
+            };
+            auto load = [&](uint32_t (&v)[4][WORDS]) {
+                if (load_i >= tiles) return;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load_scales<WORDS>(v[q], rows[q], load_s * 4 * CH, a.sk, vec);
+                load_s += 2;
+                if (load_s >= step1) {
+                    load_s = step0;
+                    load_i += stride;
+                    aim();
                 }
-                for (int s = step0; s < step1 && ok; s += 2) {
-                    uint32_t ahead[4][WORDS] = {};
-                    if (s + 2 < step1) {
+            };
+            aim();
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) load_scales<WORDS>(ahead[q], rows[q], (s + 2) * 4 * CH, a.sk, vec);
-                    }
+            for (int d = 0; d < AHEAD; ++d) load(w[d]);
+            bool ok = true;
+            int i = first, s = step0;
+            while (i < tiles && ok) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (s + h < step1 && ok) {
-                            ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
-                            if (ok) {
-                                uint8_t* to = sS + r.i * s_bytes + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
-                                const int pitch = block == 0 ? 512 : blocks * 512;
+                for (int d = 0; d < AHEAD; ++d) {
+                    if (i < tiles && ok) {
 #pragma unroll
-                                for (int c = 0; c < CH; ++c)
-                                    *reinterpret_cast<uint4*>(to + c * pitch) = make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
-                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                                __syncwarp();
-                                if (lane == 0) {
-                                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
-                                    else arrive(bar(kBarScales + r.i));
+                        for (int h = 0; h < 2; ++h) {
+                            if (s + h < step1 && ok) {
+                                ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                                if (ok) {
+#pragma unroll
+                                    for (int c = 0; c < CH; ++c)
+                                        *reinterpret_cast<uint4*>(to + r.i * s_bytes + c * pitch) =
+                                            make_uint4(w[d][0][h * CH + c], w[d][1][h * CH + c], w[d][2][h * CH + c], w[d][3][h * CH + c]);
+                                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                    __syncwarp();
+                                    if (lane == 0) {
+                                        if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
+                                        else arrive(bar(kBarScales + r.i));
+                                    }
+                                    __syncwarp();
+                                    r.next();
                                 }
-                                __syncwarp();
-                                r.next();
                             }
                         }
+                        load(w[d]);
+                        s += 2;
+                        if (s >= step1) {
+                            s = step0;
+                            i += stride;
+                        }
                     }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int k = 0; k < WORDS; ++k) w[q][k] = ahead[q][k];
                 }
             }
         }
@@ -635,13 +659,13 @@ int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int bo
                ? 0 : (int)cudaErrorInvalidValue;
 }
 
-template <int FMT, int CG>
+template <int FMT, int CG, int NB>
 int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return (int)e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);
-    cfg.blockDim = dim3(p.tokens > 128 ? 288u : 256u);
+    cfg.blockDim = dim3(NB == 2 ? 288u : 256u);
     cfg.dynamicSmemBytes = p.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -652,9 +676,15 @@ int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, cons
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CG == 2 || p.split > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<FMT, CG>, xm, wm, a);
+    e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<FMT, CG, NB>, xm, wm, a);
     if (e == cudaSuccess) count_launch(1);
     return (int)e;
+}
+
+template <int FMT>
+int launch_format(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
+    if (p.cg == 2) return launch_mx4<FMT, 2, 2>(p, xm, wm, a, stream);
+    return p.tokens > 128 ? launch_mx4<FMT, 1, 2>(p, xm, wm, a, stream) : launch_mx4<FMT, 1, 1>(p, xm, wm, a, stream);
 }
 
 int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const int* offsets, void* Y, int y_type,
@@ -691,8 +721,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     int ce = tensor_map(&xm, x_codes, M, K, p.x_box);
     if (ce == 0) ce = tensor_map(&wm, w_codes, (long long)E * N, K, kTileW);
     if (ce == 0)
-        ce = format == ELUTQ_MX4_MXFP4 ? (p.cg == 2 ? launch_mx4<ELUTQ_MX4_MXFP4, 2>(p, xm, wm, a, (cudaStream_t)stream) : launch_mx4<ELUTQ_MX4_MXFP4, 1>(p, xm, wm, a, (cudaStream_t)stream))
-                                       : (p.cg == 2 ? launch_mx4<ELUTQ_MX4_NVFP4, 2>(p, xm, wm, a, (cudaStream_t)stream) : launch_mx4<ELUTQ_MX4_NVFP4, 1>(p, xm, wm, a, (cudaStream_t)stream));
+        ce = format == ELUTQ_MX4_MXFP4 ? launch_format<ELUTQ_MX4_MXFP4>(p, xm, wm, a, (cudaStream_t)stream) : launch_format<ELUTQ_MX4_NVFP4>(p, xm, wm, a, (cudaStream_t)stream);
     if (ce == 0) return ELUTQ_OK;
     note_cuda_error(ce);
     return ELUTQ_ERR_CUDA;
