@@ -8,8 +8,10 @@
 //              N, columns of tensor memory, 8 at least: a decoding batch wastes nothing but padding to 8, and a group's rest is as wide as it is.
 //   K          in steps of 256: 128 bytes of codes a row, one 128-byte swizzle atom wide, brought by TMA into a ring of stages.
 //   scales     are row-major, while the tensor core wants, per 128 rows and 4 scales, 512 bytes with row r's four at
-//              16 (r mod 32) + 4 (r / 32).  A warp per 128 rows holds rows l, l + 32, l + 64, l + 96 in lane l, loads two steps' scales of
-//              a row at a time, some pairs ahead (across tiles), and stores the four rows' words side by side (16 bytes, no conflicts).  The MMA warp copies
+//              16 (r mod 32) + 4 (r / 32).  Lane l of a warp loads some steps' scales of rows l, l + 32, l + 64, l + 96 and
+//              stores the four rows' words side by side (16 bytes, no conflicts).  The fence that makes a step's stores visible to the tensor core also
+//              waits for the thread's loads, so none of the next ones may be in flight: two warps per 128 rows take turns, one loads
+//              while the other stores (4096 x 28672 x 4096, NVFP4: 287 us with one that loaded ahead).  The MMA warp copies
 //              them to tensor memory (tcgen05.cp) in front of the step's MMAs; copies and MMAs of one thread run in order.
 //   sums       two accumulators; the epilogue warps empty one while the next tile fills the other.  256 tokens leave no room for two beside the
 //              scales: they overlap by 48 columns, which the epilogue empties first.
@@ -35,9 +37,13 @@ constexpr int kMaxStages = 10;
 constexpr int kMaxSplit = 8;
 constexpr int kMaxSplitTokens = 64;
 constexpr int kMaxGroups = 1024;
+// Steps of scales that a warp loads at once.  A warp may wait for a stage up to a turn and a ring ahead of what has been consumed, and a barrier's
+// parity tells two uses apart only within two rings: a turn is shorter than the ring (of 3 stages at least with NB = 2, of 5 with 1).
+template <int NB>
+constexpr int kTurnOf = NB == 2 ? 2 : 4;
 constexpr int kAcc1 = 208, kScaleCols = 464;     // second accumulator; scales (48 columns)
 constexpr int kSmem = 232448;
-constexpr uint32_t kWaitLimit = 1u << 22;
+constexpr unsigned long long kWaitNs = 1000000000ull;
 
 __device__ unsigned g_status;              // 0, or what a launch on this device gave up on
 
@@ -55,9 +61,9 @@ struct Mx4Args {
     int split;                 // CTAs that share a tile's K
     int stages;
     int x_box;                 // rows of one X load
-    int x_vec, w_vec;          // bytes of one load of scales
+    int x_wide, w_wide;        // scales of a row start on 16 bytes
     int test;                  // 1: no load is issued
-    uint32_t wait_limit;
+    uint32_t wait_limit;       // polls (tests); a wait of a second runs out whatever this is
 };
 
 enum { kBarFull = 0, kBarScales = kBarFull + kMaxStages, kBarEmpty = kBarScales + kMaxStages, kBarAccFull = kBarEmpty + kMaxStages, kBarAccFree = kBarAccFull + 2,
@@ -87,16 +93,34 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).  A poll may be suspended by
+// the hardware for some tens of microseconds, so the time is what counts.
+template <bool CLUSTER>
+__device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile const uint32_t* gave_up, uint32_t limit) {
+    if (try_wait<CLUSTER>(bar, parity)) return true;
+    unsigned long long since = 0;
+    for (uint32_t i = 1; i < limit; ++i) {
+        if (try_wait<CLUSTER>(bar, parity)) return true;
+        if ((i & 15u) == 0u) {
+            if (gave_up != nullptr && *gave_up) return false;
+            const unsigned long long t = now_ns();
+            if (since == 0) since = t;
+            else if (t - since > kWaitNs) return false;
+        }
+    }
+    return false;
+}
 // By a whole warp, with one answer for it: false once anything in the CTA has given up.
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t limit) {
-    bool ok = false, over = false;
-    for (uint32_t i = 0; i < limit && !ok && !over; ++i) {
-        ok = try_wait<CLUSTER>(bar, parity);
-        over = !ok && (i & 15u) == 15u && *gave_up;
-    }
+    const bool ok = poll<CLUSTER>(bar, parity, gave_up, limit);
     if (__all_sync(0xffffffffu, ok)) return true;
-    if (!ok && !over) {
+    if (!ok) {
         *gave_up = 1;
         atomicExch(&g_status, kStatusWaitExpired);
     }
@@ -182,37 +206,20 @@ struct Ring {
     }
 };
 
-// The scales of one row: two steps, WORDS words (4 MXFP4 or 8 NVFP4).  Bytes behind the row's end are 0.
-template <int WORDS>
-__device__ __forceinline__ void load_scales(uint32_t (&w)[WORDS], const uint8_t* row, int at, int end, int vec) {
-    if (vec == 16) {
-#pragma unroll
-        for (int i = 0; i < WORDS; i += 4) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (at + 4 * i < end) v = __ldg(reinterpret_cast<const uint4*>(row + at + 4 * i));
-            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
-        }
-    } else if (vec == 4) {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) w[i] = at + 4 * i < end ? __ldg(reinterpret_cast<const uint32_t*>(row + at + 4 * i)) : 0u;
-    } else if (vec == 2) {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            const int p = at + 4 * i;
-            const uint32_t lo = p < end ? __ldg(reinterpret_cast<const uint16_t*>(row + p)) : 0u;
-            const uint32_t hi = p + 2 < end ? __ldg(reinterpret_cast<const uint16_t*>(row + p + 2)) : 0u;
-            w[i] = lo | hi << 16;
-        }
+// Up to four scales at p, which may have any alignment: bytes from `end` on are 0, and nothing outside [lo, hi) is read.
+__device__ __forceinline__ uint32_t load_word(const uint8_t* p, const uint8_t* end, const uint8_t* lo, const uint8_t* hi) {
+    if (p >= end) return 0u;
+    const uint32_t shift = 8u * (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint8_t* q = p - shift / 8u;
+    uint32_t v = 0;
+    if (q >= lo && q + 8 <= hi) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
+        v = __funnelshift_r(__ldg(w), shift != 0u ? __ldg(w + 1) : 0u, shift);
+        if (end - p < 4) v &= (1u << (8 * (int)(end - p))) - 1u;
     } else {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            uint32_t v = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (at + 4 * i + b < end) v |= (uint32_t)__ldg(row + at + 4 * i + b) << (8 * b);
-            w[i] = v;
-        }
+        for (int i = 0; i < 4 && p + i < end; ++i) v |= (uint32_t)__ldg(p + i) << (8 * i);
     }
+    return v;
 }
 
 struct Tile {
@@ -298,10 +305,12 @@ __device__ __forceinline__ void store_y(const Mx4Args& a, long long at, float v)
     else reinterpret_cast<float*>(a.Y)[at] = v;
 }
 
-// NB: blocks of 128 tokens in a tile at most.  Warps: 0 loads codes, 1 issues MMAs, 2 weights' scales, 3 (and 8: tokens 128 to 255) activations' scales, 4 to 7 epilogue.
+// NB: blocks of 128 tokens in a tile at most.  Warps: 0 loads codes, 1 issues MMAs, 4 to 7 epilogue; scales in turn: 2 and 3 weights, 8 and 9 (10 and 11) tokens
+// 0 to 127 (128 to 255).
 template <int FMT, int CG, int NB>
-__global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
+__global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
     constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
+    constexpr int kTurn = kTurnOf<NB>;
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
@@ -398,7 +407,7 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
             for (int j = 0; j < min(issued, a.stages); ++j) {
                 if (r.i == 0) r.phase ^= 1u;
                 r.i = r.i == 0 ? a.stages - 1 : r.i - 1;
-                for (uint32_t n = 0; n < limit && !try_wait<false>(bar(kBarFull + r.i), r.phase); ++n) {}
+                poll<false>(bar(kBarFull + r.i), r.phase, nullptr, limit);
             }
         }
     } else if (warp == 1 && leader) {
@@ -454,77 +463,7 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
         if (!ok) {                             // what has been issued ends in front of the tensor memory's release
             if (elect_one()) commit<CG>(bar(kBarDrain));
             __syncwarp();
-            for (uint32_t k = 0; k < limit && !try_wait<false>(bar(kBarDrain), 0u); ++k) {}
-        }
-    } else if (warp == 2 || warp == 3 || warp == 8) {
-        const int block = warp == 2 ? 0 : warp == 3 ? 1 : 2;      // weights, tokens 0 to 127, 128 to 255
-        if (block <= NB) {
-            constexpr int WORDS = 2 * CH, AHEAD = FMT == ELUTQ_MX4_MXFP4 ? 4 : 3;      // pairs of steps in flight
-            Ring r(a.stages);
-            const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
-            const int vec = block == 0 ? a.w_vec : a.x_vec;
-            const long long last = block == 0 ? (long long)a.E * a.N - 1 : a.M - 1;
-            uint8_t* to = sS + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
-            const int pitch = block == 0 ? 512 : NB * 512;
-            const uint8_t* rows[4];
-            uint32_t w[AHEAD][4][WORDS];
-            int load_i = first, load_s = step0;                   // the next pair to load
-            auto aim = [&] {
-                if (load_i >= tiles) return;
-                const Tile t = tile_at<CG>(a, table, load_i);
-                const long long row0 = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, last) * a.sk;
-            };
-            auto load = [&](uint32_t (&v)[4][WORDS]) {
-                if (load_i >= tiles) return;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) load_scales<WORDS>(v[q], rows[q], load_s * 4 * CH, a.sk, vec);
-                load_s += 2;
-                if (load_s >= step1) {
-                    load_s = step0;
-                    load_i += stride;
-                    aim();
-                }
-            };
-            aim();
-#pragma unroll
-            for (int d = 0; d < AHEAD; ++d) load(w[d]);
-            bool ok = true;
-            int i = first, s = step0;
-            while (i < tiles && ok) {
-#pragma unroll
-                for (int d = 0; d < AHEAD; ++d) {
-                    if (i < tiles && ok) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (s + h < step1 && ok) {
-                                ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
-                                if (ok) {
-#pragma unroll
-                                    for (int c = 0; c < CH; ++c)
-                                        *reinterpret_cast<uint4*>(to + r.i * s_bytes + c * pitch) =
-                                            make_uint4(w[d][0][h * CH + c], w[d][1][h * CH + c], w[d][2][h * CH + c], w[d][3][h * CH + c]);
-                                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                                    __syncwarp();
-                                    if (lane == 0) {
-                                        if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
-                                        else arrive(bar(kBarScales + r.i));
-                                    }
-                                    __syncwarp();
-                                    r.next();
-                                }
-                            }
-                        }
-                        load(w[d]);
-                        s += 2;
-                        if (s >= step1) {
-                            s = step0;
-                            i += stride;
-                        }
-                    }
-                }
-            }
+            poll<false>(bar(kBarDrain), 0u, nullptr, limit);
         }
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;                             // lanes of tensor memory
@@ -576,26 +515,103 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
                 __syncwarp();
                 continue;
             }
-            // overlapping accumulators: the 48 columns that both have first, then the other one may be filled
-            const int shared = (kMaxTokens - kAcc1) / 16, turns = overlap ? kMaxTokens / 16 : (t.count + 15) / 16;
-            for (int k = 0; k < turns; ++k) {
-                const int g = !overlap || b == 1 ? k : k < shared ? kAcc1 / 16 + k : k - shared;
-                const int c0 = 16 * g;
+            // Overlapping accumulators: the 48 columns that both have go to registers first, then the other one may be filled.
+            auto columns = [&](int c0, auto count, auto&& then) {             // 16 count columns from c0 on
+                constexpr int N16 = decltype(count)::value;
+                uint32_t v[N16][16];
                 if (c0 < t.count) {
-                    uint32_t v[16];
-                    tmem_ld16(v, acc + c0);
-                    tmem_ld_wait(v);
-                    if (col < a.N) {
-                        const long long at = (long long)(t.t0 + c0) * a.N + col;
 #pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (c0 + c < t.count) store_y(a, at + (long long)c * a.N, __uint_as_float(v[c]) * alpha);
-                    }
-                    __syncwarp();
+                    for (int g = 0; g < N16; ++g) tmem_ld16(v[g], acc + c0 + 16 * g);
+#pragma unroll
+                    for (int g = 0; g < N16; ++g) tmem_ld_wait(v[g]);
                 }
-                if (overlap && k == shared - 1) release(b ^ 1);
+                then();
+                if (c0 < t.count && col < a.N) {
+                    const long long at = (long long)(t.t0 + c0) * a.N + col;
+                    auto put = [&](auto* y, auto&& cast) {
+#pragma unroll
+                        for (int c = 0; c < 16 * N16; ++c) {
+                            if (c0 + c < t.count) *y = cast(__uint_as_float(v[c / 16][c % 16]) * alpha);
+                            y += a.N;
+                        }
+                    };
+                    if (a.y_type == ELUTQ_TYPE_F16) put(reinterpret_cast<__half*>(a.Y) + at, [](float f) { return __float2half_rn(f); });
+                    else if (a.y_type == ELUTQ_TYPE_BF16) put(reinterpret_cast<__nv_bfloat16*>(a.Y) + at, [](float f) { return __float2bfloat16_rn(f); });
+                    else put(reinterpret_cast<float*>(a.Y) + at, [](float f) { return f; });
+                }
+                __syncwarp();
+            };
+            if (overlap) {
+                columns(b == 0 ? kAcc1 : 0, IntC<(kMaxTokens - kAcc1) / 16>{}, [&] { release(b ^ 1); });
+                const int c1 = b == 0 ? 0 : kMaxTokens - kAcc1;
+                for (int c0 = c1; c0 < c1 + kAcc1; c0 += 16) columns(c0, IntC<1>{}, [] {});
+            } else {
+                for (int c0 = 0; c0 < t.count; c0 += 16) columns(c0, IntC<1>{}, [] {});
+                release(b);
             }
-            if (!overlap) release(b);
+        }
+    } else {
+        const int block = warp < 4 ? 0 : (warp - 6) >> 1, mine = warp & 1;      // weights, tokens 0 to 127, 128 to 255
+        if (warp > 1 && block <= NB) {
+            Ring r(a.stages);
+            const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
+            const bool wide = block == 0 ? a.w_wide : a.x_wide;
+            const long long all = block == 0 ? (long long)a.E * a.N : a.M;
+            uint8_t* to = sS + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
+            const int pitch = block == 0 ? 512 : NB * 512;
+            int turn = 0;
+            bool ok = true;
+            for (int i = first; i < tiles && ok; i += stride) {
+                const Tile t = tile_at<CG>(a, table, i);
+                const long long row0 = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
+                const uint8_t* rows[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, all - 1) * a.sk;
+                for (int s = step0; s < step1 && ok; s += kTurn, turn ^= 1) {
+                    const int n = min(kTurn, step1 - s);
+                    if (turn != mine) {
+                        for (int h = 0; h < n; ++h) r.next();
+                        continue;
+                    }
+                    uint32_t w[4][kTurn * CH];
+                    const int at = s * 4 * CH;
+                    if (wide) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int k = 0; k < kTurn * CH; k += 4) {
+                                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                                if (at + 4 * k < a.sk) v = __ldg(reinterpret_cast<const uint4*>(rows[q] + at + 4 * k));
+                                w[q][k] = v.x; w[q][k + 1] = v.y; w[q][k + 2] = v.z; w[q][k + 3] = v.w;
+                            }
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int k = 0; k < kTurn * CH; ++k) w[q][k] = load_word(rows[q] + at + 4 * k, rows[q] + a.sk, base, base + all * a.sk);
+                    }
+#pragma unroll
+                    for (int h = 0; h < kTurn; ++h) {
+                        if (h < n && ok) {
+                            ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                            if (ok) {
+#pragma unroll
+                                for (int c = 0; c < CH; ++c)
+                                    *reinterpret_cast<uint4*>(to + r.i * s_bytes + c * pitch) =
+                                        make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                __syncwarp();
+                                if (lane == 0) {
+                                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
+                                    else arrive(bar(kBarScales + r.i));
+                                }
+                                __syncwarp();
+                                r.next();
+                            }
+                        }
+                    }
+                }
+            }
         }
     }
     __syncwarp();
@@ -608,19 +624,19 @@ __global__ void __launch_bounds__(288, 1) mx4_gemm_kernel(const __grid_constant_
     }
 }
 
-struct Plan { int cg, tokens, x_box, split, stages, grid; size_t smem; };
+struct Plan { int cg, tokens, x_box, split, stages, grid; size_t smem; bool ok; };
 
 constexpr int kFixed = kNumBars * 8 + 16;
 
-// Ring length and shared memory of a plan whose other fields are set; false if fewer than two stages fit.
+// Ring length and shared memory of a plan whose other fields are set; false if the ring is too short.
 bool fill_plan(Plan& p, int format, int E, bool grouped) {
-    const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4;
-    const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024 + (1 + (p.tokens + 127) / 128) * ch * 512;
+    const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4, nb = p.tokens > 128 || p.cg == 2 ? 2 : 1;
+    const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024 + (1 + nb) * ch * 512;
     const int fixed = kFixed + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
     p.stages = (kSmem - fixed) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.smem = (size_t)p.stages * stage + fixed;
-    return p.stages >= 2;
+    return p.stages > (nb == 2 ? kTurnOf<2> : kTurnOf<1>);
 }
 
 Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms) {
@@ -638,15 +654,10 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms)
                                    : (long long)((N + kTileW - 1) / kTileW) * n;
     if (p.tokens <= kMaxSplitTokens)
         while (p.split < kMaxSplit && most * p.split * 2 <= num_sms && p.split * 2 <= units) p.split *= 2;
-    fill_plan(p, format, E, grouped);
+    p.ok = fill_plan(p, format, E, grouped);
     const long long teams = num_sms / p.split;
     p.grid = (int)(most < teams ? most : teams) * p.split;
     return p;
-}
-
-int vec_of(const void* base, int row) {
-    const uintptr_t v = reinterpret_cast<uintptr_t>(base) | (uintptr_t)row;
-    return v % 16 == 0 ? 16 : v % 4 == 0 ? 4 : v % 2 == 0 ? 2 : 1;
 }
 
 int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int box) {
@@ -665,7 +676,7 @@ int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, cons
     if (e != cudaSuccess) return (int)e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);
-    cfg.blockDim = dim3(NB == 2 ? 288u : 256u);
+    cfg.blockDim = dim3(NB == 2 ? 384u : 320u);
     cfg.dynamicSmemBytes = p.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -698,6 +709,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     if (!mx4_aligned(x_codes, 16) || !mx4_aligned(w_codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(offsets, 4) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
     const bool grouped = offsets != nullptr;
     const Plan p = plan_for(M, N, K, E, format, grouped, device_sm_count());
+    if (!p.ok) return ELUTQ_ERR_UNSUPPORTED;
     Mx4Args a;
     a.x_scales = reinterpret_cast<const uint8_t*>(x_scales);
     a.w_scales = reinterpret_cast<const uint8_t*>(w_scales);
@@ -713,10 +725,10 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     a.split = p.split;
     a.stages = p.stages;
     a.x_box = p.x_box;
-    a.x_vec = vec_of(x_scales, a.sk);
-    a.w_vec = vec_of(w_scales, a.sk);
+    a.x_wide = mx4_aligned(x_scales, 16) && a.sk % 16 == 0;
+    a.w_wide = mx4_aligned(w_scales, 16) && a.sk % 16 == 0;
     a.test = test_limit != 0;
-    a.wait_limit = test_limit != 0 ? test_limit : kWaitLimit;
+    a.wait_limit = test_limit != 0 ? test_limit : 0xffffffffu;
     CUtensorMap xm, wm;
     int ce = tensor_map(&xm, x_codes, M, K, p.x_box);
     if (ce == 0) ce = tensor_map(&wm, w_codes, (long long)E * N, K, kTileW);

@@ -62,6 +62,21 @@ def test_large_batches(fmt, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("M,N,K", [(2048, 20000, 1440), (1000, 30000, 1024), (64, 57344, 2048), (16, 40000, 1056)])
+def test_many_tiles_and_steps_for_each_sm(fmt, M, N, K):
+    """Rings and accumulators used many times over; some of the rows are compared."""
+    rng = np.random.default_rng(M + fmt)
+    xc, xs = _matrix(rng, M, K, fmt)
+    wc, ws = _matrix(rng, N, K, fmt)
+    Y = torch.full((M, N), float("nan"), device="cuda")
+    elutq.elutq_mx4_gemm(*_dev(xc, xs, wc, ws), Y, M, N, K, fmt)
+    assert elutq.elutq_device_status() == 0
+    assert not torch.isnan(Y).any()
+    rows = np.unique(np.concatenate([[0, M - 1], rng.integers(0, M, 14)]))
+    _assert_close(Y[torch.from_numpy(rows).cuda()], mx4.matmul(xc[rows], xs[rows], wc, ws, fmt), mx4.magnitude(xc[rows], xs[rows], wc, ws, fmt), K, "f32")
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("M,N,K", [(1, 1000, 1024), (5, 77, 1536), (70, 259, 512), (300, 300, 512)])
 def test_output_types_and_alpha(fmt, out, M, N, K):
