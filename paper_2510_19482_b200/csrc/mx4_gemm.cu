@@ -66,7 +66,7 @@ struct Mx4Args {
     uint32_t wait_limit;       // polls (tests); a wait of a second runs out whatever this is
 };
 
-enum { kBarFull = 0, kBarScales = kBarFull + kMaxStages, kBarEmpty = kBarScales + kMaxStages, kBarAccFull = kBarEmpty + kMaxStages, kBarAccFree = kBarAccFull + 2,
+enum { kBarFull = 0, kBarEmpty = kBarFull + kMaxStages, kBarAccFull = kBarEmpty + kMaxStages, kBarAccFree = kBarAccFull + 2,
        kBarPartsFull = kBarAccFree + 2, kBarPartsFree, kBarDrain, kNumBars };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -76,7 +76,11 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
-__device__ __forceinline__ void arrive_cluster(uint32_t bar) {       // bar: a shared::cluster address
+// On a barrier of another CTA (a shared::cluster address).  arrive_cluster orders this thread's accesses to shared memory for the cluster, which
+// waits for its accesses to global memory too; arrive_remote does not, and is for what a proxy or tcgen05 fence has made visible
+// (with the former, a step's scales took 1500 cycles in pairs of CTAs: 4096 x 28672 x 4096, MXFP4 288 us against SECOND).
+__device__ __forceinline__ void arrive_remote(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 __device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
@@ -113,6 +117,14 @@ __device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile con
             else if (t - since > kWaitNs) return false;
         }
     }
+    return false;
+}
+// The same by one thread, which says so when it gives up.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait_alone(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t limit) {
+    if (poll<CLUSTER>(bar, parity, gave_up, limit)) return true;
+    *gave_up = 1;
+    atomicExch(&g_status, kStatusWaitExpired);
     return false;
 }
 // By a whole warp, with one answer for it: false once anything in the CTA has given up.
@@ -206,20 +218,29 @@ struct Ring {
     }
 };
 
-// Up to four scales at p, which may have any alignment: bytes from `end` on are 0, and nothing outside [lo, hi) is read.
-__device__ __forceinline__ uint32_t load_word(const uint8_t* p, const uint8_t* end, const uint8_t* lo, const uint8_t* hi) {
-    if (p >= end) return 0u;
+// WORDS words of a row's scales from p on, p of any alignment: bytes from `end` on are 0, and nothing outside [lo, hi) is read.  By a whole warp.
+template <int WORDS>
+__device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const uint8_t* p, const uint8_t* end, const uint8_t* lo, const uint8_t* hi) {
     const uint32_t shift = 8u * (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
     const uint8_t* q = p - shift / 8u;
-    uint32_t v = 0;
-    if (q >= lo && q + 8 <= hi) {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
-        v = __funnelshift_r(__ldg(w), shift != 0u ? __ldg(w + 1) : 0u, shift);
-        if (end - p < 4) v &= (1u << (8 * (int)(end - p))) - 1u;
+    if (__all_sync(0xffffffffu, q >= lo && q + 4 * (WORDS + 1) <= hi)) {          // all but a matrix's ends
+        uint32_t v[WORDS + 1];
+#pragma unroll
+        for (int i = 0; i <= WORDS; ++i) v[i] = __ldg(reinterpret_cast<const uint32_t*>(q) + i);
+        const int left = (int)(end - p);
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            w[i] = __funnelshift_r(v[i], v[i + 1], shift);
+            if (left < 4 * i + 4) w[i] &= left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1u;
+        }
     } else {
-        for (int i = 0; i < 4 && p + i < end; ++i) v |= (uint32_t)__ldg(p + i) << (8 * i);
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            uint32_t v = 0;
+            for (int b = 0; b < 4 && p + 4 * i + b < end; ++b) v |= (uint32_t)__ldg(p + 4 * i + b) << (8 * b);
+            w[i] = v;
+        }
     }
-    return v;
 }
 
 struct Tile {
@@ -342,8 +363,7 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
     if (threadIdx.x == 0) {
         auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
         for (int i = 0; i < a.stages; ++i) {
-            init(kBarFull + i, 1);
-            init(kBarScales + i, CG * (1 + NB));
+            init(kBarFull + i, 1 + CG * (1 + NB));        // the loads; the scales of each 128 rows
             init(kBarEmpty + i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -358,14 +378,16 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
         asm volatile("prefetch.tensormap [%0];" :: "l"(&x_map) : "memory");
         asm volatile("prefetch.tensormap [%0];" :: "l"(&w_map) : "memory");
     }
-    __syncwarp();
-    grid_dependency_wait();
-    grid_launch_dependents();
-    if (a.offsets != nullptr && warp == 0) list_groups(a, table);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (CG == 2 || a.split > 1) cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (a.offsets != nullptr) {
+        if (warp == 0) list_groups(a, table);
+        __syncthreads();
+    }
     const uint32_t tmem = *tmem_slot;
 
     const int team = CG == 2 ? 2 : a.split;                       // CTAs that work on one tile
@@ -377,93 +399,93 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
     const int step1 = CG == 2 ? a.steps : min(a.steps, 2 * (int)((long long)pairs * (rank + 1) / a.split));
     const uint32_t limit = a.wait_limit;
 
+    // One lane runs the whole loop of the loads and of the MMAs: with all of a warp in it and a choice at every step, the MMA
+    // warp took 900 cycles a step of at least 512, half of them in waits that were over (4096 x 28672 x 4096, MXFP4: 224 us).
     if (warp == 0) {
-        Ring r(a.stages);
-        int issued = 0;
-        bool ok = true;
-        for (int i = first; i < tiles && ok; i += stride) {
-            const Tile t = tile_at<CG>(a, table, i);
-            const int per_cta = CG == 2 ? (t.count + 15) / 16 * 8 : (t.count + 7) / 8 * 8;
-            const int boxes = (per_cta + a.x_box - 1) / a.x_box;
-            const int w_row = t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0), x_row = t.t0 + (CG == 2 ? (int)rank * per_cta : 0);
-            const uint32_t bytes = CG * (w_bytes + boxes * a.x_box * kStepBytes);
-            for (int s = step0; s < step1; ++s) {
-                ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
-                if (!ok) break;
-                if (elect_one() && !a.test) {
+        if (elect_one() && !a.test) {
+            Ring r(a.stages);
+            int issued = 0;
+            bool ok = true;
+            for (int i = first; i < tiles && ok; i += stride) {
+                const Tile t = tile_at<CG>(a, table, i);
+                const int per_cta = CG == 2 ? (t.count + 15) / 16 * 8 : (t.count + 7) / 8 * 8;
+                const int boxes = (per_cta + a.x_box - 1) / a.x_box;
+                const int w_row = t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0), x_row = t.t0 + (CG == 2 ? (int)rank * per_cta : 0);
+                const uint32_t bytes = CG * (w_bytes + boxes * a.x_box * kStepBytes);
+                for (int s = step0; s < step1; ++s) {
+                    ok = wait_alone(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                    if (!ok) break;
                     const uint32_t full = CG == 2 ? at_rank(bar(kBarFull + r.i), 0) : bar(kBarFull + r.i);
                     if (leader) expect(bar(kBarFull + r.i), bytes);
                     tma_load<CG>(smem_u32(sW + r.i * w_bytes), &w_map, s * kStepBytes, w_row, full);
                     for (int b = 0; b < boxes; ++b)
                         tma_load<CG>(smem_u32(sX + r.i * x_bytes + b * a.x_box * kStepBytes), &x_map, s * kStepBytes, x_row + b * a.x_box, full);
+                    ++issued;
+                    r.next();
                 }
-                __syncwarp();
-                ++issued;
-                r.next();
             }
-        }
-        // a wait ran out: copies in flight still land (each stage's last ones), in front of the CTA's end
-        if (!ok && leader && !a.test) {
-            for (int j = 0; j < min(issued, a.stages); ++j) {
-                if (r.i == 0) r.phase ^= 1u;
-                r.i = r.i == 0 ? a.stages - 1 : r.i - 1;
-                poll<false>(bar(kBarFull + r.i), r.phase, nullptr, limit);
+            // a wait ran out: copies in flight still land (each stage's last ones), in front of the CTA's end
+            if (!ok && leader) {
+                for (int j = 0; j < min(issued, a.stages); ++j) {
+                    if (r.i == 0) r.phase ^= 1u;
+                    r.i = r.i == 0 ? a.stages - 1 : r.i - 1;
+                    poll<false>(bar(kBarFull + r.i), r.phase, nullptr, limit);
+                }
             }
         }
     } else if (warp == 1 && leader) {
-        Ring r(a.stages);
-        const bool overlap = a.tokens > kAcc1;
-        int n = 0;
-        bool ok = true;
-        for (int i = first; i < tiles && ok; i += stride, ++n) {
-            const Tile t = tile_at<CG>(a, table, i);
-            const int b = n & 1, use = n >> 1;
-            if (overlap) ok = n == 0 || wait<CG == 2>(bar(kBarAccFree + b), (uint32_t)(b == 1 ? use : use - 1) & 1u, gave_up, limit);
-            else ok = wait<CG == 2>(bar(kBarAccFree + b), ((uint32_t)use & 1u) ^ 1u, gave_up, limit);
-            if (!ok) break;
-            const int cols = CG == 2 ? (t.count + 15) / 16 * 16 : (t.count + 7) / 8 * 8;
-            const uint32_t idesc = 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (FMT == ELUTQ_MX4_MXFP4 ? 1u << 23 : 0u) | (uint32_t)(CG * kTileW >> 4) << 24;
-            const uint32_t acc = tmem + (b ? kAcc1 : 0), sa = tmem + kScaleCols, sb = sa + 4 * CH;
-            for (int s = step0; s < step1; ++s) {
-                ok = wait<CG == 2>(bar(kBarFull + r.i), r.phase, gave_up, limit) && wait<CG == 2>(bar(kBarScales + r.i), r.phase, gave_up, limit);
+        if (elect_one()) {
+            Ring r(a.stages);
+            const bool overlap = a.tokens > kAcc1;
+            const uint32_t sa = tmem + kScaleCols, sb = sa + 4 * CH;
+            const uint64_t da0 = operand_desc(smem_u32(sW)), db0 = operand_desc(smem_u32(sX)), ds0 = scales_desc(smem_u32(sS));
+            const int whole = a.K / 256;                          // steps of four MMAs
+            int n = 0;
+            bool ok = true;
+            for (int i = first; i < tiles && ok; i += stride, ++n) {
+                const Tile t = tile_at<CG>(a, table, i);
+                const int b = n & 1, use = n >> 1;
+                if (overlap) ok = n == 0 || wait_alone<CG == 2>(bar(kBarAccFree + b), (uint32_t)(b == 1 ? use : use - 1) & 1u, gave_up, limit);
+                else ok = wait_alone<CG == 2>(bar(kBarAccFree + b), ((uint32_t)use & 1u) ^ 1u, gave_up, limit);
                 if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint64_t da = operand_desc(smem_u32(sW + r.i * w_bytes)), db = operand_desc(smem_u32(sX + r.i * x_bytes));
-                const uint32_t ss = smem_u32(sS + r.i * s_bytes);
-                const int parts64 = min(4, (a.K - s * 256 + 63) / 64);
-                if (elect_one()) {
+                const int cols = CG == 2 ? (t.count + 15) / 16 * 16 : (t.count + 7) / 8 * 8;
+                const uint32_t idesc = 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (FMT == ELUTQ_MX4_MXFP4 ? 1u << 23 : 0u) | (uint32_t)(CG * kTileW >> 4) << 24;
+                const uint32_t acc = tmem + (b ? kAcc1 : 0);
+                for (int s = step0; s < step1; ++s) {
+                    ok = wait_alone<CG == 2>(bar(kBarFull + r.i), r.phase, gave_up, limit);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t da = da0 + (uint32_t)(r.i * w_bytes >> 4), db = db0 + (uint32_t)(r.i * x_bytes >> 4), ds = ds0 + (uint32_t)(r.i * s_bytes >> 4);
 #pragma unroll
                     for (int c = 0; c < CH; ++c) {
-                        copy_scales<CG>(sa + 4 * c, scales_desc(ss + c * 512));
+                        copy_scales<CG>(sa + 4 * c, ds + c * 32);
 #pragma unroll
-                        for (int h = 0; h < NB; ++h) copy_scales<CG>(sb + 4 * (c * NB + h), scales_desc(ss + (CH + c * NB + h) * 512));
+                        for (int h = 0; h < NB; ++h) copy_scales<CG>(sb + 4 * (c * NB + h), ds + (CH + c * NB + h) * 32);
                     }
-                    // (no condition around a whole step's MMAs: each costs their issue)
                     auto step_mma = [&](int j, uint32_t accumulate) {
                         const int c = j / SUB;
                         const uint32_t id = (uint32_t)(j % SUB) * 2u;             // which of the group's scales
                         mma<FMT, CG>(acc, da + 2 * j, db + 2 * j, idesc | id << 29 | id << 4, sa + 4 * c, sb + 4 * c * NB, accumulate);
                     };
                     step_mma(0, s > step0);
-                    if (parts64 == 4) {
+                    if (s < whole) {
                         step_mma(1, 1);
                         step_mma(2, 1);
                         step_mma(3, 1);
                     } else {
-                        if (parts64 > 1) step_mma(1, 1);
-                        if (parts64 > 2) step_mma(2, 1);
+                        if (a.K - s * 256 > 64) step_mma(1, 1);
+                        if (a.K - s * 256 > 128) step_mma(2, 1);
+                        if (a.K - s * 256 > 192) step_mma(3, 1);
                     }
                     commit<CG>(bar(kBarEmpty + r.i));
-                    if (s == step1 - 1) commit<CG>(bar(kBarAccFull + b));
+                    r.next();
                 }
-                __syncwarp();
-                r.next();
+                if (ok) commit<CG>(bar(kBarAccFull + b));
             }
-        }
-        if (!ok) {                             // what has been issued ends in front of the tensor memory's release
-            if (elect_one()) commit<CG>(bar(kBarDrain));
-            __syncwarp();
-            poll<false>(bar(kBarDrain), 0u, nullptr, limit);
+            if (!ok) {                         // what has been issued ends in front of the tensor memory's release
+                commit<CG>(bar(kBarDrain));
+                poll<false>(bar(kBarDrain), 0u, nullptr, limit);
+            }
         }
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;                             // lanes of tensor memory
@@ -484,7 +506,7 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarAccFree + which), 0));
+                    if constexpr (CG == 2) arrive_remote(at_rank(bar(kBarAccFree + which), 0));
                     else arrive(bar(kBarAccFree + which));
                 }
                 __syncwarp();
@@ -586,9 +608,7 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                             }
                     } else {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int k = 0; k < kTurn * CH; ++k) w[q][k] = load_word(rows[q] + at + 4 * k, rows[q] + a.sk, base, base + all * a.sk);
+                        for (int q = 0; q < 4; ++q) load_words(w[q], rows[q] + at, rows[q] + a.sk, base, base + all * a.sk);
                     }
 #pragma unroll
                     for (int h = 0; h < kTurn; ++h) {
@@ -602,8 +622,8 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                                 __syncwarp();
                                 if (lane == 0) {
-                                    if constexpr (CG == 2) arrive_cluster(at_rank(bar(kBarScales + r.i), 0));
-                                    else arrive(bar(kBarScales + r.i));
+                                    if constexpr (CG == 2) arrive_remote(at_rank(bar(kBarFull + r.i), 0));
+                                    else arrive(bar(kBarFull + r.i));
                                 }
                                 __syncwarp();
                                 r.next();
@@ -639,6 +659,12 @@ bool fill_plan(Plan& p, int format, int E, bool grouped) {
     return p.stages > (nb == 2 ? kTurnOf<2> : kTurnOf<1>);
 }
 
+#ifdef MX4_TUNE
+}
+extern "C" { int mx4_force_cg = 0, mx4_force_tokens = 0, mx4_force_split = 0; }
+namespace {
+#endif
+
 Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms) {
     Plan p = {};
     const int units = (K + 511) / 512;
@@ -649,14 +675,26 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms)
     const int n = (per + kMaxTokens - 1) / kMaxTokens;
     p.tokens = ((per + n - 1) / n + 7) / 8 * 8;
     if (p.tokens > 32) p.tokens = (p.tokens + 31) / 32 * 32;
-    p.x_box = grouped ? (p.tokens > 32 ? 32 : p.tokens) : p.tokens;
-    const long long most = grouped ? (long long)((N + kTileW - 1) / kTileW) * ((M + p.tokens - 1) / p.tokens + (E < M ? E : M))
-                                   : (long long)((N + kTileW - 1) / kTileW) * n;
-    if (p.tokens <= kMaxSplitTokens)
-        while (p.split < kMaxSplit && most * p.split * 2 <= num_sms && p.split * 2 <= units) p.split *= 2;
+    if (!grouped && M > 128 && N > 128) p.cg = 2;
+#ifdef MX4_TUNE
+    if (mx4_force_cg) p.cg = mx4_force_cg;
+    if (mx4_force_tokens) p.tokens = mx4_force_tokens;
+#endif
+    if (p.cg == 2) p.tokens = (p.tokens + 15) / 16 * 16;
+    p.x_box = grouped ? (p.tokens > 32 ? 32 : p.tokens) : p.tokens / p.cg;
+    if (grouped && p.cg == 2) p.x_box = p.tokens > 64 ? 32 : p.tokens / 2;
+    const int rows = kTileW * p.cg;
+    const long long most = grouped ? (long long)((N + rows - 1) / rows) * ((M + p.tokens - 1) / p.tokens + (E < M ? E : M))
+                                   : (long long)((N + rows - 1) / rows) * ((M + p.tokens - 1) / p.tokens);
+    if (p.tokens <= kMaxSplitTokens && p.cg == 1)
+        while (p.split < kMaxSplit && most * (p.split + 1) <= num_sms && p.split + 1 <= units) ++p.split;
+#ifdef MX4_TUNE
+    if (mx4_force_split) p.split = mx4_force_split;
+#endif
     p.ok = fill_plan(p, format, E, grouped);
-    const long long teams = num_sms / p.split;
-    p.grid = (int)(most < teams ? most : teams) * p.split;
+    const int team = p.cg == 2 ? 2 : p.split;
+    const long long teams = p.cg == 2 ? num_sms / 2 : p.split > 1 ? resident_clusters(p.split) : num_sms;
+    p.grid = (int)(most < teams ? most : teams) * team;
     return p;
 }
 
