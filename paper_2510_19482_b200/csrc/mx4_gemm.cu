@@ -37,12 +37,19 @@ constexpr int kMaxStages = 10;
 constexpr int kMaxSplit = 8;
 constexpr int kMaxSplitTokens = 64;
 constexpr int kMaxGroups = 1024;
-// Steps of scales that a warp loads at once.  A warp may wait for a stage up to a turn and a ring ahead of what has been consumed, and a barrier's
-// parity tells two uses apart only within two rings: a turn is shorter than the ring (of 3 stages at least with NB = 2, of 5 with 1).
+// The warps of 128 rows' scales take turns of so many steps.  A warp whose turn has come may wait for a use of a stage that is (turns - 1) * steps +
+// stages ahead of what has been consumed, and a barrier's parity tells uses apart only within two rings: the first term has to be less than
+// the ring's length.
 template <int NB>
-constexpr int kTurnOf = NB == 2 ? 2 : 4;
-constexpr int kAcc1 = 208, kScaleCols = 464;     // second accumulator; scales (48 columns)
+constexpr int kTurns = NB == 2 ? 3 : 2;
+template <int NB>
+constexpr int kTurnSteps = NB == 2 ? 2 : 4;
+template <int NB>
+constexpr int kThreads = 32 * (6 + (1 + NB) * kTurns<NB>);
+constexpr int kAcc1 = kMaxTokens - 48, kScaleCols = 2 * kMaxTokens - 48;     // second accumulator, which shares 48 columns with the first; scales (48 columns)
 constexpr int kSmem = 232448;
+constexpr int kChunk = kMaxTokens - kAcc1;        // columns that the epilogue takes at once
+constexpr int kTurnBytes = 4 * kChunk * 64;      // 32 weight rows of them for each epilogue warp, 16 bits each
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
 __device__ unsigned g_status;              // 0, or what a launch on this device gave up on
@@ -61,6 +68,7 @@ struct Mx4Args {
     int split;                 // CTAs that share a tile's K
     int stages;
     int x_box;                 // rows of one X load
+    int turn;                  // the epilogue turns 16-bit results in shared memory
     int x_wide, w_wide;        // scales of a row start on 16 bytes
     int test;                  // 1: no load is issued
     uint32_t wait_limit;       // polls (tests); a wait of a second runs out whatever this is
@@ -208,6 +216,16 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16]) {     // names t
                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
 
+// 16 lanes of tensor memory x 16 columns, as fragments: a thread's registers 0 and 1 hold row lane / 4, columns 2 (lane mod 4) and one more, 2 and 3 the same of
+// row lane / 4 + 8, 4 to 7 the same 8 columns on.
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t* r, uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void store_transposed(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" :: "r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
 // A ring's stage and the parity of its use
 struct Ring {
     int len, i = 0;
@@ -326,12 +344,13 @@ __device__ __forceinline__ void store_y(const Mx4Args& a, long long at, float v)
     else reinterpret_cast<float*>(a.Y)[at] = v;
 }
 
-// NB: blocks of 128 tokens in a tile at most.  Warps: 0 loads codes, 1 issues MMAs, 4 to 7 epilogue; scales in turn: 2 and 3 weights, 8 and 9 (10 and 11) tokens
-// 0 to 127 (128 to 255).
-template <int FMT, int CG, int NB>
-__global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
+// CG: CTAs of a pair; NB: blocks of 128 tokens in a tile at most (pairs: two).  Warps: 0 loads codes, 1 issues MMAs, 4 to 7 epilogue, 2, 3 and 8 on scales, kTurns for the weights, then
+// for tokens 0 to 127, then for 128 to 255.
+template <int FMT, int CG>
+__global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
     constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
-    constexpr int kTurn = kTurnOf<NB>;
+    constexpr int NB = CG;
+    constexpr int kTurn = kTurnSteps<NB>, TURNS = kTurns<NB>;
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
@@ -340,7 +359,8 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
     uint8_t* sX = sW + a.stages * w_bytes;
     uint8_t* sS = sX + a.stages * x_bytes;
     float* parts = reinterpret_cast<float*>(sS + a.stages * s_bytes);                 // [tokens][128], clusters only
-    uint64_t* bars = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(parts) + (a.split > 1 ? a.tokens * kTileW * 4 : 0));
+    uint8_t* sT = reinterpret_cast<uint8_t*>(parts) + (a.split > 1 ? a.tokens * kTileW * 4 : 0);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(sT + (a.turn ? kTurnBytes : 0));
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
     volatile uint32_t* gave_up = tmem_slot + 1;
     int* table = reinterpret_cast<int*>(tmem_slot + 2);
@@ -537,23 +557,23 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                 __syncwarp();
                 continue;
             }
-            // Overlapping accumulators: the 48 columns that both have go to registers first, then the other one may be filled.
-            auto columns = [&](int c0, auto count, auto&& then) {             // 16 count columns from c0 on
-                constexpr int N16 = decltype(count)::value;
-                uint32_t v[N16][16];
-                if (c0 < t.count) {
+            // 48 columns at a time, whose reads of tensor memory are all in flight together (16 at a time took 11000 cycles for 256 beside
+            // MMAs that needed 8200).  Overlapping accumulators: the 48 that both have come first; once they are in registers the other
+            // accumulator may be filled.
+            constexpr int G = kChunk / 16;
+            auto columns = [&](int c0, int end, auto&& then) {
+                uint32_t v[G][16];
 #pragma unroll
-                    for (int g = 0; g < N16; ++g) tmem_ld16(v[g], acc + c0 + 16 * g);
+                for (int g = 0; g < G; ++g) tmem_ld16(v[g], acc + c0 + 16 * g);       // (columns behind the last one are not used)
 #pragma unroll
-                    for (int g = 0; g < N16; ++g) tmem_ld_wait(v[g]);
-                }
+                for (int g = 0; g < G; ++g) tmem_ld_wait(v[g]);
                 then();
-                if (c0 < t.count && col < a.N) {
+                if (col < a.N) {
                     const long long at = (long long)(t.t0 + c0) * a.N + col;
                     auto put = [&](auto* y, auto&& cast) {
 #pragma unroll
-                        for (int c = 0; c < 16 * N16; ++c) {
-                            if (c0 + c < t.count) *y = cast(__uint_as_float(v[c / 16][c % 16]) * alpha);
+                        for (int c = 0; c < kChunk; ++c) {
+                            if (c0 + c < end) *y = cast(__uint_as_float(v[c / 16][c % 16]) * alpha);
                             y += a.N;
                         }
                     };
@@ -563,18 +583,70 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                 }
                 __syncwarp();
             };
-            if (overlap) {
-                columns(b == 0 ? kAcc1 : 0, IntC<(kMaxTokens - kAcc1) / 16>{}, [&] { release(b ^ 1); });
-                const int c1 = b == 0 ? 0 : kMaxTokens - kAcc1;
-                for (int c0 = c1; c0 < c1 + kAcc1; c0 += 16) columns(c0, IntC<1>{}, [] {});
-            } else {
-                for (int c0 = 0; c0 < t.count; c0 += 16) columns(c0, IntC<1>{}, [] {});
-                release(b);
-            }
+            // The same for 16-bit results whose rows start on 16 bytes: fragments are stored transposed, a block of 16 tokens x 32 weight rows at a time, read
+            // back as 16 bytes of a token's row and stored so: 2 stores of 8 x 64 bytes instead of 16 of 64.  The 16-byte pieces of two tokens'
+            // rows share a line of 128 bytes, in an order by the line's number: no conflicts either way.
+            auto columns_turned = [&](int c0, int end, auto&& then, auto half) {
+                uint32_t v[G][16];
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    tmem_ld_fragments(v[g], acc + c0 + 16 * g);
+                    tmem_ld_fragments(v[g] + 8, acc + (16u << 16) + c0 + 16 * g);
+                }
+#pragma unroll
+                for (int g = 0; g < G; ++g) tmem_ld_wait(v[g]);
+                then();
+                auto two = [&](uint32_t x, uint32_t y) -> uint32_t {
+                    const float fx = __uint_as_float(x) * alpha, fy = __uint_as_float(y) * alpha;
+                    if constexpr (decltype(half)::value) {
+                        const __half2 h = __floats2half2_rn(fx, fy);
+                        return *reinterpret_cast<const uint32_t*>(&h);
+                    } else {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(fx, fy);
+                        return *reinterpret_cast<const uint32_t*>(&h);
+                    }
+                };
+                uint8_t* mine = sT + quarter * (kChunk * 64);
+                const int token = 8 * (lane >> 4) + (lane & 7), piece = (lane >> 3) & 1;      // where this lane's row of a matrix goes
+                const uint32_t to = smem_u32(mine + token * 64 + ((piece ^ ((token >> 1) & 3)) * 16));
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        store_transposed((to + g * 1024) ^ (32u * h), two(v[g][8 * h], v[g][8 * h + 1]), two(v[g][8 * h + 2], v[g][8 * h + 3]),
+                                         two(v[g][8 * h + 4], v[g][8 * h + 5]), two(v[g][8 * h + 6], v[g][8 * h + 7]));
+                __syncwarp();
+                const int col0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32 + 8 * (lane & 3);
+                const uint8_t* from = mine + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
+                uint4 y[2 * G];
+#pragma unroll
+                for (int k = 0; k < 2 * G; ++k) y[k] = *reinterpret_cast<const uint4*>(from + 512 * k);
+                uint16_t* row = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0 + (lane >> 2)) * a.N + col0;
+                const int rest = col0 < a.N ? end - c0 - (lane >> 2) : 0;
+#pragma unroll
+                for (int k = 0; k < 2 * G; ++k) {
+                    if (8 * k < rest) *reinterpret_cast<uint4*>(row) = y[k];
+                    row += 8 * a.N;
+                }
+                __syncwarp();
+            };
+            auto all_columns = [&](auto&& some) {
+                if (overlap) {
+                    const int c0 = b == 0 ? kAcc1 : 0, c1 = b == 0 ? 0 : kChunk, end = min(t.count, c1 + kAcc1);
+                    some(c0, min(t.count, c0 + kChunk), [&] { release(b ^ 1); });
+                    for (int c = c1; c < end; c += kChunk) some(c, end, [] {});
+                } else {
+                    for (int c = 0; c < t.count; c += kChunk) some(c, t.count, [] {});
+                    release(b);
+                }
+            };
+            if (!a.turn) all_columns(columns);
+            else if (a.y_type == ELUTQ_TYPE_F16) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, IntC<1>{}); });
+            else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, IntC<0>{}); });
         }
     } else {
-        const int block = warp < 4 ? 0 : (warp - 6) >> 1, mine = warp & 1;      // weights, tokens 0 to 127, 128 to 255
-        if (warp > 1 && block <= NB) {
+        const int helper = warp < 4 ? warp - 2 : warp - 6, block = helper / TURNS, mine = helper % TURNS;      // weights, tokens 0 to 127, 128 to 255
+        if (helper >= 0 && block <= NB) {
             Ring r(a.stages);
             const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
             const bool wide = block == 0 ? a.w_wide : a.x_wide;
@@ -589,7 +661,7 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
                 const uint8_t* rows[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, all - 1) * a.sk;
-                for (int s = step0; s < step1 && ok; s += kTurn, turn ^= 1) {
+                for (int s = step0; s < step1 && ok; s += kTurn, turn = turn + 1 == TURNS ? 0 : turn + 1) {
                     const int n = min(kTurn, step1 - s);
                     if (turn != mine) {
                         for (int h = 0; h < n; ++h) r.next();
@@ -644,19 +716,19 @@ __global__ void __launch_bounds__(NB == 2 ? 384 : 320, 1) mx4_gemm_kernel(const 
     }
 }
 
-struct Plan { int cg, tokens, x_box, split, stages, grid; size_t smem; bool ok; };
+struct Plan { int cg, tokens, x_box, split, stages, grid, turn; size_t smem; bool ok; };
 
 constexpr int kFixed = kNumBars * 8 + 16;
 
 // Ring length and shared memory of a plan whose other fields are set; false if the ring is too short.
 bool fill_plan(Plan& p, int format, int E, bool grouped) {
-    const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4, nb = p.tokens > 128 || p.cg == 2 ? 2 : 1;
+    const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4, nb = p.cg;
     const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024 + (1 + nb) * ch * 512;
-    const int fixed = kFixed + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
+    const int fixed = kFixed + (p.turn ? kTurnBytes : 0) + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
     p.stages = (kSmem - fixed) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.smem = (size_t)p.stages * stage + fixed;
-    return p.stages > (nb == 2 ? kTurnOf<2> : kTurnOf<1>);
+    return p.stages > (nb == 2 ? (kTurns<2> - 1) * kTurnSteps<2> : (kTurns<1> - 1) * kTurnSteps<1>);
 }
 
 #ifdef MX4_TUNE
@@ -665,7 +737,7 @@ extern "C" { int mx4_force_cg = 0, mx4_force_tokens = 0, mx4_force_split = 0; }
 namespace {
 #endif
 
-Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms) {
+Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int y_type, int num_sms) {
     Plan p = {};
     const int units = (K + 511) / 512;
     p.cg = 1;
@@ -675,7 +747,7 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms)
     const int n = (per + kMaxTokens - 1) / kMaxTokens;
     p.tokens = ((per + n - 1) / n + 7) / 8 * 8;
     if (p.tokens > 32) p.tokens = (p.tokens + 31) / 32 * 32;
-    if (!grouped && M > 128 && N > 128) p.cg = 2;
+    if (p.tokens > 128) p.cg = 2;
 #ifdef MX4_TUNE
     if (mx4_force_cg) p.cg = mx4_force_cg;
     if (mx4_force_tokens) p.tokens = mx4_force_tokens;
@@ -691,6 +763,7 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int num_sms)
 #ifdef MX4_TUNE
     if (mx4_force_split) p.split = mx4_force_split;
 #endif
+    p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && N % 8 == 0;
     p.ok = fill_plan(p, format, E, grouped);
     const int team = p.cg == 2 ? 2 : p.split;
     const long long teams = p.cg == 2 ? num_sms / 2 : p.split > 1 ? resident_clusters(p.split) : num_sms;
@@ -708,13 +781,13 @@ int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int bo
                ? 0 : (int)cudaErrorInvalidValue;
 }
 
-template <int FMT, int CG, int NB>
+template <int FMT, int CG>
 int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return (int)e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);
-    cfg.blockDim = dim3(NB == 2 ? 384u : 320u);
+    cfg.blockDim = dim3((unsigned)kThreads<CG>);
     cfg.dynamicSmemBytes = p.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -725,15 +798,14 @@ int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, cons
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CG == 2 || p.split > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<FMT, CG, NB>, xm, wm, a);
+    e = cudaLaunchKernelEx(&cfg, mx4_gemm_kernel<FMT, CG>, xm, wm, a);
     if (e == cudaSuccess) count_launch(1);
     return (int)e;
 }
 
 template <int FMT>
 int launch_format(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
-    if (p.cg == 2) return launch_mx4<FMT, 2, 2>(p, xm, wm, a, stream);
-    return p.tokens > 128 ? launch_mx4<FMT, 1, 2>(p, xm, wm, a, stream) : launch_mx4<FMT, 1, 1>(p, xm, wm, a, stream);
+    return p.cg == 2 ? launch_mx4<FMT, 2>(p, xm, wm, a, stream) : launch_mx4<FMT, 1>(p, xm, wm, a, stream);
 }
 
 int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, const int* offsets, void* Y, int y_type,
@@ -746,7 +818,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     if (M > 0x3fffffff || (long long)E * N > 0x3fffffffLL) return ELUTQ_ERR_SHAPE;           // rows are 32-bit coordinates
     if (!mx4_aligned(x_codes, 16) || !mx4_aligned(w_codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(offsets, 4) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
     const bool grouped = offsets != nullptr;
-    const Plan p = plan_for(M, N, K, E, format, grouped, device_sm_count());
+    const Plan p = plan_for(M, N, K, E, format, grouped, y_type, device_sm_count());
     if (!p.ok) return ELUTQ_ERR_UNSUPPORTED;
     Mx4Args a;
     a.x_scales = reinterpret_cast<const uint8_t*>(x_scales);
@@ -763,6 +835,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     a.split = p.split;
     a.stages = p.stages;
     a.x_box = p.x_box;
+    a.turn = p.turn;
     a.x_wide = mx4_aligned(x_scales, 16) && a.sk % 16 == 0;
     a.w_wide = mx4_aligned(w_scales, 16) && a.sk % 16 == 0;
     a.test = test_limit != 0;

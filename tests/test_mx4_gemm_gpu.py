@@ -78,7 +78,7 @@ def test_many_tiles_and_steps_for_each_sm(fmt, M, N, K):
 
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", [(1, 1000, 1024), (5, 77, 1536), (70, 259, 512), (300, 300, 512)])
+@pytest.mark.parametrize("M,N,K", [(1, 1000, 1024), (5, 77, 1536), (70, 259, 512), (300, 300, 512), (300, 1048, 512), (128, 1000, 256), (9, 200, 256), (250, 136, 64), (1030, 2056, 96)])
 def test_output_types_and_alpha(fmt, out, M, N, K):
     _gemm(np.random.default_rng(M + N + K), M, N, K, fmt, out, alpha=None if fmt == 0 else 0.0037)
     _gemm(np.random.default_rng(M + N + K), M, N, K, fmt, out, alpha=-1.7)
