@@ -11,7 +11,7 @@
 //              16 (r mod 32) + 4 (r / 32).  Lane l of a warp loads some steps' scales of rows l, l + 32, l + 64, l + 96 and
 //              stores the four rows' words side by side (16 bytes, no conflicts).  The fence that makes a step's stores visible to the tensor core also
 //              waits for the thread's loads, so none of the next ones may be in flight: two warps per 128 rows take turns, one loads
-//              while the other stores (4096 x 28672 x 4096, NVFP4: 287 us with one that loaded ahead).  The MMA warp copies
+//              while the other stores.  The MMA warp copies
 //              them to tensor memory (tcgen05.cp) in front of the step's MMAs; copies and MMAs of one thread run in order.
 //   sums       two accumulators; the epilogue warps empty one while the next tile fills the other.  256 tokens leave no room for two beside the
 //              scales: they overlap by 48 columns, which the epilogue empties first.
@@ -37,15 +37,12 @@ constexpr int kMaxStages = 10;
 constexpr int kMaxSplit = 8;
 constexpr int kMaxSplitTokens = 64;
 constexpr int kMaxGroups = 1024;
-// The warps of 128 rows' scales take turns of so many steps.  A warp whose turn has come may wait for a use of a stage that is (turns - 1) * steps +
-// stages ahead of what has been consumed, and a barrier's parity tells uses apart only within two rings: the first term has to be less than
-// the ring's length.
+// Scales come in turns of four steps into a ring of two, one fence and one arrival for a turn; the two warps of 128 rows take alternate turns.  (A warp waits
+// for a use of the ring one turn ahead of the other's: within what a barrier's parity tells apart.)  A step at a time, three warps could not keep up with
+// the MMAs, as the fence takes 400 to 1000 cycles (4096 x 28672 x 4096, MXFP4 203 us, NVFP4 246).
+constexpr int kTurn = 4, kTurns = 2;
 template <int NB>
-constexpr int kTurns = NB == 2 ? 3 : 2;
-template <int NB>
-constexpr int kTurnSteps = NB == 2 ? 2 : 4;
-template <int NB>
-constexpr int kThreads = 32 * (6 + (1 + NB) * kTurns<NB>);
+constexpr int kThreads = 32 * (6 + (1 + NB) * 2);
 constexpr int kAcc1 = kMaxTokens - 48, kScaleCols = 2 * kMaxTokens - 48;     // second accumulator, which shares 48 columns with the first; scales (48 columns)
 constexpr int kSmem = 232448;
 constexpr int kChunk = kMaxTokens - kAcc1;        // columns that the epilogue takes at once
@@ -74,7 +71,7 @@ struct Mx4Args {
     uint32_t wait_limit;       // polls (tests); a wait of a second runs out whatever this is
 };
 
-enum { kBarFull = 0, kBarEmpty = kBarFull + kMaxStages, kBarAccFull = kBarEmpty + kMaxStages, kBarAccFree = kBarAccFull + 2,
+enum { kBarFull = 0, kBarEmpty = kBarFull + kMaxStages, kBarScalesFull = kBarEmpty + kMaxStages, kBarScalesEmpty = kBarScalesFull + kTurns, kBarAccFull = kBarScalesEmpty + kTurns, kBarAccFree = kBarAccFull + 2,
        kBarPartsFull = kBarAccFree + 2, kBarPartsFree, kBarDrain, kNumBars };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -350,15 +347,14 @@ template <int FMT, int CG>
 __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
     constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
     constexpr int NB = CG;
-    constexpr int kTurn = kTurnSteps<NB>, TURNS = kTurns<NB>;
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
-    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + NB) * CH * 512;
+    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + NB) * CH * 512;       // (scales: of a step)
     uint8_t* sW = smem;
     uint8_t* sX = sW + a.stages * w_bytes;
     uint8_t* sS = sX + a.stages * x_bytes;
-    float* parts = reinterpret_cast<float*>(sS + a.stages * s_bytes);                 // [tokens][128], clusters only
+    float* parts = reinterpret_cast<float*>(sS + kTurns * kTurn * s_bytes);                 // [tokens][128], clusters only
     uint8_t* sT = reinterpret_cast<uint8_t*>(parts) + (a.split > 1 ? a.tokens * kTileW * 4 : 0);
     uint64_t* bars = reinterpret_cast<uint64_t*>(sT + (a.turn ? kTurnBytes : 0));
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
@@ -383,8 +379,12 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     if (threadIdx.x == 0) {
         auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
         for (int i = 0; i < a.stages; ++i) {
-            init(kBarFull + i, 1 + CG * (1 + NB));        // the loads; the scales of each 128 rows
+            init(kBarFull + i, 1);
             init(kBarEmpty + i, 1);
+        }
+        for (int i = 0; i < kTurns; ++i) {
+            init(kBarScalesFull + i, CG * (1 + NB));
+            init(kBarScalesEmpty + i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             init(kBarAccFull + i, 1);
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
         }
     } else if (warp == 1 && leader) {
         if (elect_one()) {
-            Ring r(a.stages);
+            Ring r(a.stages), rs(kTurns);
             const bool overlap = a.tokens > kAcc1;
             const uint32_t sa = tmem + kScaleCols, sb = sa + 4 * CH;
             const uint64_t da0 = operand_desc(smem_u32(sW)), db0 = operand_desc(smem_u32(sX)), ds0 = scales_desc(smem_u32(sS));
@@ -472,10 +472,12 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 const uint32_t idesc = 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (FMT == ELUTQ_MX4_MXFP4 ? 1u << 23 : 0u) | (uint32_t)(CG * kTileW >> 4) << 24;
                 const uint32_t acc = tmem + (b ? kAcc1 : 0);
                 for (int s = step0; s < step1; ++s) {
+                    const int in_turn = (s - step0) % kTurn;
                     ok = wait_alone<CG == 2>(bar(kBarFull + r.i), r.phase, gave_up, limit);
+                    if (in_turn == 0) ok = ok && wait_alone<CG == 2>(bar(kBarScalesFull + rs.i), rs.phase, gave_up, limit);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = da0 + (uint32_t)(r.i * w_bytes >> 4), db = db0 + (uint32_t)(r.i * x_bytes >> 4), ds = ds0 + (uint32_t)(r.i * s_bytes >> 4);
+                    const uint64_t da = da0 + (uint32_t)(r.i * w_bytes >> 4), db = db0 + (uint32_t)(r.i * x_bytes >> 4), ds = ds0 + (uint32_t)((rs.i * kTurn + in_turn) * s_bytes >> 4);
 #pragma unroll
                     for (int c = 0; c < CH; ++c) {
                         copy_scales<CG>(sa + 4 * c, ds + c * 32);
@@ -499,6 +501,10 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                     }
                     commit<CG>(bar(kBarEmpty + r.i));
                     r.next();
+                    if (in_turn == kTurn - 1 || s == step1 - 1) {
+                        commit<CG>(bar(kBarScalesEmpty + rs.i));
+                        rs.next();
+                    }
                 }
                 if (ok) commit<CG>(bar(kBarAccFull + b));
             }
@@ -645,9 +651,9 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, IntC<0>{}); });
         }
     } else {
-        const int helper = warp < 4 ? warp - 2 : warp - 6, block = helper / TURNS, mine = helper % TURNS;      // weights, tokens 0 to 127, 128 to 255
+        const int helper = warp < 4 ? warp - 2 : warp - 6, block = helper >> 1;      // weights, tokens 0 to 127, 128 to 255
         if (helper >= 0 && block <= NB) {
-            Ring r(a.stages);
+            Ring r(kTurns);
             const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
             const bool wide = block == 0 ? a.w_wide : a.x_wide;
             const long long all = block == 0 ? (long long)a.E * a.N : a.M;
@@ -661,12 +667,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 const uint8_t* rows[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, all - 1) * a.sk;
-                for (int s = step0; s < step1 && ok; s += kTurn, turn = turn + 1 == TURNS ? 0 : turn + 1) {
-                    const int n = min(kTurn, step1 - s);
-                    if (turn != mine) {
-                        for (int h = 0; h < n; ++h) r.next();
-                        continue;
-                    }
+                for (int s = step0; s < step1 && ok; s += kTurn, turn ^= 1, r.next()) {
+                    if (turn != (helper & 1)) continue;
                     uint32_t w[4][kTurn * CH];
                     const int at = s * 4 * CH;
                     if (wide) {
@@ -682,26 +684,21 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
                         for (int q = 0; q < 4; ++q) load_words(w[q], rows[q] + at, rows[q] + a.sk, base, base + all * a.sk);
                     }
+                    ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                    if (!ok) break;
 #pragma unroll
-                    for (int h = 0; h < kTurn; ++h) {
-                        if (h < n && ok) {
-                            ok = wait(bar(kBarEmpty + r.i), r.phase ^ 1u, gave_up, limit);
-                            if (ok) {
+                    for (int h = 0; h < kTurn; ++h)
 #pragma unroll
-                                for (int c = 0; c < CH; ++c)
-                                    *reinterpret_cast<uint4*>(to + r.i * s_bytes + c * pitch) =
-                                        make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
-                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                                __syncwarp();
-                                if (lane == 0) {
-                                    if constexpr (CG == 2) arrive_remote(at_rank(bar(kBarFull + r.i), 0));
-                                    else arrive(bar(kBarFull + r.i));
-                                }
-                                __syncwarp();
-                                r.next();
-                            }
-                        }
+                        for (int c = 0; c < CH; ++c)
+                            *reinterpret_cast<uint4*>(to + (r.i * kTurn + h) * s_bytes + c * pitch) =
+                                make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 2) arrive_remote(at_rank(bar(kBarScalesFull + r.i), 0));
+                        else arrive(bar(kBarScalesFull + r.i));
                     }
+                    __syncwarp();
                 }
             }
         }
@@ -723,12 +720,12 @@ constexpr int kFixed = kNumBars * 8 + 16;
 // Ring length and shared memory of a plan whose other fields are set; false if the ring is too short.
 bool fill_plan(Plan& p, int format, int E, bool grouped) {
     const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4, nb = p.cg;
-    const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024 + (1 + nb) * ch * 512;
-    const int fixed = kFixed + (p.turn ? kTurnBytes : 0) + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
+    const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024;
+    const int fixed = kFixed + kTurns * kTurn * (1 + nb) * ch * 512 + (p.turn ? kTurnBytes : 0) + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
     p.stages = (kSmem - fixed) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.smem = (size_t)p.stages * stage + fixed;
-    return p.stages > (nb == 2 ? (kTurns<2> - 1) * kTurnSteps<2> : (kTurns<1> - 1) * kTurnSteps<1>);
+    return p.stages >= 2;
 }
 
 #ifdef MX4_TUNE
