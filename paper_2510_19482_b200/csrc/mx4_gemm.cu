@@ -8,8 +8,7 @@
 //              N, columns of tensor memory, 8 at least: a decoding batch wastes nothing but padding to 8, and a group's rest is as wide as it is.
 //   K          in steps of 256: 128 bytes of codes a row, one 128-byte swizzle atom wide, brought by TMA into a ring of stages.
 //   scales     are row-major, while the tensor core wants, per 128 rows and 4 scales, 512 bytes with row r's four at
-//              16 (r mod 32) + 4 (r / 32).  Lane l of a warp loads some steps' scales of rows l, l + 32, l + 64, l + 96 and
-//              stores the four rows' words side by side (16 bytes, no conflicts).  The fence that makes a step's stores visible to the tensor core also
+//              16 (r mod 32) + 4 (r / 32): a warp per 128 rows loads and stores them so, four steps at a time.  The fence that makes a step's stores visible to the tensor core also
 //              waits for the thread's loads, so none of the next ones may be in flight: two warps per 128 rows take turns, one loads
 //              while the other stores.  The MMA warp copies
 //              them to tensor memory (tcgen05.cp) in front of the step's MMAs; copies and MMAs of one thread run in order.
@@ -233,29 +232,29 @@ struct Ring {
     }
 };
 
-// WORDS words of a row's scales from p on, p of any alignment: bytes from `end` on are 0, and nothing outside [lo, hi) is read.  By a whole warp.
-template <int WORDS>
-__device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const uint8_t* p, const uint8_t* end, const uint8_t* lo, const uint8_t* hi) {
-    const uint32_t shift = 8u * (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
-    const uint8_t* q = p - shift / 8u;
-    if (__all_sync(0xffffffffu, q >= lo && q + 4 * (WORDS + 1) <= hi)) {          // all but a matrix's ends
-        uint32_t v[WORDS + 1];
+// Four words of a row's scales from p on, p of any alignment; bytes from `end` on are 0.  The first form reads the aligned words around them, up to 20 bytes from
+// p rounded down to 4; the second nothing but the bytes.
+__device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, const uint8_t* end) {
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
+    uint32_t v[5];
 #pragma unroll
-        for (int i = 0; i <= WORDS; ++i) v[i] = __ldg(reinterpret_cast<const uint32_t*>(q) + i);
-        const int left = (int)(end - p);
+    for (int i = 0; i < 5; ++i) v[i] = __ldg(q + i);
+    const int left = (int)(end - p);
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            w[i] = __funnelshift_r(v[i], v[i + 1], shift);
-            if (left < 4 * i + 4) w[i] &= left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1u;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            uint32_t v = 0;
-            for (int b = 0; b < 4 && p + 4 * i + b < end; ++b) v |= (uint32_t)__ldg(p + 4 * i + b) << (8 * b);
-            w[i] = v;
-        }
+    for (int i = 0; i < 4; ++i) {
+        w[i] = __funnelshift_r(v[i], v[i + 1], 8u * off);
+        if (left < 4 * i + 4) w[i] &= left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1u;
     }
+}
+__device__ __noinline__ uint4 load_bytes(const uint8_t* p, const uint8_t* end) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+        for (int b = 0; b < 4 && p + 4 * i + b < end; ++b) w[i] |= (uint32_t)__ldg(p + 4 * i + b) << (8 * b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 struct Tile {
@@ -350,7 +349,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
-    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + NB) * CH * 512;       // (scales: of a step)
+    const int w_bytes = kTileW * kStepBytes, s_bytes = (1 + NB) * CH * 512 + 32;      // (scales: of a step, and 32 bytes that move the next step's banks)
     uint8_t* sW = smem;
     uint8_t* sX = sW + a.stages * w_bytes;
     uint8_t* sS = sX + a.stages * x_bytes;
@@ -657,41 +656,52 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             const uint8_t* base = block == 0 ? a.w_scales : a.x_scales;
             const bool wide = block == 0 ? a.w_wide : a.x_wide;
             const long long all = block == 0 ? (long long)a.E * a.N : a.M;
-            uint8_t* to = sS + (block == 0 ? 0 : CH + block - 1) * 512 + lane * 16;
-            const int pitch = block == 0 ? 512 : NB * 512;
+            // A lane's pieces: 16 bytes of a row's turn (64 bytes NVFP4, 32 MXFP4), in rows r + 32 q with neighbours in q and r; the four words of a
+            // piece go to as many groups of 512 bytes, without conflicts.  (A lane per row, 4 or 2 pieces of it, touched 32 lines a load
+            // instead of 8 or 16, and NVFP4 was bound by that: 4096 x 28672 x 4096 245 us.)
+            constexpr int PIECES = CH, LOADS = 4 * PIECES, ROWS = 8 / PIECES;             // pieces of a row; loads; rows r of a load
+            const int piece = lane % PIECES, q = lane / PIECES % 4, r0 = lane / (4 * PIECES);
+            const int first_word = block == 0 ? 0 : CH + block - 1, pitch = block == 0 ? 1 : NB;
+            uint8_t* to = sS + first_word * 512 + r0 * 16 + q * 4;
             int turn = 0;
             bool ok = true;
             for (int i = first; i < tiles && ok; i += stride) {
                 const Tile t = tile_at<CG>(a, table, i);
-                const long long row0 = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
-                const uint8_t* rows[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) rows[q] = base + min(row0 + lane + 32 * q, all - 1) * a.sk;
+                const long long row0 = (block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1)) + r0 + 32 * q;
                 for (int s = step0; s < step1 && ok; s += kTurn, turn ^= 1, r.next()) {
                     if (turn != (helper & 1)) continue;
-                    uint32_t w[4][kTurn * CH];
-                    const int at = s * 4 * CH;
+                    uint32_t w[LOADS][4];
+                    const int at = s * 4 * CH + 16 * piece;
                     if (wide) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int k = 0; k < kTurn * CH; k += 4) {
-                                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                                if (at + 4 * k < a.sk) v = __ldg(reinterpret_cast<const uint4*>(rows[q] + at + 4 * k));
-                                w[q][k] = v.x; w[q][k + 1] = v.y; w[q][k + 2] = v.z; w[q][k + 3] = v.w;
-                            }
+                        for (int k = 0; k < LOADS; ++k) {
+                            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                            if (at < a.sk) v = __ldg(reinterpret_cast<const uint4*>(base + min(row0 + ROWS * k, all - 1) * a.sk + at));
+                            w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
+                        }
                     } else {
+                        // whole aligned words, but for the ends of the matrix (rows ascend with k)
+                        auto row_at = [&](int k) { return base + min(row0 + ROWS * k, all - 1) * a.sk; };
+                        const bool inside = row_at(0) + at - 3 >= base && row_at(LOADS - 1) + at + 20 <= base + all * a.sk;
+                        if (__all_sync(0xffffffffu, inside)) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) load_words(w[q], rows[q] + at, rows[q] + a.sk, base, base + all * a.sk);
+                            for (int k = 0; k < LOADS; ++k) load_words(w[k], row_at(k) + at, row_at(k) + a.sk);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < LOADS; ++k) {
+                                const uint4 v = load_bytes(row_at(k) + at, row_at(k) + a.sk);
+                                w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
+                            }
+                        }
                     }
                     ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
                     if (!ok) break;
+                    uint8_t* slot = to + (r.i * kTurn + piece * 4 / CH) * s_bytes;
 #pragma unroll
-                    for (int h = 0; h < kTurn; ++h)
+                    for (int k = 0; k < LOADS; ++k)
 #pragma unroll
-                        for (int c = 0; c < CH; ++c)
-                            *reinterpret_cast<uint4*>(to + (r.i * kTurn + h) * s_bytes + c * pitch) =
-                                make_uint4(w[0][h * CH + c], w[1][h * CH + c], w[2][h * CH + c], w[3][h * CH + c]);
+                        for (int c = 0; c < 4; ++c)
+                            *reinterpret_cast<uint32_t*>(slot + (c / CH) * s_bytes + (c % CH) * pitch * 512 + ROWS * k * 16) = w[k][c];
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
@@ -721,7 +731,7 @@ constexpr int kFixed = kNumBars * 8 + 16;
 bool fill_plan(Plan& p, int format, int E, bool grouped) {
     const int ch = format == ELUTQ_MX4_MXFP4 ? 2 : 4, nb = p.cg;
     const int stage = kTileW * kStepBytes + (p.tokens / p.cg + 7) / 8 * 1024;
-    const int fixed = kFixed + kTurns * kTurn * (1 + nb) * ch * 512 + (p.turn ? kTurnBytes : 0) + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
+    const int fixed = kFixed + kTurns * kTurn * ((1 + nb) * ch * 512 + 32) + (p.turn ? kTurnBytes : 0) + (p.split > 1 ? p.tokens * kTileW * 4 : 0) + (grouped ? (3 * E + 1) * 4 : 0);
     p.stages = (kSmem - fixed) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.smem = (size_t)p.stages * stage + fixed;
