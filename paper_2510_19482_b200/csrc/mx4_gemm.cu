@@ -232,29 +232,44 @@ struct Ring {
     }
 };
 
-// Four words of a row's scales from p on, p of any alignment; bytes from `end` on are 0.  The first form reads the aligned words around them, up to 20 bytes from
-// p rounded down to 4; the second nothing but the bytes.
-__device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, const uint8_t* end) {
+// Scales of any alignment are read as the aligned words around them; of the words that the matrix shares with its surroundings only the bytes that
+// belong to it are read, once.
+struct Ends {
+    const uint32_t *lo, *hi;       // whole words: [lo, hi)
+    uint32_t head, tail;           // the words in front of lo and at hi
+};
+__device__ __forceinline__ Ends ends_of(const uint8_t* base, const uint8_t* end) {
+    Ends e;
+    e.lo = reinterpret_cast<const uint32_t*>((reinterpret_cast<uintptr_t>(base) + 3) & ~(uintptr_t)3);
+    e.hi = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(end) & ~(uintptr_t)3);
+    auto bytes_at = [&](const uint32_t* word) {
+        uint32_t v = 0;
+        for (int b = 0; b < 4; ++b) {
+            const uint8_t* p = reinterpret_cast<const uint8_t*>(word) + b;
+            if (p >= base && p < end) v |= (uint32_t)__ldg(p) << (8 * b);
+        }
+        return v;
+    };
+    e.head = bytes_at(e.lo - 1);
+    e.tail = bytes_at(e.hi);
+    return e;
+}
+// Four words of a row's scales from p on; bytes from `end` (of the row) on are 0.
+__device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, const uint8_t* end, const Ends& e) {
     const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
     const uint32_t* q = reinterpret_cast<const uint32_t*>(p - off);
     uint32_t v[5];
 #pragma unroll
-    for (int i = 0; i < 5; ++i) v[i] = __ldg(q + i);
+    for (int i = 0; i < 5; ++i) {
+        v[i] = q + i == e.hi ? e.tail : q + i == e.lo - 1 ? e.head : 0u;
+        if (q + i >= e.lo && q + i < e.hi) v[i] = __ldg(q + i);
+    }
     const int left = (int)(end - p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         w[i] = __funnelshift_r(v[i], v[i + 1], 8u * off);
         if (left < 4 * i + 4) w[i] &= left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1u;
     }
-}
-__device__ __noinline__ uint4 load_bytes(const uint8_t* p, const uint8_t* end) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = 0;
-        for (int b = 0; b < 4 && p + 4 * i + b < end; ++b) w[i] |= (uint32_t)__ldg(p + 4 * i + b) << (8 * b);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 struct Tile {
@@ -401,10 +416,13 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     __syncthreads();
     if (CG == 2 || a.split > 1) cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    grid_dependency_wait();
+    // What reads or writes global memory waits for the kernels in front of this one: the groups' borders here, each role otherwise where it begins.
     grid_launch_dependents();
     if (a.offsets != nullptr) {
-        if (warp == 0) list_groups(a, table);
+        if (warp == 0) {
+            grid_dependency_wait();
+            list_groups(a, table);
+        }
         __syncthreads();
     }
     const uint32_t tmem = *tmem_slot;
@@ -425,6 +443,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             Ring r(a.stages);
             int issued = 0;
             bool ok = true;
+            grid_dependency_wait();
             for (int i = first; i < tiles && ok; i += stride) {
                 const Tile t = tile_at<CG>(a, table, i);
                 const int per_cta = CG == 2 ? (t.count + 15) / 16 * 8 : (t.count + 7) / 8 * 8;
@@ -514,6 +533,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
         }
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;                             // lanes of tensor memory
+        grid_dependency_wait();
         const bool overlap = a.tokens > kAcc1;
         int n = 0;
         bool ok = true;
@@ -557,6 +577,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                         if (col < a.N) store_y(a, (long long)(t.t0 + c) * a.N + col, sum * alpha);
                     }
                 }
+                if (i + stride >= tiles) break;                   // nothing comes behind it
                 ok = epilogue_agrees(ok);
                 if (threadIdx.x - 128u < (unsigned)a.split) arrive_cluster(at_rank(bar(kBarPartsFree), threadIdx.x - 128u));
                 __syncwarp();
@@ -665,6 +686,9 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             uint8_t* to = sS + first_word * 512 + r0 * 16 + q * 4;
             int turn = 0;
             bool ok = true;
+            grid_dependency_wait();
+            Ends ends = {};
+            if (!wide) ends = ends_of(base, base + all * a.sk);
             for (int i = first; i < tiles && ok; i += stride) {
                 const Tile t = tile_at<CG>(a, table, i);
                 const long long row0 = (block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1)) + r0 + 32 * q;
@@ -680,18 +704,10 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                             w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
                         }
                     } else {
-                        // whole aligned words, but for the ends of the matrix (rows ascend with k)
-                        auto row_at = [&](int k) { return base + min(row0 + ROWS * k, all - 1) * a.sk; };
-                        const bool inside = row_at(0) + at - 3 >= base && row_at(LOADS - 1) + at + 20 <= base + all * a.sk;
-                        if (__all_sync(0xffffffffu, inside)) {
 #pragma unroll
-                            for (int k = 0; k < LOADS; ++k) load_words(w[k], row_at(k) + at, row_at(k) + a.sk);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < LOADS; ++k) {
-                                const uint4 v = load_bytes(row_at(k) + at, row_at(k) + a.sk);
-                                w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
-                            }
+                        for (int k = 0; k < LOADS; ++k) {
+                            const uint8_t* row = base + min(row0 + ROWS * k, all - 1) * a.sk;
+                            load_words(w[k], row + at, row + a.sk, ends);
                         }
                     }
                     ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
