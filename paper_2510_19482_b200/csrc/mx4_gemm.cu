@@ -22,6 +22,8 @@
 // Every wait is bounded: the thread whose wait runs out raises the device's status word, and all roles leave their loops.
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "mx4.cuh"
 #include "tensor_map.cuh"
 
@@ -571,10 +573,21 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 __syncwarp();
                 ok = wait<true>(bar(kBarPartsFull), (uint32_t)n & 1u, gave_up, limit);
                 if (ok) {
-                    for (int c = (int)rank; c < t.count; c += a.split) {
-                        float sum = 0.0f;
-                        for (int s = 0; s < a.split; ++s) sum += ld_cluster_f32(parts + c * kTileW + row, (unsigned)s);
-                        if (col < a.N) store_y(a, (long long)(t.t0 + c) * a.N + col, sum * alpha);
+                    // eight of this CTA's columns at a time: as many loads in flight
+                    for (int c0 = (int)rank; c0 < t.count; c0 += 8 * a.split) {
+                        float sum[8] = {};
+                        for (int s = 0; s < a.split; ++s) {
+                            const uint32_t from = at_rank(smem_u32(parts + row), (uint32_t)s);
+                            float v[8];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c)
+                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[c]) : "r"(from + (uint32_t)(min(c0 + c * a.split, t.count - 1) * kTileW * 4)) : "memory");
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) sum[c] += v[c];
+                        }
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            if (c0 + c * a.split < t.count && col < a.N) store_y(a, (long long)(t.t0 + c0 + c * a.split) * a.N + col, sum[c] * alpha);
                     }
                 }
                 if (i + stride >= tiles) break;                   // nothing comes behind it
@@ -754,38 +767,83 @@ bool fill_plan(Plan& p, int format, int E, bool grouped) {
     return p.stages >= 2;
 }
 
+// Time in us of `tiles` tiles (weights of `groups` matrices in all): a launch's fixed part, which grows with the tokens that a tile's epilogue stores, and the
+// longest of three: steps of the busiest SMs, weights from HBM, operands from L2.  A further tile's steps overlap with the last one's epilogue.  Parts of a
+// cluster cost their exchange.  Fitted to 4400 calls (1000 to 57344 weight rows, K 1024 to 14336, 1 to 512 tokens), 10 % off in the mean; a choice by it
+// costs 1 % against the best plan measured, 15 % at most (10240 x 8192, 512 tokens).
+double estimate_us(long long tiles, double groups, int N, int K, int format, int cg, int tokens, int split, int num_sms) {
+    const int steps = (K + 255) / 256, units = (steps + 1) / 2;
+    const long long teams = cg == 2 ? num_sms / 2 : split > 1 ? resident_clusters(split) : num_sms;
+    const long long rounds = (tiles + teams - 1) / teams;
+    const int own = split > 1 ? 2 * ((units + split - 1) / split) : steps;
+    const double row = 128.0 + 256.0 / mx4_block(format), step_us = (cg == 2 ? 0.25 : 0.24) + 0.0001 * tokens + (format == ELUTQ_MX4_NVFP4 ? 0.028 : 0.0);
+    const double sm = rounds * own * step_us - 0.086 * (rounds - 1), hbm = groups * N * steps * row / 5.54e6;
+    const double l2 = (double)tiles * steps * (cg * kTileW + tokens) * row / 10.6e6;
+    const double longest = sm > hbm ? (sm > l2 ? sm : l2) : (hbm > l2 ? hbm : l2);
+    const double exchange = split > 1 ? 1.26 + 0.256 * split + 0.0057 * tokens * split * rounds : 0.0;
+    return 3.36 + 0.009 * tokens + (cg == 2 ? 0.63 : 0.0) + longest + exchange;
+}
+
 #ifdef MX4_TUNE
 }
 extern "C" { int mx4_force_cg = 0, mx4_force_tokens = 0, mx4_force_split = 0; }
 namespace {
 #endif
 
+int round_up(int v, int m) { return (v + m - 1) / m * m; }
+
+// Tile and cluster of a call.  Dense: the least estimate over tiles that share the rows evenly (as few as possible, one or two more, twice as many) and clusters of up to
+// 8.  Groups: how many rows each has is known on the device only, and a tile's height on the host follows the mean; too much of it costs little (a
+// tile is as wide as its rows; the ring gets shorter), too little reads weights again: us with 8, 16, 32, 64, 96, 128 rows and with pairs of 256,
+// 128 experts of 1536 x 2048, MXFP4, 1024 rows (8 each) -, 39.7, 40.9, 40.8, 40.7, 42.4, -; 4096 rows (32 each) -, -, 49, 42.6, 42.4, 44.0, 46.2;
+// 64 of 4096 x 2048, 8192 rows (128 each) -, -, -, 102.7, 78.1, 74.6, 63.4.
 Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int y_type, int num_sms) {
     Plan p = {};
+    double best = 0.0;
+    auto consider = [&](int cg, int tokens, int split, long long tiles, double groups) {
+        const double us = estimate_us(tiles, groups, N, K, format, cg, tokens, split, num_sms);
+        if (best == 0.0 || us < best) {
+            best = us;
+            p.cg = cg;
+            p.tokens = tokens;
+            p.split = split;
+        }
+    };
     const int units = (K + 511) / 512;
-    p.cg = 1;
-    p.split = 1;
-    // rows of a tile: all of a small batch, even shares of a large one; a group's are not known here
-    const int per = grouped ? (M + E - 1) / E * 2 : M;
-    const int n = (per + kMaxTokens - 1) / kMaxTokens;
-    p.tokens = ((per + n - 1) / n + 7) / 8 * 8;
-    if (p.tokens > 32) p.tokens = (p.tokens + 31) / 32 * 32;
-    if (p.tokens > 128) p.cg = 2;
+    if (grouped) {
+        const int mean = (M + E - 1) / E;
+        const int cg = mean > 96 ? 2 : 1;
+        int tokens = mean <= 8 ? 32 : mean <= 16 ? 64 : mean <= 48 ? 96 : mean <= 96 ? 128 : 256;
+        if (tokens > round_up(M, 8)) tokens = round_up(M, 8);
+        const int busy = E < M ? E : M;
+        for (int split = 1; split <= (tokens <= kMaxSplitTokens ? kMaxSplit : 1); split *= 2)
+            if (split <= units) consider(cg, tokens, split, (long long)((N + cg * kTileW - 1) / (cg * kTileW)) * (busy + (M - busy) / tokens), busy);
+    } else {
+        for (int cg = 1; cg <= 2; ++cg) {
+            const int least = (M + 128 * cg - 1) / (128 * cg);
+            for (int k = 0; k < 4; ++k) {
+                const int n = k < 3 ? least + k : 2 * least;
+                if (n > least && M <= 32) continue;
+                int tokens = round_up((M + n - 1) / n, 8);
+                if (tokens > 32) tokens = round_up(tokens, 32);
+                if (tokens > 128 * cg || (cg == 2 && tokens < 64)) continue;
+                const long long tiles = (long long)((N + cg * kTileW - 1) / (cg * kTileW)) * ((M + tokens - 1) / tokens);
+                for (int split = 1; split <= (cg == 1 && tokens <= kMaxSplitTokens ? kMaxSplit : 1); split *= 2)
+                    if (split <= units) consider(cg, tokens, split, tiles, 1.0);
+            }
+        }
+    }
 #ifdef MX4_TUNE
     if (mx4_force_cg) p.cg = mx4_force_cg;
     if (mx4_force_tokens) p.tokens = mx4_force_tokens;
-#endif
-    if (p.cg == 2) p.tokens = (p.tokens + 15) / 16 * 16;
-    p.x_box = grouped ? (p.tokens > 32 ? 32 : p.tokens) : p.tokens / p.cg;
-    if (grouped && p.cg == 2) p.x_box = p.tokens > 64 ? 32 : p.tokens / 2;
-    const int rows = kTileW * p.cg;
-    const long long most = grouped ? (long long)((N + rows - 1) / rows) * ((M + p.tokens - 1) / p.tokens + (E < M ? E : M))
-                                   : (long long)((N + rows - 1) / rows) * ((M + p.tokens - 1) / p.tokens);
-    if (p.tokens <= kMaxSplitTokens && p.cg == 1)
-        while (p.split < kMaxSplit && most * (p.split + 1) <= num_sms && p.split + 1 <= units) ++p.split;
-#ifdef MX4_TUNE
     if (mx4_force_split) p.split = mx4_force_split;
 #endif
+    if (p.cg == 2) p.tokens = round_up(p.tokens, 16);
+    // rows of one load: dense, all of a tile's; of groups, whose tiles are of any height, up to 32
+    const int rows = p.tokens / p.cg;
+    p.x_box = !grouped ? rows : rows % 32 == 0 ? 32 : rows % 16 == 0 ? 16 : 8;
+    const long long w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
+    const long long most = w_tiles * ((M + p.tokens - 1) / p.tokens + (grouped ? (E < M ? E : M) : 0));
     p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && N % 8 == 0;
     p.ok = fill_plan(p, format, E, grouped);
     const int team = p.cg == 2 ? 2 : p.split;
@@ -806,8 +864,17 @@ int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int bo
 
 template <int FMT, int CG>
 int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    // once for each device (a call would take half a microsecond of the host's time)
+    static std::atomic<unsigned long long> ready{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return (int)e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(ready.load(std::memory_order_acquire) & bit)) {
+        e = cudaFuncSetAttribute(mx4_gemm_kernel<FMT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return (int)e;
+        ready.fetch_or(bit, std::memory_order_release);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);
     cfg.blockDim = dim3((unsigned)kThreads<CG>);
