@@ -269,13 +269,14 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
     """X fp16, bf16 or fp32 [x_rows, K] (or [x_rows, 2 K], SwiGLU), unit stride along a row -> (codes uint8 [rows, K/2], scales uint8 [rows, K/B])."""
     import torch
     if codes is None:
-        codes = torch.empty((rows, K // 2), dtype=torch.uint8, device=X.device)
+        codes = X.new_empty((rows, K // 2), dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty((rows, K // (32 if fmt == MX4_MXFP4 else 16)), dtype=torch.uint8, device=X.device)
-    if X.dim() != 2 or X.stride(1) != 1:
+        scales = X.new_empty((rows, K // (32 if fmt == MX4_MXFP4 else 16)), dtype=torch.uint8)
+    stride = X.stride()
+    if len(stride) != 2 or stride[1] != 1:
         raise ElutqError(-2, "elutq_mx4_quantize")
-    _check(lib().elutq_mx4_quantize(_ptr(X), _type(X), X.shape[0], X.stride(0), rows, K, fmt, flags, _ptr(prescale), _ptr(index), index_div,
-                                    _ptr(n_rows), _ptr(codes), _ptr(scales), _stream(stream)), "elutq_mx4_quantize")
+    _check(lib().elutq_mx4_quantize(X.data_ptr(), _type(X), X.shape[0], stride[0], rows, K, fmt, flags, _ptr(prescale), _ptr(index), index_div,
+                                    _ptr(n_rows), codes.data_ptr(), scales.data_ptr(), _stream(stream)), "elutq_mx4_quantize")
     return codes, scales
 
 

@@ -8,14 +8,15 @@
 //   code    the E2M1 value nearest to value / scale, ties to the even code, 6 at most, with the value's sign
 //
 // NVFP4's quotient: a code has to be that of the exact value / scale, and a value half-way between two codes is common (a scale has
-// four significant bits, a half-way point three).  r = 1 / s rounded to nearest, q = y r and one correction by the remainder
-// y - q s (exact in a fused multiply-add) give the quotient rounded to nearest: a true tie is hit exactly, and
+// four significant bits, a half-way point three).  r = 1 / s within a unit in the last place, q = y r and one correction by the remainder
+// y - q s (exact in a fused multiply-add) give the quotient rounded to nearest: what is left is 2^-21 of a unit, and a quotient by four bits
+// is a 30th of a unit or more from where rounding changes, unless it is exact.  So a true tie is hit exactly, and
 // for 16-bit inputs nothing else rounds onto a half-way point (y and the point times s have at most 11 bits between them).  For
 // 24-bit values something can: by the remainder's sign the quotient is then rounded to odd (cut off, and the last bit set if anything
 // was left), which no half-way point is.
 //
-// Bound: HBM.  A thread takes 16 columns (one load of 32 bytes for 16-bit inputs, one block of NVFP4, half a block of MXFP4, whose
-// amax it shares with its neighbour) and stores 8 bytes of codes; 32 bytes a thread in flight are 64 KB an SM.
+// Bound: HBM.  A thread takes 32 columns (loads and stores of 32 bytes, whole sectors; one block of MXFP4 or two of NVFP4, so no amax is shared between
+// threads) and moves 16 bytes of codes.  With 16 columns and stores of 16 bytes 14336 x 4096 values came back at 4.7 TB/s.
 #include <cuda_bf16.h>
 
 #include "mx4.cuh"
@@ -24,7 +25,7 @@ namespace elutq {
 
 namespace {
 
-constexpr int kChunk = 16;                 // columns of a thread
+constexpr int kChunk = 32;                 // columns of a thread
 
 struct QuantArgs {
     const void* X;
@@ -32,12 +33,13 @@ struct QuantArgs {
     const float* prescale;     // null: 1
     const int* index;          // null: row r of X; otherwise row index[r] / div (none: zeros)
     const int* n_rows;         // null: all
-    uint2* codes;
+    uint4* codes;
     uint8_t* scales;
     int row0, rows, K;         // this launch: rows [row0, row0 + rows)
     long long x_rows;          // rows of X, times div
     Div per_row, div;          // chunks of a row; the index's divisor
     int wide;                  // rows of X start on 32 bytes
+    int pairs;                 // scales start on 2 bytes
 };
 
 // 32 bytes at p, 32-byte aligned with WIDE and 16-byte aligned otherwise
@@ -52,28 +54,27 @@ __device__ __forceinline__ void load32(uint32_t (&v)[8], const void* p) {
     }
 }
 
-// 16 values as fp32
-template <int TYPE, bool WIDE>
-__device__ __forceinline__ void load_chunk(float (&y)[kChunk], const void* X, long long at) {
-    uint32_t v[8];
-    if constexpr (TYPE == ELUTQ_TYPE_F32) {
+// COUNT values as fp32
+template <int TYPE, bool WIDE, int COUNT>
+__device__ __forceinline__ void load_values(float* y, const void* X, long long at) {
+    constexpr int EACH = TYPE == ELUTQ_TYPE_F32 ? 8 : 16;
+    uint32_t v[COUNT / EACH][8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            load32<WIDE>(v, reinterpret_cast<const float*>(X) + at + 8 * h);
+    for (int h = 0; h < COUNT / EACH; ++h)
+        load32<WIDE>(v[h], reinterpret_cast<const uint8_t*>(X) + (at + EACH * h) * (TYPE == ELUTQ_TYPE_F32 ? 4 : 2));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[8 * h + i] = __uint_as_float(v[i]);
-        }
-    } else {
-        load32<WIDE>(v, reinterpret_cast<const uint16_t*>(X) + at);
+    for (int h = 0; h < COUNT / EACH; ++h) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (TYPE == ELUTQ_TYPE_F16) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-                y[2 * i] = f.x;
-                y[2 * i + 1] = f.y;
+            if constexpr (TYPE == ELUTQ_TYPE_F32) {
+                y[8 * h + i] = __uint_as_float(v[h][i]);
+            } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[h][i]));
+                y[16 * h + 2 * i] = f.x;
+                y[16 * h + 2 * i + 1] = f.y;
             } else {
-                y[2 * i] = __uint_as_float(v[i] << 16);
-                y[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+                y[16 * h + 2 * i] = __uint_as_float(v[h][i] << 16);
+                y[16 * h + 2 * i + 1] = __uint_as_float(v[h][i] & 0xffff0000u);
             }
         }
     }
@@ -96,17 +97,27 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)byte));
     return __half2float(__ushort_as_half((uint16_t)h));
 }
-// FULL: values of up to 24 bits; otherwise of up to 11
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float reciprocal(float x) {                // one unit in the last place off at most
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// FULL: values of up to 24 bits; otherwise of up to 11.  (The remainder is taken negative: so the sign of a zero survives.)
 template <bool FULL>
 __device__ __forceinline__ float quotient(float y, float s, float r) {
     float q = y * r;
-    q = fmaf(fmaf(-q, s, y), r, q);
+    q = fmaf(fmaf(q, s, -y), -r, q);
     if constexpr (FULL) {
-        const float rest = fmaf(-q, s, y);
-        const int below = (__float_as_int(rest) ^ __float_as_int(q)) < 0 ? 1 : 0;      // the exact quotient's magnitude is below |q|
-        if (rest != 0.0f && q != 0.0f) q = __int_as_float((__float_as_int(q) - below) | 1);
+        const float over = fmaf(q, s, -y);
+        const int above = (__float_as_int(over) ^ __float_as_int(q)) < 0 ? 0 : 1;      // |q| is above the exact quotient's magnitude
+        if (over != 0.0f && q != 0.0f) q = __int_as_float((__float_as_int(q) - above) | 1);
     }
-    return copysignf(q, y);                    // (the correction makes +0 of -0)
+    return q;
 }
 
 template <int FMT, int TYPE, bool SWIGLU, bool WIDE>
@@ -121,13 +132,18 @@ __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int 
     }
     if (some) {
         const long long at = src * a.ld + (long long)chunk * kChunk;
-        load_chunk<TYPE, WIDE>(y, a.X, at);
         if constexpr (SWIGLU) {
-            float u[kChunk];
-            load_chunk<TYPE, WIDE>(u, a.X, at + a.K);
             // silu(g) u in fp32 (a few units in the last place)
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) y[i] = __fdividef(y[i], 1.0f + expf(-y[i])) * u[i];
+            for (int h = 0; h < kChunk; h += 16) {
+                float u[16];
+                load_values<TYPE, WIDE, 16>(y + h, a.X, at + h);
+                load_values<TYPE, WIDE, 16>(u, a.X, at + h + a.K);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[h + i] = __fdividef(y[h + i], 1.0f + expf(-y[h + i])) * u[i];
+            }
+        } else {
+            load_values<TYPE, WIDE, kChunk>(y, a.X, at);
         }
     } else {
 #pragma unroll
@@ -138,114 +154,127 @@ __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int 
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) y[i] *= p;
     }
-    // the largest magnitude as an integer: infinity and NaN are above every number
-    uint32_t top = 0;
+    constexpr int B = FMT == ELUTQ_MX4_MXFP4 ? 32 : 16;
+    uint32_t bytes[kChunk / B], codes[4];
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
-    if constexpr (FMT == ELUTQ_MX4_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const bool bad = top >= 0x7f800000u;
-
-    uint32_t byte;
-    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
-        const int e = max((int)(top >> 23) - 2, 0);
-        byte = bad ? 255u : (uint32_t)e;
-        const float f = __uint_as_float((uint32_t)(254 - min(e, 252)) << 23);            // 2^(127 - e)
+    for (int g = 0; g < kChunk / B; ++g) {
+        float* v = y + g * B;
+        // the largest magnitude, two values an instruction; a NaN stays one
+        float most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) y[i] *= f;
-    } else {
-        uint16_t two;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(__fdiv_rn(__uint_as_float(top), 6.0f)));
-        byte = bad ? 127u : (uint32_t)two & 0xffu;
-        const float s = e4m3_value(byte), r = byte == 0u ? 0.0f : __frcp_rn(s);
-        const bool full = TYPE == ELUTQ_TYPE_F32 || SWIGLU || a.prescale != nullptr;
-        if (full) {
+        for (int i = 0; i < B; i += 2) most = max_abs(most, v[i], v[i + 1]);
+        const uint32_t top = __float_as_uint(most);
+        const bool bad = top >= 0x7f800000u;
+        if constexpr (FMT == ELUTQ_MX4_MXFP4) {
+            const int e = max((int)(top >> 23) - 2, 0);
+            bytes[g] = bad ? 255u : (uint32_t)e;
+            const float f = __uint_as_float((uint32_t)(254 - min(e, 252)) << 23);            // 2^(127 - e)
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) y[i] = quotient<true>(y[i], s, r);
+            for (int i = 0; i < B; ++i) v[i] *= f;
         } else {
+            uint16_t two;
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(quotient<false>(__uint_as_float(top), 6.0f, 1.0f / 6.0f)));
+            bytes[g] = bad ? 127u : (uint32_t)two & 0xffu;
+            const float s = e4m3_value(bytes[g]), r = bytes[g] == 0u ? 0.0f : reciprocal(s);
+            // (a SwiGLU value is a few units in its last place off anyway)
+            if (!SWIGLU && (TYPE == ELUTQ_TYPE_F32 || a.prescale != nullptr)) {
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) y[i] = quotient<false>(y[i], s, r);
+                for (int i = 0; i < B; ++i) v[i] = quotient<true>(v[i], s, r);
+            } else {
+#pragma unroll
+                for (int i = 0; i < B; ++i) v[i] = quotient<false>(v[i], s, r);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < B / 8; ++i) codes[g * (B / 8) + i] = bad ? 0u : codes_of(v + 8 * i);
     }
-    uint2 codes = make_uint2(codes_of(y), codes_of(y + 8));
-    if (bad) codes = make_uint2(0u, 0u);
     const long long at = (long long)row * a.per_row.d + chunk;
-    a.codes[at] = codes;
+    a.codes[at] = make_uint4(codes[0], codes[1], codes[2], codes[3]);
     if constexpr (FMT == ELUTQ_MX4_MXFP4) {
-        if ((chunk & 1) == 0) a.scales[at >> 1] = (uint8_t)byte;
+        a.scales[at] = (uint8_t)bytes[0];
+    } else if (a.pairs) {
+        reinterpret_cast<uint16_t*>(a.scales)[at] = (uint16_t)(bytes[0] | bytes[1] << 8);
     } else {
-        a.scales[at] = (uint8_t)byte;
+        a.scales[2 * at] = (uint8_t)bytes[0];
+        a.scales[2 * at + 1] = (uint8_t)bytes[1];
     }
 }
 
-// A thread per chunk of 16 columns.  A row has an even number of chunks, so the two halves of a block of 32 are neighbouring lanes and
-// leave together.
+// A thread per chunk of 32 columns.
 template <int FMT, int TYPE, bool SWIGLU>
 __global__ void __launch_bounds__(256) mx4_quantize_kernel(const QuantArgs a) {
     const unsigned id = blockIdx.x * blockDim.x + threadIdx.x;
     const int local = a.per_row.of((int)id), chunk = (int)id - local * a.per_row.d, row = a.row0 + local;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int limit = a.n_rows != nullptr ? min(__ldg(a.n_rows), a.row0 + a.rows) : a.row0 + a.rows;
-    const bool mine = row < limit;
-    if (!__any_sync(0xffffffffu, mine)) return;
-    // lanes without work run on the last row that has some (the shuffle wants whole warps): the same bytes are stored twice
-    const int r = mine ? row : limit - 1;
-    if (a.wide) quantise_chunk<FMT, TYPE, SWIGLU, true>(a, r, chunk);
-    else quantise_chunk<FMT, TYPE, SWIGLU, false>(a, r, chunk);
+    if (row >= (a.n_rows != nullptr ? min(__ldg(a.n_rows), a.row0 + a.rows) : a.row0 + a.rows)) return;
+    if (a.wide) quantise_chunk<FMT, TYPE, SWIGLU, true>(a, row, chunk);
+    else quantise_chunk<FMT, TYPE, SWIGLU, false>(a, row, chunk);
 }
 
-template <int TYPE>
-__device__ __forceinline__ void store_chunk(void* Y, long long at, const float (&v)[kChunk]) {
-    uint32_t w[TYPE == ELUTQ_TYPE_F32 ? 16 : 8];
-#pragma unroll
-    for (int i = 0; i < kChunk / 2; ++i) {
-        if constexpr (TYPE == ELUTQ_TYPE_F32) {
-            w[2 * i] = __float_as_uint(v[2 * i]);
-            w[2 * i + 1] = __float_as_uint(v[2 * i + 1]);
-        } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
-            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        } else {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
+template <bool WIDE>
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+    if constexpr (WIDE) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
     }
-    constexpr int N4 = TYPE == ELUTQ_TYPE_F32 ? 4 : 2;
-    uint4* p = reinterpret_cast<uint4*>(Y) + at * N4;
-#pragma unroll
-    for (int i = 0; i < N4; ++i) p[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
 
 // value = alpha * code * scale: the product of code and scale is exact in fp32 (two and four significant bits), alpha's is
 // rounded to fp32 and the result once more to its type.
+template <int FMT, int TYPE, bool WIDE>
+__device__ __forceinline__ void dequantise_chunk(const uint4* codes, const uint8_t* scales, const float* alpha, void* Y, long long at) {
+    const uint4 c = __ldg(codes + at);
+    const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+    const float f = alpha != nullptr ? __ldg(alpha) : 1.0f;
+    float s[2];
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
+        const uint32_t byte = __ldg(scales + at);
+        s[0] = s[1] = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+    } else {
+        s[0] = e4m3_value(__ldg(scales + 2 * at));
+        s[1] = e4m3_value(__ldg(scales + 2 * at + 1));
+    }
+    uint32_t w[TYPE == ELUTQ_TYPE_F32 ? 32 : 16];
+#pragma unroll
+    for (int i = 0; i < kChunk / 2; ++i) {
+        const uint32_t b = (word[i / 4] >> (8 * (i & 3))) & 0xffu;
+        uint32_t h;
+        asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "h"((uint16_t)b));
+        const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        const float x = two.x * s[i / 8] * f, y = two.y * s[i / 8] * f;
+        if constexpr (TYPE == ELUTQ_TYPE_F32) {
+            w[2 * i] = __float_as_uint(x);
+            w[2 * i + 1] = __float_as_uint(y);
+        } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
+            const __half2 v = __floats2half2_rn(x, y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&v);
+        } else {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+            w[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+    }
+    constexpr int BYTES = TYPE == ELUTQ_TYPE_F32 ? 128 : 64;
+#pragma unroll
+    for (int i = 0; i < BYTES / 32; ++i) store32<WIDE>(reinterpret_cast<uint8_t*>(Y) + at * BYTES + 32 * i, w + 8 * i);
+}
+
 template <int FMT, int TYPE>
-__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint2* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ alpha,
-                                                             void* Y, long long chunks) {
+__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint4* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ alpha,
+                                                             void* Y, long long chunks, int wide) {
     const long long at = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     grid_dependency_wait();
     grid_launch_dependents();
     if (at >= chunks) return;
-    const uint2 c = __ldg(codes + at);
-    const uint32_t byte = __ldg(scales + (FMT == ELUTQ_MX4_MXFP4 ? at >> 1 : at));
-    float s;
-    if constexpr (FMT == ELUTQ_MX4_MXFP4) s = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-    else s = e4m3_value(byte);
-    const float f = alpha != nullptr ? __ldg(alpha) : 1.0f;
-    float v[kChunk];
-#pragma unroll
-    for (int i = 0; i < kChunk / 2; ++i) {
-        const uint32_t b = ((i < 4 ? c.x : c.y) >> (8 * (i & 3))) & 0xffu;
-        uint32_t h;
-        asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "h"((uint16_t)b));
-        const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        v[2 * i] = two.x * s * f;
-        v[2 * i + 1] = two.y * s * f;
-    }
-    store_chunk<TYPE>(Y, at, v);
+    if (wide) dequantise_chunk<FMT, TYPE, true>(codes, scales, alpha, Y, at);
+    else dequantise_chunk<FMT, TYPE, false>(codes, scales, alpha, Y, at);
 }
 
-// Few chunks: small blocks, so that more SMs have some.  (8 x 4096: 32 blocks of 64 instead of 8 of 256.)
-inline unsigned threads_for(long long chunks, int num_sms) { return chunks < 256LL * num_sms ? 64u : 256u; }
+// Few chunks: small blocks, so that more SMs have some.  (8 x 4096: 32 blocks of 32 instead of 4 of 256.)
+inline unsigned threads_for(long long chunks, int num_sms) { return chunks < 64LL * num_sms ? 32u : chunks < 256LL * num_sms ? 64u : 256u; }
 
 template <class K, class... A>
 int launch(K kernel, long long chunks, cudaStream_t stream, const A&... args) {
@@ -303,7 +332,8 @@ extern "C" int elutq_mx4_quantize(const void* X, int x_type, int x_rows, long lo
     a.prescale = prescale;
     a.index = index;
     a.n_rows = n_rows;
-    a.codes = reinterpret_cast<uint2*>(codes);
+    a.codes = reinterpret_cast<uint4*>(codes);
+    a.pairs = mx4_aligned(scales, 2);
     a.scales = reinterpret_cast<uint8_t*>(scales);
     a.K = K;
     a.x_rows = (long long)x_rows * (index != nullptr ? index_div : 1);
@@ -341,10 +371,11 @@ extern "C" int elutq_mx4_dequantize(const void* codes, const void* scales, int r
     if (!mx4_aligned(codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
     const long long chunks = (long long)rows * (K / kChunk);
     if (chunks > 64LL * 0x7fffffffLL) return ELUTQ_ERR_SHAPE;                 // (blocks of a launch)
-    const uint2* c = reinterpret_cast<const uint2*>(codes);
+    const uint4* c = reinterpret_cast<const uint4*>(codes);
+    const int wide = mx4_aligned(Y, 32);
     const uint8_t* s = reinterpret_cast<const uint8_t*>(scales);
     int ce = 0;
-    auto go = [&](auto kernel) { ce = launch(kernel, chunks, (cudaStream_t)stream, c, s, alpha, Y, chunks); };
+    auto go = [&](auto kernel) { ce = launch(kernel, chunks, (cudaStream_t)stream, c, s, alpha, Y, chunks, wide); };
     if (format == ELUTQ_MX4_MXFP4) {
         if (y_type == ELUTQ_TYPE_F16) go(mx4_dequantize_kernel<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_F16>);
         else if (y_type == ELUTQ_TYPE_BF16) go(mx4_dequantize_kernel<ELUTQ_MX4_MXFP4, ELUTQ_TYPE_BF16>);
