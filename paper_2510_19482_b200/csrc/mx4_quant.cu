@@ -54,28 +54,24 @@ __device__ __forceinline__ void load32(uint32_t (&v)[8], const void* p) {
     }
 }
 
-// COUNT values as fp32
-template <int TYPE, bool WIDE, int COUNT>
-__device__ __forceinline__ void load_values(float* y, const void* X, long long at) {
-    constexpr int EACH = TYPE == ELUTQ_TYPE_F32 ? 8 : 16;
-    uint32_t v[COUNT / EACH][8];
+// 32 bytes of X from element `at` on, and their values: 8 of fp32, 16 of 16 bits
+template <int TYPE, bool WIDE>
+__device__ __forceinline__ void load_raw(uint32_t (&v)[8], const void* X, long long at) {
+    load32<WIDE>(v, reinterpret_cast<const uint8_t*>(X) + at * (TYPE == ELUTQ_TYPE_F32 ? 4 : 2));
+}
+template <int TYPE>
+__device__ __forceinline__ void values_of(float* y, const uint32_t (&v)[8]) {
 #pragma unroll
-    for (int h = 0; h < COUNT / EACH; ++h)
-        load32<WIDE>(v[h], reinterpret_cast<const uint8_t*>(X) + (at + EACH * h) * (TYPE == ELUTQ_TYPE_F32 ? 4 : 2));
-#pragma unroll
-    for (int h = 0; h < COUNT / EACH; ++h) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (TYPE == ELUTQ_TYPE_F32) {
-                y[8 * h + i] = __uint_as_float(v[h][i]);
-            } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[h][i]));
-                y[16 * h + 2 * i] = f.x;
-                y[16 * h + 2 * i + 1] = f.y;
-            } else {
-                y[16 * h + 2 * i] = __uint_as_float(v[h][i] << 16);
-                y[16 * h + 2 * i + 1] = __uint_as_float(v[h][i] & 0xffff0000u);
-            }
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (TYPE == ELUTQ_TYPE_F32) {
+            y[i] = __uint_as_float(v[i]);
+        } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+            y[2 * i] = f.x;
+            y[2 * i + 1] = f.y;
+        } else {
+            y[2 * i] = __uint_as_float(v[i] << 16);
+            y[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
         }
     }
 }
@@ -107,6 +103,21 @@ __device__ __forceinline__ float reciprocal(float x) {                // one uni
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// g / (1 + exp(-g)) within a few units in the last place.  exp(-g) = 2^t 2^lo with t = -g log2(e) rounded and lo what that left, also of
+// the constant (|lo| < 2^-17), 2^lo = 1 + lo ln 2.  Below -87 the result is that at -87, 10^-36.
+template <int TYPE>
+__device__ __forceinline__ float silu(float g) {
+    float e, r, x;
+    asm("max.NaN.f32 %0, %0, 0fC2AE0000;" : "+f"(g));              // -87
+    if constexpr (TYPE == ELUTQ_TYPE_F16) x = g;
+    else asm("min.NaN.f32 %0, %1, 0f42C80000;" : "=f"(x) : "f"(g));     // 100: nothing in exp(-g) to add to 1 (t of more than 10^38 is infinite)
+    const float t = x * -1.44269502f;
+    const float lo = fmaf(x, -1.92596303e-8f, fmaf(x, -1.44269502f, -t));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
+    e = fmaf(e, lo * 0.693147182f, e);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return g * r;
+}
 // FULL: values of up to 24 bits; otherwise of up to 11.  (The remainder is taken negative: so the sign of a zero survives.)
 template <bool FULL>
 __device__ __forceinline__ float quotient(float y, float s, float r) {
@@ -134,16 +145,32 @@ __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int 
         const long long at = src * a.ld + (long long)chunk * kChunk;
         if constexpr (SWIGLU) {
             // silu(g) u in fp32 (a few units in the last place)
+            // (all loads in flight first, 16 columns at a time where that takes too many registers)
+            constexpr int PART = TYPE == ELUTQ_TYPE_F32 ? 16 : kChunk, EACH = TYPE == ELUTQ_TYPE_F32 ? 8 : 16;
 #pragma unroll
-            for (int h = 0; h < kChunk; h += 16) {
-                float u[16];
-                load_values<TYPE, WIDE, 16>(y + h, a.X, at + h);
-                load_values<TYPE, WIDE, 16>(u, a.X, at + h + a.K);
+            for (int h = 0; h < kChunk; h += PART) {
+                uint32_t g[PART / EACH][8], u[PART / EACH][8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[h + i] = __fdividef(y[h + i], 1.0f + expf(-y[h + i])) * u[i];
+                for (int k = 0; k < PART / EACH; ++k) {
+                    load_raw<TYPE, WIDE>(g[k], a.X, at + h + EACH * k);
+                    load_raw<TYPE, WIDE>(u[k], a.X, at + h + EACH * k + a.K);
+                }
+#pragma unroll
+                for (int k = 0; k < PART / EACH; ++k) {
+                    float up[EACH];
+                    values_of<TYPE>(y + h + EACH * k, g[k]);
+                    values_of<TYPE>(up, u[k]);
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) y[h + EACH * k + i] = silu<TYPE>(y[h + EACH * k + i]) * up[i];
+                }
             }
         } else {
-            load_values<TYPE, WIDE, kChunk>(y, a.X, at);
+            constexpr int EACH = TYPE == ELUTQ_TYPE_F32 ? 8 : 16;
+            uint32_t v[kChunk / EACH][8];
+#pragma unroll
+            for (int k = 0; k < kChunk / EACH; ++k) load_raw<TYPE, WIDE>(v[k], a.X, at + EACH * k);
+#pragma unroll
+            for (int k = 0; k < kChunk / EACH; ++k) values_of<TYPE>(y + EACH * k, v[k]);
         }
     } else {
 #pragma unroll
@@ -225,22 +252,34 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
 
 // value = alpha * code * scale: the product of code and scale is exact in fp32 (two and four significant bits), alpha's is
 // rounded to fp32 and the result once more to its type.
+// Columns of a thread: 64 bytes of results.
+template <int TYPE>
+constexpr int kBack = TYPE == ELUTQ_TYPE_F32 ? 16 : 32;
+
 template <int FMT, int TYPE, bool WIDE>
-__device__ __forceinline__ void dequantise_chunk(const uint4* codes, const uint8_t* scales, const float* alpha, void* Y, long long at) {
-    const uint4 c = __ldg(codes + at);
-    const uint32_t word[4] = {c.x, c.y, c.z, c.w};
-    const float f = alpha != nullptr ? __ldg(alpha) : 1.0f;
-    float s[2];
-    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
-        const uint32_t byte = __ldg(scales + at);
-        s[0] = s[1] = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+__device__ __forceinline__ void dequantise_chunk(const uint8_t* codes, const uint8_t* scales, const float* alpha, void* Y, long long at) {
+    constexpr int COLS = kBack<TYPE>;
+    uint32_t word[4];
+    if constexpr (COLS == 32) {
+        const uint4 c = __ldg(reinterpret_cast<const uint4*>(codes) + at);
+        word[0] = c.x; word[1] = c.y; word[2] = c.z; word[3] = c.w;
     } else {
-        s[0] = e4m3_value(__ldg(scales + 2 * at));
-        s[1] = e4m3_value(__ldg(scales + 2 * at + 1));
+        const uint2 c = __ldg(reinterpret_cast<const uint2*>(codes) + at);
+        word[0] = c.x; word[1] = c.y;
     }
-    uint32_t w[TYPE == ELUTQ_TYPE_F32 ? 32 : 16];
+    const float f = alpha != nullptr ? __ldg(alpha) : 1.0f;
+    float s[COLS / 16];
+    if constexpr (FMT == ELUTQ_MX4_MXFP4) {
+        const uint32_t byte = __ldg(scales + (COLS == 32 ? at : at >> 1));
+        s[0] = byte == 255u ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+        s[COLS / 16 - 1] = s[0];
+    } else {
 #pragma unroll
-    for (int i = 0; i < kChunk / 2; ++i) {
+        for (int i = 0; i < COLS / 16; ++i) s[i] = e4m3_value(__ldg(scales + COLS / 16 * at + i));
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < COLS / 2; ++i) {
         const uint32_t b = (word[i / 4] >> (8 * (i & 3))) & 0xffu;
         uint32_t h;
         asm("{\n\t.reg .b8 t, u;\n\tmov.b16 {t, u}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, t;\n\t}" : "=r"(h) : "h"((uint16_t)b));
@@ -257,13 +296,12 @@ __device__ __forceinline__ void dequantise_chunk(const uint4* codes, const uint8
             w[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
     }
-    constexpr int BYTES = TYPE == ELUTQ_TYPE_F32 ? 128 : 64;
 #pragma unroll
-    for (int i = 0; i < BYTES / 32; ++i) store32<WIDE>(reinterpret_cast<uint8_t*>(Y) + at * BYTES + 32 * i, w + 8 * i);
+    for (int i = 0; i < 2; ++i) store32<WIDE>(reinterpret_cast<uint8_t*>(Y) + at * 64 + 32 * i, w + 8 * i);
 }
 
 template <int FMT, int TYPE>
-__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint4* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ alpha,
+__global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ alpha,
                                                              void* Y, long long chunks, int wide) {
     const long long at = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     grid_dependency_wait();
@@ -369,9 +407,9 @@ extern "C" int elutq_mx4_dequantize(const void* codes, const void* scales, int r
     const int st = mx4_check(format, rows, K);
     if (st != ELUTQ_OK) return st;
     if (!mx4_aligned(codes, 16) || !mx4_aligned(Y, 16) || !mx4_aligned(alpha, 4)) return ELUTQ_ERR_ALIGN;
-    const long long chunks = (long long)rows * (K / kChunk);
+    const long long chunks = (long long)rows * (K / (y_type == ELUTQ_TYPE_F32 ? kBack<ELUTQ_TYPE_F32> : kBack<ELUTQ_TYPE_F16>));
     if (chunks > 64LL * 0x7fffffffLL) return ELUTQ_ERR_SHAPE;                 // (blocks of a launch)
-    const uint4* c = reinterpret_cast<const uint4*>(codes);
+    const uint8_t* c = reinterpret_cast<const uint8_t*>(codes);
     const int wide = mx4_aligned(Y, 32);
     const uint8_t* s = reinterpret_cast<const uint8_t*>(scales);
     int ce = 0;

@@ -138,6 +138,25 @@ def test_swiglu_then_quantise(fmt, ty, rows, K):
 
 
 @pytest.mark.parametrize("fmt", [0, 1])
+def test_swiglu_far_out(fmt):
+    """A gate of minus infinity or far below closes (nothing left of u); infinities and NaN elsewhere make their block NaN."""
+    K, inf, nan = 64, float("inf"), float("nan")
+    X = torch.ones((12, 2 * K))
+    far = [(-inf, 2.0, 0), (-3e38, 2.0, 0), (-1000.0, 2.0, 0), (-88.0, -2.0, 0), (3e38, 0.0, 0), (90.0, 3.0, 270.0), (inf, 1.0, nan), (1.0, inf, nan), (0.0, inf, nan),
+           (nan, 1.0, nan), (1.0, nan, nan), (-inf, nan, nan)]
+    for r, (g, u, _) in enumerate(far):
+        X[r, 7], X[r, K + 7] = g, u
+    codes, scales = elutq.elutq_mx4_quantize(X.cuda(), 12, K, fmt, flags=elutq.MX4_FLAG_SWIGLU)
+    Y = torch.empty((12, K), device="cuda")
+    elutq.elutq_mx4_dequantize(codes, scales, Y, 12, K, fmt)
+    B = mx4.BLOCK[fmt]
+    y = np.full((12, K), 1 / (1 + np.exp(-1.0)), dtype=np.float32)
+    y[:, 7] = [w for _, _, w in far]
+    assert np.array_equal(np.nan_to_num(Y.cpu().double().numpy(), nan=-1.0), np.nan_to_num(mx4.values(*mx4.quantize(y, fmt), fmt), nan=-1.0))
+    assert torch.isnan(Y[6:, :B]).all() and not torch.isnan(Y[:, B:]).any()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
 def test_dequantise_every_byte(fmt, out):
     """Every code under every scale byte.  One rounding to fp32 (alpha's product) and one to the output's type."""
