@@ -245,16 +245,46 @@ def elutq_hlq_fit(W, q: int, G: int, t_max: int = 10, trace: bool = False, strea
     return (planes, scales, offsets, tr) if trace else (planes, scales, offsets)
 
 
-_TYPES = None
+_TORCH = None
 
 
-def _type(t) -> int:
-    """ELUTQ_TYPE_ of a tensor (-1: none, which the library refuses)."""
-    global _TYPES
-    if _TYPES is None:
+def _torch():
+    """(torch, {dtype: ELUTQ_TYPE_})"""
+    global _TORCH
+    if _TORCH is None:
         import torch
-        _TYPES = {torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_F32}
-    return _TYPES.get(t.dtype, -1)
+        _TORCH = (torch, {torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_F32})
+    return _TORCH
+
+
+def _refuse(where: str, why: str):
+    raise ElutqError(-1, f"{where} ({why})")
+
+
+def _dense(where: str, t, name: str, dtype, numel: int, device: int) -> int:
+    """Address of a dense tensor of a type, a size at least and a device (kernels read addresses as they are); None -> NULL."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != device:
+        _refuse(where, f"{name}: {dtype}, dense, {numel} values at least on device {device} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _result(where: str, Y, numel: int, device: int):
+    """(address, ELUTQ_TYPE_) of a dense result."""
+    kind = _torch()[1].get(Y.dtype, -1)
+    if kind < 0 or Y.numel() < numel or not Y.is_contiguous() or Y.get_device() != device:
+        _refuse(where, f"result: fp16, bf16 or fp32, dense, {numel} values at least on device {device} wanted, got {Y.dtype} {tuple(Y.shape)} on {Y.device}")
+    return Y.data_ptr(), kind
+
+
+def _device(where: str, t) -> int:
+    """The tensor's device, which has to be the current one."""
+    torch = _torch()[0]
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        _refuse(where, f"tensors on the current CUDA device wanted, got one on {t.device}")
+    return device
 
 
 def elutq_mx4_bytes(fmt: int, rows: int, K: int):
@@ -264,39 +294,72 @@ def elutq_mx4_bytes(fmt: int, rows: int, K: int):
     return codes.value, scales.value
 
 
+def _mx4_block(fmt: int) -> int:
+    return 32 if fmt == MX4_MXFP4 else 16
+
+
 def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, flags: int = 0, prescale=None, index=None, index_div: int = 1,
                        n_rows=None, stream=None):
-    """X fp16, bf16 or fp32 [x_rows, K] (or [x_rows, 2 K], SwiGLU), unit stride along a row -> (codes uint8 [rows, K/2], scales uint8 [rows, K/B])."""
-    import torch
-    if codes is None:
-        codes = X.new_empty((rows, K // 2), dtype=torch.uint8)
-    if scales is None:
-        scales = X.new_empty((rows, K // (32 if fmt == MX4_MXFP4 else 16)), dtype=torch.uint8)
-    stride = X.stride()
-    if len(stride) != 2 or stride[1] != 1:
-        raise ElutqError(-2, "elutq_mx4_quantize")
-    _check(lib().elutq_mx4_quantize(X.data_ptr(), _type(X), X.shape[0], stride[0], rows, K, fmt, flags, _ptr(prescale), _ptr(index), index_div,
-                                    _ptr(n_rows), codes.data_ptr(), scales.data_ptr(), _stream(stream)), "elutq_mx4_quantize")
+    """X fp16, bf16 or fp32 [x_rows, K] (or [x_rows, 2 K], SwiGLU), unit stride along a row -> (codes uint8 [rows, K/2], scales uint8 [rows, K/B]).
+    index int32 [rows], n_rows int32 [1], prescale fp32 [1]."""
+    where = "elutq_mx4_quantize"
+    torch, types = _torch()
+    device = _device(where, X)
+    shape, stride = X.shape, X.stride()
+    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K):
+        _refuse(where, f"X: [x_rows, {2 * K if flags & MX4_FLAG_SWIGLU else K}] with unit stride along a row wanted, got {tuple(shape)}, strides {stride}")
+    half, blocks = K // 2, K // _mx4_block(fmt)
+    c = (codes := X.new_empty((rows, half), dtype=torch.uint8)).data_ptr() if codes is None else _dense(where, codes, "codes", torch.uint8, rows * half, device)
+    s = (scales := X.new_empty((rows, blocks), dtype=torch.uint8)).data_ptr() if scales is None else _dense(where, scales, "scales", torch.uint8, rows * blocks, device)
+    _check(lib().elutq_mx4_quantize(X.data_ptr(), types.get(X.dtype, -1), shape[0], stride[0], rows, K, fmt, flags,
+                                    _dense(where, prescale, "prescale", torch.float32, 1, device), _dense(where, index, "index", torch.int32, rows, device),
+                                    index_div, _dense(where, n_rows, "n_rows", torch.int32, 1, device), c, s, _stream(stream)), where)
     return codes, scales
 
 
 def elutq_mx4_dequantize(codes, scales, Y, rows: int, K: int, fmt: int, alpha=None, stream=None) -> None:
-    _check(lib().elutq_mx4_dequantize(_ptr(codes), _ptr(scales), rows, K, fmt, _ptr(alpha), _ptr(Y), _type(Y), _stream(stream)), "elutq_mx4_dequantize")
+    """codes, scales -> Y fp16, bf16 or fp32 [rows, K]; alpha fp32 [1]."""
+    where = "elutq_mx4_dequantize"
+    torch = _torch()[0]
+    device = _device(where, codes)
+    y, kind = _result(where, Y, rows * K, device)
+    _check(lib().elutq_mx4_dequantize(_dense(where, codes, "codes", torch.uint8, rows * (K // 2), device),
+                                      _dense(where, scales, "scales", torch.uint8, rows * (K // _mx4_block(fmt)), device), rows, K, fmt,
+                                      _dense(where, alpha, "alpha", torch.float32, 1, device), y, kind, _stream(stream)), where)
+
+
+def _mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, rows, K, fmt, device):
+    u8, half, blocks = _torch()[0].uint8, K // 2, K // _mx4_block(fmt)
+    return (_dense(where, x_codes, "x_codes", u8, M * half, device), _dense(where, x_scales, "x_scales", u8, M * blocks, device),
+            _dense(where, w_codes, "w_codes", u8, rows * half, device), _dense(where, w_scales, "w_scales", u8, rows * blocks, device))
 
 
 def elutq_mx4_gemm(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, alpha=None, stream=None) -> None:
-    _check(lib().elutq_mx4_gemm(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(Y), _type(Y), M, N, K, fmt, _ptr(alpha),
-                                _stream(stream)), "elutq_mx4_gemm")
+    """Y fp16, bf16 or fp32 [M, N] = alpha X W^T; codes and scales of X [M, K] and W [N, K]; alpha fp32 [1]."""
+    where = "elutq_mx4_gemm"
+    device = _device(where, Y)
+    y, kind = _result(where, Y, M * N, device)
+    _check(lib().elutq_mx4_gemm(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, N, K, fmt, device), y, kind, M, N, K, fmt,
+                                _dense(where, alpha, "alpha", _torch()[0].float32, 1, device), _stream(stream)), where)
 
 
 def elutq_mx4_gemm_grouped(x_codes, x_scales, w_codes, w_scales, offsets, Y, M: int, N: int, K: int, E: int, fmt: int, alpha=None, stream=None) -> None:
-    _check(lib().elutq_mx4_gemm_grouped(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(offsets), _ptr(Y), _type(Y), M, N, K, E, fmt,
-                                        _ptr(alpha), _stream(stream)), "elutq_mx4_gemm_grouped")
+    """Rows offsets[e] .. offsets[e+1] of X [M, K] times W_e^T: W [E * N, K], offsets int32 [E + 1], alpha fp32 [E]."""
+    where = "elutq_mx4_gemm_grouped"
+    torch = _torch()[0]
+    device = _device(where, Y)
+    y, kind = _result(where, Y, M * N, device)
+    _check(lib().elutq_mx4_gemm_grouped(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, E * N, K, fmt, device),
+                                        _dense(where, offsets, "offsets", torch.int32, E + 1, device), y, kind, M, N, K, E, fmt,
+                                        _dense(where, alpha, "alpha", torch.float32, E, device), _stream(stream)), where)
 
 
 def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, wait_limit: int, stream=None) -> None:
-    _check(lib().elutq_mx4_test_wait_expiry(_ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(Y), _type(Y), M, N, K, fmt, wait_limit,
-                                            _stream(stream)), "elutq_mx4_test_wait_expiry")
+    where = "elutq_mx4_test_wait_expiry"
+    device = _device(where, Y)
+    y, kind = _result(where, Y, M * N, device)
+    _check(lib().elutq_mx4_test_wait_expiry(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, N, K, fmt, device), y, kind, M, N, K, fmt,
+                                            wait_limit, _stream(stream)), where)
 
 
 def elutq_device_status(stream=None) -> int:

@@ -418,8 +418,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     __syncthreads();
     if (CG == 2 || a.split > 1) cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // What reads or writes global memory waits for the kernels in front of this one: the groups' borders here, each role otherwise where it begins.
-    grid_launch_dependents();
+    // What reads or writes global memory waits for the kernels in front of this one: the groups' borders here, each role otherwise where it begins.  (The next
+    // kernel may start once this one's loader has waited: kernels of this library that read weights ahead of their own wait rely on that.)
     if (a.offsets != nullptr) {
         if (warp == 0) {
             grid_dependency_wait();
@@ -446,6 +446,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             int issued = 0;
             bool ok = true;
             grid_dependency_wait();
+            grid_launch_dependents();
             for (int i = first; i < tiles && ok; i += stride) {
                 const Tile t = tile_at<CG>(a, table, i);
                 const int per_cta = CG == 2 ? (t.count + 15) / 16 * 8 : (t.count + 7) / 8 * 8;
@@ -910,6 +911,8 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     const bool grouped = offsets != nullptr;
     const Plan p = plan_for(M, N, K, E, format, grouped, y_type, device_sm_count());
     if (!p.ok) return ELUTQ_ERR_UNSUPPORTED;
+    const int w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
+    if ((long long)w_tiles * ((M + p.tokens - 1) / p.tokens + (grouped ? E : 0)) > 0x3fffffffLL) return ELUTQ_ERR_SHAPE;
     Mx4Args a;
     a.x_scales = reinterpret_cast<const uint8_t*>(x_scales);
     a.w_scales = reinterpret_cast<const uint8_t*>(w_scales);
@@ -920,7 +923,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     a.M = M; a.N = N; a.K = K; a.E = E;
     a.sk = K / mx4_block(format);
     a.tokens = p.tokens;
-    a.w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
+    a.w_tiles = w_tiles;
     a.steps = (K + 255) / 256;
     a.split = p.split;
     a.stages = p.stages;

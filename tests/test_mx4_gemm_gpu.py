@@ -256,3 +256,124 @@ def test_waits_that_run_out_are_reported():
         assert elutq.elutq_device_status() == 0
         elutq.elutq_mx4_gemm(*args, Y, M, N, K, 0)
         assert elutq.elutq_device_status() == 0
+
+
+def test_what_the_binding_turns_down():
+    rng = np.random.default_rng(0)
+    M, N, K, E = 8, 64, 128, 2
+    xc, xs, wc, ws = _dev(*_matrix(rng, M, K, 0), *_matrix(rng, E * N, K, 0))
+    Y = torch.zeros((M, N), device="cuda")
+    off = torch.tensor([0, 3, 8], dtype=torch.int32, device="cuda")
+    X = torch.randn((M, K), device="cuda")
+    before = elutq.elutq_launch_count()
+
+    def refused(call):
+        with pytest.raises(elutq.ElutqError) as e:
+            call()
+        assert e.value.status == -1
+
+    def gemm(xc=xc, xs=xs, wc=wc, ws=ws, Y=Y, alpha=None):
+        elutq.elutq_mx4_gemm(xc, xs, wc, ws, Y, M, N, K, 0, alpha=alpha)
+
+    def grouped(offsets=off, wc=wc, alpha=None):
+        elutq.elutq_mx4_gemm_grouped(xc, xs, wc, ws, offsets, Y, M, N, K, E, 0, alpha=alpha)
+
+    refused(lambda: gemm(xc=xc.cpu()))
+    refused(lambda: gemm(Y=Y.cpu()))
+    refused(lambda: gemm(xc=xc[:-1]))
+    refused(lambda: gemm(ws=ws[:10]))
+    refused(lambda: gemm(xs=xs.float()))
+    refused(lambda: gemm(Y=Y.double()))
+    refused(lambda: gemm(Y=torch.zeros((N, M), device="cuda").T))
+    refused(lambda: gemm(alpha=torch.ones(1, dtype=torch.float64, device="cuda")))
+    refused(lambda: gemm(wc=torch.cat([wc, wc], dim=1)[:, : K // 2]))
+    refused(lambda: grouped(offsets=off.long()))
+    refused(lambda: grouped(offsets=off[:2]))
+    refused(lambda: grouped(wc=wc[:N]))
+    refused(lambda: grouped(alpha=torch.ones(1, device="cuda")))
+    refused(lambda: elutq.elutq_mx4_quantize(X.cpu(), M, K, 0))
+    refused(lambda: elutq.elutq_mx4_quantize(X, M, K, 0, flags=elutq.MX4_FLAG_SWIGLU))
+    refused(lambda: elutq.elutq_mx4_quantize(X.T, M, K, 0))
+    refused(lambda: elutq.elutq_mx4_quantize(X, M, K, 0, index=torch.zeros(M, dtype=torch.int64, device="cuda")))
+    refused(lambda: elutq.elutq_mx4_quantize(X, M, K, 0, n_rows=torch.zeros(1, dtype=torch.int32)))
+    refused(lambda: elutq.elutq_mx4_quantize(X, M, K, 0, codes=xc[:-1]))
+    refused(lambda: elutq.elutq_mx4_dequantize(xc, xs, Y[:, :32].contiguous(), M, K, 0))
+    refused(lambda: elutq.elutq_mx4_quantize(X.double(), M, K, 0))
+    assert elutq.elutq_launch_count() == before
+    gemm()
+    grouped()
+    assert elutq.elutq_device_status() == 0
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (40, 3000, 2048), (512, 2048, 1024)])
+def test_operands_written_just_before(M, N, K):
+    """Weights, activations and factor come from kernels right in front of the product, over and over, with nothing waited for; another product and an HLQ layer
+    that has just been packed come behind it."""
+    from gpu_util import x_dev
+    import workloads
+    from oracle import hlq
+    from workloads import synth
+
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    W = [torch.randn((N, K), generator=gen, device="cuda").bfloat16() for _ in range(3)]
+    X = [torch.randn((M, K), generator=gen, device="cuda").bfloat16() for _ in range(3)]
+    factors = [0.5, 2.0, -1.0]
+    qw, qx = [elutq.elutq_mx4_quantize(w, N, K, 1) for w in W], [elutq.elutq_mx4_quantize(x, M, K, 1) for x in X]
+    want = []
+    for i in range(3):
+        y = torch.empty((M, N), device="cuda")
+        elutq.elutq_mx4_gemm(*qx[i], *qw[i], y, M, N, K, 1)
+        torch.cuda.synchronize()
+        want.append(y * factors[i])
+    layers = [workloads.hlq_layer(i, "behind", 2, 128, 512, 1024) for i in range(2)]
+    hx = synth.activations(1, "behind/x", 1, 1024)
+    planes = [(torch.from_numpy(l.planes).cuda(), *(torch.from_numpy(v.view(np.int16)).cuda().view(torch.float16) for v in (l.scales, l.offsets))) for l in layers]
+    packed = elutq.elutq_pack(*planes[0], 2, 128, 512, 1024)
+    hxd = x_dev(hx)
+    wc, ws, xc, xs, alpha = torch.empty_like(qw[0][0]), torch.empty_like(qw[0][1]), torch.empty_like(qx[0][0]), torch.empty_like(qx[0][1]), torch.empty(1, device="cuda")
+    outs, hys = [torch.empty((M, N), device="cuda") for _ in range(12)], [torch.empty((1, 512), dtype=torch.float16, device="cuda") for _ in range(12)]
+    torch.cuda.synchronize()
+    for k in range(12):
+        i = k % 3
+        elutq.elutq_pack(*planes[k % 2], 2, 128, 512, 1024, packed=packed)
+        elutq.elutq_mx4_quantize(W[i], N, K, 1, codes=wc, scales=ws)
+        elutq.elutq_mx4_quantize(X[i], M, K, 1, codes=xc, scales=xs)
+        alpha.fill_(factors[i])
+        elutq.elutq_mx4_gemm(xc, xs, wc, ws, outs[k], M, N, K, 1, alpha=alpha)
+        elutq.elutq_lut_gemm(hxd, packed, hys[k], 1, 512, 1024)
+    torch.cuda.synchronize()
+    for k in range(12):
+        assert torch.equal(outs[k], want[k % 3]), k
+        l = layers[k % 2]
+        assert hlq.rel_fro_error(hys[k].cpu().numpy(), hlq.matmul(hx, l.planes, l.scales, l.offsets, 128)) <= 1e-3
+
+
+def test_more_than_2_31_values():
+    """Offsets beyond 32 bits: the last rows of large weights, results and inputs."""
+    K, N, M = 64, 70_000, 33_000                     # Y: 2.3e9 values
+    rng = np.random.default_rng(9)
+    xc, xs = _matrix(rng, M, K, 0)
+    wc, ws = _matrix(rng, N, K, 0)
+    Y = torch.empty((M, N), dtype=torch.float16, device="cuda")
+    elutq.elutq_mx4_gemm(*_dev(xc, xs, wc, ws), Y, M, N, K, 0)
+    rows = np.array([0, 12_345, M - 2, M - 1])
+    part = (xc[rows], xs[rows], wc, ws)
+    _assert_close(Y[torch.from_numpy(rows).cuda()], mx4.matmul(*part, 0), mx4.magnitude(*part, 0), K, "f16")
+    del Y
+    # weights of more than 2^32 values (2^31 bytes of codes), the last rows of which are compared
+    K, N, M = 16384, 300_000, 3
+    xc, xs = _matrix(rng, M, K, 0)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    wc = torch.randint(0, 256, (N, K // 2), generator=gen, dtype=torch.uint8, device="cuda")
+    ws = torch.randint(122, 130, (N, K // 32), generator=gen, dtype=torch.uint8, device="cuda")
+    Y = torch.empty((M, N), device="cuda")
+    elutq.elutq_mx4_gemm(*_dev(xc, xs), wc, ws, Y, M, N, K, 0)
+    part = (xc, xs, wc[-300:].cpu().numpy(), ws[-300:].cpu().numpy())
+    _assert_close(Y[:, -300:], mx4.matmul(*part, 0), mx4.magnitude(*part, 0), K, "f32")
+    # the same bytes back as values and as codes again
+    V = torch.empty((N, K), dtype=torch.bfloat16, device="cuda")
+    elutq.elutq_mx4_dequantize(wc, ws, V, N, K, 0)
+    assert np.array_equal(V[-40:].double().cpu().numpy(), mx4.values(wc[-40:].cpu().numpy(), ws[-40:].cpu().numpy(), 0))
+    c2, s2 = elutq.elutq_mx4_quantize(V, N, K, 0)
+    want = mx4.quantize(V[-40:].float().cpu().numpy(), 0)
+    assert np.array_equal(c2[-40:].cpu().numpy(), want[0]) and np.array_equal(s2[-40:].cpu().numpy(), want[1])

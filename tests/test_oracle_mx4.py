@@ -108,8 +108,13 @@ def test_refusals_of_the_products():
     assert elutq.elutq_launch_count() == before
 
 
-def test_the_binding_refuses_what_it_cannot_marshal():
-    with pytest.raises(elutq.ElutqError):
-        elutq.elutq_mx4_quantize(torch.zeros((4, 64), dtype=torch.float64), 4, 64, 0, stream=0)
-    with pytest.raises(elutq.ElutqError):
-        elutq.elutq_mx4_quantize(torch.zeros((64, 4), dtype=torch.float16).T, 4, 64, 0, stream=0)
+def test_the_binding_refuses_host_memory():
+    """Kernels read addresses as they are: what is not on the current device is turned down before any call."""
+    x, c, s = torch.zeros((4, 64), dtype=torch.float16), torch.zeros((4, 32), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.uint8)
+    before = elutq.elutq_launch_count()
+    if not torch.cuda.is_available():
+        for call in (lambda: elutq.elutq_mx4_quantize(x, 4, 64, 0, stream=0), lambda: elutq.elutq_mx4_dequantize(c, s, x, 4, 64, 0, stream=0),
+                     lambda: elutq.elutq_mx4_gemm(c, s, c, s, x, 4, 4, 64, 0, stream=0)):
+            with pytest.raises(elutq.ElutqError):
+                call()
+    assert elutq.elutq_launch_count() == before
