@@ -249,42 +249,28 @@ _TORCH = None
 
 
 def _torch():
-    """(torch, {dtype: ELUTQ_TYPE_})"""
+    """(torch, {dtype: ELUTQ_TYPE_}, function: current device, function: a device's current stream)"""
     global _TORCH
     if _TORCH is None:
         import torch
-        _TORCH = (torch, {torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_F32})
+        device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        _TORCH = (torch, {torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16, torch.float32: TYPE_F32}, device, raw)
     return _TORCH
 
 
-def _refuse(where: str, why: str):
-    raise ElutqError(-1, f"{where} ({why})")
+def _refuse(where: str, wanted: str, *tensors):
+    got = ", ".join("nothing" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ' with gaps'}" for t in tensors)
+    raise ElutqError(-1, f"{where} ({wanted}, dense and on the current CUDA device; got {got})")
 
 
-def _dense(where: str, t, name: str, dtype, numel: int, device: int) -> int:
-    """Address of a dense tensor of a type, a size at least and a device (kernels read addresses as they are); None -> NULL."""
+def _small(where: str, name: str, t, dtype, numel: int, device: int) -> int:
+    """Address of a small operand; None -> NULL."""
     if t is None:
         return 0
     if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous() or t.get_device() != device:
-        _refuse(where, f"{name}: {dtype}, dense, {numel} values at least on device {device} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        _refuse(where, f"{name}: {numel} values of {dtype} wanted", t)
     return t.data_ptr()
-
-
-def _result(where: str, Y, numel: int, device: int):
-    """(address, ELUTQ_TYPE_) of a dense result."""
-    kind = _torch()[1].get(Y.dtype, -1)
-    if kind < 0 or Y.numel() < numel or not Y.is_contiguous() or Y.get_device() != device:
-        _refuse(where, f"result: fp16, bf16 or fp32, dense, {numel} values at least on device {device} wanted, got {Y.dtype} {tuple(Y.shape)} on {Y.device}")
-    return Y.data_ptr(), kind
-
-
-def _device(where: str, t) -> int:
-    """The tensor's device, which has to be the current one."""
-    torch = _torch()[0]
-    device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
-        _refuse(where, f"tensors on the current CUDA device wanted, got one on {t.device}")
-    return device
 
 
 def elutq_mx4_bytes(fmt: int, rows: int, K: int):
@@ -303,63 +289,84 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
     """X fp16, bf16 or fp32 [x_rows, K] (or [x_rows, 2 K], SwiGLU), unit stride along a row -> (codes uint8 [rows, K/2], scales uint8 [rows, K/B]).
     index int32 [rows], n_rows int32 [1], prescale fp32 [1]."""
     where = "elutq_mx4_quantize"
-    torch, types = _torch()
-    device = _device(where, X)
+    torch, types, current, raw = _torch()
+    if not X.is_cuda:
+        _refuse(where, "X: a CUDA tensor wanted", X)
+    d = current()
     shape, stride = X.shape, X.stride()
-    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K):
-        _refuse(where, f"X: [x_rows, {2 * K if flags & MX4_FLAG_SWIGLU else K}] with unit stride along a row wanted, got {tuple(shape)}, strides {stride}")
+    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K) or X.get_device() != d:
+        _refuse(where, f"X: [x_rows, {2 * K if flags & MX4_FLAG_SWIGLU else K}] with unit stride along a row wanted", X)
     half, blocks = K // 2, K // _mx4_block(fmt)
-    c = (codes := X.new_empty((rows, half), dtype=torch.uint8)).data_ptr() if codes is None else _dense(where, codes, "codes", torch.uint8, rows * half, device)
-    s = (scales := X.new_empty((rows, blocks), dtype=torch.uint8)).data_ptr() if scales is None else _dense(where, scales, "scales", torch.uint8, rows * blocks, device)
+    if codes is None:
+        codes = X.new_empty((rows, half), dtype=torch.uint8)
+    elif codes.nbytes != rows * half or not codes.is_contiguous() or codes.get_device() != d:
+        _refuse(where, f"codes: {rows * half} bytes wanted", codes)
+    if scales is None:
+        scales = X.new_empty((rows, blocks), dtype=torch.uint8)
+    elif scales.nbytes != rows * blocks or not scales.is_contiguous() or scales.get_device() != d:
+        _refuse(where, f"scales: {rows * blocks} bytes wanted", scales)
     _check(lib().elutq_mx4_quantize(X.data_ptr(), types.get(X.dtype, -1), shape[0], stride[0], rows, K, fmt, flags,
-                                    _dense(where, prescale, "prescale", torch.float32, 1, device), _dense(where, index, "index", torch.int32, rows, device),
-                                    index_div, _dense(where, n_rows, "n_rows", torch.int32, 1, device), c, s, _stream(stream)), where)
+                                    _small(where, "prescale", prescale, torch.float32, 1, d), _small(where, "index", index, torch.int32, rows, d), index_div,
+                                    _small(where, "n_rows", n_rows, torch.int32, 1, d), codes.data_ptr(), scales.data_ptr(),
+                                    raw(d) if stream is None else _stream(stream)), where)
     return codes, scales
 
 
 def elutq_mx4_dequantize(codes, scales, Y, rows: int, K: int, fmt: int, alpha=None, stream=None) -> None:
     """codes, scales -> Y fp16, bf16 or fp32 [rows, K]; alpha fp32 [1]."""
     where = "elutq_mx4_dequantize"
-    torch = _torch()[0]
-    device = _device(where, codes)
-    y, kind = _result(where, Y, rows * K, device)
-    _check(lib().elutq_mx4_dequantize(_dense(where, codes, "codes", torch.uint8, rows * (K // 2), device),
-                                      _dense(where, scales, "scales", torch.uint8, rows * (K // _mx4_block(fmt)), device), rows, K, fmt,
-                                      _dense(where, alpha, "alpha", torch.float32, 1, device), y, kind, _stream(stream)), where)
+    torch, types, current, raw = _torch()
+    if not Y.is_cuda:
+        _refuse(where, "a CUDA tensor wanted", Y)
+    d = current()
+    if (codes.nbytes != rows * (K // 2) or not codes.is_contiguous() or codes.get_device() != d or
+            scales.nbytes != rows * (K // _mx4_block(fmt)) or not scales.is_contiguous() or scales.get_device() != d or
+            Y.numel() != rows * K or not Y.is_contiguous() or Y.get_device() != d):
+        _refuse(where, f"codes, scales: {rows * (K // 2)} and {rows * (K // _mx4_block(fmt))} bytes, Y: {rows} x {K} values wanted", codes, scales, Y)
+    _check(lib().elutq_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, K, fmt, _small(where, "alpha", alpha, torch.float32, 1, d),
+                                      Y.data_ptr(), types.get(Y.dtype, -1), raw(d) if stream is None else _stream(stream)), where)
 
 
-def _mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, rows, K, fmt, device):
-    u8, half, blocks = _torch()[0].uint8, K // 2, K // _mx4_block(fmt)
-    return (_dense(where, x_codes, "x_codes", u8, M * half, device), _dense(where, x_scales, "x_scales", u8, M * blocks, device),
-            _dense(where, w_codes, "w_codes", u8, rows * half, device), _dense(where, w_scales, "w_scales", u8, rows * blocks, device))
+def _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, rows, fmt):
+    """The product's operands and result are dense, of the right size (codes and scales are bytes, whatever type they go by) and on the current device."""
+    if not Y.is_cuda:
+        _refuse(where, "a CUDA tensor wanted", Y)
+    d, half, blocks = _TORCH[2](), K // 2, K // _mx4_block(fmt)
+    if (x_codes.nbytes != M * half or not x_codes.is_contiguous() or x_codes.get_device() != d or
+            x_scales.nbytes != M * blocks or not x_scales.is_contiguous() or x_scales.get_device() != d or
+            w_codes.nbytes != rows * half or not w_codes.is_contiguous() or w_codes.get_device() != d or
+            w_scales.nbytes != rows * blocks or not w_scales.is_contiguous() or w_scales.get_device() != d or
+            Y.numel() != M * N or not Y.is_contiguous() or Y.get_device() != d):
+        _refuse(where, f"X: {M * half} and {M * blocks} bytes, W: {rows * half} and {rows * blocks} bytes, Y: {M} x {N} values wanted",
+                x_codes, x_scales, w_codes, w_scales, Y)
+    return d
 
 
 def elutq_mx4_gemm(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, alpha=None, stream=None) -> None:
     """Y fp16, bf16 or fp32 [M, N] = alpha X W^T; codes and scales of X [M, K] and W [N, K]; alpha fp32 [1]."""
     where = "elutq_mx4_gemm"
-    device = _device(where, Y)
-    y, kind = _result(where, Y, M * N, device)
-    _check(lib().elutq_mx4_gemm(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, N, K, fmt, device), y, kind, M, N, K, fmt,
-                                _dense(where, alpha, "alpha", _torch()[0].float32, 1, device), _stream(stream)), where)
+    torch, types, _, raw = _torch()
+    d = _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
+    _check(lib().elutq_mx4_gemm(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(), types.get(Y.dtype, -1), M, N, K,
+                                fmt, _small(where, "alpha", alpha, torch.float32, 1, d), raw(d) if stream is None else _stream(stream)), where)
 
 
 def elutq_mx4_gemm_grouped(x_codes, x_scales, w_codes, w_scales, offsets, Y, M: int, N: int, K: int, E: int, fmt: int, alpha=None, stream=None) -> None:
     """Rows offsets[e] .. offsets[e+1] of X [M, K] times W_e^T: W [E * N, K], offsets int32 [E + 1], alpha fp32 [E]."""
     where = "elutq_mx4_gemm_grouped"
-    torch = _torch()[0]
-    device = _device(where, Y)
-    y, kind = _result(where, Y, M * N, device)
-    _check(lib().elutq_mx4_gemm_grouped(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, E * N, K, fmt, device),
-                                        _dense(where, offsets, "offsets", torch.int32, E + 1, device), y, kind, M, N, K, E, fmt,
-                                        _dense(where, alpha, "alpha", torch.float32, E, device), _stream(stream)), where)
+    torch, types, _, raw = _torch()
+    d = _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, E * N, fmt)
+    _check(lib().elutq_mx4_gemm_grouped(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
+                                        _small(where, "offsets", offsets, torch.int32, E + 1, d), Y.data_ptr(), types.get(Y.dtype, -1), M, N, K, E, fmt,
+                                        _small(where, "alpha", alpha, torch.float32, E, d), raw(d) if stream is None else _stream(stream)), where)
 
 
 def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, wait_limit: int, stream=None) -> None:
     where = "elutq_mx4_test_wait_expiry"
-    device = _device(where, Y)
-    y, kind = _result(where, Y, M * N, device)
-    _check(lib().elutq_mx4_test_wait_expiry(*_mx4_operands(where, x_codes, x_scales, w_codes, w_scales, M, N, K, fmt, device), y, kind, M, N, K, fmt,
-                                            wait_limit, _stream(stream)), where)
+    types = _torch()[1]
+    _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
+    _check(lib().elutq_mx4_test_wait_expiry(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(),
+                                            types.get(Y.dtype, -1), M, N, K, fmt, wait_limit, _stream(stream)), where)
 
 
 def elutq_device_status(stream=None) -> int:

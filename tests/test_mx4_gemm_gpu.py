@@ -272,7 +272,7 @@ def test_what_the_binding_turns_down():
             call()
         assert e.value.status == -1
 
-    def gemm(xc=xc, xs=xs, wc=wc, ws=ws, Y=Y, alpha=None):
+    def gemm(xc=xc, xs=xs, wc=wc[:N], ws=ws[:N], Y=Y, alpha=None):
         elutq.elutq_mx4_gemm(xc, xs, wc, ws, Y, M, N, K, 0, alpha=alpha)
 
     def grouped(offsets=off, wc=wc, alpha=None):
@@ -286,7 +286,8 @@ def test_what_the_binding_turns_down():
     refused(lambda: gemm(Y=Y.double()))
     refused(lambda: gemm(Y=torch.zeros((N, M), device="cuda").T))
     refused(lambda: gemm(alpha=torch.ones(1, dtype=torch.float64, device="cuda")))
-    refused(lambda: gemm(wc=torch.cat([wc, wc], dim=1)[:, : K // 2]))
+    refused(lambda: gemm(wc=wc))
+    refused(lambda: gemm(wc=torch.cat([wc, wc], dim=1)[:N, : K // 2]))
     refused(lambda: grouped(offsets=off.long()))
     refused(lambda: grouped(offsets=off[:2]))
     refused(lambda: grouped(wc=wc[:N]))
