@@ -44,9 +44,15 @@ constexpr int kMaxGroups = 1024;
 constexpr int kTurn = 4, kTurns = 2;
 template <int NB>
 constexpr int kThreads = 32 * (6 + (1 + NB) * 2);
-constexpr int kAcc1 = kMaxTokens - 48, kScaleCols = 2 * kMaxTokens - 48;     // second accumulator, which shares 48 columns with the first; scales (48 columns)
+// Columns of tensor memory: scales at the end (48 NVFP4, 24 MXFP4 for pairs), in front of them two accumulators.  Tiles of up to kApart tokens have both to themselves;
+// higher ones share kShared columns of them.
+template <int FMT>
+constexpr int kScaleCols = FMT == ELUTQ_MX4_NVFP4 ? 464 : 488;
+template <int FMT>
+constexpr int kApart = kScaleCols<FMT> / 2 / 16 * 16;
+constexpr int kShared = 48;
 constexpr int kSmem = 232448;
-constexpr int kChunk = kMaxTokens - kAcc1;        // columns that the epilogue takes at once
+constexpr int kChunk = kShared;            // columns that the epilogue takes at once
 constexpr int kTurnBytes = 4 * kChunk * 64;      // 32 weight rows of them for each epilogue warp, 16 bits each
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
@@ -363,6 +369,8 @@ template <int FMT, int CG>
 __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map, const Mx4Args a) {
     constexpr int CH = FMT == ELUTQ_MX4_MXFP4 ? 2 : 4;            // groups of four scales in a step
     constexpr int NB = CG;
+    const bool overlap = a.tokens > kApart<FMT>;
+    const int acc1 = overlap ? kMaxTokens - kShared : kApart<FMT>;                      // the second accumulator
     constexpr int SUB = 4 / CH;                                   // MMAs (64 k) that share a group
     extern __shared__ __align__(1024) uint8_t smem[];
     const int x_bytes = (a.tokens / CG + 7) / 8 * 1024;           // of a stage
@@ -477,8 +485,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     } else if (warp == 1 && leader) {
         if (elect_one()) {
             Ring r(a.stages), rs(kTurns);
-            const bool overlap = a.tokens > kAcc1;
-            const uint32_t sa = tmem + kScaleCols, sb = sa + 4 * CH;
+            const uint32_t sa = tmem + kScaleCols<FMT>, sb = sa + 4 * CH;
             const uint64_t da0 = operand_desc(smem_u32(sW)), db0 = operand_desc(smem_u32(sX)), ds0 = scales_desc(smem_u32(sS));
             const int whole = a.K / 256;                          // steps of four MMAs
             int n = 0;
@@ -491,7 +498,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 if (!ok) break;
                 const int cols = CG == 2 ? (t.count + 15) / 16 * 16 : (t.count + 7) / 8 * 8;
                 const uint32_t idesc = 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (FMT == ELUTQ_MX4_MXFP4 ? 1u << 23 : 0u) | (uint32_t)(CG * kTileW >> 4) << 24;
-                const uint32_t acc = tmem + (b ? kAcc1 : 0);
+                const uint32_t acc = tmem + (b ? acc1 : 0);
                 for (int s = step0; s < step1; ++s) {
                     const int in_turn = (s - step0) % kTurn;
                     ok = wait_alone<CG == 2>(bar(kBarFull + r.i), r.phase, gave_up, limit);
@@ -537,7 +544,6 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
     } else if (warp >= 4 && warp < 8) {
         const int quarter = warp & 3;                             // lanes of tensor memory
         grid_dependency_wait();
-        const bool overlap = a.tokens > kAcc1;
         int n = 0;
         bool ok = true;
         for (int i = first; i < tiles && ok; i += stride, ++n) {
@@ -547,7 +553,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             if (a.split > 1) ok = epilogue_agrees(ok && wait<true>(bar(kBarPartsFree), ((uint32_t)n & 1u) ^ 1u, gave_up, limit));
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t acc = tmem + (b ? kAcc1 : 0) + ((uint32_t)(quarter * 32) << 16);
+            const uint32_t acc = tmem + (b ? acc1 : 0) + ((uint32_t)(quarter * 32) << 16);
             const float alpha = a.alpha != nullptr ? __ldg(a.alpha + t.e) : 1.0f;
             const int row = quarter * 32 + lane, col = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + row;
             auto release = [&](int which) {
@@ -672,7 +678,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             };
             auto all_columns = [&](auto&& some) {
                 if (overlap) {
-                    const int c0 = b == 0 ? kAcc1 : 0, c1 = b == 0 ? 0 : kChunk, end = min(t.count, c1 + kAcc1);
+                    const int c0 = b == 0 ? acc1 : 0, c1 = b == 0 ? 0 : kShared, end = min(t.count, c1 + acc1);
                     some(c0, min(t.count, c0 + kChunk), [&] { release(b ^ 1); });
                     for (int c = c1; c < end; c += kChunk) some(c, end, [] {});
                 } else {
