@@ -72,6 +72,7 @@ struct Mx4Args {
     int split;                 // CTAs that share a tile's K
     int stages;
     int x_box;                 // rows of one X load
+    int once;                  // weights are read by one tile of tokens
     int turn;                  // the epilogue turns 16-bit results in shared memory
     int x_wide, w_wide;        // scales of a row start on 16 bytes
     int test;                  // 1: no load is issued
@@ -171,6 +172,15 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
     else
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                      :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint64_t policy) {
+    if constexpr (CG == 2)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
 }
 // K-major, 128-byte swizzle, 1024 bytes per 8 rows
 __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr) {
@@ -453,6 +463,11 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             Ring r(a.stages);
             int issued = 0;
             bool ok = true;
+            // Weights that one tile of tokens reads are not wanted again: their lines make room first (us without and with it: 64 x 57344 x 8192 NVFP4 51.2 and 46.4,
+            // 64 experts of 4096 x 2048 with 64 rows 30.4 and 27.6, 1 x 28672 x 4096 14.8 and 14.1).  All other loads go without a policy: with one that says nothing
+            // the experts took 31.9.
+            uint64_t once;
+            asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
             grid_dependency_wait();
             grid_launch_dependents();
             for (int i = first; i < tiles && ok; i += stride) {
@@ -466,7 +481,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                     if (!ok) break;
                     const uint32_t full = CG == 2 ? at_rank(bar(kBarFull + r.i), 0) : bar(kBarFull + r.i);
                     if (leader) expect(bar(kBarFull + r.i), bytes);
-                    tma_load<CG>(smem_u32(sW + r.i * w_bytes), &w_map, s * kStepBytes, w_row, full);
+                    if (a.once) tma_load<CG>(smem_u32(sW + r.i * w_bytes), &w_map, s * kStepBytes, w_row, full, once);
+                    else tma_load<CG>(smem_u32(sW + r.i * w_bytes), &w_map, s * kStepBytes, w_row, full);
                     for (int b = 0; b < boxes; ++b)
                         tma_load<CG>(smem_u32(sX + r.i * x_bytes + b * a.x_box * kStepBytes), &x_map, s * kStepBytes, x_row + b * a.x_box, full);
                     ++issued;
@@ -934,6 +950,7 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
     a.split = p.split;
     a.stages = p.stages;
     a.x_box = p.x_box;
+    a.once = (grouped ? (M + E - 1) / E : M) <= p.tokens;
     a.turn = p.turn;
     a.x_wide = mx4_aligned(x_scales, 16) && a.sk % 16 == 0;
     a.w_wide = mx4_aligned(w_scales, 16) && a.sk % 16 == 0;
