@@ -802,6 +802,7 @@ bool fill_plan(Plan& p, int format, int E, bool grouped) {
 double estimate_us(long long tiles, double groups, int N, int K, int format, int cg, int tokens, int split, int num_sms) {
     const int steps = (K + 255) / 256, units = (steps + 1) / 2;
     const long long teams = cg == 2 ? num_sms / 2 : split > 1 ? resident_clusters(split) : num_sms;
+    if (teams <= 0) return 1e30;
     const long long rounds = (tiles + teams - 1) / teams;
     const int own = split > 1 ? 2 * ((units + split - 1) / split) : steps;
     const double row = 128.0 + 256.0 / mx4_block(format), step_us = (cg == 2 ? 0.25 : 0.24) + 0.0001 * tokens + (format == ELUTQ_MX4_NVFP4 ? 0.028 : 0.0);

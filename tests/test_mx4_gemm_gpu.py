@@ -169,6 +169,38 @@ def test_odd_scale_bases_and_extreme_scales(fmt):
         _assert_close(Y, want, A, K, "f32", f"offset {off}")
 
 
+def test_the_ends_of_the_power_of_two_scales():
+    """E8M0 bytes 0 to 254: scales of both operands whose product is 1, or near the ends of fp32."""
+    rng = np.random.default_rng(12)
+    M, N, K = 9, 140, 128
+    xc, _ = _matrix(rng, M, K, 0)
+    wc, _ = _matrix(rng, N, K, 0)
+    for bx, bw in ((0, 254), (254, 0), (1, 253), (127, 127), (0, 127 + 8), (20, 140), (254, 100), (190, 180)):
+        xs, ws = np.full((M, K // 32), bx, dtype=np.uint8), np.full((N, K // 32), bw, dtype=np.uint8)
+        Y = torch.full((M, N), float("nan"), device="cuda")
+        elutq.elutq_mx4_gemm(*_dev(xc, xs, wc, ws), Y, M, N, K, 0)
+        _assert_close(Y, mx4.matmul(xc, xs, wc, ws, 0), mx4.magnitude(xc, xs, wc, ws, 0), K, "f32", f"{bx}, {bw}")
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_calls(seed):
+    rng = np.random.default_rng(1000 + seed)
+
+    def log(lo, hi):
+        return int(round(lo * (hi / lo) ** rng.random()))
+
+    for _ in range(3):
+        fmt, out = int(rng.integers(0, 2)), ["f16", "bf16", "f32"][int(rng.integers(0, 3))]
+        K = 32 * log(1, 90)
+        if rng.random() < 0.5:
+            _gemm(rng, log(1, 700), log(1, 3000), K, fmt, out, alpha=None if rng.random() < 0.5 else float(np.exp2(rng.integers(-9, 3))))
+        else:
+            E = log(1, 60)
+            sizes = rng.multinomial(log(1, 900), rng.dirichlet(np.full(E, 0.3)))
+            borders = [0, *np.cumsum(sizes).tolist()]
+            _grouped(rng, borders, log(1, 700), K, E, fmt, out, max(borders[-1], 1) + int(rng.integers(0, 20)), alpha=np.exp2(rng.integers(-9, 3, E)).astype(np.float32))
+
+
 def test_neighbouring_memory_is_left_alone():
     rng = np.random.default_rng(2)
     for M, N in ((1, 130), (13, 129), (130, 257), (300, 129)):
