@@ -457,7 +457,7 @@ int elutq_mx4_test_wait_expiry(const void* x_codes, const void* x_scales, const 
                                int y_type, int M, int N, int K, int format, unsigned wait_limit, void* stream);
 
 /*
- * Device-side status of the library-owned scratch of `stream` (synchronises the stream).
+ * Device-side status of the library-owned scratch of `stream` and of the current device's 4-bit products (synchronises the stream).
  * *status is 0 unless a kernel gave up on a bounded wait (then a non-zero code that stays set
  * until elutq_release_scratch).  Kernels never spin without a limit.  While it is set, the finalize kernels
  * of calls with a K split write no Y.
