@@ -290,11 +290,8 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
     index int32 [rows], n_rows int32 [1], prescale fp32 [1]."""
     where = "elutq_mx4_quantize"
     torch, types, current, raw = _torch()
-    if not X.is_cuda:
-        _refuse(where, "X: a CUDA tensor wanted", X)
-    d = current()
-    shape, stride = X.shape, X.stride()
-    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K) or X.get_device() != d:
+    d, shape, stride = X.get_device(), X.shape, X.stride()
+    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K) or d < 0 or d != current():
         _refuse(where, f"X: [x_rows, {2 * K if flags & MX4_FLAG_SWIGLU else K}] with unit stride along a row wanted", X)
     half, blocks = K // 2, K // _mx4_block(fmt)
     if codes is None:
@@ -316,27 +313,35 @@ def elutq_mx4_dequantize(codes, scales, Y, rows: int, K: int, fmt: int, alpha=No
     """codes, scales -> Y fp16, bf16 or fp32 [rows, K]; alpha fp32 [1]."""
     where = "elutq_mx4_dequantize"
     torch, types, current, raw = _torch()
-    if not Y.is_cuda:
-        _refuse(where, "a CUDA tensor wanted", Y)
-    d = current()
-    if (codes.nbytes != rows * (K // 2) or not codes.is_contiguous() or codes.get_device() != d or
+    d = Y.get_device()
+    if (d < 0 or d != current() or codes.nbytes != rows * (K // 2) or not codes.is_contiguous() or codes.get_device() != d or
             scales.nbytes != rows * (K // _mx4_block(fmt)) or not scales.is_contiguous() or scales.get_device() != d or
-            Y.numel() != rows * K or not Y.is_contiguous() or Y.get_device() != d):
+            Y.numel() != rows * K or not Y.is_contiguous()):
         _refuse(where, f"codes, scales: {rows * (K // 2)} and {rows * (K // _mx4_block(fmt))} bytes, Y: {rows} x {K} values wanted", codes, scales, Y)
     _check(lib().elutq_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, K, fmt, _small(where, "alpha", alpha, torch.float32, 1, d),
                                       Y.data_ptr(), types.get(Y.dtype, -1), raw(d) if stream is None else _stream(stream)), where)
 
 
+_PRODUCTS = None
+
+
+def _products():
+    """What a call of the products needs, looked up once: their C functions, ELUTQ_TYPE_ by dtype, the current device and a device's current stream."""
+    global _PRODUCTS
+    if _PRODUCTS is None:
+        _, types, current, raw = _torch()
+        _PRODUCTS = (lib().elutq_mx4_gemm, lib().elutq_mx4_gemm_grouped, types, current, raw)
+    return _PRODUCTS
+
+
 def _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, rows, fmt):
     """The product's operands and result are dense, of the right size (codes and scales are bytes, whatever type they go by) and on the current device."""
-    if not Y.is_cuda:
-        _refuse(where, "a CUDA tensor wanted", Y)
-    d, half, blocks = _TORCH[2](), K // 2, K // _mx4_block(fmt)
-    if (x_codes.nbytes != M * half or not x_codes.is_contiguous() or x_codes.get_device() != d or
+    d, half, blocks = Y.get_device(), K // 2, K // 32 if fmt == MX4_MXFP4 else K // 16
+    if (d < 0 or d != _PRODUCTS[3]() or Y.numel() != M * N or not Y.is_contiguous() or
+            x_codes.nbytes != M * half or not x_codes.is_contiguous() or x_codes.get_device() != d or
             x_scales.nbytes != M * blocks or not x_scales.is_contiguous() or x_scales.get_device() != d or
             w_codes.nbytes != rows * half or not w_codes.is_contiguous() or w_codes.get_device() != d or
-            w_scales.nbytes != rows * blocks or not w_scales.is_contiguous() or w_scales.get_device() != d or
-            Y.numel() != M * N or not Y.is_contiguous() or Y.get_device() != d):
+            w_scales.nbytes != rows * blocks or not w_scales.is_contiguous() or w_scales.get_device() != d):
         _refuse(where, f"X: {M * half} and {M * blocks} bytes, W: {rows * half} and {rows * blocks} bytes, Y: {M} x {N} values wanted",
                 x_codes, x_scales, w_codes, w_scales, Y)
     return d
@@ -344,26 +349,29 @@ def _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, rows, fm
 
 def elutq_mx4_gemm(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, alpha=None, stream=None) -> None:
     """Y fp16, bf16 or fp32 [M, N] = alpha X W^T; codes and scales of X [M, K] and W [N, K]; alpha fp32 [1]."""
-    where = "elutq_mx4_gemm"
-    torch, types, _, raw = _torch()
-    d = _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
-    _check(lib().elutq_mx4_gemm(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(), types.get(Y.dtype, -1), M, N, K,
-                                fmt, _small(where, "alpha", alpha, torch.float32, 1, d), raw(d) if stream is None else _stream(stream)), where)
+    gemm, _, types, _, raw = _PRODUCTS or _products()
+    d = _mx4_check("elutq_mx4_gemm", x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
+    status = gemm(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(), types.get(Y.dtype, -1), M, N, K, fmt,
+                  0 if alpha is None else _small("elutq_mx4_gemm", "alpha", alpha, _TORCH[0].float32, 1, d), raw(d) if stream is None else _stream(stream))
+    if status != 0:
+        raise ElutqError(status, "elutq_mx4_gemm")
 
 
 def elutq_mx4_gemm_grouped(x_codes, x_scales, w_codes, w_scales, offsets, Y, M: int, N: int, K: int, E: int, fmt: int, alpha=None, stream=None) -> None:
     """Rows offsets[e] .. offsets[e+1] of X [M, K] times W_e^T: W [E * N, K], offsets int32 [E + 1], alpha fp32 [E]."""
     where = "elutq_mx4_gemm_grouped"
-    torch, types, _, raw = _torch()
+    _, grouped, types, _, raw = _PRODUCTS or _products()
     d = _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, E * N, fmt)
-    _check(lib().elutq_mx4_gemm_grouped(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(),
-                                        _small(where, "offsets", offsets, torch.int32, E + 1, d), Y.data_ptr(), types.get(Y.dtype, -1), M, N, K, E, fmt,
-                                        _small(where, "alpha", alpha, torch.float32, E, d), raw(d) if stream is None else _stream(stream)), where)
+    status = grouped(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), _small(where, "offsets", offsets, _TORCH[0].int32, E + 1, d),
+                     Y.data_ptr(), types.get(Y.dtype, -1), M, N, K, E, fmt, 0 if alpha is None else _small(where, "alpha", alpha, _TORCH[0].float32, E, d),
+                     raw(d) if stream is None else _stream(stream))
+    if status != 0:
+        raise ElutqError(status, where)
 
 
 def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, N: int, K: int, fmt: int, wait_limit: int, stream=None) -> None:
     where = "elutq_mx4_test_wait_expiry"
-    types = _torch()[1]
+    types = _products()[2]
     _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
     _check(lib().elutq_mx4_test_wait_expiry(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(),
                                             types.get(Y.dtype, -1), M, N, K, fmt, wait_limit, _stream(stream)), where)
