@@ -28,6 +28,7 @@
 #include <cuda_bf16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "mx4.cuh"
 #include "tensor_map.cuh"
@@ -293,6 +294,17 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, c
         w[i] = __funnelshift_r(v[i], v[i + 1], 8u * off);
         if (left < 4 * i + 4) w[i] &= left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1u;
     }
+}
+
+// The same from the three aligned pieces of 8 bytes that the words lie in, all of them inside the matrix and the row.
+__device__ __forceinline__ void load_inner(uint32_t (&w)[4], const uint8_t* p) {
+    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 7u;
+    const uint2* q = reinterpret_cast<const uint2*>(p - off);
+    const uint2 a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
+    const bool one = off & 4;
+    const uint32_t m[5] = {one ? a.y : a.x, one ? b.x : a.y, one ? b.y : b.x, one ? c.x : b.y, one ? c.y : c.x};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(m[i], m[i + 1], 8u * (off & 3u));
 }
 
 struct Tile {
@@ -637,11 +649,13 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 then();
                 if (col < a.N) {
                     const long long at = (long long)(t.t0 + c0) * a.N + col;
-                    auto put = [&](auto* y, auto&& cast) {
+                    auto put = [&](auto* y, auto&& cast) {            // four pointers: a short chain of additions
+                        decltype(y) to[4] = {y, y + a.N, y + 2 * a.N, y + 3 * a.N};
+                        const bool all = c0 + kChunk <= end;
 #pragma unroll
                         for (int c = 0; c < kChunk; ++c) {
-                            if (c0 + c < end) *y = cast(__uint_as_float(v[c / 16][c % 16]) * alpha);
-                            y += a.N;
+                            if (all || c0 + c < end) *to[c % 4] = cast(__uint_as_float(v[c / 16][c % 16]) * alpha);
+                            to[c % 4] += 4 * a.N;
                         }
                     };
                     if (a.y_type == ELUTQ_TYPE_F16) put(reinterpret_cast<__half*>(a.Y) + at, [](float f) { return __float2half_rn(f); });
@@ -650,10 +664,11 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 }
                 __syncwarp();
             };
-            // The same for 16-bit results whose rows start on 16 bytes: fragments are stored transposed, a block of 16 tokens x 32 weight rows at a time, read
-            // back as 16 bytes of a token's row and stored so: 2 stores of 8 x 64 bytes instead of 16 of 64.  The 16-byte pieces of two tokens'
+            // The same for 16-bit results whose rows start on 4, 8 or 16 bytes: fragments are stored transposed, a block of 16 tokens x 32 weight rows at a time, read
+            // back as so many bytes of a token's row and stored so: with 16 bytes 2 stores of 8 x 64 instead of 16 of 64.  The 16-byte pieces of two tokens'
             // rows share a line of 128 bytes, in an order by the line's number: no conflicts either way.
-            auto columns_turned = [&](int c0, int end, auto&& then, auto half) {
+            auto columns_turned = [&](int c0, int end, auto&& then, auto half, auto width) {
+                constexpr int W = decltype(width)::value, LANES = 64 / W, AT_ONCE = 32 / LANES;      // bytes of a store; lanes of a row; rows
                 uint32_t v[G][16];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
@@ -683,17 +698,24 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                         store_transposed((to + g * 1024) ^ (32u * h), two(v[g][8 * h], v[g][8 * h + 1]), two(v[g][8 * h + 2], v[g][8 * h + 3]),
                                          two(v[g][8 * h + 4], v[g][8 * h + 5]), two(v[g][8 * h + 6], v[g][8 * h + 7]));
                 __syncwarp();
-                const int col0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32 + 8 * (lane & 3);
-                const uint8_t* from = mine + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) * 16);
-                uint4 y[2 * G];
+                const int part = lane % LANES, tok0 = lane / LANES, col0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32 + part * (W / 2);
+                uint16_t* out = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0 + tok0) * a.N + col0;
+                const int rest = col0 < a.N ? end - c0 - tok0 : 0;
+                using V = typename std::conditional<W == 16, uint4, typename std::conditional<W == 8, uint2, uint32_t>::type>::type;
+                constexpr int N_ST = kChunk / AT_ONCE, BATCH = N_ST < 6 ? N_ST : 6;
 #pragma unroll
-                for (int k = 0; k < 2 * G; ++k) y[k] = *reinterpret_cast<const uint4*>(from + 512 * k);
-                uint16_t* row = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0 + (lane >> 2)) * a.N + col0;
-                const int rest = col0 < a.N ? end - c0 - (lane >> 2) : 0;
+                for (int k0 = 0; k0 < N_ST; k0 += BATCH) {
+                    V y[BATCH];
 #pragma unroll
-                for (int k = 0; k < 2 * G; ++k) {
-                    if (8 * k < rest) *reinterpret_cast<uint4*>(row) = y[k];
-                    row += 8 * a.N;
+                    for (int k = 0; k < BATCH; ++k) {
+                        const int tok = AT_ONCE * (k0 + k) + tok0;
+                        y[k] = *reinterpret_cast<const V*>(mine + tok * 64 + (((part * W / 16) ^ ((tok >> 1) & 3)) * 16) + part * W % 16);
+                    }
+#pragma unroll
+                    for (int k = 0; k < BATCH; ++k) {
+                        if (AT_ONCE * (k0 + k) < rest) *reinterpret_cast<V*>(out) = y[k];
+                        out += AT_ONCE * a.N;
+                    }
                 }
                 __syncwarp();
             };
@@ -707,9 +729,15 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                     release(b);
                 }
             };
+            // (a row's alignment decides the width of its stores)
+            auto turned = [&](auto half) {
+                if (a.N % 8 == 0) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<16>{}); });
+                else if (a.N % 4 == 0) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<8>{}); });
+                else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<4>{}); });
+            };
             if (!a.turn) all_columns(columns);
-            else if (a.y_type == ELUTQ_TYPE_F16) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, IntC<1>{}); });
-            else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, IntC<0>{}); });
+            else if (a.y_type == ELUTQ_TYPE_F16) turned(IntC<1>{});
+            else turned(IntC<0>{});
         }
     } else {
         const int helper = warp < 4 ? warp - 2 : warp - 6, block = helper >> 1;      // weights, tokens 0 to 127, 128 to 255
@@ -737,12 +765,28 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                     if (turn != (helper & 1)) continue;
                     uint32_t w[LOADS][4];
                     const int at = s * 4 * CH + 16 * piece;
+                    // whether all that the 128 rows' loads may touch, up to 7 bytes in front and 24 from a piece on, is the matrix's
+                    const long long top = row0 - r0 - 32 * q;
+                    const bool inner = top * a.sk + s * 4 * CH >= 8 && (top + 127) * a.sk + s * 4 * CH + 16 * PIECES + 8 <= all * a.sk;
                     if (wide) {
 #pragma unroll
                         for (int k = 0; k < LOADS; ++k) {
                             uint4 v = make_uint4(0u, 0u, 0u, 0u);
                             if (at < a.sk) v = __ldg(reinterpret_cast<const uint4*>(base + min(row0 + ROWS * k, all - 1) * a.sk + at));
                             w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
+                        }
+                    } else if (inner) {
+                        const uint8_t* p = base + row0 * a.sk + at;
+#pragma unroll
+                        for (int k = 0; k < LOADS; ++k) load_inner(w[k], p + k * (ROWS * a.sk));
+                        if (s * 4 * CH + 16 * PIECES > a.sk) {                 // bytes behind the rows' end
+                            const int left = a.sk - at;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const uint32_t mask = left >= 4 * c + 4 ? 0xffffffffu : left <= 4 * c ? 0u : (1u << (8 * (left - 4 * c))) - 1u;
+#pragma unroll
+                                for (int k = 0; k < LOADS; ++k) w[k][c] &= mask;
+                            }
                         }
                     } else {
 #pragma unroll
@@ -873,7 +917,7 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int y_type, 
     p.x_box = !grouped ? rows : rows % 32 == 0 ? 32 : rows % 16 == 0 ? 16 : 8;
     const long long w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
     const long long most = w_tiles * ((M + p.tokens - 1) / p.tokens + (grouped ? (E < M ? E : M) : 0));
-    p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && N % 8 == 0;
+    p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && N % 2 == 0;
     p.ok = fill_plan(p, format, E, grouped);
     const int team = p.cg == 2 ? 2 : p.split;
     const long long teams = p.cg == 2 ? num_sms / 2 : p.split > 1 ? resident_clusters(p.split) : num_sms;

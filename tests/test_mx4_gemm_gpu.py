@@ -61,6 +61,43 @@ def test_large_batches(fmt, M, N, K):
     _gemm(np.random.default_rng(M * N + K + fmt), M, N, K, fmt, "f32")
 
 
+@pytest.mark.parametrize("out", ["f16", "bf16"])
+@pytest.mark.parametrize("N", [1, 31, 33, 127, 129, 250, 257, 511, 514, 1001, 1003, 1012])
+@pytest.mark.parametrize("M", [9, 65, 130, 300])
+def test_rows_of_results_that_start_anywhere(out, N, M):
+    """16-bit results of every alignment, and what is beside them is left alone."""
+    rng = np.random.default_rng(M + N)
+    K = 160
+    xc, xs = _matrix(rng, M, K, 1)
+    wc, ws = _matrix(rng, N, K, 1)
+    buf = torch.full((M * N + 64,), float("nan"), dtype=TYPES[out], device="cuda")
+    Y = buf[32 : 32 + M * N].reshape(M, N)
+    elutq.elutq_mx4_gemm(*_dev(xc, xs, wc, ws), Y, M, N, K, 1, alpha=torch.tensor([0.01], device="cuda"))
+    assert torch.isnan(buf[:32]).all() and torch.isnan(buf[32 + M * N :]).all()
+    f = float(np.float32(0.01))
+    _assert_close(Y, mx4.matmul(xc, xs, wc, ws, 1, f), mx4.magnitude(xc, xs, wc, ws, 1, f), K, out)
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("M,N,K", [(3, 40, 32 * 17), (140, 300, 32 * 33), (300, 333, 32 * 101), (40, 130, 32 * 7)])
+def test_scales_of_every_alignment(fmt, M, N, K):
+    """Rows of an odd number of scales from every base: first and last rows next to memory that is not theirs (NaN scales)."""
+    rng = np.random.default_rng(M + K)
+    xc, xs = _matrix(rng, M, K, fmt)
+    wc, ws = _matrix(rng, N, K, fmt)
+    want, A = mx4.matmul(xc, xs, wc, ws, fmt), mx4.magnitude(xc, xs, wc, ws, fmt)
+    dxc, dwc = _dev(xc, wc)
+    for off in range(0, 18):
+        odd = []
+        for s in (xs, ws):
+            buf = torch.full((s.size + 64,), 255 if fmt == 0 else 127, dtype=torch.uint8, device="cuda")
+            buf[off : off + s.size] = torch.from_numpy(s).cuda().reshape(-1)
+            odd.append(buf[off : off + s.size])
+        Y = torch.full((M, N), float("nan"), device="cuda")
+        elutq.elutq_mx4_gemm(dxc, odd[0], dwc, odd[1], Y, M, N, K, fmt)
+        _assert_close(Y, want, A, K, "f32", f"offset {off}")
+
+
 @pytest.mark.parametrize("fmt", [0, 1])
 @pytest.mark.parametrize("M,N,K", [(2048, 20000, 1440), (1000, 30000, 1024), (64, 57344, 2048), (16, 40000, 1056)])
 def test_many_tiles_and_steps_for_each_sm(fmt, M, N, K):
