@@ -765,9 +765,11 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                     if (turn != (helper & 1)) continue;
                     uint32_t w[LOADS][4];
                     const int at = s * 4 * CH + 16 * piece;
-                    // whether all that the 128 rows' loads may touch, up to 7 bytes in front and 24 from a piece on, is the matrix's
+                    // Whether all that the 128 rows' loads may touch, up to 7 bytes in front and 24 from a piece on, is the matrix's.  Not asked with few tokens: their
+                    // block always ends with the matrix, and two unrolled forms side by side cost more instruction fetches than the shorter one saves
+                    // (106 x 20587 x 8416 NVFP4 39 us without, 45 with; 1536 x 32056 x 2080 95 and 75).
                     const long long top = row0 - r0 - 32 * q;
-                    const bool inner = top * a.sk + s * 4 * CH >= 8 && (top + 127) * a.sk + s * 4 * CH + 16 * PIECES + 8 <= all * a.sk;
+                    const bool inner = CG == 2 && top * a.sk + s * 4 * CH >= 8 && (top + 127) * a.sk + s * 4 * CH + 16 * PIECES + 8 <= all * a.sk;
                     if (wide) {
 #pragma unroll
                         for (int k = 0; k < LOADS; ++k) {
