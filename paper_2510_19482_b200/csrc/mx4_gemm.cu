@@ -658,17 +658,20 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                             to[c % 4] += 4 * a.N;
                         }
                     };
-                    if (a.y_type == ELUTQ_TYPE_F16) put(reinterpret_cast<__half*>(a.Y) + at, [](float f) { return __float2half_rn(f); });
-                    else if (a.y_type == ELUTQ_TYPE_BF16) put(reinterpret_cast<__nv_bfloat16*>(a.Y) + at, [](float f) { return __float2bfloat16_rn(f); });
+                    if (CG == 1 && a.y_type == ELUTQ_TYPE_F16) put(reinterpret_cast<__half*>(a.Y) + at, [](float f) { return __float2half_rn(f); });
+                    else if (CG == 1 && a.y_type == ELUTQ_TYPE_BF16) put(reinterpret_cast<__nv_bfloat16*>(a.Y) + at, [](float f) { return __float2bfloat16_rn(f); });
                     else put(reinterpret_cast<float*>(a.Y) + at, [](float f) { return f; });
                 }
                 __syncwarp();
             };
             // The same for 16-bit results whose rows start on 4, 8 or 16 bytes: fragments are stored transposed, a block of 16 tokens x 32 weight rows at a time, read
             // back as so many bytes of a token's row and stored so: with 16 bytes 2 stores of 8 x 64 instead of 16 of 64.  The 16-byte pieces of two tokens'
-            // rows share a line of 128 bytes, in an order by the line's number: no conflicts either way.
+            // rows share a line of 128 bytes, in an order by the line's number: no conflicts either way.  With an odd N every second row starts in the middle of 4
+            // bytes: its words are made of two, and its first and last value go by themselves (857 x 41529 x 1472 MXFP4 58 -> 49 us); with few tokens a value at a
+            // time is 5 to 9 % faster.
             auto columns_turned = [&](int c0, int end, auto&& then, auto half, auto width) {
-                constexpr int W = decltype(width)::value, LANES = 64 / W, AT_ONCE = 32 / LANES;      // bytes of a store; lanes of a row; rows
+                constexpr bool odd_n = decltype(width)::value == 2;          // every second row starts in the middle of 4 bytes
+                constexpr int W = odd_n ? 4 : decltype(width)::value, LANES = 64 / W, AT_ONCE = 32 / LANES;      // bytes of a store; lanes of a row; rows
                 uint32_t v[G][16];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
@@ -698,23 +701,58 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                         store_transposed((to + g * 1024) ^ (32u * h), two(v[g][8 * h], v[g][8 * h + 1]), two(v[g][8 * h + 2], v[g][8 * h + 3]),
                                          two(v[g][8 * h + 4], v[g][8 * h + 5]), two(v[g][8 * h + 6], v[g][8 * h + 7]));
                 __syncwarp();
-                const int part = lane % LANES, tok0 = lane / LANES, col0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32 + part * (W / 2);
-                uint16_t* out = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0 + tok0) * a.N + col0;
-                const int rest = col0 < a.N ? end - c0 - tok0 : 0;
-                using V = typename std::conditional<W == 16, uint4, typename std::conditional<W == 8, uint2, uint32_t>::type>::type;
-                constexpr int N_ST = kChunk / AT_ONCE, BATCH = N_ST < 6 ? N_ST : 6;
+                if constexpr (odd_n) {
+                    const int n0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32;
+                    auto at = [&](int tok, int value) { return mine + tok * 64 + (((value >> 3) ^ ((tok >> 1) & 3)) * 16) + (value & 7) * 2; };
+                    uint16_t* out = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0) * a.N + n0;
+                    if (n0 + 32 <= a.N) {
+                        const int part = lane & 15, tok0 = lane >> 4;
+                        const bool odd = (t.t0 + c0 + tok0) & 1;             // of all this lane's tokens
+                        const int rest = odd && part == 15 ? 0 : end - c0 - tok0;
+                        uint16_t* to2 = out + (long long)tok0 * a.N + 2 * part + odd;
 #pragma unroll
-                for (int k0 = 0; k0 < N_ST; k0 += BATCH) {
-                    V y[BATCH];
+                        for (int k0 = 0; k0 < kChunk / 2; k0 += 6) {
+                            uint32_t y[6];
 #pragma unroll
-                    for (int k = 0; k < BATCH; ++k) {
-                        const int tok = AT_ONCE * (k0 + k) + tok0;
-                        y[k] = *reinterpret_cast<const V*>(mine + tok * 64 + (((part * W / 16) ^ ((tok >> 1) & 3)) * 16) + part * W % 16);
+                            for (int k = 0; k < 6; ++k) {
+                                const int tok = 2 * (k0 + k) + tok0;
+                                const uint32_t x = *reinterpret_cast<const uint32_t*>(at(tok, 2 * part)), z = *reinterpret_cast<const uint32_t*>(at(tok, min(2 * part + 2, 30)));
+                                y[k] = odd ? __funnelshift_r(x, z, 16) : x;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 6; ++k) {
+                                if (2 * (k0 + k) < rest) *reinterpret_cast<uint32_t*>(to2) = y[k];
+                                to2 += 2 * a.N;
+                            }
+                        }
+                        const int first_odd = (t.t0 + c0 + 1) & 1, value = lane & 1 ? 31 : 0;      // the ends of those rows
+#pragma unroll
+                        for (int k = 0; k < (kChunk + 31) / 32; ++k) {
+                            const int tok = 32 * k + 2 * (lane >> 1) + first_odd;
+                            if (tok < kChunk && c0 + tok < end) out[(long long)tok * a.N + value] = *reinterpret_cast<const uint16_t*>(at(tok, value));
+                        }
+                    } else if (n0 + lane < a.N) {                            // the matrix's last columns
+                        for (int tok = 0; tok < min(kChunk, end - c0); ++tok) out[(long long)tok * a.N + lane] = *reinterpret_cast<const uint16_t*>(at(tok, lane));
                     }
+                } else {
+                    const int part = lane % LANES, tok0 = lane / LANES, col0 = t.n0 + (CG == 2 ? (int)rank * kTileW : 0) + quarter * 32 + part * (W / 2);
+                    uint16_t* out = reinterpret_cast<uint16_t*>(a.Y) + (long long)(t.t0 + c0 + tok0) * a.N + col0;
+                    const int rest = col0 < a.N ? end - c0 - tok0 : 0;
+                    using V = typename std::conditional<W == 16, uint4, typename std::conditional<W == 8, uint2, uint32_t>::type>::type;
+                    constexpr int N_ST = kChunk / AT_ONCE, BATCH = N_ST < 6 ? N_ST : 6;
 #pragma unroll
-                    for (int k = 0; k < BATCH; ++k) {
-                        if (AT_ONCE * (k0 + k) < rest) *reinterpret_cast<V*>(out) = y[k];
-                        out += AT_ONCE * a.N;
+                    for (int k0 = 0; k0 < N_ST; k0 += BATCH) {
+                        V y[BATCH];
+#pragma unroll
+                        for (int k = 0; k < BATCH; ++k) {
+                            const int tok = AT_ONCE * (k0 + k) + tok0;
+                            y[k] = *reinterpret_cast<const V*>(mine + tok * 64 + (((part * W / 16) ^ ((tok >> 1) & 3)) * 16) + part * W % 16);
+                        }
+#pragma unroll
+                        for (int k = 0; k < BATCH; ++k) {
+                            if (AT_ONCE * (k0 + k) < rest) *reinterpret_cast<V*>(out) = y[k];
+                            out += AT_ONCE * a.N;
+                        }
                     }
                 }
                 __syncwarp();
@@ -733,7 +771,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             auto turned = [&](auto half) {
                 if (a.N % 8 == 0) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<16>{}); });
                 else if (a.N % 4 == 0) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<8>{}); });
-                else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<4>{}); });
+                else if (CG == 1 || a.N % 2 == 0) all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<4>{}); });
+                else all_columns([&](int c0, int end, auto&& then) { columns_turned(c0, end, then, half, IntC<2>{}); });
             };
             if (!a.turn) all_columns(columns);
             else if (a.y_type == ELUTQ_TYPE_F16) turned(IntC<1>{});
@@ -859,12 +898,6 @@ double estimate_us(long long tiles, double groups, int N, int K, int format, int
     return 3.36 + 0.009 * tokens + (cg == 2 ? 0.63 : 0.0) + longest + exchange;
 }
 
-#ifdef MX4_TUNE
-}
-extern "C" { int mx4_force_cg = 0, mx4_force_tokens = 0, mx4_force_split = 0; }
-namespace {
-#endif
-
 int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
 // Tile and cluster of a call.  Dense: the least estimate over tiles that share the rows evenly (as few as possible, one or two more, twice as many) and clusters of up to
@@ -908,18 +941,13 @@ Plan plan_for(int M, int N, int K, int E, int format, bool grouped, int y_type, 
             }
         }
     }
-#ifdef MX4_TUNE
-    if (mx4_force_cg) p.cg = mx4_force_cg;
-    if (mx4_force_tokens) p.tokens = mx4_force_tokens;
-    if (mx4_force_split) p.split = mx4_force_split;
-#endif
     if (p.cg == 2) p.tokens = round_up(p.tokens, 16);
     // rows of one load: dense, all of a tile's; of groups, whose tiles are of any height, up to 32
     const int rows = p.tokens / p.cg;
     p.x_box = !grouped ? rows : rows % 32 == 0 ? 32 : rows % 16 == 0 ? 16 : 8;
     const long long w_tiles = (N + p.cg * kTileW - 1) / (p.cg * kTileW);
     const long long most = w_tiles * ((M + p.tokens - 1) / p.tokens + (grouped ? (E < M ? E : M) : 0));
-    p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && N % 2 == 0;
+    p.turn = p.split == 1 && y_type != ELUTQ_TYPE_F32 && (p.cg == 2 || N % 2 == 0);
     p.ok = fill_plan(p, format, E, grouped);
     const int team = p.cg == 2 ? 2 : p.split;
     const long long teams = p.cg == 2 ? num_sms / 2 : p.split > 1 ? resident_clusters(p.split) : num_sms;

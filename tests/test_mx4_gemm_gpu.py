@@ -156,6 +156,16 @@ def test_groups(fmt, name, sizes, N, K):
     _grouped(rng, [b + 3 for b in borders], N, K, len(sizes), fmt, "bf16", M + 11, alpha=rng.standard_normal(len(sizes)).astype(np.float32))
 
 
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("N", [257, 511, 515, 543, 770])
+def test_groups_whose_rows_of_results_start_anywhere(fmt, N):
+    """Groups from odd and even rows on, large enough for tiles of two CTAs, in 16 bits."""
+    rng = np.random.default_rng(N + fmt)
+    borders = [1, 300, 301, 301, 811, 1000]
+    _grouped(rng, borders, N, 224, 5, fmt, "bf16", 1003, alpha=rng.standard_normal(5).astype(np.float32))
+    _grouped(rng, [b - 1 for b in borders], N, 224, 5, fmt, "f16", 1003, alpha=np.full(5, 2.0**-9, dtype=np.float32))
+
+
 def test_borders_out_of_order_and_out_of_range():
     rng = np.random.default_rng(1)
     for borders in ([0, 20, 10, 30], [-5, 10, 2**31 - 1, 40], [0, 100, 100, 100], [40, 30, 20, 10], [-9, -7, -3, -1], [7, 3, 12, 9]):
