@@ -42,7 +42,9 @@ constexpr int kMaxTokens = 256;            // tokens of a tile
 constexpr int kStepBytes = 128;            // codes of a row in a step: 256 k
 constexpr int kMaxStages = 10;
 constexpr int kMaxSplit = 8;
-constexpr int kMaxSplitTokens = 64;
+// Tiles that a cluster may share.  Their sums take 512 bytes of shared memory a token, and the exchange grows with the tokens: 80 x 5120 x 13824 NVFP4 18.3 us
+// up to 64 tokens, 16.1 up to 96; 128 x 4096 x 14336 MXFP4 15.0 up to 96, 18.2 up to 128.
+constexpr int kMaxSplitTokens = 96;
 constexpr int kMaxGroups = 1024;
 // Scales come in turns of four steps into a ring of two, one fence and one arrival for a turn; the two warps of 128 rows take alternate turns.  (A warp waits
 // for a use of the ring one turn ahead of the other's: within what a barrier's parity tells apart.)  A step at a time, three warps could not keep up with

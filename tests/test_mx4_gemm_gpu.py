@@ -166,6 +166,13 @@ def test_groups_whose_rows_of_results_start_anywhere(fmt, N):
     _grouped(rng, [b - 1 for b in borders], N, 224, 5, fmt, "f16", 1003, alpha=np.full(5, 2.0**-9, dtype=np.float32))
 
 
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("M,N,K", [(66, 130, 4096), (80, 300, 7200), (96, 1000, 3584), (96, 4096, 4128), (150, 257, 2880), (190, 128, 9216)])
+def test_clusters_over_many_rows(fmt, M, N, K):
+    _gemm(np.random.default_rng(M * N + K + fmt), M, N, K, fmt, "f32")
+    _gemm(np.random.default_rng(M * N + K + fmt), M, N, K, fmt, "bf16", alpha=0.37)
+
+
 def test_borders_out_of_order_and_out_of_range():
     rng = np.random.default_rng(1)
     for borders in ([0, 20, 10, 30], [-5, 10, 2**31 - 1, 40], [0, 100, 100, 100], [40, 30, 20, 10], [-9, -7, -3, -1], [7, 3, 12, 9]):
