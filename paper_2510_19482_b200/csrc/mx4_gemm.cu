@@ -258,8 +258,8 @@ struct Ring {
     }
 };
 
-// Scales of any alignment are read as the aligned words around them; of the words that the matrix shares with its surroundings only the bytes that
-// belong to it are read, once.
+// The first and last scales of a matrix of any alignment are read as the aligned words around them; of the words that the matrix shares with its
+// surroundings only the bytes that belong to it are.
 struct Ends {
     const uint32_t *lo, *hi;       // whole words: [lo, hi)
     uint32_t head, tail;           // the words in front of lo and at hi
@@ -298,15 +298,12 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, c
     }
 }
 
-// The same from the three aligned pieces of 8 bytes that the words lie in, all of them inside the matrix and the row.
-__device__ __forceinline__ void load_inner(uint32_t (&w)[4], const uint8_t* p) {
-    const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 7u;
-    const uint2* q = reinterpret_cast<const uint2*>(p - off);
-    const uint2 a = __ldg(q), b = __ldg(q + 1), c = __ldg(q + 2);
-    const bool one = off & 4;
-    const uint32_t m[5] = {one ? a.y : a.x, one ? b.x : a.y, one ? b.y : b.x, one ? c.x : b.y, one ? c.y : c.x};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(m[i], m[i + 1], 8u * (off & 3u));
+// The aligned 16 bytes around p if they lie in [first, last), else 0.
+__device__ __forceinline__ void load_piece(uint32_t (&w)[4], const uint8_t* p, const uint8_t* first, const uint8_t* last) {
+    const uint8_t* q = p - ((uint32_t)reinterpret_cast<uintptr_t>(p) & 15u);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (q >= first && q + 16 <= last) v = __ldg(reinterpret_cast<const uint4*>(q));
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
 }
 
 struct Tile {
@@ -792,60 +789,133 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             // instead of 8 or 16, and NVFP4 was bound by that: 4096 x 28672 x 4096 245 us.)
             constexpr int PIECES = CH, LOADS = 4 * PIECES, ROWS = 8 / PIECES;             // pieces of a row; loads; rows r of a load
             const int piece = lane % PIECES, q = lane / PIECES % 4, r0 = lane / (4 * PIECES);
+            // Of scales whose rows start elsewhere, a lane has pieces of rows c + 8 k (NVFP4) or c + 16 k: by so many rows a row's start moves by 0 or 8 in
+            // 16 bytes, and where a lane's words go is the same for every second k.  Lines touched by a load bound this too: its four lanes of a row meet in a
+            // bank when they store, and pieces of different rows, whose words do not, took 1536 x 32056 x 2080 NVFP4 from 81 to 100 us.  Words of 4 bytes loaded by
+            // every lane for its own piece, 5 for 16 bytes: 8 x 6577 x 5952 NVFP4 11.4 us instead of 10.3, 34 rows of 11 experts of 5690 x 4160 33 instead of 29,
+            // with pairs 2 to 4 % less.
+            constexpr int EVERY = 32 / PIECES;
+            const int row_c = lane / PIECES;
             const int first_word = block == 0 ? 0 : CH + block - 1, pitch = block == 0 ? 1 : NB;
-            uint8_t* to = sS + first_word * 512 + r0 * 16 + q * 4;
+            uint8_t* to = sS + first_word * 512;
             int turn = 0;
             bool ok = true;
             grid_dependency_wait();
-            Ends ends = {};
-            if (!wide) ends = ends_of(base, base + all * a.sk);
+            const uint8_t *first16 = base, *last16 = base;                        // the matrix's whole pieces of 16 bytes
+            if (!wide) {
+                first16 = base + (16u - (uint32_t)reinterpret_cast<uintptr_t>(base)) % 16u;
+                last16 = base + all * a.sk - (reinterpret_cast<uintptr_t>(base + all * a.sk) & 15);
+            }
+            // of a row's words in a turn, where number d goes
+            auto place = [&](int d) { return d / CH * s_bytes + d % CH * pitch * 512; };
             for (int i = first; i < tiles && ok; i += stride) {
                 const Tile t = tile_at<CG>(a, table, i);
-                const long long row0 = (block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1)) + r0 + 32 * q;
+                const long long top = block == 0 ? (long long)t.e * a.N + t.n0 + (CG == 2 ? (int)rank * kTileW : 0) : t.t0 + 128 * (block - 1);
                 for (int s = step0; s < step1 && ok; s += kTurn, turn ^= 1, r.next()) {
                     if (turn != (helper & 1)) continue;
                     uint32_t w[LOADS][4];
                     const int at = s * 4 * CH + 16 * piece;
-                    // Whether all that the 128 rows' loads may touch, up to 7 bytes in front and 24 from a piece on, is the matrix's.  Not asked with few tokens: their
-                    // block always ends with the matrix, and two unrolled forms side by side cost more instruction fetches than the shorter one saves
-                    // (106 x 20587 x 8416 NVFP4 39 us without, 45 with; 1536 x 32056 x 2080 95 and 75).
-                    const long long top = row0 - r0 - 32 * q;
-                    const bool inner = CG == 2 && top * a.sk + s * 4 * CH >= 8 && (top + 127) * a.sk + s * 4 * CH + 16 * PIECES + 8 <= all * a.sk;
                     if (wide) {
+                        const long long row0 = top + r0 + 32 * q;
 #pragma unroll
                         for (int k = 0; k < LOADS; ++k) {
                             uint4 v = make_uint4(0u, 0u, 0u, 0u);
                             if (at < a.sk) v = __ldg(reinterpret_cast<const uint4*>(base + min(row0 + ROWS * k, all - 1) * a.sk + at));
                             w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
                         }
-                    } else if (inner) {
-                        const uint8_t* p = base + row0 * a.sk + at;
+                        ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                        if (!ok) break;
+                        uint8_t* slot = to + r.i * kTurn * s_bytes + place(4 * piece) + r0 * 16 + q * 4;
 #pragma unroll
-                        for (int k = 0; k < LOADS; ++k) load_inner(w[k], p + k * (ROWS * a.sk));
-                        if (s * 4 * CH + 16 * PIECES > a.sk) {                 // bytes behind the rows' end
-                            const int left = a.sk - at;
+                        for (int k = 0; k < LOADS; ++k)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const uint32_t mask = left >= 4 * c + 4 ? 0xffffffffu : left <= 4 * c ? 0u : (1u << (8 * (left - 4 * c))) - 1u;
-#pragma unroll
-                                for (int k = 0; k < LOADS; ++k) w[k][c] &= mask;
-                            }
-                        }
+                            for (int c = 0; c < 4; ++c)
+                                *reinterpret_cast<uint32_t*>(slot + (c / CH) * s_bytes + (c % CH) * pitch * 512 + ROWS * k * 16) = w[k][c];
                     } else {
+                        // The aligned piece that a lane's 16 bytes of a row begin in; the one behind the row's last by its lane k % PIECES.  Bytes are
+                        // moved within words, with the next lane's first; words need not move, as each goes to where it belongs (the first ones of a
+                        // row may belong to the turn before).  Pieces that are not wholly the matrix's come last, row by row.
+                        const uint8_t* p = base + (top + row_c) * a.sk + at;
+                        const long long pace = (long long)EVERY * a.sk;
+                        uint32_t behind[4][4];
+#pragma unroll
+                        for (int k = 0; k < LOADS; ++k) load_piece(w[k], p + k * pace, first16, last16);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) load_piece(behind[m], p + (m * PIECES + piece) * pace + 16 * (PIECES - piece), first16, last16);
+                        const uint32_t off0 = (uint32_t)reinterpret_cast<uintptr_t>(p), shift = 8u * (off0 & 3u);
+                        const int lead[2] = {(int)(off0 >> 2 & 3u), (int)((off0 + (uint32_t)pace) >> 2 & 3u)};      // even k, odd k
 #pragma unroll
                         for (int k = 0; k < LOADS; ++k) {
-                            const uint8_t* row = base + min(row0 + ROWS * k, all - 1) * a.sk;
-                            load_words(w[k], row + at, row + a.sk, ends);
+                            const uint32_t beside = __shfl_down_sync(0xffffffffu, w[k][0], 1), last = __shfl_sync(0xffffffffu, behind[k / PIECES][0], k % PIECES, PIECES);
+                            const uint32_t next = piece == PIECES - 1 ? last : beside;
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) w[k][c] = __funnelshift_r(w[k][c], c < 3 ? w[k][c + 1] : next, shift);
+                        }
+                        const int lead_b = piece & 1 ? lead[1] : lead[0];
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+#pragma unroll
+                            for (int c = 0; c < 3; ++c) behind[m][c] = __funnelshift_r(behind[m][c], behind[m][c + 1], shift);
+                        if (s * 4 * CH + 16 * PIECES > a.sk) {                 // bytes behind the rows' end
+                            auto mask = [&](int d) {
+                                const int left = a.sk - s * 4 * CH - 4 * d;
+                                return left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                            };
+#pragma unroll
+                            for (int odd = 0; odd < 2; ++odd)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    const uint32_t keep = mask(4 * piece + c - lead[odd]);
+#pragma unroll
+                                    for (int k = odd; k < LOADS; k += 2) w[k][c] &= keep;
+                                }
+#pragma unroll
+                            for (int c = 0; c < 3; ++c) {
+                                const uint32_t keep = mask(4 * PIECES + c - lead_b);
+#pragma unroll
+                                for (int m = 0; m < 4; ++m) behind[m][c] &= keep;
+                            }
+                        }
+                        ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
+                        if (!ok) break;
+                        uint8_t* slot = to + r.i * kTurn * s_bytes;
+                        // row c + EVERY k of 128 is number c + EVERY (k % PIECES) of 32s number k / PIECES
+#pragma unroll
+                        for (int odd = 0; odd < 2; ++odd)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const int d = 4 * piece + c - lead[odd];
+                                if (d >= 0) {
+                                    uint8_t* dst = slot + place(d) + row_c * 16;
+#pragma unroll
+                                    for (int k = odd; k < LOADS; k += 2) *reinterpret_cast<uint32_t*>(dst + k % PIECES * EVERY * 16 + k / PIECES * 4) = w[k][c];
+                                }
+                            }
+#pragma unroll
+                        for (int c = 0; c < 3; ++c)
+                            if (c < lead_b) {
+                                uint8_t* dst = slot + place(4 * PIECES + c - lead_b) + (row_c + EVERY * piece) * 16;
+#pragma unroll
+                                for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dst + m * 4) = behind[m][c];
+                            }
+                        const long long below = min(top + 128, all);            // rows of the matrix end here
+                        if (top * a.sk + s * 4 * CH < first16 - base || (below - 1) * a.sk + min(s * 4 * CH + 16 * PIECES, a.sk) > last16 - base) {
+                            __syncwarp();
+                            const Ends ends = ends_of(base, base + all * a.sk);
+#pragma unroll 1
+                            for (int k = 0; k < LOADS; ++k) {
+                                const uint8_t* b = p + k * pace;
+                                const bool edge = top + row_c + EVERY * k < all && at < a.sk && (b < first16 || b + min(16, a.sk - at) > last16);
+                                if (!__any_sync(0xffffffffu, edge)) continue;
+                                const uint8_t* row = base + min(top + row_c + EVERY * k, all - 1) * a.sk;
+                                uint32_t f[4];
+                                load_words(f, row + at, row + a.sk, ends);
+#pragma unroll
+                                for (int c = 0; c < 4; ++c)
+                                    if (edge) *reinterpret_cast<uint32_t*>(slot + place(4 * piece + c) + (row_c + k % PIECES * EVERY) * 16 + k / PIECES * 4) = f[c];
+                            }
                         }
                     }
-                    ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
-                    if (!ok) break;
-                    uint8_t* slot = to + (r.i * kTurn + piece * 4 / CH) * s_bytes;
-#pragma unroll
-                    for (int k = 0; k < LOADS; ++k)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            *reinterpret_cast<uint32_t*>(slot + (c / CH) * s_bytes + (c % CH) * pitch * 512 + ROWS * k * 16) = w[k][c];
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {

@@ -173,6 +173,31 @@ def test_clusters_over_many_rows(fmt, M, N, K):
     _gemm(np.random.default_rng(M * N + K + fmt), M, N, K, fmt, "bf16", alpha=0.37)
 
 
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("K", [32, 64, 96, 160, 288, 480, 1056, 2144])
+def test_groups_with_scales_of_every_alignment(fmt, K):
+    """Borders anywhere, rows of few scales: pieces in front of the first and behind the last row belong to others."""
+    rng = np.random.default_rng(K + fmt)
+    sizes, N = [1, 2, 0, 37, 200], 35
+    borders = [0, *np.cumsum(sizes).tolist()]
+    M, E = borders[-1], len(sizes)
+    xc, xs = _matrix(rng, M, K, fmt)
+    wc, ws = _matrix(rng, E * N, K, fmt)
+    dxc, dwc, db = *_dev(xc, wc), torch.tensor(borders, dtype=torch.int32, device="cuda")
+    for off in (0, 1, 5, 8, 13, 15):
+        odd = []
+        for s in (xs, ws):
+            buf = torch.full((s.size + 64,), 255 if fmt == 0 else 127, dtype=torch.uint8, device="cuda")
+            buf[off : off + s.size] = torch.from_numpy(s).cuda().reshape(-1)
+            odd.append(buf[off : off + s.size])
+        Y = torch.full((M, N), float("nan"), device="cuda")
+        elutq.elutq_mx4_gemm_grouped(dxc, odd[0], dwc, odd[1], db, Y, M, N, K, E, fmt)
+        for e, (lo, hi) in enumerate(zip(borders, borders[1:])):
+            if hi > lo:
+                w = wc[e * N : (e + 1) * N], ws[e * N : (e + 1) * N]
+                _assert_close(Y[lo:hi], mx4.matmul(xc[lo:hi], xs[lo:hi], *w, fmt, 1.0), mx4.magnitude(xc[lo:hi], xs[lo:hi], *w, fmt, 1.0), K, "f32", f"group {e}, {off}")
+
+
 def test_borders_out_of_order_and_out_of_range():
     rng = np.random.default_rng(1)
     for borders in ([0, 20, 10, 30], [-5, 10, 2**31 - 1, 40], [0, 100, 100, 100], [40, 30, 20, 10], [-9, -7, -3, -1], [7, 3, 12, 9]):
