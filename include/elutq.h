@@ -434,7 +434,8 @@ int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K,
 /*
  * Y[M][N] (y_type, dense, 16-byte aligned) = alpha * X[M][K] * W[N][K]^T of two matrices in the same format.  Products are exact, sums
  * are fp32 in the tensor core's order, the result is multiplied by alpha (NULL: 1, or device float [1]) in fp32 and
- * rounded once to y_type.  A row whose scales or values are NaN gives NaN.  Any M and N from 1 to 2^30 - 1.
+ * rounded once to y_type.  A row whose scales or values are NaN gives NaN.  Any M and N from 1 to 2^30 - 1, K up
+ * to 2^28.
  */
 int elutq_mx4_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y, int y_type,
                    int M, int N, int K, int format, const float* alpha, void* stream);

@@ -30,3 +30,21 @@ def test_rows_of_more_than_2_28_results(M, N, out):
         assert not torch.isnan(Y[r]).any(), r
     del wc, ws, Y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("M,N", [(1, 1), (40, 3)])
+def test_the_longest_k(fmt, M, N):
+    """Codes of 0 but for a few along K, the last among them: sums are exact."""
+    K, B = 1 << 28, mx4.BLOCK[fmt]
+    one = 127 if fmt == 0 else 56
+    xc, wc = (torch.zeros((n, K // 2), dtype=torch.uint8, device="cuda") for n in (M, N))
+    xs, ws = (torch.full((n, K // B), one, dtype=torch.uint8, device="cuda") for n in (M, N))
+    at = [0, 777, K // 4, K // 2 - 256, K // 2 - 1]                 # bytes of a row; their high halves: 1, 1.5, ...
+    for i, k in enumerate(at):
+        xc[:, k] = 0x20
+        wc[:, k] = 0x10 * (i + 1)
+    Y = torch.full((M, N), float("nan"), device="cuda")
+    elutq.elutq_mx4_gemm(xc, xs, wc, ws, Y, M, N, K, fmt)
+    assert elutq.elutq_device_status() == 0
+    assert (Y == float(mx4.E2M1[1 : 1 + len(at)].sum())).all()
