@@ -524,6 +524,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             const int whole = a.K / 256;                          // steps of four MMAs
             int n = 0;
             bool ok = true;
+            grid_dependency_wait();                               // (touches nothing itself: the clock of its waits starts behind the kernels in front)
             for (int i = first; i < tiles && ok; i += stride, ++n) {
                 const Tile t = tile_at<CG>(a, table, i);
                 const int b = n & 1, use = n >> 1;
