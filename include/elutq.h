@@ -405,7 +405,7 @@ int elutq_hlq_fit(const void* W, int q, int G, int N, int K, int t_max, uint8_t*
 #define ELUTQ_TYPE_BF16 1
 #define ELUTQ_TYPE_F32  2
 
-#define ELUTQ_MX4_FLAG_SWIGLU 0x1u /* a row of X holds 2 K values [g | u]; silu(g) * u, formed in fp32, is quantised */
+#define ELUTQ_MX4_FLAG_SWIGLU 0x1u /* a row of X holds 2 K values [g | u]; silu(g) * u, formed in fp32, is quantised (silu(-infinity) is 0) */
 
 /* Sizes in bytes of the codes and the scales of a matrix.  Pure function, no CUDA call. */
 int elutq_mx4_bytes(int format, int rows, int K, size_t* code_bytes, size_t* scale_bytes);

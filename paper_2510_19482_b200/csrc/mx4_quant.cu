@@ -59,21 +59,24 @@ template <int TYPE, bool WIDE>
 __device__ __forceinline__ void load_raw(uint32_t (&v)[8], const void* X, long long at) {
     load32<WIDE>(v, reinterpret_cast<const uint8_t*>(X) + at * (TYPE == ELUTQ_TYPE_F32 ? 4 : 2));
 }
+// A word's values: one of fp32, two of 16 bits
+template <int TYPE>
+__device__ __forceinline__ void word_values(float* y, uint32_t v) {
+    if constexpr (TYPE == ELUTQ_TYPE_F32) {
+        y[0] = __uint_as_float(v);
+    } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+        y[0] = f.x;
+        y[1] = f.y;
+    } else {
+        y[0] = __uint_as_float(v << 16);
+        y[1] = __uint_as_float(v & 0xffff0000u);
+    }
+}
 template <int TYPE>
 __device__ __forceinline__ void values_of(float* y, const uint32_t (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (TYPE == ELUTQ_TYPE_F32) {
-            y[i] = __uint_as_float(v[i]);
-        } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-            y[2 * i] = f.x;
-            y[2 * i + 1] = f.y;
-        } else {
-            y[2 * i] = __uint_as_float(v[i] << 16);
-            y[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-        }
-    }
+    for (int i = 0; i < 8; ++i) word_values<TYPE>(y + (TYPE == ELUTQ_TYPE_F32 ? i : 2 * i), v[i]);
 }
 
 // Eight values (already divided by their scale) as a word of codes, the first in the lowest bits
@@ -104,19 +107,40 @@ __device__ __forceinline__ float reciprocal(float x) {                // one uni
     return r;
 }
 // g / (1 + exp(-g)) within a few units in the last place.  exp(-g) = 2^t 2^lo with t = -g log2(e) rounded and lo what that left, also of
-// the constant (|lo| < 2^-17), 2^lo = 1 + lo ln 2.  Below -87 the result is that at -87, 10^-36.
-template <int TYPE>
-__device__ __forceinline__ float silu(float g) {
-    float e, r, x;
-    asm("max.NaN.f32 %0, %0, 0fC2AE0000;" : "+f"(g));              // -87
-    if constexpr (TYPE == ELUTQ_TYPE_F16) x = g;
-    else asm("min.NaN.f32 %0, %1, 0f42C80000;" : "=f"(x) : "f"(g));     // 100: nothing in exp(-g) to add to 1 (t of more than 10^38 is infinite)
-    const float t = x * -1.44269502f;
-    const float lo = fmaf(x, -1.92596303e-8f, fmaf(x, -1.44269502f, -t));
+// the constant (|lo| < 2^-17), 2^lo = 1 + lo ln 2.  Where exp(-g) is
+// above kOpen (g below -63.7) or NaN (g above 10^38), gate_far_out has the result.
+__device__ __forceinline__ float silu(float g, float& e) {
+    float r;
+    const float t = g * -1.44269502f;
+    const float lo = fmaf(g, -1.92596303e-8f, fmaf(g, -1.44269502f, -t));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t));
     e = fmaf(e, lo * 0.693147182f, e);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return g * r;
+}
+// silu(g) u for |g| above 60.  Below zero exp(g) may have left the range of fp32 though its product with u has not: 1 + exp(-g) is exp(-g) there, so
+// g exp(g) u, with exp(g) = 2^n h (h within 2^-22) and the powers of two last, in two steps that are both normal.  The first step only rounds what the second takes
+// to 0, so a subnormal result is rounded once.  Below -200 nothing is left of the largest u; -inf counts as such (0 u).
+constexpr float kOpen = 0x1p92f;
+__device__ __forceinline__ float gate_far_out(float g, float u) {
+    if (g > 0.0f) return g * u;
+    g = fmaxf(g, -200.0f);
+    const float n = rintf(g * 1.44269502f);
+    float h;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(fmaf(g, 1.92596303e-8f, fmaf(g, 1.44269502f, -n))));
+    const int m = (int)n + 40, half = m >> 1;                          // -249 to -47
+    return g * h * 0x1p-40f * u * __int_as_float((127 + half) << 23) * __int_as_float((127 + m - half) << 23);
+}
+// Of a word of gates, with that of u `apart` words on: the values given, those of gates far out replaced
+template <int TYPE>
+__device__ __noinline__ float2 far_out_word(const uint32_t* gates, int apart, float y0, float y1) {
+    float gate[2], up[2];
+    word_values<TYPE>(gate, __ldg(gates));
+    word_values<TYPE>(up, __ldg(gates + apart));
+    if (fabsf(gate[0]) > 60.0f) y0 = gate_far_out(gate[0], up[0]);
+    if constexpr (TYPE == ELUTQ_TYPE_F32) return make_float2(y0, y0);
+    if (fabsf(gate[1]) > 60.0f) y1 = gate_far_out(gate[1], up[1]);
+    return make_float2(y0, y1);
 }
 // FULL: values of up to 24 bits; otherwise of up to 11.  (The remainder is taken negative: so the sign of a zero survives.)
 template <bool FULL>
@@ -149,6 +173,7 @@ __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int 
             constexpr int PART = TYPE == ELUTQ_TYPE_F32 ? 16 : kChunk, EACH = TYPE == ELUTQ_TYPE_F32 ? 8 : 16;
 #pragma unroll
             for (int h = 0; h < kChunk; h += PART) {
+                float most = 0.0f;
                 uint32_t g[PART / EACH][8], u[PART / EACH][8];
 #pragma unroll
                 for (int k = 0; k < PART / EACH; ++k) {
@@ -161,7 +186,24 @@ __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int 
                     values_of<TYPE>(y + h + EACH * k, g[k]);
                     values_of<TYPE>(up, u[k]);
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) y[h + EACH * k + i] = silu<TYPE>(y[h + EACH * k + i]) * up[i];
+                    for (int i = 0; i < EACH; i += 2) {
+                        float e[2];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) y[h + EACH * k + i + c] = silu(y[h + EACH * k + i + c], e[c]) * up[i + c];
+                        most = max_abs(most, e[0], e[1]);
+                    }
+                }
+                // (read again and by calls: there are no registers to keep them in, and with the code in line 16-bit types spilled 288 bytes.  Ordinary values are level with a
+                // form that holds gates at -87, 4096 x 14336 fp16 43.6 us, bf16 47.4 for 49.7, fp32 86.0 for 84.4; a gate far out in every chunk costs three to five times that.)
+                if (!(most <= kOpen)) {
+                    constexpr int W = TYPE == ELUTQ_TYPE_F32 ? 1 : 2;                      // values of a word
+                    const uint32_t* words = reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(a.X) + (at + h) * (4 / W));
+#pragma unroll
+                    for (int i = 0; i < PART; i += W) {
+                        const float2 two = far_out_word<TYPE>(words + i / W, a.K / W, y[h + i], y[h + i + W - 1]);
+                        y[h + i] = two.x;
+                        y[h + i + W - 1] = two.y;
+                    }
                 }
             }
         } else {
