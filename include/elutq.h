@@ -481,7 +481,8 @@ int elutq_test_wait_expiry(const void* X, const void* packed, float* Y, int M, i
  * points); lets a benchmark count its launches. */
 unsigned long long elutq_launch_count(void);
 
-/* Release every library-owned scratch/staging buffer (synchronises the device). */
+/* Release every library-owned scratch/staging buffer (synchronises the device) and clear the status of the 4-bit products on
+ * every device that one was launched on.  With nothing to release or clear: no CUDA call. */
 int elutq_release_scratch(void);
 
 #ifdef __cplusplus

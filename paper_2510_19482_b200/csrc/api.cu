@@ -473,7 +473,7 @@ int elutq_device_status(void* stream, int* status) {
     e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e);
     unsigned word = 0;
-    e = (cudaError_t)mx4_status(&word);
+    e = (cudaError_t)mx4_status(&word, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e);
     *status = (int)word;
     if (!ptr || word != 0) return ELUTQ_OK;

@@ -18,8 +18,9 @@ inline int mx4_check(int format, int rows, int K) {
 }
 inline bool mx4_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// The status word of the current device's 4-bit products (mx4_gemm.cu): a cudaError_t value each.
-int mx4_status(unsigned* word);
+// The status words of the 4-bit products, one a device (mx4_gemm.cu); a cudaError_t value each.  The current device's, copied in `stream` (which is waited for): no CUDA
+// call but the device's number where no product has been launched on it.  Clearing: of every device that one has been launched on, which is waited for.
+int mx4_status(unsigned* word, cudaStream_t stream);
 int mx4_clear_status();
 
 }  // namespace elutq

@@ -1042,6 +1042,10 @@ int tensor_map(CUtensorMap* map, const void* base, long long rows, int K, int bo
                ? 0 : (int)cudaErrorInvalidValue;
 }
 
+// Devices that products have been launched on, a bit for each number modulo 64
+std::atomic<unsigned long long> g_devices{0};
+inline unsigned long long device_bit(int dev) { return 1ull << (dev & 63); }
+
 template <int FMT, int CG>
 int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, const Mx4Args& a, cudaStream_t stream) {
     // once for each device (a call would take half a microsecond of the host's time)
@@ -1055,6 +1059,7 @@ int launch_mx4(const Plan& p, const CUtensorMap& xm, const CUtensorMap& wm, cons
         if (e != cudaSuccess) return (int)e;
         ready.fetch_or(bit, std::memory_order_release);
     }
+    if (!(g_devices.load(std::memory_order_relaxed) & device_bit(dev))) g_devices.fetch_or(device_bit(dev));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid);
     cfg.blockDim = dim3((unsigned)kThreads<CG>);
@@ -1126,10 +1131,32 @@ int run_mx4(const void* x_codes, const void* x_scales, const void* w_codes, cons
 
 }  // namespace
 
-int mx4_status(unsigned* word) { return (int)cudaMemcpyFromSymbol(word, g_status, sizeof(*word)); }
+int mx4_status(unsigned* word, cudaStream_t stream) {
+    *word = 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || !(g_devices.load() & device_bit(dev))) return (int)e;
+    // (not in the default stream, which would wait for all others and end a capture of one)
+    e = cudaMemcpyFromSymbolAsync(word, g_status, sizeof(*word), 0, cudaMemcpyDeviceToHost, stream);
+    return (int)(e != cudaSuccess ? e : cudaStreamSynchronize(stream));
+}
 int mx4_clear_status() {
-    const unsigned zero = 0;
-    return (int)cudaMemcpyToSymbol(g_status, &zero, sizeof(zero));
+    const unsigned long long devices = g_devices.load();
+    if (devices == 0) return 0;
+    int count = 0, current = 0;
+    cudaError_t first = cudaGetDeviceCount(&count);
+    if (first == cudaSuccess) first = cudaGetDevice(&current);
+    if (first != cudaSuccess) return (int)first;
+    for (int dev = 0; dev < count; ++dev) {
+        if (!(devices & device_bit(dev))) continue;
+        const unsigned zero = 0;
+        cudaError_t e = cudaSetDevice(dev);
+        if (e == cudaSuccess) e = cudaDeviceSynchronize();
+        if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(zero));
+        if (e != cudaSuccess && first == cudaSuccess) first = e;
+    }
+    const cudaError_t e = cudaSetDevice(current);
+    return (int)(first != cudaSuccess ? first : e);
 }
 
 }  // namespace elutq
