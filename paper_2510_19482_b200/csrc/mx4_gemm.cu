@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 __syncwarp();
                 continue;
             }
-            // (N is below 2^30: a step of up to four rows fits 32 bits without a sign, one of eight does not.)
+            // (N is below 2^30: a step of two rows fits 32 bits, one of three or four fits without a sign, one of eight does not.)
             // 48 columns at a time, whose reads of tensor memory are all in flight together (16 at a time took 11000 cycles for 256 beside
             // MMAs that needed 8200).  Overlapping accumulators: the 48 that both have come first; once they are in registers the other
             // accumulator may be filled.
@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                 if (col < a.N) {
                     const long long at = (long long)(t.t0 + c0) * a.N + col;
                     auto put = [&](auto* y, auto&& cast) {            // four pointers: a short chain of additions
-                        decltype(y) to[4] = {y, y + a.N, y + 2u * (unsigned)a.N, y + 3u * (unsigned)a.N};
+                        decltype(y) to[4] = {y, y + a.N, y + 2 * a.N, y + 3u * (unsigned)a.N};
                         const bool all = c0 + kChunk <= end;
 #pragma unroll
                         for (int c = 0; c < kChunk; ++c) {
@@ -725,7 +725,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
                             for (int k = 0; k < 6; ++k) {
                                 if (2 * (k0 + k) < rest) *reinterpret_cast<uint32_t*>(to2) = y[k];
-                                to2 += 2u * (unsigned)a.N;
+                                to2 += 2 * a.N;
                             }
                         }
                         const int first_odd = (t.t0 + c0 + 1) & 1, value = lane & 1 ? 31 : 0;      // the ends of those rows
@@ -754,8 +754,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
                         for (int k = 0; k < BATCH; ++k) {
                             if (AT_ONCE * (k0 + k) < rest) *reinterpret_cast<V*>(out) = y[k];
-                            out += AT_ONCE / 2 * (unsigned)a.N;
-                            out += AT_ONCE / 2 * (unsigned)a.N;
+                            if constexpr (AT_ONCE == 8) out += 4u * (unsigned)a.N;
+                            out += (AT_ONCE < 4 ? AT_ONCE : 4u) * (unsigned)a.N;
                         }
                     }
                 }
