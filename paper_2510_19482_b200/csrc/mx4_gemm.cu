@@ -305,11 +305,10 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[4], const uint8_t* p, c
     }
 }
 
-// The aligned 16 bytes around p if they lie in [first, last), else 0.
-__device__ __forceinline__ void load_piece(uint32_t (&w)[4], const uint8_t* p, const uint8_t* first, const uint8_t* last) {
-    const uint8_t* q = p - ((uint32_t)reinterpret_cast<uintptr_t>(p) & 15u);
+// The 16 bytes at q (aligned) if `some`, else 0.
+__device__ __forceinline__ void load_piece(uint32_t (&w)[4], const uint8_t* q, bool some) {
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (q >= first && q + 16 <= last) v = __ldg(reinterpret_cast<const uint4*>(q));
+    if (some) v = __ldg(reinterpret_cast<const uint4*>(q));
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
 }
 
@@ -798,8 +797,8 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             // instead of 8 or 16, and NVFP4 was bound by that: 4096 x 28672 x 4096 245 us.)
             constexpr int PIECES = CH, LOADS = 4 * PIECES, ROWS = 8 / PIECES;             // pieces of a row; loads; rows r of a load
             const int piece = lane % PIECES, q = lane / PIECES % 4, r0 = lane / (4 * PIECES);
-            // Of scales whose rows start elsewhere, a lane has pieces of rows c + 8 k (NVFP4) or c + 16 k: by so many rows a row's start moves by 0 or 8 in
-            // 16 bytes, and where a lane's words go is the same for every second k.  Lines touched by a load bound this too: its four lanes of a row meet in a
+            // Of scales whose rows start elsewhere, a lane has pieces of rows c + 8 k (NVFP4, whose rows are an even number of bytes) or c + 16 k: all of these start at
+            // the same place in 16 bytes, and where a lane's words go is the same for every k.  Lines touched by a load bound this too: its four lanes of a row meet in a
             // bank when they store, and pieces of different rows, whose words do not, took 1536 x 32056 x 2080 NVFP4 from 81 to 100 us.  Words of 4 bytes loaded by
             // every lane for its own piece, 5 for 16 bytes: 8 x 6577 x 5952 NVFP4 11.4 us instead of 10.3, 34 rows of 11 experts of 5690 x 4160 33 instead of 29,
             // with pairs 2 to 4 % less.
@@ -845,14 +844,20 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
                         // moved within words, with the next lane's first; words need not move, as each goes to where it belongs (the first ones of a
                         // row may belong to the turn before).  Pieces that are not wholly the matrix's come last, row by row.
                         const uint8_t* p = base + (top + row_c) * a.sk + at;
-                        const long long pace = (long long)EVERY * a.sk;
+                        const unsigned pace = EVERY * (unsigned)a.sk;                  // (K is 2^28 at most)
+                        const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u, shift = 8u * (off & 3u);
+                        const int lead = (int)(off >> 2);                      // words in front of a row's
+                        // how far behind q0 whole pieces begin (128 rows are less than 2^31 bytes); only the first one can lie in front of the matrix
+                        const uint8_t* q0 = p - off;
+                        const int room = (int)max(min((long long)(last16 - q0) - 16, 0x7fffffffLL), -1LL);
                         uint32_t behind[4][4];
 #pragma unroll
-                        for (int k = 0; k < LOADS; ++k) load_piece(w[k], p + k * pace, first16, last16);
+                        for (int k = 0; k < LOADS; ++k) load_piece(w[k], q0 + k * pace, (k > 0 || q0 >= first16) && (int)(k * pace) <= room);
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) load_piece(behind[m], p + (m * PIECES + piece) * pace + 16 * (PIECES - piece), first16, last16);
-                        const uint32_t off0 = (uint32_t)reinterpret_cast<uintptr_t>(p), shift = 8u * (off0 & 3u);
-                        const int lead[2] = {(int)(off0 >> 2 & 3u), (int)((off0 + (uint32_t)pace) >> 2 & 3u)};      // even k, odd k
+                        for (int m = 0; m < 4; ++m) {
+                            const unsigned by = (m * PIECES + piece) * pace + 16 * (PIECES - piece);
+                            load_piece(behind[m], q0 + by, (int)by <= room);
+                        }
 #pragma unroll
                         for (int k = 0; k < LOADS; ++k) {
                             const uint32_t beside = __shfl_down_sync(0xffffffffu, w[k][0], 1), last = __shfl_sync(0xffffffffu, behind[k / PIECES][0], k % PIECES, PIECES);
@@ -860,52 +865,40 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
 #pragma unroll
                             for (int c = 0; c < 4; ++c) w[k][c] = __funnelshift_r(w[k][c], c < 3 ? w[k][c + 1] : next, shift);
                         }
-                        const int lead_b = piece & 1 ? lead[1] : lead[0];
 #pragma unroll
                         for (int m = 0; m < 4; ++m)
 #pragma unroll
                             for (int c = 0; c < 3; ++c) behind[m][c] = __funnelshift_r(behind[m][c], behind[m][c + 1], shift);
+                        uint32_t keep[7] = {~0u, ~0u, ~0u, ~0u, ~0u, ~0u, ~0u};
                         if (s * 4 * CH + 16 * PIECES > a.sk) {                 // bytes behind the rows' end
                             auto mask = [&](int d) {
                                 const int left = a.sk - s * 4 * CH - 4 * d;
                                 return left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
                             };
 #pragma unroll
-                            for (int odd = 0; odd < 2; ++odd)
+                            for (int c = 0; c < 4; ++c) keep[c] = mask(4 * piece + c - lead);
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const uint32_t keep = mask(4 * piece + c - lead[odd]);
-#pragma unroll
-                                    for (int k = odd; k < LOADS; k += 2) w[k][c] &= keep;
-                                }
-#pragma unroll
-                            for (int c = 0; c < 3; ++c) {
-                                const uint32_t keep = mask(4 * PIECES + c - lead_b);
-#pragma unroll
-                                for (int m = 0; m < 4; ++m) behind[m][c] &= keep;
-                            }
+                            for (int c = 0; c < 3; ++c) keep[4 + c] = mask(4 * PIECES + c - lead);
                         }
                         ok = wait(bar(kBarScalesEmpty + r.i), r.phase ^ 1u, gave_up, limit);
                         if (!ok) break;
                         uint8_t* slot = to + r.i * kTurn * s_bytes;
                         // row c + EVERY k of 128 is number c + EVERY (k % PIECES) of 32s number k / PIECES
 #pragma unroll
-                        for (int odd = 0; odd < 2; ++odd)
+                        for (int c = 0; c < 4; ++c) {
+                            const int d = 4 * piece + c - lead;
+                            if (d >= 0) {
+                                uint8_t* dst = slot + place(d) + row_c * 16;
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const int d = 4 * piece + c - lead[odd];
-                                if (d >= 0) {
-                                    uint8_t* dst = slot + place(d) + row_c * 16;
-#pragma unroll
-                                    for (int k = odd; k < LOADS; k += 2) *reinterpret_cast<uint32_t*>(dst + k % PIECES * EVERY * 16 + k / PIECES * 4) = w[k][c];
-                                }
+                                for (int k = 0; k < LOADS; ++k) *reinterpret_cast<uint32_t*>(dst + k % PIECES * EVERY * 16 + k / PIECES * 4) = w[k][c] & keep[c];
                             }
+                        }
 #pragma unroll
                         for (int c = 0; c < 3; ++c)
-                            if (c < lead_b) {
-                                uint8_t* dst = slot + place(4 * PIECES + c - lead_b) + (row_c + EVERY * piece) * 16;
+                            if (c < lead) {
+                                uint8_t* dst = slot + place(4 * PIECES + c - lead) + (row_c + EVERY * piece) * 16;
 #pragma unroll
-                                for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dst + m * 4) = behind[m][c];
+                                for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dst + m * 4) = behind[m][c] & keep[4 + c];
                             }
                         const long long below = min(top + 128, all);            // rows of the matrix end here
                         if (top * a.sk + s * 4 * CH < first16 - base || (below - 1) * a.sk + min(s * 4 * CH + 16 * PIECES, a.sk) > last16 - base) {
