@@ -99,10 +99,13 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
-// On a barrier of another CTA (a shared::cluster address).  arrive_cluster orders this thread's accesses to shared memory for the cluster, which
-// waits for its accesses to global memory too; arrive_remote does not, and is for what a proxy or tcgen05 fence has made visible
-// (with the former, a step's scales took 1500 cycles in pairs of CTAs: 4096 x 28672 x 4096, MXFP4 296 us against 224).
-__device__ __forceinline__ void arrive_remote(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory"); }
+// On a barrier of another CTA (a shared::cluster address).  arrive_cluster orders all accesses in front of it for the cluster, which waits for those to global
+// memory too; arrive_remote only those to this CTA's shared memory, which is what a pair's scales need beside their proxy fence, and a pair's accumulators beside tcgen05's
+// (with the former 4096 x 28672 x 4096 takes 276 us instead of 220; an arrival that orders nothing beyond the CTA would save less than 1 % more).
+__device__ __forceinline__ void arrive_remote(uint32_t bar) {
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
