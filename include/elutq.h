@@ -427,7 +427,8 @@ int elutq_mx4_quantize(const void* X, int x_type, int x_rows, long long ld, int 
                        const float* prescale, const int* index, int index_div, const int* n_rows, void* codes, void* scales,
                        void* stream);
 
-/* Y[rows][K] (y_type, dense, 16-byte aligned) = alpha * code * scale.  alpha: NULL (1), or device float [1]. */
+/* Y[rows][K] (y_type, dense, 16-byte aligned) = alpha * (code * scale).  alpha: NULL (1), or device float [1].  code * scale is formed in fp32, exact but for the
+ * last two MXFP4 scales (bytes 253 and 254, which the quantiser never writes): codes of 4 and more, and of 2 and more, are infinite there, whatever alpha is. */
 int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K, int format, const float* alpha, void* Y,
                          int y_type, void* stream);
 

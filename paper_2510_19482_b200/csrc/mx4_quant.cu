@@ -293,8 +293,8 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
     }
 }
 
-// value = alpha * code * scale: the product of code and scale is exact in fp32 (two and four significant bits), alpha's is
-// rounded to fp32 and the result once more to its type.
+// value = alpha * (code * scale): the product of code and scale is exact in fp32 (two and four significant bits), or infinite: 4 * 2^126 and
+// 2 * 2^127 are beyond fp32, and alpha does not bring them back.  alpha's product is rounded to fp32 and the result once more to its type.
 // Columns of a thread: 64 bytes of results.
 template <int TYPE>
 constexpr int kBack = TYPE == ELUTQ_TYPE_F32 ? 16 : 32;
