@@ -395,8 +395,9 @@ int elutq_hlq_fit(const void* W, int q, int G, int N, int K, int t_max, uint8_t*
  *           ELUTQ_MX4_MXFP4  B = 32, E8M0: 2^(byte - 127), 255 = NaN
  *           ELUTQ_MX4_NVFP4  B = 16, E4M3 without a sign, 127 = NaN; one fp32 factor for the whole matrix on top, which the
  *                            caller keeps (prescale when quantising, alpha afterwards)
- * both dense and row-major, K a multiple of 32, any number of rows.  `codes` must be 16-byte aligned.  All pointers are
- * device memory; nothing is allocated, nothing is synchronised, every call can be captured into a graph.
+ * both dense and row-major, K a multiple of 32, at least one row (a call with none is refused, as everywhere in this
+ * library).  `codes` must be 16-byte aligned.  All pointers are device memory; nothing is allocated, nothing is
+ * synchronised, every call can be captured into a graph.
  */
 #define ELUTQ_MX4_MXFP4 0
 #define ELUTQ_MX4_NVFP4 1
@@ -435,8 +436,7 @@ int elutq_mx4_dequantize(const void* codes, const void* scales, int rows, int K,
 /*
  * Y[M][N] (y_type, dense, 16-byte aligned) = alpha * X[M][K] * W[N][K]^T of two matrices in the same format.  Products are exact, sums
  * are fp32 in the tensor core's order, the result is multiplied by alpha (NULL: 1, or device float [1]) in fp32 and
- * rounded once to y_type.  A row whose scales or values are NaN gives NaN.  Any M and N from 1 to 2^30 - 1, K up
- * to 2^28.
+ * rounded once to y_type.  A row whose scales or values are NaN gives NaN.  Any M and N from 1 to 2^30 - 1, K up to 2^28.
  */
 int elutq_mx4_gemm(const void* x_codes, const void* x_scales, const void* w_codes, const void* w_scales, void* Y, int y_type,
                    int M, int N, int K, int format, const float* alpha, void* stream);
