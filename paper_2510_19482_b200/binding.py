@@ -291,8 +291,9 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
     where = "elutq_mx4_quantize"
     torch, types, current, raw = _torch()
     d, shape, stride = X.get_device(), X.shape, X.stride()
-    if len(stride) != 2 or stride[1] != 1 or shape[1] < (2 * K if flags & MX4_FLAG_SWIGLU else K) or d < 0 or d != current():
-        _refuse(where, f"X: [x_rows, {2 * K if flags & MX4_FLAG_SWIGLU else K}] with unit stride along a row wanted", X)
+    width = 2 * K if flags & MX4_FLAG_SWIGLU else K
+    if len(stride) != 2 or stride[1] != 1 or shape[1] < width or d < 0 or d != current():
+        _refuse(where, f"X: [x_rows, {width}] with unit stride along a row wanted", X)
     half, blocks = K // 2, K // _mx4_block(fmt)
     if codes is None:
         codes = X.new_empty((rows, half), dtype=torch.uint8)
@@ -302,7 +303,7 @@ def elutq_mx4_quantize(X, rows: int, K: int, fmt: int, codes=None, scales=None, 
         scales = X.new_empty((rows, blocks), dtype=torch.uint8)
     elif scales.nbytes != rows * blocks or not scales.is_contiguous() or scales.get_device() != d:
         _refuse(where, f"scales: {rows * blocks} bytes wanted", scales)
-    _check(lib().elutq_mx4_quantize(X.data_ptr(), types.get(X.dtype, -1), shape[0], stride[0], rows, K, fmt, flags,
+    _check(lib().elutq_mx4_quantize(X.data_ptr(), types.get(X.dtype, -1), shape[0], stride[0] if shape[0] > 1 else width, rows, K, fmt, flags,
                                     _small(where, "prescale", prescale, torch.float32, 1, d), _small(where, "index", index, torch.int32, rows, d), index_div,
                                     _small(where, "n_rows", n_rows, torch.int32, 1, d), codes.data_ptr(), scales.data_ptr(),
                                     raw(d) if stream is None else _stream(stream)), where)
