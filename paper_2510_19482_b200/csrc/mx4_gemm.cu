@@ -23,8 +23,8 @@
 //
 // Measured (one B200, us, weights from HBM): 1 x 6144 x 4096 MXFP4 7.0, 64 x 57344 x 8192 NVFP4 46 (5.9 TB/s; 54 in long runs at the
 // power limit), 64 rows over 64 experts of 4096 x 2048 27 (DRAM reads 1.00 of the bytes there are), 4096 x 28672 x 4096 190 to 200 (4.8 to 5.1
-// PFLOP/s; 222 in long runs).  Bound: latencies of a launch, HBM, or at many tokens the tensor core under the card's power limit: a step
-// of 256 k takes 675 to 710 cycles for 512 of MMAs, at a clock of 1.4 GHz.
+// PFLOP/s; 227 in long runs).  Bound: latencies of a launch, HBM, or at many tokens power: a step of 256 k takes 675 to 710 cycles for 512 of
+// MMAs, at a clock of 1.35 GHz in long runs (with all codes zero the same call takes 154 and 158 us; L2 is 46 % busy).
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -802,7 +802,7 @@ __global__ void __launch_bounds__(kThreads<CG>, 1) mx4_gemm_kernel(const __grid_
             const int piece = lane % PIECES, q = lane / PIECES % 4, r0 = lane / (4 * PIECES);
             // Of scales whose rows start elsewhere, a lane has pieces of rows c + 8 k (NVFP4, whose rows are an even number of bytes) or c + 16 k: all of these start at
             // the same place in 16 bytes, and where a lane's words go is the same for every k.  Lines touched by a load bound this too: its four lanes of a row meet in a
-            // bank when they store, and pieces of different rows, whose words do not, took 1536 x 32056 x 2080 NVFP4 from 81 to 100 us.  Words of 4 bytes loaded by
+            // bank when they store, and pieces of different rows, whose words do not, took 1536 x 32056 x 2080 NVFP4 from 81 to 100 us when that was tried.  Words of 4 bytes loaded by
             // every lane for its own piece, 5 for 16 bytes: 8 x 6577 x 5952 NVFP4 11.4 us instead of 10.3, 34 rows of 11 experts of 5690 x 4160 33 instead of 29,
             // with pairs 2 to 4 % less.
             constexpr int EVERY = 32 / PIECES;
@@ -958,9 +958,10 @@ bool fill_plan(Plan& p, int format, int E, bool grouped) {
 }
 
 // Time in us of `tiles` tiles (weights of `groups` matrices in all): a launch's fixed part, which grows with the tokens that a tile's epilogue stores, and the
-// longest of three: steps of the busiest SMs, weights from HBM, operands from L2.  A further tile's steps overlap with the last one's epilogue.  Parts of a
-// cluster cost their exchange.  Fitted to 4400 calls (1000 to 57344 weight rows, K 1024 to 14336, 1 to 512 tokens), 10 % off in the mean; a choice by it
-// costs 1 % against the best plan measured, 15 % at most (10240 x 8192, 512 tokens).
+// longest of three: steps of the busiest SMs, weights from HBM, all tiles' operands (a rate that stands for L2 and, at many tokens, for power).  A
+// further tile's steps overlap with the last one's epilogue.  Parts of a cluster cost their exchange.  Fitted to 4400 calls (1000 to 57344 weight rows,
+// K 1024 to 14336, 1 to 512 tokens; used for more as well), 10 % off in the mean; a choice by it costs 1 % against the best plan measured, 15 % at
+// most (10240 x 8192, 512 tokens).
 double estimate_us(long long tiles, double groups, int N, int K, int format, int cg, int tokens, int split, int num_sms) {
     const int steps = (K + 255) / 256, units = (steps + 1) / 2;
     const long long teams = cg == 2 ? num_sms / 2 : split > 1 ? resident_clusters(split) : num_sms;
