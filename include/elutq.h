@@ -459,6 +459,93 @@ int elutq_mx4_test_wait_expiry(const void* x_codes, const void* x_scales, const 
                                int y_type, int M, int N, int K, int format, unsigned wait_limit, void* stream);
 
 /*
+ * The attention of a serving step: what lies between the q/k/v linear and the o linear of a layer (no counterpart in the paper).
+ *
+ * Paged cache.  Keys and values of tokens lie in pages of page_size tokens, [n_pages][heads][page_size] rows of head_dim values each, dense:
+ *   ELUTQ_KV_16     rows of 16-bit values (`type`)
+ *   ELUTQ_KV_E4M3   rows of E4M3 bytes; a value is byte * factor[head]
+ *   ELUTQ_KV_NVFP4  rows of head_dim / 2 bytes of codes and head_dim / 16 bytes of block scales as in elutq_mx4_quantize; a value is code * scale * factor[head]
+ * k_factor, v_factor: device float [heads], positive, or NULL (1); not used at 16 bits.  k and v 32-byte aligned, scales 16-byte.  head_dim 64 or 128; page_size a
+ * multiple of 16; n_pages * page_size below 2^31.  `type` (ELUTQ_TYPE_F16 or _BF16) is also that of the entries' queries, keys, values and results.
+ * A token's slot is page * page_size + its place in the page.  A sequence's pages are a row of a table, device int [B][pages], rows ld_table apart.  The
+ * struct lies in host memory and is read during the call only.
+ *
+ * Dense rows are [tokens][n][head_dim]: heads side by side, tokens ld elements apart, 16-byte aligned, ld a multiple of 8 (a merged q/k/v result can be passed in place).
+ * All other pointers are device memory; nothing is allocated, nothing is synchronised, every call can be captured into a graph.  As everywhere in this library, a call
+ * with no token or no sequence is refused; a sequence of length 0 is not.
+ */
+#define ELUTQ_KV_16    0
+#define ELUTQ_KV_E4M3  1
+#define ELUTQ_KV_NVFP4 2
+
+typedef struct elutq_kv_cache {
+    void *k, *v;
+    void *k_scales, *v_scales;             /* ELUTQ_KV_NVFP4 only */
+    const float *k_factor, *v_factor;
+    int format, type;
+    int n_pages, heads, page_size, head_dim;
+} elutq_kv_cache;
+
+/* Sizes in bytes of k (as of v) and of its scales.  Pure function, no CUDA call. */
+int elutq_kv_bytes(int format, int n_pages, int heads, int page_size, int head_dim, size_t* data_bytes, size_t* scale_bytes);
+
+/*
+ * Angles of rotary positions: table[n_pos][rot_dim] (float, device, 16-byte aligned), a row's first half cosines, the second sines of position * f_i, times
+ * `magnitude`; formed in 64 bits and rounded once.  f_i = theta^(-2 i / rot_dim), i < rot_dim / 2; rot_dim a multiple of 16.
+ *   ELUTQ_ROPE_PLAIN   f_i
+ *   ELUTQ_ROPE_LINEAR  f_i / factor
+ *   ELUTQ_ROPE_BANDS   f_i where the pair turns `high` times or more over `original` positions, f_i / factor where it turns `low` times or less, and between them
+ *                      f_i * (s + (1 - s) / factor) with s = (turns - low) / (high - low)
+ * factor >= 1; parameters that a scaling does not name are not looked at.
+ */
+#define ELUTQ_ROPE_PLAIN  0
+#define ELUTQ_ROPE_LINEAR 1
+#define ELUTQ_ROPE_BANDS  2
+int elutq_rope_table(float* table, int n_pos, int rot_dim, double theta, int scaling, double factor, double low, double high, double original, double magnitude,
+                     void* stream);
+
+/*
+ * New tokens: queries and keys are rotated, keys and values go into the cache.
+ *   q, q_out     [tokens][n_q_heads]; the rotated queries go to q_out (which may be q, with the same ld).  n_q_heads 0: none
+ *   k, v         [tokens][heads]
+ *   k_out        NULL, or [tokens][heads]: the rotated keys, in 16 bits (for elutq_attn_prefill); may be k
+ *   slots        device int [tokens], distinct.  A slot outside the cache (-1): the token is not stored.  (Where two tokens name one slot, that row's contents are
+ *                undefined.)
+ *   rope         NULL: no rotation (positions, n_pos, rot_dim are not looked at).  Otherwise a table as of elutq_rope_table, n_pos rows of rot_dim
+ *                (<= head_dim: the rest of a head is not rotated); positions: device int [tokens].  A token whose position is outside
+ *                [0, n_pos) is left out: nothing is written for it
+ *   flags        0: values i and i + rot_dim / 2 are a pair; ELUTQ_ROPE_INTERLEAVED: values 2 i and 2 i + 1
+ * y1 = x1 c - x2 s, y2 = x2 c + x1 s, every product and sum rounded to fp32.  16 bits: rounded once more.  E4M3, NVFP4: y * (1 / factor), each rounded to fp32,
+ * goes to the nearest E4M3 value (448 at most; a NaN stays one), or is quantised in blocks of 16 as by elutq_mx4_quantize.
+ */
+#define ELUTQ_ROPE_INTERLEAVED 0x1u
+int elutq_kv_write(const elutq_kv_cache* cache, const void* q, long long ldq, void* q_out, long long ldqo, int n_q_heads, const void* k, long long ldk, void* k_out,
+                   long long ldko, const void* v, long long ldv, int tokens, const int* slots, const int* positions, const float* rope, int n_pos, int rot_dim,
+                   unsigned flags, void* stream);
+
+/*
+ * Ranges of sequences back to dense rows: rows cu[b] .. cu[b+1] - 1 of k_out and v_out [rows][heads] are the tokens from first[b] on (NULL: 0) of sequence b.
+ *   cu   device int [B + 1], ascending.  Rows in front of cu[0] and from cu[B] on are left as they were.  A token without a page (outside the table, or a page
+ *        outside the cache) gives zeros
+ * code * scale is exact, its product with the factor is rounded to fp32 and then to the type.
+ */
+int elutq_kv_read(const elutq_kv_cache* cache, const int* table, long long ld_table, int pages, const int* first, const int* cu, int B, int rows, void* k_out,
+                  long long ldk, void* v_out, long long ldv, void* stream);
+
+/*
+ * Attention of the last new_tokens tokens of every sequence over its part of the cache (which holds them already):
+ *   q, out  [B * new_tokens][n_q_heads], sequence by sequence; query heads h * n_q_heads / heads .. belong to key head h
+ *   lens    device int [B]: tokens of the sequence, the new ones among them; cut to what the table has room for
+ * out = softmax(scale * q K^T) V; new token i sees tokens 0 .. lens[b] - new_tokens + i.  A row that sees nothing is zeros.  What lies in pages behind that is not
+ * looked at, whatever it is; tokens on a page outside the cache count as masked.  scale > 0.  Products of 16-bit values, fp32 sums; the weights of a row are rounded to
+ * 16 bits (relative to 2^14 times the least that still counts) for the product with V.
+ * The workspace belongs to one call at a time (calls of one stream follow one another) and needs no initialisation.  Results are the same bit for bit in every call.
+ */
+int elutq_attn_decode_workspace_bytes(int n_q_heads, int heads, int head_dim, int new_tokens, size_t* bytes);
+int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq, void* out, long long ldo, const int* table, long long ld_table, int pages,
+                      const int* lens, int B, int new_tokens, int n_q_heads, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Device-side status of the library-owned scratch of `stream` and of the current device's 4-bit products (synchronises the stream).
  * *status is 0 unless a kernel gave up on a bounded wait (then a non-zero code that stays set
  * until elutq_release_scratch).  Kernels never spin without a limit.  While it is set, the finalize kernels

@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
+from ctypes import c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -26,11 +26,20 @@ KERNEL_DECODE, KERNEL_LOOK_UP, KERNEL_FRAGMENT, KERNEL_TENSOR_MEMORY, KERNEL_SHA
 MX4_MXFP4, MX4_NVFP4 = 0, 1
 MX4_FLAG_SWIGLU = 0x1
 TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
+KV_16, KV_E4M3, KV_NVFP4 = 0, 1, 2
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS = 0, 1, 2
+ROPE_INTERLEAVED = 0x1
 
 
 class GemvCall(ctypes.Structure):
     """elutq_gemv_call: one M = 1 call of a chain."""
     _fields_ = [("X", c_void_p), ("packed", c_void_p), ("Y", c_void_p), ("N", c_int), ("K", c_int), ("flags", c_uint)]
+
+
+class KvCacheDesc(ctypes.Structure):
+    """elutq_kv_cache."""
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scales", c_void_p), ("v_scales", c_void_p), ("k_factor", c_void_p), ("v_factor", c_void_p),
+                ("format", c_int), ("type", c_int), ("n_pages", c_int), ("heads", c_int), ("page_size", c_int), ("head_dim", c_int)]
 
 
 class ElutqError(RuntimeError):
@@ -78,6 +87,14 @@ _SIGNATURES = {
     "elutq_chain_status": (c_int, [c_void_p, c_void_p, ctypes.POINTER(c_int)]),
     "elutq_chain_forget": (c_int, [c_void_p]),
     "elutq_chain_shares": (c_int, [c_int, c_int, c_int, c_int, c_int, ctypes.POINTER(c_int), ctypes.POINTER(c_int)]),
+    "elutq_kv_bytes": (c_int, [c_int, c_int, c_int, c_int, c_int, ctypes.POINTER(c_size_t), ctypes.POINTER(c_size_t)]),
+    "elutq_rope_table": (c_int, [c_void_p, c_int, c_int, c_double, c_int, c_double, c_double, c_double, c_double, c_double, c_void_p]),
+    "elutq_kv_write": (c_int, [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int,
+                               c_void_p, c_void_p, c_void_p, c_int, c_int, c_uint, c_void_p]),
+    "elutq_kv_read": (c_int, [c_void_p, c_void_p, c_longlong, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p]),
+    "elutq_attn_decode_workspace_bytes": (c_int, [c_int, c_int, c_int, c_int, ctypes.POINTER(c_size_t)]),
+    "elutq_attn_decode": (c_int, [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_int, c_int, c_int, c_float,
+                                  c_void_p, c_size_t, c_void_p]),
     "elutq_device_status": (c_int, [c_void_p, ctypes.POINTER(c_int)]),
     "elutq_launch_count": (c_ulonglong, []),
     "elutq_release_scratch": (c_int, []),
@@ -376,6 +393,146 @@ def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, 
     _mx4_check(where, x_codes, x_scales, w_codes, w_scales, Y, M, N, K, N, fmt)
     _check(lib().elutq_mx4_test_wait_expiry(x_codes.data_ptr(), x_scales.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), Y.data_ptr(),
                                             types.get(Y.dtype, -1), M, N, K, fmt, wait_limit, _stream(stream)), where)
+
+
+class KvCache:
+    """A paged cache: k, v [n_pages, heads, page_size, row] (KV_16: values of `dtype`; KV_E4M3: bytes; KV_NVFP4: head_dim / 2 bytes of codes, with
+    scales [n_pages, heads, page_size, head_dim / 16] of bytes), all dense; factors fp32 [heads] or None.  `dtype`: of queries, keys, values and results."""
+
+    __slots__ = ("desc", "address", "device", "dtype", "heads", "head_dim", "tensors")
+
+    def __init__(self, fmt: int, dtype, k, v, k_scales=None, v_scales=None, k_factor=None, v_factor=None):
+        where = "KvCache"
+        torch, types, _, _ = _torch()
+        d, shape = k.get_device(), k.shape
+        kind = types.get(dtype, -1)
+        if kind not in (TYPE_F16, TYPE_BF16) or fmt not in (KV_16, KV_E4M3, KV_NVFP4) or len(shape) != 4 or d < 0:
+            _refuse(where, "a format, torch.float16 or torch.bfloat16, and k, v of four dimensions wanted", k, v)
+        pages, heads, page, dim = shape
+        if fmt == KV_16:
+            if k.dtype is not dtype or v.dtype is not dtype:
+                _refuse(where, f"k, v of {dtype} wanted", k, v)
+        else:
+            if k.element_size() != 1 or v.element_size() != 1:
+                _refuse(where, "k, v of bytes wanted", k, v)
+            if fmt == KV_NVFP4:
+                dim *= 2
+        if v.shape != shape or v.get_device() != d or not k.is_contiguous() or not v.is_contiguous():
+            _refuse(where, "k, v of one shape wanted", k, v)
+        addresses = [0, 0]
+        if fmt == KV_NVFP4:
+            for i, s in enumerate((k_scales, v_scales)):
+                if s is None or s.nbytes != pages * heads * page * (dim // 16) or s.element_size() != 1 or not s.is_contiguous() or s.get_device() != d:
+                    _refuse(where, f"scales: {pages * heads * page * (dim // 16)} bytes wanted", s)
+                addresses[i] = s.data_ptr()
+        self.desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), addresses[0], addresses[1], _small(where, "k_factor", k_factor, torch.float32, heads, d),
+                                _small(where, "v_factor", v_factor, torch.float32, heads, d), fmt, kind, pages, heads, page, dim)
+        self.address = ctypes.addressof(self.desc)
+        self.device, self.dtype, self.heads, self.head_dim = d, dtype, heads, dim
+        self.tensors = (k, v, k_scales, v_scales, k_factor, v_factor)      # (they live as long as the descriptor names them)
+
+
+def elutq_kv_bytes(fmt: int, n_pages: int, heads: int, page_size: int, head_dim: int):
+    """(bytes of k, as of v; bytes of its scales)."""
+    data, scales = c_size_t(0), c_size_t(0)
+    _check(lib().elutq_kv_bytes(fmt, n_pages, heads, page_size, head_dim, ctypes.byref(data), ctypes.byref(scales)), "elutq_kv_bytes")
+    return data.value, scales.value
+
+
+def elutq_rope_table(n_pos: int, rot_dim: int, theta: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                     original: float = 8192.0, magnitude: float = 1.0, table=None, stream=None):
+    """Cosines and sines of positions, fp32 [n_pos, rot_dim] (allocated here when not given)."""
+    torch, _, current, _ = _torch()
+    d = current()
+    if table is None:
+        table = torch.empty((n_pos, rot_dim), device=f"cuda:{d}")
+    _check(lib().elutq_rope_table(_small("elutq_rope_table", "table", table, torch.float32, n_pos * rot_dim, d), n_pos, rot_dim, theta, scaling, factor, low, high,
+                                  original, magnitude, _stream(stream)), "elutq_rope_table")
+    return table
+
+
+def _rows(where: str, name: str, t, n: int, D: int, dtype, device: int, rows: int = -1) -> int:
+    """Distance between the tokens of [rows, n, D] with heads side by side, in elements."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != n or shape[2] != D or t.dtype is not dtype or t.get_device() != device or (rows >= 0 and shape[0] != rows):
+        _refuse(where, f"{name}: {'' if rows < 0 else rows} tokens of {n} heads of {D} values of {dtype} wanted", t)
+    ld, head, one = t.stride()
+    if one != 1 or (n > 1 and head != D):
+        _refuse(where, f"{name}: the heads of a token side by side wanted", t)
+    return ld if shape[0] > 1 else n * D
+
+
+def _table(where: str, table, B: int, device: int) -> int:
+    """Distance between the rows of a table of pages int32 [B, pages]."""
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != B or table.dtype is not _TORCH[0].int32 or table.get_device() != device or (shape[1] > 1 and table.stride(1) != 1):
+        _refuse(where, f"table: int32, {B} rows of pages wanted", table)
+    return table.stride(0) if B > 1 else shape[1]
+
+
+def elutq_kv_write(cache: KvCache, k, v, slots, q=None, q_out=None, positions=None, rope=None, flags: int = 0, k_out=None, stream=None) -> None:
+    """k, v [tokens, heads, head_dim] into the cache, q and k rotated; slots, positions int32 [tokens], rope fp32 [n_pos, rot_dim].
+    q [tokens, query heads, head_dim] -> q_out; the rotated keys -> k_out, if given."""
+    where = "elutq_kv_write"
+    torch, _, current, raw = _torch()
+    d, H, D, dtype, rows = cache.device, cache.heads, cache.head_dim, cache.dtype, k.shape[0]
+    if d != current() or (q is None) != (q_out is None) or (rope is not None and (positions is None or rope.dim() != 2)):
+        _refuse(where, "q with q_out, and rope [n_pos, rot_dim] with positions wanted", k, q, q_out, rope, positions)
+    ldk, ldv = _rows(where, "k", k, H, D, dtype, d), _rows(where, "v", v, H, D, dtype, d, rows)
+    n = ldq = ldqo = ldko = n_pos = rot = 0
+    if q is not None:
+        n = q.shape[1] if q.dim() == 3 else -1
+        ldq, ldqo = _rows(where, "q", q, n, D, dtype, d, rows), _rows(where, "q_out", q_out, n, D, dtype, d, rows)
+    if k_out is not None:
+        ldko = _rows(where, "k_out", k_out, H, D, dtype, d, rows)
+    if rope is not None:
+        n_pos, rot = rope.shape
+    _check(lib().elutq_kv_write(cache.address, _ptr(q), ldq, _ptr(q_out), ldqo, n, k.data_ptr(), ldk, _ptr(k_out), ldko, v.data_ptr(), ldv, rows,
+                                _small(where, "slots", slots, torch.int32, rows, d), _small(where, "positions", positions, torch.int32, rows, d),
+                                _small(where, "rope", rope, torch.float32, n_pos * rot, d), n_pos, rot, flags, raw(d) if stream is None else _stream(stream)), where)
+
+
+def elutq_kv_read(cache: KvCache, table, first, cu, k_out, v_out, stream=None) -> None:
+    """Tokens first[b] .. of every sequence to rows cu[b] .. cu[b+1] of k_out, v_out [rows, heads, head_dim]; table int32 [B, pages], first int32 [B] or None,
+    cu int32 [B + 1]."""
+    where = "elutq_kv_read"
+    torch, _, current, raw = _torch()
+    d, H, D, dtype, B, rows = cache.device, cache.heads, cache.head_dim, cache.dtype, table.shape[0], k_out.shape[0]
+    if d != current():
+        _refuse(where, f"a cache on the current device wanted, cuda:{d} given", k_out)
+    ldk, ldv = _rows(where, "k_out", k_out, H, D, dtype, d), _rows(where, "v_out", v_out, H, D, dtype, d, rows)
+    ld = _table(where, table, B, d)
+    _check(lib().elutq_kv_read(cache.address, table.data_ptr(), ld, table.shape[1], _small(where, "first", first, torch.int32, B, d),
+                               _small(where, "cu", cu, torch.int32, B + 1, d), B, rows, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv,
+                               raw(d) if stream is None else _stream(stream)), where)
+
+
+def elutq_attn_decode_workspace_bytes(n_q_heads: int, heads: int, head_dim: int, new_tokens: int = 1) -> int:
+    out = c_size_t(0)
+    _check(lib().elutq_attn_decode_workspace_bytes(n_q_heads, heads, head_dim, new_tokens, ctypes.byref(out)), "elutq_attn_decode_workspace_bytes")
+    return out.value
+
+
+def elutq_attn_decode(cache: KvCache, q, out, table, lens, new_tokens: int = 1, scale=None, workspace=None, stream=None) -> None:
+    """out = attention of q [B * new_tokens, query heads, head_dim], the last tokens of the sequences, over the cache; table int32 [B, pages], lens int32 [B].
+    scale None: head_dim ** -0.5.  workspace None: taken from torch's allocator (give one with a stream that is not torch's current one)."""
+    where = "elutq_attn_decode"
+    torch, _, current, raw = _torch()
+    d, D, dtype, B = cache.device, cache.head_dim, cache.dtype, table.shape[0]
+    if d != current() or q.dim() != 3:
+        _refuse(where, f"a cache on the current device (cuda:{d} given) and q [tokens, heads, head_dim] wanted", q)
+    n = q.shape[1]
+    ldq, ldo = _rows(where, "q", q, n, D, dtype, d, B * new_tokens), _rows(where, "out", out, n, D, dtype, d, B * new_tokens)
+    ld = _table(where, table, B, d)
+    if workspace is None:
+        if stream is not None:
+            _refuse(where, "a stream of one's own needs a workspace of its own", q)
+        workspace = q.new_empty(elutq_attn_decode_workspace_bytes(n, cache.heads, D, new_tokens), dtype=torch.uint8)
+    elif not workspace.is_contiguous() or workspace.get_device() != d:
+        _refuse(where, "workspace wanted", workspace)
+    _check(lib().elutq_attn_decode(cache.address, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, table.shape[1], _small(where, "lens", lens, torch.int32, B, d),
+                                   B, new_tokens, n, D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes,
+                                   raw(d) if stream is None else _stream(stream)), where)
 
 
 def elutq_device_status(stream=None) -> int:

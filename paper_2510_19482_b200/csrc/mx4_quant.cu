@@ -17,8 +17,6 @@
 //
 // Bound: HBM.  A thread takes 32 columns (loads and stores of 32 bytes, whole sectors; one block of MXFP4 or two of NVFP4, so no amax is shared between
 // threads) and moves 16 bytes of codes.  With 16 columns and stores of 16 bytes 14336 x 4096 values came back at 4.7 TB/s.
-#include <cuda_bf16.h>
-
 #include "mx4.cuh"
 
 namespace elutq {
@@ -42,36 +40,10 @@ struct QuantArgs {
     int pairs;                 // scales start on 2 bytes
 };
 
-// 32 bytes at p, 32-byte aligned with WIDE and 16-byte aligned otherwise
-template <bool WIDE>
-__device__ __forceinline__ void load32(uint32_t (&v)[8], const void* p) {
-    if constexpr (WIDE) {
-        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
-    } else {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)), b = __ldg(reinterpret_cast<const uint4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-}
-
 // 32 bytes of X from element `at` on, and their values: 8 of fp32, 16 of 16 bits
 template <int TYPE, bool WIDE>
 __device__ __forceinline__ void load_raw(uint32_t (&v)[8], const void* X, long long at) {
     load32<WIDE>(v, reinterpret_cast<const uint8_t*>(X) + at * (TYPE == ELUTQ_TYPE_F32 ? 4 : 2));
-}
-// A word's values: one of fp32, two of 16 bits
-template <int TYPE>
-__device__ __forceinline__ void word_values(float* y, uint32_t v) {
-    if constexpr (TYPE == ELUTQ_TYPE_F32) {
-        y[0] = __uint_as_float(v);
-    } else if constexpr (TYPE == ELUTQ_TYPE_F16) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
-        y[0] = f.x;
-        y[1] = f.y;
-    } else {
-        y[0] = __uint_as_float(v << 16);
-        y[1] = __uint_as_float(v & 0xffff0000u);
-    }
 }
 template <int TYPE>
 __device__ __forceinline__ void values_of(float* y, const uint32_t (&v)[8]) {
@@ -79,33 +51,6 @@ __device__ __forceinline__ void values_of(float* y, const uint32_t (&v)[8]) {
     for (int i = 0; i < 8; ++i) word_values<TYPE>(y + (TYPE == ELUTQ_TYPE_F32 ? i : 2 * i), v[i]);
 }
 
-// Eight values (already divided by their scale) as a word of codes, the first in the lowest bits
-__device__ __forceinline__ uint32_t codes_of(const float* v) {
-    uint32_t d;
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
-        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
-        : "=r"(d) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return d;
-}
-__device__ __forceinline__ float e4m3_value(uint32_t byte) {
-    uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)byte));
-    return __half2float(__ushort_as_half((uint16_t)h));
-}
-__device__ __forceinline__ float max_abs(float a, float b, float c) {
-    float d;
-    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-__device__ __forceinline__ float reciprocal(float x) {                // one unit in the last place off at most
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 // g / (1 + exp(-g)) within a few units in the last place.  exp(-g) = 2^t 2^lo with t = -g log2(e) rounded and lo what that left, also of
 // the constant (|lo| < 2^-17), 2^lo = 1 + lo ln 2.  Where exp(-g) is
 // above kOpen (g below -63.7) or NaN (g above 10^38), gate_far_out has the result.
@@ -142,19 +87,6 @@ __device__ __noinline__ float2 far_out_word(const uint32_t* gates, int apart, fl
     if (fabsf(gate[1]) > 60.0f) y1 = gate_far_out(gate[1], up[1]);
     return make_float2(y0, y1);
 }
-// FULL: values of up to 24 bits; otherwise of up to 11.  (The remainder is taken negative: so the sign of a zero survives.)
-template <bool FULL>
-__device__ __forceinline__ float quotient(float y, float s, float r) {
-    float q = y * r;
-    q = fmaf(fmaf(q, s, -y), -r, q);
-    if constexpr (FULL) {
-        const float over = fmaf(q, s, -y);
-        const int above = (__float_as_int(over) ^ __float_as_int(q)) < 0 ? 0 : 1;      // |q| is above the exact quotient's magnitude
-        if (over != 0.0f && q != 0.0f) q = __int_as_float((__float_as_int(q) - above) | 1);
-    }
-    return q;
-}
-
 template <int FMT, int TYPE, bool SWIGLU, bool WIDE>
 __device__ __forceinline__ void quantise_chunk(const QuantArgs& a, int row, int chunk) {
     float y[kChunk];
@@ -280,17 +212,6 @@ __global__ void __launch_bounds__(128, SWIGLU ? (TYPE == ELUTQ_TYPE_F32 ? 6 : 8)
     if (row >= (a.n_rows != nullptr ? min(__ldg(a.n_rows), a.row0 + a.rows) : a.row0 + a.rows)) return;
     if (a.wide) quantise_chunk<FMT, TYPE, SWIGLU, true>(a, row, chunk);
     else quantise_chunk<FMT, TYPE, SWIGLU, false>(a, row, chunk);
-}
-
-template <bool WIDE>
-__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
-    if constexpr (WIDE) {
-        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                     :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-    } else {
-        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
 }
 
 // value = alpha * (code * scale): the product of code and scale is exact in fp32 (two and four significant bits), or infinite: 4 * 2^126 and
