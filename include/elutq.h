@@ -546,7 +546,27 @@ int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq,
                       const int* lens, int B, int new_tokens, int n_q_heads, float scale, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Device-side status of the library-owned scratch of `stream` and of the current device's 4-bit products (synchronises the stream).
+ * Attention over prompts that lie one behind the other: queries cu_q[b] .. cu_q[b+1] - 1 over keys cu_k[b] .. cu_k[b+1] - 1.
+ *   q, out      [total_q][n_q_heads]; k, v [total_k][heads]; values of `type` (ELUTQ_TYPE_F16 or _BF16); query heads h * n_q_heads / heads .. belong to key head h
+ *   cu_q, cu_k  device int [B + 1], ascending, in [0, total_q] and [0, total_k]; the host does not read them.  Borders out of order or out of range are cut.  A
+ *               sequence may be empty.  Rows of out that belong to no sequence are left as they were
+ *   max_q       queries of the longest sequence, or more; queries of a sequence from max_q (rounded up to 128) on are left out
+ *   flags       0: causal, the last query sees all keys of its sequence and every one before it one key less (so keys of an earlier part of the prompt come in
+ *               front); ELUTQ_ATTN_ALL_KEYS: every query sees all keys
+ * out = softmax(scale * q K^T) V; a row that sees nothing is zeros.  No row is touched by what it does not see, infinities and NaN among that.  scale > 0.  Products of 16-bit
+ * values, fp32 sums; the weights of a row are rounded to `type` for the product with V.
+ */
+#define ELUTQ_ATTN_ALL_KEYS 0x1u
+int elutq_attn_prefill(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
+                       const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags, void* stream);
+
+/* Test entry for its bounded waits, as elutq_mx4_test_wait_expiry. */
+int elutq_attn_test_wait_expiry(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
+                                const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags,
+                                unsigned wait_limit, void* stream);
+
+/*
+ * Device-side status of the library-owned scratch of `stream` and of the current device's 4-bit products and prompts' attention (synchronises the stream).
  * *status is 0 unless a kernel gave up on a bounded wait (then a non-zero code that stays set
  * until elutq_release_scratch).  Kernels never spin without a limit.  While it is set, the finalize kernels
  * of calls with a K split write no Y.
@@ -569,8 +589,8 @@ int elutq_test_wait_expiry(const void* X, const void* packed, float* Y, int M, i
  * points); lets a benchmark count its launches. */
 unsigned long long elutq_launch_count(void);
 
-/* Release every library-owned scratch/staging buffer (synchronises the device) and clear the status of the 4-bit products on
- * every device that one was launched on.  With nothing to release or clear: no CUDA call. */
+/* Release every library-owned scratch/staging buffer (synchronises the device) and clear the status of the 4-bit products and of the
+ * prompts' attention on every device that one was launched on.  With nothing to release or clear: no CUDA call. */
 int elutq_release_scratch(void);
 
 #ifdef __cplusplus

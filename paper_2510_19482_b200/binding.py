@@ -29,6 +29,7 @@ TYPE_F16, TYPE_BF16, TYPE_F32 = 0, 1, 2
 KV_16, KV_E4M3, KV_NVFP4 = 0, 1, 2
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS = 0, 1, 2
 ROPE_INTERLEAVED = 0x1
+ATTN_ALL_KEYS = 0x1
 
 
 class GemvCall(ctypes.Structure):
@@ -95,6 +96,10 @@ _SIGNATURES = {
     "elutq_attn_decode_workspace_bytes": (c_int, [c_int, c_int, c_int, c_int, ctypes.POINTER(c_size_t)]),
     "elutq_attn_decode": (c_int, [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_int, c_int, c_int, c_float,
                                   c_void_p, c_size_t, c_void_p]),
+    "elutq_attn_prefill": (c_int, [c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_float, c_uint,
+                                   c_void_p]),
+    "elutq_attn_test_wait_expiry": (c_int, [c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_float, c_uint,
+                                            c_uint, c_void_p]),
     "elutq_device_status": (c_int, [c_void_p, ctypes.POINTER(c_int)]),
     "elutq_launch_count": (c_ulonglong, []),
     "elutq_release_scratch": (c_int, []),
@@ -533,6 +538,29 @@ def elutq_attn_decode(cache: KvCache, q, out, table, lens, new_tokens: int = 1, 
     _check(lib().elutq_attn_decode(cache.address, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, table.shape[1], _small(where, "lens", lens, torch.int32, B, d),
                                    B, new_tokens, n, D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes,
                                    raw(d) if stream is None else _stream(stream)), where)
+
+
+def _prefill(where: str, q, k, v, out, cu_q, cu_k, max_q, scale, causal, stream, *more) -> None:
+    torch, types, current, raw = _torch()
+    d, dtype = q.get_device(), q.dtype
+    if q.dim() != 3 or k.dim() != 3 or d < 0 or d != current():
+        _refuse(where, "q, k [tokens, heads, head_dim] wanted", q, k)
+    (rows, n, D), (keys, H, _) = q.shape, k.shape
+    B = cu_q.numel() - 1
+    _check(getattr(lib(), where)(q.data_ptr(), _rows(where, "q", q, n, D, dtype, d), k.data_ptr(), _rows(where, "k", k, H, D, dtype, d), v.data_ptr(), _rows(where, "v", v, H, D, dtype, d, keys),
+                                 out.data_ptr(), _rows(where, "out", out, n, D, dtype, d, rows), types.get(dtype, -1), _small(where, "cu_q", cu_q, torch.int32, B + 1, d),
+                                 _small(where, "cu_k", cu_k, torch.int32, B + 1, d), B, max_q, rows, keys, n, H, D, D ** -0.5 if scale is None else scale,
+                                 0 if causal else ATTN_ALL_KEYS, *more, raw(d) if stream is None else _stream(stream)), where)
+
+
+def elutq_attn_prefill(q, k, v, out, cu_q, cu_k, max_q: int, scale=None, causal: bool = True, stream=None) -> None:
+    """out = attention of prompts one behind the other: q, out fp16 or bf16 [total_q, query heads, head_dim], k, v [total_k, heads, head_dim],
+    cu_q, cu_k int32 [B + 1]; scale None: head_dim ** -0.5."""
+    _prefill("elutq_attn_prefill", q, k, v, out, cu_q, cu_k, max_q, scale, causal, stream)
+
+
+def elutq_attn_test_wait_expiry(q, k, v, out, cu_q, cu_k, max_q: int, wait_limit: int, scale=None, causal: bool = True, stream=None) -> None:
+    _prefill("elutq_attn_test_wait_expiry", q, k, v, out, cu_q, cu_k, max_q, scale, causal, stream, wait_limit)
 
 
 def elutq_device_status(stream=None) -> int:

@@ -10,7 +10,7 @@
 #include <utility>
 
 #include "common.cuh"
-#include "mx4.cuh"
+#include "kv.cuh"
 
 namespace elutq {
 
@@ -475,6 +475,10 @@ int elutq_device_status(void* stream, int* status) {
     unsigned word = 0;
     e = (cudaError_t)mx4_status(&word, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e);
+    if (word == 0) {
+        e = (cudaError_t)attn_status(&word, (cudaStream_t)stream);
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
     *status = (int)word;
     if (!ptr || word != 0) return ELUTQ_OK;
     e = cudaMemcpy(&word, ptr, sizeof(word), cudaMemcpyDeviceToHost);
@@ -498,8 +502,8 @@ int elutq_release_scratch(void) {
         if (e != cudaSuccess && first == cudaSuccess) first = e;
     }
     g_parked.clear();
-    const cudaError_t e = (cudaError_t)mx4_clear_status();
-    if (e != cudaSuccess && first == cudaSuccess) first = e;
+    for (int ce : {mx4_clear_status(), attn_clear_status()})
+        if (ce != 0 && first == cudaSuccess) first = (cudaError_t)ce;
     if (first != cudaSuccess) return cuda_fail(first);
     return ELUTQ_OK;
 }

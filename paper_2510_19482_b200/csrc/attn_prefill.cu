@@ -1,0 +1,608 @@
+// Attention over whole prompts that lie one behind the other, causal or not, with grouped heads, on tcgen05.
+//
+//   o_i = sum_j 2^(x_ij - m_i) V_j / sum_j 2^(x_ij - m_i),   x_ij = log2(e) scale q_i . K_j,   j < n_k - n_q + 1 + i (causal) or j < n_k
+//
+// work       A CTA takes two tiles of 128 query rows that share keys: neighbouring (row block, query head) pairs of one key head, so the heads of a group on the same rows
+//            where a group is even.  Keys and values come in tiles of 128 by TMA (128-byte swizzle) into one ring; the two query tiles use each of them once.
+//            The longest row blocks come first in the grid.
+// roles      A warpgroup for each query tile: a thread owns a row, reads its 128 scores from tensor memory, forms the weights and writes them back as 16-bit values
+//            over the scores, where the tensor core takes them as the first operand of P V.  One thread issues all MMAs: while one tile's scores are with
+//            its warpgroup, the other tile's products run.  One warp loads.
+// memory     Tensor memory: scores / weights and results of both tiles, 4 x 128 columns.
+// softmax    A row's maximum moves only when a tile rises more than 2^10 above it; the warp then scales its results in tensor memory.  Weights stay below 2^14.  Maximum, sum
+//            and results are fp32.
+// masked     Scores are selected, and V rows behind a sequence (the next one's, or whatever lies behind the last) are replaced by zeros in shared memory.  A weight of zero
+//            times a V that is not finite would still be NaN, for a row in front of such a token in the same tile: rows whose result is not finite are formed again,
+//            one by one, from what they see.  Finite inputs never come there.
+//
+// Every wait is bounded: the thread whose wait runs out raises the device's status word, and all roles leave their loops.
+#include <atomic>
+
+#include "kv.cuh"
+#include "tensor_map.cuh"
+
+namespace elutq {
+
+namespace {
+
+constexpr int kTile = 128;                 // query rows of a tile, keys of a tile
+constexpr int kRing = 5;                   // tiles of keys and values on their way
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kThreads = 384;
+// Registers of a thread: of the launch's 168 the two warpgroups of the softmax get more, the third less (2 x 208 + 80 is below 3 x 168).
+constexpr int kRowRegs = 208, kOtherRegs = 80;
+constexpr float kNone = 1e30f;               // offset of a row that has seen no key: any score rises above it
+constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
+constexpr unsigned long long kWaitNs = 1000000000ull;
+constexpr int kScores = 0, kResults = 256;   // columns of tensor memory, 128 for each tile
+
+__device__ unsigned g_attn_status;         // 0, or what a launch on this device gave up on
+
+struct PrefillArgs {
+    const int *cu_q, *cu_k;
+    const uint8_t *q, *k, *v;
+    uint8_t* out;
+    long long ldq, ldk, ldv, ldo;          // elements between tokens
+    int total_q, total_k;
+    int heads, group;                      // key heads; query heads of each
+    int causal, type;
+    float scale;                           // times log2(e)
+    int test;                              // 1: no load is issued
+    uint32_t wait_limit;                   // polls (tests); a wait of a second runs out whatever this is
+};
+
+enum { kBarQ = 0, kBarFull = 2, kBarEmpty = kBarFull + kRing, kBarScores = kBarEmpty + kRing, kBarWeights = kBarScores + 2, kBarDone = kBarWeights + 2, kBarTail = kBarDone + 2, kBarDrain, kNumBars };
+
+template <int D>
+constexpr int kTileBytes = kTile * D * 2;
+template <int D>
+constexpr int kSmem = (2 + kRing) * kTileBytes<D> + kNumBars * 8 + 16;
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).
+__device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile const uint32_t* gave_up, uint32_t limit) {
+    if (try_wait(bar, parity)) return true;
+    unsigned long long since = 0;
+    for (uint32_t i = 1; i < limit; ++i) {
+        if (try_wait(bar, parity)) return true;
+        if ((i & 15u) == 0u) {
+            if (gave_up != nullptr && *gave_up) return false;
+            const unsigned long long t = now_ns();
+            if (since == 0) since = t;
+            else if (t - since > kWaitNs) return false;
+        }
+    }
+    return false;
+}
+__device__ __forceinline__ bool wait_alone(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t limit) {
+    if (poll(bar, parity, gave_up, limit)) return true;
+    *gave_up = 1;
+    atomicExch(&g_attn_status, kStatusWaitExpired);
+    return false;
+}
+// By a whole warp, with one answer for it.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t limit) {
+    const bool ok = poll(bar, parity, gave_up, limit);
+    if (__all_sync(0xffffffffu, ok)) return true;
+    if (!ok) {
+        *gave_up = 1;
+        atomicExch(&g_attn_status, kStatusWaitExpired);
+    }
+    __syncwarp();
+    return false;
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// K-major, 128-byte swizzle, 1024 bytes per 8 rows
+__device__ __forceinline__ uint64_t rows_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// The same tile with the rows as the inner index of the product: 64 columns (128 bytes) to a swizzled block, 1024 bytes per 8 rows, the next 64 columns a whole block on
+__device__ __forceinline__ uint64_t columns_desc(uint32_t saddr) {
+    return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)((kTile * 128) >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+#define ELUTQ_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define ELUTQ_B8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+#define ELUTQ_I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+__device__ __forceinline__ void tmem_ld32(uint32_t* r, uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+                 "%26, %27, %28, %29, %30, %31}, [%32];"
+                 : ELUTQ_R8(r, 0), ELUTQ_R8(r, 8), ELUTQ_R8(r, 16), ELUTQ_R8(r, 24) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {         // names the registers: nothing may use them earlier
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : ELUTQ_B8(r, 0), ELUTQ_B8(r, 8), ELUTQ_B8(r, 16), ELUTQ_B8(r, 24) :: "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, "
+                 "%26, %27, %28, %29, %30, %31, %32};"
+                 :: "r"(addr), ELUTQ_I8(r, 0), ELUTQ_I8(r, 8), ELUTQ_I8(r, 16), ELUTQ_I8(r, 24) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t d;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack(uint32_t v) {
+    float y[2];
+    word_values<BF16 ? ELUTQ_TYPE_BF16 : ELUTQ_TYPE_F16>(y, v);
+    return make_float2(y[0], y[1]);
+}
+
+// One row by a warp, from the first `sees` keys: a lane takes D / 32 dimensions.
+template <int D, bool BF16>
+__device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const uint8_t* v, long long ldk, long long ldv, int sees, float scale, uint8_t* out) {
+    constexpr int W = D / 64;              // words of a lane
+    const int lane = threadIdx.x & 31;
+    float x[2 * W], o[2 * W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float2 t = unpack<BF16>(reinterpret_cast<const uint32_t*>(q)[lane * W + i]);
+        x[2 * i] = t.x; x[2 * i + 1] = t.y;
+        o[2 * i] = o[2 * i + 1] = 0.0f;
+    }
+    float top = -INFINITY, sum = 0.0f;
+    for (int j = 0; j < sees; ++j) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float2 t = unpack<BF16>(__ldg(reinterpret_cast<const uint32_t*>(k + 2 * j * ldk) + lane * W + i));
+            s = fmaf(x[2 * i], t.x, fmaf(x[2 * i + 1], t.y, s));
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        s *= scale;
+        const float m = fmaxf(top, s);     // (a NaN does not move it, and reaches the sum below)
+        const float by = top == m ? 1.0f : exp2f(top - m), p = s == -INFINITY ? 0.0f : exp2f(s - m);
+        top = m;
+        sum = fmaf(sum, by, p);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float2 t = unpack<BF16>(__ldg(reinterpret_cast<const uint32_t*>(v + 2 * j * ldv) + lane * W + i));
+            o[2 * i] = fmaf(o[2 * i], by, p * t.x);
+            o[2 * i + 1] = fmaf(o[2 * i + 1], by, p * t.y);
+        }
+    }
+    const float r = 1.0f / sum;
+#pragma unroll
+    for (int i = 0; i < W; ++i) reinterpret_cast<uint32_t*>(out)[lane * W + i] = sum == 0.0f ? 0u : pack<BF16>(o[2 * i] * r, o[2 * i + 1] * r);
+}
+
+struct Tile {
+    int head, row0, tiles;                 // query head, first row in the sequence, tiles of keys
+};
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constant__ CUtensorMap km, const __grid_constant__ CUtensorMap vm,
+                                                                   const PrefillArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    constexpr int BYTES = kTileBytes<D>, HALVES = D / 64;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (2 + kRing) * BYTES);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+    volatile uint32_t* gave_up = tmem_slot + 1;
+    const uint32_t bar0 = smem_u32(bars), smem0 = smem_u32(smem);
+    auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+
+    grid_dependency_wait();
+    // ---- this CTA's tiles ----------------------------------------------------------------------------------------------------------------------
+    const int b = blockIdx.x / a.heads, h = blockIdx.x - b * a.heads, pair = gridDim.y - 1 - blockIdx.y;
+    const int q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q), nq = min(max(__ldg(a.cu_q + b + 1), q0), a.total_q) - q0;
+    const int k0 = min(max(__ldg(a.cu_k + b), 0), a.total_k), nk = min(max(__ldg(a.cu_k + b + 1), k0), a.total_k) - k0;
+    const int shift = nk - nq, count = (nq + kTile - 1) / kTile * a.group;
+    if (2 * pair >= count) return;
+    auto tile_of = [&](int i) {
+        Tile t;
+        const int n = 2 * pair + i, blk = n / a.group;
+        t.head = h * a.group + (n - blk * a.group);
+        t.row0 = blk * kTile;
+        const int sees = a.causal ? min(nk, min(t.row0 + kTile, nq) + shift) : nk;
+        t.tiles = n < count ? (max(sees, 0) + kTile - 1) / kTile : 0;
+        return t;
+    };
+    const Tile ta = tile_of(0), tb = tile_of(1);
+    const int most = max(ta.tiles, tb.tiles);
+    const bool tail = most > 0 && most * kTile > nk;          // the last tile of keys reaches behind the sequence
+
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(tmem_slot)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
+        for (int i = 0; i < kNumBars; ++i) init(i, i == kBarWeights || i == kBarWeights + 1 ? 4 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gave_up = 0;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    grid_launch_dependents();              // (with tensor memory in hand: a kernel that waits for this one may want some too)
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t limit = a.wait_limit;
+
+    if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
+        if (warp == kLoadWarp) {
+            // ---- loads: the query tiles, then keys and values of tile after tile ---------------------------------------------------------------------------
+            int issued = 0;
+            bool ok = true;
+            if (lane == 0 && !a.test) {
+                for (int i = 0; i < 2; ++i) {
+                    const Tile& t = i == 0 ? ta : tb;
+                    if (t.tiles == 0) continue;
+                    expect(bar(kBarQ + i), BYTES);
+                    for (int s = 0; s < HALVES; ++s) tma_load(smem0 + i * BYTES + s * (kTile * 128), &qm, 64 * s, t.head, q0 + t.row0, bar(kBarQ + i));
+                }
+                for (int n = 0; n < 2 * most && ok; ++n) {
+                    const int slot = n % kRing;
+                    ok = wait_alone(bar(kBarEmpty + slot), (uint32_t)(n / kRing & 1) ^ 1u, gave_up, limit);
+                    if (!ok) break;
+                    expect(bar(kBarFull + slot), BYTES);
+                    for (int s = 0; s < HALVES; ++s)
+                        tma_load(smem0 + (2 + slot) * BYTES + s * (kTile * 128), n & 1 ? &vm : &km, 64 * s, h, k0 + (n >> 1) * kTile, bar(kBarFull + slot));
+                    ++issued;
+                }
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            issued = __shfl_sync(0xffffffffu, issued, 0);
+            if (ok && tail && !a.test) {
+                // V rows behind the sequence: zeros
+                const int n = 2 * most - 1, slot = n % kRing;
+                if (wait_warp(bar(kBarFull + slot), (uint32_t)(n / kRing) & 1u, gave_up, limit)) {
+                    for (int i = (nk - (most - 1) * kTile) * 8 + lane; i < kTile * 8; i += 32)
+                        for (int s = 0; s < HALVES; ++s) *reinterpret_cast<uint4*>(smem + (2 + slot) * BYTES + s * (kTile * 128) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive(bar(kBarTail));
+                }
+            }
+            if (*gave_up) {
+                // what is on its way lands before the CTA leaves
+                for (int i = 0; i < 2; ++i)
+                    if ((i == 0 ? ta : tb).tiles != 0 && !a.test) poll(bar(kBarQ + i), 0, nullptr, 0xffffffffu);
+                for (int n = max(0, issued - kRing); n < issued; ++n) poll(bar(kBarFull + n % kRing), (uint32_t)(n / kRing) & 1u, nullptr, 0xffffffffu);
+            }
+        } else if (warp == kMmaWarp) {
+            // ---- MMAs ------------------------------------------------------------------------------------------------------------------------------
+            if (elect_one()) {
+                constexpr uint32_t kTypes = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u);
+                constexpr uint32_t kQK = kTypes | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
+                constexpr uint32_t kPV = kTypes | (1u << 16) | (uint32_t)(D >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
+                bool ok = true;
+                auto scores = [&](int i, int j) {                 // tile i times keys j
+                    const int slot = 2 * j % kRing;
+                    const uint64_t q = rows_desc(smem0 + i * BYTES), k = rows_desc(smem0 + (2 + slot) * BYTES);
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s) {
+                        const uint64_t at = (uint64_t)((s & 3) * 2 + (s >> 2) * (kTile * 128 >> 4));
+                        mma_ss(tmem + kScores + i * kTile, q + at, k + at, kQK, s != 0);
+                    }
+                    commit(bar(kBarScores + i));
+                };
+                auto products = [&](int i, int j) {
+                    const int slot = (2 * j + 1) % kRing;
+                    const uint64_t v = columns_desc(smem0 + (2 + slot) * BYTES);
+#pragma unroll
+                    for (int s = 0; s < kTile / 16; ++s)
+                        mma_ts(tmem + kResults + i * kTile, tmem + kScores + i * kTile + 8 * s, v + (uint64_t)(s * (2048 >> 4)), kPV, j != 0 || s != 0);
+                };
+                auto full = [&](int n) { return wait_alone(bar(kBarFull + n % kRing), (uint32_t)(n / kRing) & 1u, gave_up, limit); };
+                if (most > 0) {
+                    ok = full(0);
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        if ((i == 0 ? ta : tb).tiles == 0) continue;
+                        ok = wait_alone(bar(kBarQ + i), 0, gave_up, limit);
+                        fence_after();
+                        if (ok) scores(i, 0);
+                    }
+                    if (ok) commit(bar(kBarEmpty));
+                }
+                for (int j = 0; j < most && ok; ++j) {
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        const int tiles = (i == 0 ? ta : tb).tiles;
+                        if (j >= tiles) continue;
+                        ok = full(2 * j + 1);
+                        if (ok && tail && j == most - 1) ok = wait_alone(bar(kBarTail), 0, gave_up, limit);
+                        if (ok) ok = wait_alone(bar(kBarWeights + i), (uint32_t)j & 1u, gave_up, limit);
+                        if (!ok) break;
+                        fence_after();
+                        products(i, j);
+                        if (j + 1 == tiles) {
+                            commit(bar(kBarDone + i));
+                        } else {
+                            ok = full(2 * j + 2);
+                            if (ok) scores(i, j + 1);
+                        }
+                    }
+                    if (!ok) break;
+                    commit(bar(kBarEmpty + (2 * j + 1) % kRing));
+                    if (j + 1 < most) commit(bar(kBarEmpty + (2 * j + 2) % kRing));
+                }
+                // (MMAs in flight read shared memory, and their commits arrive there)
+                commit(bar(kBarDrain));
+                poll(bar(kBarDrain), 0, nullptr, 0xffffffffu);
+            }
+            __syncwarp();
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRowRegs));
+        // ---- softmax: a thread to a row -------------------------------------------------------------------------------------------------------------
+        const int i = warp >> 2;
+        const Tile t = i == 0 ? ta : tb;
+        const int row = t.row0 + (tid & 127);
+        const int sees = a.causal ? max(min(nk, row + 1 + shift), 0) : nk;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21, sc = tmem + lanes + kScores + i * kTile, res = tmem + lanes + kResults + i * kTile;
+        float off = kNone, sum = 0.0f;
+        bool ok = true;
+        for (int j = 0; j < t.tiles; ++j) {
+            ok = wait_warp(bar(kBarScores + i), (uint32_t)j & 1u, gave_up, limit);
+            if (!ok) break;
+            fence_after();
+            uint32_t s[kTile];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, sc + 32 * c);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
+            const int left = sees - j * kTile;
+            if (__any_sync(0xffffffffu, left < kTile)) {
+#pragma unroll
+                for (int c = 0; c < kTile; ++c)
+                    if (c >= left) s[c] = 0xff800000u;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < kTile; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+            if (__any_sync(0xffffffffu, fmaf(top, a.scale, off) > kRise)) {
+                const float to = top == -INFINITY ? off : fminf(off, kBase - top * a.scale);
+                const float by = exp2_approx(to - off);
+                off = to;
+                sum *= by;
+                if (j > 0) {                                  // (the products so far are done: the scores came behind them)
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(o, res + 32 * c);
+                        tmem_ld_wait32(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                        tmem_st32(res + 32 * c, o);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float lo = exp2_approx(fmaf(__uint_as_float(s[64 * c + 2 * e]), a.scale, off)), hi = exp2_approx(fmaf(__uint_as_float(s[64 * c + 2 * e + 1]), a.scale, off));
+                    sum += lo + hi;
+                    w[e] = pack<BF16>(lo, hi);
+                }
+                tmem_st32(sc + 32 * c, w);
+            }
+            tmem_st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(bar(kBarWeights + i));
+        }
+        if (2 * pair + i < count && ok) {
+            uint8_t* out = a.out + 2 * ((long long)(q0 + row) * a.ldo + (long long)t.head * D);
+            const float r = sum == 0.0f ? 0.0f : 1.0f / sum;
+            float check = 0.0f;
+            if (t.tiles > 0) {
+                ok = wait_warp(bar(kBarDone + i), 0, gave_up, limit);
+                fence_after();
+            }
+            if (ok) {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    if (t.tiles > 0) {
+                        tmem_ld32(o, res + 32 * c);
+                        tmem_ld_wait32(o);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float lo = __uint_as_float(o[2 * e]) * r, hi = __uint_as_float(o[2 * e + 1]) * r;
+                        check = fmaf(0.0f, lo, fmaf(0.0f, hi, check));
+                        o[e] = pack<BF16>(lo, hi);
+                    }
+                    if (row < nq) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out)[4 * c + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    }
+                }
+                uint32_t again = __ballot_sync(0xffffffffu, check != 0.0f && row < nq);      // (NaN: something was not finite)
+                while (again != 0) {
+                    const int l = __ffs(again) - 1;
+                    again &= again - 1;
+                    const int rr = t.row0 + 32 * (warp & 3) + l;
+                    __syncwarp();                             // (the row's own stores come first)
+                    row_alone<D, BF16>(a.q + 2 * ((long long)(q0 + rr) * a.ldq + (long long)t.head * D), a.k + 2 * ((long long)k0 * a.ldk + (long long)h * D),
+                                       a.v + 2 * ((long long)k0 * a.ldv + (long long)h * D), a.ldk, a.ldv, a.causal ? max(min(nk, rr + 1 + shift), 0) : nk, a.scale,
+                                       a.out + 2 * ((long long)(q0 + rr) * a.ldo + (long long)t.head * D));
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "n"(512) : "memory");
+}
+
+// [tokens][heads][D] of 16-bit values, boxes of 64 values x 128 tokens of one head
+int rows_map(CUtensorMap* map, const void* base, int tokens, int heads, int D, long long ld, bool bf16) {
+    const EncodeTiledFn enc = encode_tiled_fn();
+    if (!enc) return (int)cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, 1, kTile}, elem[3] = {1, 1, 1};
+    return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? 0 : (int)cudaErrorInvalidValue;
+}
+
+std::atomic<unsigned long long> g_devices{0};      // devices that this was launched on, a bit for each number modulo 64
+inline unsigned long long device_bit(int dev) { return 1ull << (dev & 63); }
+
+template <int D, bool BF16>
+int launch_prefill(const CUtensorMap& qm, const CUtensorMap& km, const CUtensorMap& vm, const PrefillArgs& a, dim3 grid, cudaStream_t stream) {
+    // once for each device (a call would take half a microsecond of the host's time)
+    static std::atomic<unsigned long long> ready{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return (int)e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(ready.load(std::memory_order_acquire) & bit)) {
+        e = cudaFuncSetAttribute(attn_prefill_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<D>);
+        if (e != cudaSuccess) return (int)e;
+        ready.fetch_or(bit, std::memory_order_release);
+    }
+    if (!(g_devices.load(std::memory_order_relaxed) & device_bit(dev))) g_devices.fetch_or(device_bit(dev));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem<D>;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, attn_prefill_kernel<D, BF16>, qm, km, vm, a);
+    if (e == cudaSuccess) count_launch(1);
+    return (int)e;
+}
+
+int run_prefill(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q, const int* cu_k, int B,
+                int max_q, int total_q, int total_k, int n_q_heads, int heads, int D, float scale, unsigned flags, uint32_t test_limit, void* stream) {
+    if (!q || !k || !v || !out || !cu_q || !cu_k || B <= 0 || max_q <= 0 || total_q <= 0 || total_k <= 0 || n_q_heads <= 0 || heads <= 0) return ELUTQ_ERR_INVALID_ARG;
+    if ((type != ELUTQ_TYPE_F16 && type != ELUTQ_TYPE_BF16) || (flags & ~ELUTQ_ATTN_ALL_KEYS) || !(scale > 0.0f) || !(scale < 1e30f)) return ELUTQ_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return ELUTQ_ERR_UNSUPPORTED;
+    if (n_q_heads % heads != 0) return ELUTQ_ERR_SHAPE;
+    int st;
+    if ((st = kv_rows_check(q, ldq, n_q_heads, D)) != ELUTQ_OK || (st = kv_rows_check(k, ldk, heads, D)) != ELUTQ_OK || (st = kv_rows_check(v, ldv, heads, D)) != ELUTQ_OK ||
+        (st = kv_rows_check(out, ldo, n_q_heads, D)) != ELUTQ_OK)
+        return st;
+    if (!mx4_aligned(cu_q, 4) || !mx4_aligned(cu_k, 4)) return ELUTQ_ERR_ALIGN;
+    // strides of a tensor map are below 2^40 bytes; coordinates and row numbers 32 bits; blocks of a launch
+    const long long most_ld = 1LL << 38;
+    const int group = n_q_heads / heads;
+    const long long pairs = (((long long)max_q + kTile - 1) / kTile * group + 1) / 2;
+    if (ldq > most_ld || ldk > most_ld || ldv > most_ld || total_q > 0x3fffffff || total_k > 0x3fffffff || pairs > 0xffff || (long long)B * heads > 0x7fffffffLL) return ELUTQ_ERR_SHAPE;
+    PrefillArgs a;
+    a.cu_q = cu_q; a.cu_k = cu_k;
+    a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v;
+    a.out = (uint8_t*)out;
+    a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
+    a.total_q = total_q; a.total_k = total_k;
+    a.heads = heads;
+    a.group = group;
+    a.causal = (flags & ELUTQ_ATTN_ALL_KEYS) == 0;
+    a.type = type;
+    a.scale = scale * 1.44269504088896340736f;
+    a.test = test_limit != 0;
+    a.wait_limit = test_limit != 0 ? test_limit : 0xffffffffu;
+    const bool bf16 = type == ELUTQ_TYPE_BF16;
+    CUtensorMap qm, km, vm;
+    int ce = rows_map(&qm, q, total_q, n_q_heads, D, ldq, bf16);
+    if (ce == 0) ce = rows_map(&km, k, total_k, heads, D, ldk, bf16);
+    if (ce == 0) ce = rows_map(&vm, v, total_k, heads, D, ldv, bf16);
+    const dim3 grid((unsigned)(B * heads), (unsigned)pairs);
+    if (ce == 0)
+        ce = D == 128 ? (bf16 ? launch_prefill<128, true>(qm, km, vm, a, grid, (cudaStream_t)stream) : launch_prefill<128, false>(qm, km, vm, a, grid, (cudaStream_t)stream))
+                      : (bf16 ? launch_prefill<64, true>(qm, km, vm, a, grid, (cudaStream_t)stream) : launch_prefill<64, false>(qm, km, vm, a, grid, (cudaStream_t)stream));
+    if (ce == 0) return ELUTQ_OK;
+    note_cuda_error(ce);
+    return ELUTQ_ERR_CUDA;
+}
+
+}  // namespace
+
+int attn_status(unsigned* word, cudaStream_t stream) {
+    *word = 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || !(g_devices.load() & device_bit(dev))) return (int)e;
+    e = cudaMemcpyFromSymbolAsync(word, g_attn_status, sizeof(*word), 0, cudaMemcpyDeviceToHost, stream);
+    return (int)(e != cudaSuccess ? e : cudaStreamSynchronize(stream));
+}
+int attn_clear_status() {
+    const unsigned long long devices = g_devices.load();
+    if (devices == 0) return 0;
+    int count = 0, current = 0;
+    cudaError_t first = cudaGetDeviceCount(&count);
+    if (first == cudaSuccess) first = cudaGetDevice(&current);
+    if (first != cudaSuccess) return (int)first;
+    for (int dev = 0; dev < count; ++dev) {
+        if (!(devices & device_bit(dev))) continue;
+        const unsigned zero = 0;
+        cudaError_t e = cudaSetDevice(dev);
+        if (e == cudaSuccess) e = cudaDeviceSynchronize();
+        if (e == cudaSuccess) e = cudaMemcpyToSymbol(g_attn_status, &zero, sizeof(zero));
+        if (e != cudaSuccess && first == cudaSuccess) first = e;
+    }
+    const cudaError_t e = cudaSetDevice(current);
+    return (int)(first != cudaSuccess ? first : e);
+}
+
+}  // namespace elutq
+
+using namespace elutq;
+
+extern "C" int elutq_attn_prefill(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
+                                  const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags, void* stream) {
+    return run_prefill(q, ldq, k, ldk, v, ldv, out, ldo, type, cu_q, cu_k, B, max_q, total_q, total_k, n_q_heads, heads, head_dim, scale, flags, 0, stream);
+}
+
+extern "C" int elutq_attn_test_wait_expiry(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
+                                           const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags,
+                                           unsigned wait_limit, void* stream) {
+    if (wait_limit == 0) return ELUTQ_ERR_INVALID_ARG;
+    return run_prefill(q, ldq, k, ldk, v, ldv, out, ldo, type, cu_q, cu_k, B, max_q, total_q, total_k, n_q_heads, heads, head_dim, scale, flags, wait_limit, stream);
+}

@@ -52,4 +52,8 @@ inline int kv_rows_check(const void* p, long long ld, int heads, int head_dim) {
     return !mx4_aligned(p, 16) || ld % 8 != 0 ? ELUTQ_ERR_ALIGN : ELUTQ_OK;
 }
 
+// The status words of the prompts' attention, one a device (attn_prefill.cu): as mx4_status and mx4_clear_status.
+int attn_status(unsigned* word, cudaStream_t stream);
+int attn_clear_status();
+
 }  // namespace elutq

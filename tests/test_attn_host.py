@@ -103,3 +103,23 @@ def test_arguments_of_a_table_of_angles():
         assert call(**kw) == -1, kw
     assert call(rot=24) == -2 and call(table=72) == -3
     assert elutq.elutq_launch_count() == before
+
+
+def prefill(entry="elutq_attn_prefill", more=(), **kw):
+    good = dict(q=64, ldq=512, k=128, ldk=256, v=256, ldv=256, out=512, ldo=512, type=0, cu_q=8, cu_k=16, B=2, max_q=10, total_q=20, total_k=30, n=4, heads=2, D=128, scale=0.1, flags=0)
+    return getattr(elutq.lib(), entry)(*(good | kw).values(), *more, None)
+
+
+@pytest.mark.parametrize("entry,more", [("elutq_attn_prefill", ()), ("elutq_attn_test_wait_expiry", (5,))])
+def test_arguments_of_a_prompt(entry, more):
+    before = elutq.elutq_launch_count()
+    for kw in (dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(cu_q=0), dict(cu_k=0), dict(B=0), dict(max_q=0), dict(total_q=0), dict(total_k=0), dict(n=0), dict(heads=0), dict(type=2),
+               dict(flags=2), dict(scale=0.0), dict(scale=float("nan"))):
+        assert prefill(entry, more, **kw) == -1, kw
+    assert prefill(entry, more, D=96) == -5
+    for kw in (dict(n=5, ldq=1024, ldo=1024), dict(ldq=504), dict(ldk=248), dict(ldv=128), dict(ldo=504), dict(total_q=1 << 30), dict(ldk=1 << 39), dict(max_q=2 ** 31 - 1)):
+        assert prefill(entry, more, **kw) == -2, kw
+    for kw in (dict(q=72), dict(ldq=516), dict(k=130), dict(ldk=257), dict(v=264), dict(out=520), dict(cu_q=9), dict(cu_k=18)):
+        assert prefill(entry, more, **kw) == -3, kw
+    assert prefill("elutq_attn_test_wait_expiry", (0,)) == -1
+    assert elutq.elutq_launch_count() == before
