@@ -5,8 +5,10 @@
 // work       Query rows of one key head (the heads that share it, times the new tokens) are the N of both products, 8 or 16 at a time, the cache's tokens the
 //            M of the first and head dimensions the M of the second: with 4 or 8 heads to a key head no row of the tensor core's tiles is left empty.
 //              S^T [tokens x rows] = K Q^T,   O^T [dims x rows] += V^T P^T
-//            The order of an inner index is free, so a lane takes whole 16-byte pieces of K rows and of V rows from global memory straight into the
-//            registers of the fragments: no shared memory, no transposition but that of P (movmatrix) and of pairs of V rows (byte permutes).
+//            The order of an inner index is free, so a lane takes whole 16-byte pieces of K rows and of V rows as fragments: no transposition but that of P
+//            (movmatrix) and of pairs of V rows (byte permutes, on the codes).
+// loads      Every warp has a ring of stages of its own in shared memory, filled by asynchronous copies of 16 bytes to a lane, so a warp never waits for another within a
+//            segment.  Pieces are placed so that the fragments' reads meet no bank twice.  Rows behind a sequence and on pages that do not exist come as zeros.
 // split      All (sequence, key head, rows) segments laid behind one another, in tiles, are cut into equal shares, one for each CTA that the GPU holds: lengths may
 //            be as ragged as they like.  The warps of a CTA take the tiles of a segment in turn and join through shared memory; a segment that lies within one share
 //            is finished there, the parts of others go to the workspace and a second kernel joins them in their order.
@@ -15,10 +17,12 @@
 // codes      E4M3 and E2M1 values, also times an E4M3 block scale, are exact in fp16, so both products are fp16 ones, with q brought to fp16 by a power of two for each row.
 //            The heads' factors are multiplied into the scale and into the result.
 //
-// Masked places never reach the result, whatever they hold: scores are selected, V rows behind the sequence are replaced by zeros, and in the last tiles, where
+// Masked places never reach the result, whatever they hold: scores are selected, V rows behind the sequence are zeros, and in the last tiles, where
 // the new tokens of a sequence see different lengths, every token's product is formed by itself.
 //
 // Bound: HBM (the cache), for few tokens the latency of table, keys, joining.
+#include <atomic>
+
 #include "kv.cuh"
 
 namespace elutq {
@@ -42,13 +46,17 @@ struct DecodeArgs {
     int type;
     float scale;               // times log2(e)
     float* parts;
+    int4* begun;               // of each share, the segment that begins in it and goes on in the next ones: sequence, key head, tile of rows, parts (0: none)
     long long cap;             // wide * page_size: tokens that the table has room for
 };
 
-__host__ __device__ constexpr int tile_tokens(int format, int D) {
-    const int row = format == ELUTQ_KV_16 ? 2 * D : format == ELUTQ_KV_E4M3 ? D : D / 2;
-    return 4096 / row > 64 ? 64 : 4096 / row;
-}
+__host__ __device__ constexpr int row_bytes(int format, int D) { return format == ELUTQ_KV_16 ? 2 * D : format == ELUTQ_KV_E4M3 ? D : D / 2; }
+// Tokens of a stage
+__host__ __device__ constexpr int tile_tokens(int format, int D) { return row_bytes(format, D) >= 128 ? 16 : 32; }
+__host__ __device__ constexpr int stage_bytes(int format, int D) { return tile_tokens(format, D) * 2 * (row_bytes(format, D) + (format == ELUTQ_KV_NVFP4 ? D / 16 : 0)); }
+__host__ __device__ constexpr int stages_of(int format, int D) { return stage_bytes(format, D) > 4608 ? 2 : 13824 / stage_bytes(format, D); }
+// CTAs that an SM holds: by shared memory, and by the registers that the results take
+__host__ __device__ constexpr int resident(int format, int D, int nt) { return format == ELUTQ_KV_NVFP4 ? 3 - (nt == 2 && D == 128) : nt == 2 && D == 128 ? 2 : stage_bytes(format, D) > 4608 ? 3 : nt == 2 ? 3 : 4; }
 
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
     const long long n = __ldg(a.lens + b);
@@ -90,47 +98,47 @@ __device__ __forceinline__ uint32_t e4m3_pair(uint32_t bytes) {           // of 
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)bytes));
     return h;
 }
-__device__ __forceinline__ uint32_t e2m1_pair(uint32_t byte) {            // of the low 8 bits, as fp16
-    uint32_t h;
-    asm("{\n\t.reg .b8 b, x, y, z;\n\tmov.b32 {b, x, y, z}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(h) : "r"(byte));
-    return h;
+// All codes of a word as fp16, two at a time.  (Bytes unpacked in one piece: the conversion takes its byte from any place of a register, while a shift in front of it costs as
+// much as the conversion itself.)
+__device__ __forceinline__ void e4m3_pairs(uint32_t (&h)[2], uint32_t w) {
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(h[0]), "=r"(h[1]) : "r"(w));
+}
+__device__ __forceinline__ void e2m1_pairs(uint32_t (&h)[4], uint32_t w) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// 16 bytes to shared memory, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, bool some) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
 }
 template <int BYTES>
-__device__ __forceinline__ void load_stream(uint32_t* w, const uint8_t* p) {
-    if constexpr (BYTES == 16) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-    else if constexpr (BYTES == 8) asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    else asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+__device__ __forceinline__ void read_shared(uint32_t* w, uint32_t addr) {
+    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
+    else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
+}
+__device__ __forceinline__ uint32_t read_shared_u8(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint32_t read_shared_u16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
+    return v;
 }
 
-// Where a share begins: its first segment's sequence and the units in front of that sequence.
-struct Place {
-    long long before, total;
-    int b;
-};
 template <int TT>
 __device__ __forceinline__ int tiles_of(int len) { return (len + TT - 1) / TT; }
 
-// Units (tiles of segments) in front of sequence `upto` and of all sequences, by the whole block.
+// Units (tiles of segments) of all sequences, by a warp.
 template <int TT>
-__device__ __forceinline__ void count_units(const DecodeArgs& a, int upto, long long& before, long long& total, long long* scratch) {
-    long long mine = 0, front = 0;
-    const int each = a.c.heads * a.row_tiles;
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
-        const long long n = (long long)tiles_of<TT>(length_of(a, b)) * each;
-        mine += n;
-        if (b < upto) front += n;
-    }
+__device__ __forceinline__ long long count_units(const DecodeArgs& a) {
+    long long total = 0;
+    for (int b = threadIdx.x & 31; b < a.B; b += 32) total += tiles_of<TT>(length_of(a, b));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        mine += __shfl_xor_sync(0xffffffffu, mine, o);
-        front += __shfl_xor_sync(0xffffffffu, front, o);
-    }
-    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) == 0) { scratch[2 * warp] = mine; scratch[2 * warp + 1] = front; }
-    __syncthreads();
-    total = before = 0;
-    for (int w = 0; w < warps; ++w) { total += scratch[2 * w]; before += scratch[2 * w + 1]; }
-    __syncthreads();
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    return total * a.c.heads * a.row_tiles;
 }
 // Units of a share: all CTAs take the same, at least one tile for each warp.
 __device__ __forceinline__ long long share_of(long long total, int ctas) {
@@ -139,65 +147,76 @@ __device__ __forceinline__ long long share_of(long long total, int ctas) {
 }
 
 template <int D, int FMT, bool BF16, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(const DecodeArgs a) {
-    constexpr int TT = tile_tokens(FMT, D), SUB = TT / 16, NC = 8 * NT;
-    constexpr int ROW = FMT == ELUTQ_KV_16 ? 2 * D : FMT == ELUTQ_KV_E4M3 ? D : D / 2;
+__global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_kernel(const DecodeArgs a) {
+    constexpr int TT = tile_tokens(FMT, D), SUB = TT / 16, NC = 8 * NT, S = stages_of(FMT, D), STAGE = stage_bytes(FMT, D);
+    constexpr int ROW = row_bytes(FMT, D), PIECES = ROW / 16;
     constexpr int PER_WORD = FMT == ELUTQ_KV_16 ? 2 : FMT == ELUTQ_KV_E4M3 ? 4 : 8;      // values of a word
     constexpr int KW = ROW / 16, KC = KW < 4 ? KW : 4;       // words of a K row in a lane; of a piece
     constexpr int VW = ROW / 32, VC = VW < 4 ? VW : 4;
     constexpr int STEPS = D / 16;                            // of 16 head dimensions; also 16-dimension tiles of the result
     constexpr bool SCALED = FMT == ELUTQ_KV_NVFP4;
     constexpr int PAD = D + 4;
-    __shared__ __align__(16) float s_o[kWarps][NC][PAD];
+    constexpr int V0 = TT * ROW, KS0 = 2 * TT * ROW, VS0 = KS0 + TT * (D / 16);          // in a stage: K, V, their scales
+    extern __shared__ __align__(1024) uint8_t smem[];
+    // (the warps' parts lie over their rings, which are empty by then)
+    float (*s_o)[NC][PAD] = reinterpret_cast<float (*)[NC][PAD]>(smem);
     __shared__ float s_off[kWarps][NC], s_sum[kWarps][NC];
-    __shared__ long long s_scan[2 * kWarps];
-    __shared__ long long s_before;
-    __shared__ int s_b;
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * STAGE);
     grid_dependency_wait();
     grid_launch_dependents();
 
     // ---- this CTA's share -----------------------------------------------------------------------------------------------------------------------
     const int each = a.c.heads * a.row_tiles;
-    long long share, f0, f1;
+    long long before = 0, f0, f1;
+    int b = 0;
     {
-        // (a run of sequences to a thread; the thread whose run holds the first unit walks it)
-        const int run = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, tid * run), b1 = min(a.B, b0 + run);
-        long long mine = 0;
-        for (int b = b0; b < b1; ++b) mine += (long long)tiles_of<TT>(length_of(a, b)) * each;
-        long long incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (lane == 31) s_scan[warp] = incl;
-        __syncthreads();
-        long long front = incl - mine, total = 0;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) front += s_scan[w];
-            total += s_scan[w];
-        }
-        share = share_of(total, gridDim.x);
+        const long long total = count_units<TT>(a);
+        const long long share = share_of(total, gridDim.x);
         f0 = blockIdx.x * share;
         f1 = f0 + share < total ? f0 + share : total;
-        if (f0 >= f1) return;                                 // (the whole CTA)
-        if (f0 >= front && f0 < front + mine) {
-            int b = b0;
-            for (; b < b1; ++b) {
-                const long long n = (long long)tiles_of<TT>(length_of(a, b)) * each;
-                if (f0 < front + n) break;
-                front += n;
-            }
-            s_before = front;
-            s_b = b;
+        // sequences without a token: zeros
+        for (int e = blockIdx.x; e < a.B; e += gridDim.x)
+            if (length_of(a, e) == 0)
+                for (long long i = tid; i < (long long)a.fresh * a.c.heads * a.group * (D / 8); i += kThreads) {
+                    const long long tok = i / (a.c.heads * a.group * (D / 8));
+                    reinterpret_cast<uint4*>(a.out + 2 * ((long long)e * a.fresh + tok) * a.ldo)[i - tok * (a.c.heads * a.group * (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
+                }
+        if (f0 >= f1) {                                       // (the whole CTA)
+            if (tid == 0) a.begun[blockIdx.x] = make_int4(0, 0, 0, 0);
+            return;
         }
-        __syncthreads();
+        // the sequence that the first unit belongs to: 32 at a time
+        for (;; b += 32) {
+            const long long mine = b + lane < a.B ? (long long)tiles_of<TT>(length_of(a, b + lane)) * each : 0;
+            long long incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            const uint32_t behind = __ballot_sync(0xffffffffu, before + incl > f0);
+            if (behind != 0) {
+                const int l = __ffs(behind) - 1;
+                before += __shfl_sync(0xffffffffu, incl - mine, l);
+                b += l;
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
     }
-    int b = s_b;
-    long long before = s_before;
 
+    // where a lane copies to and reads from.  A piece's place in its row is its number with some bits of the row's number turned: the eight lanes that are served together
+    // read two K rows, or four V rows, of which every second.
+    auto k_turn = [](int r) { return PIECES >= 8 ? (r & 1) << 2 : 0; };
+    auto v_turn = [](int r) { return PIECES >= 8 ? (r >> 1 & 3) << 1 : PIECES == 4 ? r >> 1 & 3 : 0; };
+    constexpr int ROWS = 32 / PIECES;                         // rows of a copy of the warp
+    const int cr = lane / PIECES, cc = lane % PIECES;
+    const uint32_t k_read = ring + g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
+    const uint32_t v_read = ring + V0 + 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g);
+
+    bool recorded = false;
     for (long long f = f0; f < f1;) {
         const int len = length_of(a, b), tiles = tiles_of<TT>(len);
         if (tiles == 0) { ++b; continue; }
@@ -209,68 +228,55 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
         const int least = len - a.fresh + 1;                  // tokens that the first of the new tokens sees
         const int mine = warp < count ? (count - warp + kWarps - 1) / kWarps : 0;        // this warp's tiles: tile0 + warp + n kWarps
 
-        // ---- loads -----------------------------------------------------------------------------------------------------------------------------
-        uint32_t kr[SUB][2][KW], vr[SUB][4][VW];
-        uint32_t ksc[SUB][2], vsc[SUB];
-        uint32_t there = 0;                                   // sub-tiles of the K in hand whose page exists
+        // ---- copies ----------------------------------------------------------------------------------------------------------------------------
+        uint32_t there = 0;                                   // a bit for each 16 tokens of the stages: their page exists
         int ids = -1;                                         // lane i: page of the i-th of 32 16-token pieces of this warp's tiles
-        auto fetch_ids = [&](int n) {                         // for tiles n, n + 1, .. of this warp
-            const int tile = tile0 + warp + (n + lane / SUB) * kWarps;
-            const int tok = tile * TT + (lane % SUB) * 16;
-            ids = -1;
-            if (n + lane / SUB < mine && tok < len) ids = __ldg(pages + a.c.page.of(tok));
-            if (ids >= a.c.n_pages) ids = -1;
-        };
-        auto row_of = [&](int n, int s) {                     // first row of a piece (whatever page: see `there`)
-            const int tok = (tile0 + warp + n * kWarps) * TT + 16 * s;
-            const int page = max(0, __shfl_sync(0xffffffffu, ids, (n * SUB + s) & 31));
-            return ((long long)page * a.c.heads + h) * a.c.page_size + (tok - a.c.page.of(tok) * a.c.page_size);
-        };
-        auto load_k = [&](int n) {
-            if (((n * SUB) & 31) == 0) fetch_ids(n);
-            there = 0;
+        auto copy = [&](int n, int slot) {
+            if (((n * SUB) & 31) == 0) {
+                const int tok = (tile0 + warp + (n + lane / SUB) * kWarps) * TT + (lane % SUB) * 16;
+                ids = -1;
+                if (n + lane / SUB < mine && tok < len) ids = __ldg(pages + a.c.page.of(tok));
+                if (ids >= a.c.n_pages) ids = -1;
+            }
+            const int tok0 = (tile0 + warp + n * kWarps) * TT;
+            const uint32_t at = ring + slot * STAGE;
+            [[maybe_unused]] long long rows[SUB];
+            there &= ~(((1u << SUB) - 1u) << (slot * SUB));
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
-                const long long row = row_of(n, s);
-                const bool ok = __shfl_sync(0xffffffffu, ids, (n * SUB + s) & 31) >= 0;
-                there |= (uint32_t)ok << s;
+                const int tok = tok0 + 16 * s, id = __shfl_sync(0xffffffffu, ids, (n * SUB + s) & 31);
+                there |= (uint32_t)(id >= 0) << (slot * SUB + s);
+                const long long row = ((long long)max(id, 0) * a.c.heads + h) * a.c.page_size + (tok - a.c.page.of(tok) * a.c.page_size);
+                rows[s] = row;
+                const int some = id >= 0 ? min(len - tok, 16) : 0;
+                const uint8_t *ksrc = a.c.k + row * ROW + lane * 16, *vsrc = a.c.v + row * ROW + lane * 16;
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const uint8_t* p = a.c.k + (row + g + 8 * r) * ROW + t * (4 * KC);
+                for (int i = 0; i < 16 / ROWS; ++i) {
+                    const int r = i * ROWS + cr;
+                    copy16(at + (16 * s + r) * ROW + 16 * (cc ^ k_turn(r)), ksrc + i * 512, r < some);
+                    copy16(at + V0 + (16 * s + r) * ROW + 16 * (cc ^ v_turn(r)), vsrc + i * 512, r < some);
+                }
+            }
+            if constexpr (SCALED) {
+                // 16 tokens' scales are 128 or 64 bytes; a lane takes the same 16 of K and of V
+                constexpr int LANES = D / 16;             // of 16 tokens
+                if (lane < SUB * LANES) {
+                    const int s = lane / LANES, part = lane % LANES;
+                    long long row = rows[0];
 #pragma unroll
-                    for (int i = 0; i < KW / KC; ++i) load_stream<4 * KC>(&kr[s][r][i * KC], p + i * (16 * KC));
-                    if constexpr (SCALED) {
-                        const uint8_t* q = a.c.ks + (row + g + 8 * r) * (D / 16);
-                        ksc[s][r] = D == 128 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(q) + t) : (uint32_t)__ldg(q + t);
-                    }
+                    for (int i = 1; i < SUB; ++i) row = s == i ? rows[i] : row;
+                    const bool ok = there >> (slot * SUB + s) & 1u;
+                    // (rows behind the sequence too: within the page, finite or not, they meet codes of zero; a NaN is taken out where they are used)
+                    copy16(at + KS0 + lane * 16, a.c.ks + row * (D / 16) + part * 16, ok);
+                    copy16(at + VS0 + lane * 16, a.c.vs + row * (D / 16) + part * 16, ok);
                 }
             }
         };
-        auto load_v = [&](int n) {                            // (behind load_k of the same tile)
+        auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                const long long row = row_of(n, s);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int tok = 2 * t + (r & 1) + 8 * (r >> 1);
-                    const uint8_t* p = a.c.v + (row + tok) * ROW + g * (4 * VC);
-#pragma unroll
-                    for (int i = 0; i < VW / VC; ++i) load_stream<4 * VC>(&vr[s][r][i * VC], p + i * (32 * VC));
-                }
-                if constexpr (SCALED) {
-                    uint32_t v = 0;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int tok = 2 * t + (r & 1) + 8 * (r >> 1);
-                        v |= (uint32_t)__ldg(a.c.vs + (row + tok) * (D / 16) + (D == 128 ? g : g / 2)) << (8 * r);
-                    }
-                    vsc[s] = v;
-                }
-            }
-        };
-        if (mine > 0) {
-            load_k(0);
-            load_v(0);
+        for (int n = 0; n < S; ++n) {
+            if (n < mine) copy(n, n);
+            commit();
         }
 
         // ---- query rows as fragments: column g of each eight; the columns of this lane's scores are 2 t and 2 t + 1 -------------------------------
@@ -331,8 +337,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.0f;
 
-        for (int n = 0; n < mine; ++n) {
+        for (int n = 0, slot = 0; n < mine; ++n) {
             const int tok0 = (tile0 + warp + n * kWarps) * TT;
+            const uint32_t at = slot * STAGE;
+            asm volatile("cp.async.wait_group %0;" :: "n"(S - 1) : "memory");
+            __syncwarp();
             // ---- scores ----------------------------------------------------------------------------------------------------------------------
             float sc[SUB][NT][4];
 #pragma unroll
@@ -341,38 +350,40 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sc[s][nt][i] = 0.0f;
+                uint32_t kr[2][KW];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < KW / KC; ++i) read_shared<4 * KC>(&kr[r][i * KC], (k_read ^ (i * 64)) + at + (16 * s + 8 * r) * ROW);
                 [[maybe_unused]] uint32_t blk[2][2];          // [row][block of this lane]: scale, in both halves
                 if constexpr (SCALED) {
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const uint32_t two = e4m3_pair(ksc[s][r]);
+                        const uint32_t p = ring + at + KS0 + (16 * s + g + 8 * r) * (D / 16);
+                        const uint32_t two = e4m3_pair(D == 128 ? read_shared_u16(p + 2 * t) : read_shared_u8(p + t));
                         blk[r][0] = prmt(two, two, 0x1010);
                         blk[r][1] = prmt(two, two, 0x3232);
                     }
                 }
 #pragma unroll
                 for (int w = 0; w < KW; ++w) {                // a word of both rows: PER_WORD / 4 steps
-                    uint32_t x[2][PER_WORD / 2];
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const uint32_t v = kr[s][r][w];
-                        if constexpr (FMT == ELUTQ_KV_16) {
-                            x[r][0] = v;
-                        } else if constexpr (FMT == ELUTQ_KV_E4M3) {
-                            x[r][0] = e4m3_pair(v);
-                            x[r][1] = e4m3_pair(v >> 16);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) x[r][i] = hmul2(e2m1_pair(v >> (8 * i)), blk[r][w / 2]);
-                        }
-                    }
                     if constexpr (FMT == ELUTQ_KV_16) {
                         if (w % 2 == 1) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                mma<BF16>(sc[s][nt], kr[s][0][w - 1], kr[s][1][w - 1], kr[s][0][w], kr[s][1][w], qf[nt][w / 2][0], qf[nt][w / 2][1]);
+                            for (int nt = 0; nt < NT; ++nt) mma<BF16>(sc[s][nt], kr[0][w - 1], kr[1][w - 1], kr[0][w], kr[1][w], qf[nt][w / 2][0], qf[nt][w / 2][1]);
                         }
                     } else {
+                        uint32_t x[2][PER_WORD / 2];
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            if constexpr (FMT == ELUTQ_KV_E4M3) {
+                                e4m3_pairs(x[r], kr[r][w]);
+                            } else {
+                                e2m1_pairs(x[r], kr[r][w]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) x[r][i] = hmul2(x[r][i], blk[r][w / 2]);
+                            }
+                        }
 #pragma unroll
                         for (int i = 0; i < PER_WORD / 4; ++i)
 #pragma unroll
@@ -381,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
                     }
                 }
             }
-            const uint32_t pages_there = there;
+            const uint32_t pages_there = there >> (slot * SUB) & ((1u << SUB) - 1u);
             const bool last = tok0 + TT > least;              // some column may not see all of the tile
             if (last || pages_there != (1u << SUB) - 1u) {
 #pragma unroll
@@ -440,85 +451,106 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
                     pf[s][nt][1] = transposed(pack<BF16>(p[2], p[3]));
                 }
             // ---- P V ---------------------------------------------------------------------------------------------------------------------------
-            if (tok0 + TT > len || pages_there != (1u << SUB) - 1u) {        // rows that no column sees: zeros
+            // V rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of 16 tokens as fragments.  Tile m of the result: dimensions 2 m and 2 m + 1 of this lane's, the two tokens of a pair side by side.
+            // Codes are brought side by side before they are converted.
+            uint32_t vr[4][VW];
+            uint32_t vsc[2];
+            auto read_v = [&](int s) {
 #pragma unroll
-                for (int s = 0; s < SUB; ++s)
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (tok0 + 16 * s + 2 * t + (r & 1) + 8 * (r >> 1) >= len || !(pages_there >> s & 1u)) {
-#pragma unroll
-                            for (int i = 0; i < VW; ++i) vr[s][r][i] = 0;
-                            if constexpr (SCALED) vsc[s] &= ~(0xffu << (8 * r));
-                        }
-            }
-            // V rows of a piece as fragments: word w of its four rows holds dimensions 2 w, 2 w + 1 of this lane's, tile w of the result
-            auto v_word = [&](int s, int r, int w) {
-                if constexpr (FMT == ELUTQ_KV_16) return vr[s][r][w];
-                else if constexpr (FMT == ELUTQ_KV_E4M3) return e4m3_pair(vr[s][r][w / 2] >> (16 * (w & 1)));
-                else return e2m1_pair(vr[s][r][w / 4] >> (8 * (w & 3)));
-            };
-            auto v_fragment = [&](int s, int w, uint32_t (&x)[4]) {
-                const uint32_t r0 = v_word(s, 0, w), r1 = v_word(s, 1, w), r2 = v_word(s, 2, w), r3 = v_word(s, 3, w);
-                x[0] = prmt(r0, r1, 0x5410);
-                x[1] = prmt(r0, r1, 0x7632);
-                x[2] = prmt(r2, r3, 0x5410);
-                x[3] = prmt(r2, r3, 0x7632);
+                    for (int i = 0; i < VW / VC; ++i) read_shared<4 * VC>(&vr[r][i * VC], v_read + at + (16 * s + (r & 1) + 8 * (r >> 1)) * ROW + i * 128);
                 if constexpr (SCALED) {
-                    const uint32_t lo = e4m3_pair(vsc[s]), hi = e4m3_pair(vsc[s] >> 16);
-                    x[0] = hmul2(x[0], lo);
-                    x[1] = hmul2(x[1], lo);
-                    x[2] = hmul2(x[2], hi);
-                    x[3] = hmul2(x[3], hi);
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const int tok = 16 * s + 2 * t + 8 * p;
+                        const uint32_t q = ring + at + VS0 + tok * (D / 16) + (D == 128 ? g : g / 2);
+                        uint32_t bytes = read_shared_u8(q) | read_shared_u8(q + D / 16) << 8;
+                        if (tok0 + TT > len) bytes &= (tok0 + tok < len ? 0xffu : 0u) | (tok0 + tok + 1 < len ? 0xff00u : 0u);
+                        vsc[p] = e4m3_pair(bytes);
+                    }
+                }
+            };
+            constexpr int MS = FMT == ELUTQ_KV_16 ? 1 : FMT == ELUTQ_KV_E4M3 ? 2 : 4;      // tiles of the result from a word of the four rows
+            auto v_fragments = [&](int w, uint32_t (&x)[MS][4]) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const uint32_t v0 = vr[2 * p][w], v1 = vr[2 * p + 1][w];
+                    if constexpr (FMT == ELUTQ_KV_16) {
+                        x[0][2 * p] = prmt(v0, v1, 0x5410);
+                        x[0][2 * p + 1] = prmt(v0, v1, 0x7632);
+                    } else if constexpr (FMT == ELUTQ_KV_E4M3) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t h[2];
+                            e4m3_pairs(h, prmt(v0, v1, i == 0 ? 0x5140 : 0x7362));
+                            x[i][2 * p] = h[0];
+                            x[i][2 * p + 1] = h[1];
+                        }
+                    } else {
+                        uint32_t lo[4], hi[4];
+                        e2m1_pairs(lo, (v0 & 0x0f0f0f0fu) | (v1 << 4 & 0xf0f0f0f0u));
+                        e2m1_pairs(hi, (v0 >> 4 & 0x0f0f0f0fu) | (v1 & 0xf0f0f0f0u));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            x[i][2 * p] = hmul2(lo[i], vsc[p]);
+                            x[i][2 * p + 1] = hmul2(hi[i], vsc[p]);
+                        }
+                    }
                 }
             };
             if (!last || a.fresh == 1) {
 #pragma unroll
-                for (int s = 0; s < SUB; ++s)
+                for (int s = 0; s < SUB; ++s) {
+                    read_v(s);
 #pragma unroll
-                    for (int m = 0; m < STEPS; ++m) {
-                        uint32_t x[4];
-                        v_fragment(s, m, x);
+                    for (int w = 0; w < VW; ++w) {
+                        uint32_t x[MS][4];
+                        v_fragments(w, x);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<BF16>(o[m][nt], x[0], x[1], x[2], x[3], pf[s][nt][0], pf[s][nt][1]);
+                        for (int i = 0; i < MS; ++i)
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma<BF16>(o[w * MS + i][nt], x[i][0], x[i][1], x[i][2], x[i][3], pf[s][nt][0], pf[s][nt][1]);
                     }
+                }
             } else {
                 // each new token's columns by themselves, with V rows that it does not see replaced by zeros
                 const int first = rt * NC / a.group, end = min(a.fresh, (rt * NC + NC - 1) / a.group + 1);
                 for (int nw = first; nw < end; ++nw) {
                     const int sees = least + nw;
 #pragma unroll
-                    for (int m = 0; m < STEPS; ++m) {
-                        float part[NT][4];
+                    for (int s = 0; s < SUB; ++s) {
+                        read_v(s);
+                        const int tok = tok0 + 16 * s + 2 * t;
+                        const uint32_t lo = (tok < sees ? 0xffffu : 0u) | (tok + 1 < sees ? 0xffff0000u : 0u);
+                        const uint32_t hi = (tok + 8 < sees ? 0xffffu : 0u) | (tok + 9 < sees ? 0xffff0000u : 0u);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                        for (int w = 0; w < VW; ++w) {
+                            uint32_t x[MS][4];
+                            v_fragments(w, x);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) part[nt][i] = 0.0f;
+                            for (int m = 0; m < MS; ++m)
 #pragma unroll
-                        for (int s = 0; s < SUB; ++s) {
-                            uint32_t x[4];
-                            v_fragment(s, m, x);
-                            const int tok = tok0 + 16 * s + 2 * t;
-                            const uint32_t lo = (tok < sees ? 0xffffu : 0u) | (tok + 1 < sees ? 0xffff0000u : 0u);
-                            const uint32_t hi = (tok + 8 < sees ? 0xffffu : 0u) | (tok + 9 < sees ? 0xffff0000u : 0u);
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                    mma<BF16>(part, x[m][0] & lo, x[m][1] & lo, x[m][2] & hi, x[m][3] & hi, pf[s][nt][0], pf[s][nt][1]);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma<BF16>(part[nt], x[0] & lo, x[1] & lo, x[2] & hi, x[3] & hi, pf[s][nt][0], pf[s][nt][1]);
+                                    for (int i = 0; i < 4; ++i)
+                                        if (limit[nt][i & 1] == sees) o[w * MS + m][nt][i] += part[i];
+                                }
                         }
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (limit[nt][i & 1] == sees) o[m][nt][i] += part[nt][i];
                     }
                 }
             }
-            if (n + 1 < mine) {
-                load_k(n + 1);
-                load_v(n + 1);
-            }
+            __syncwarp();
+            if (n + S < mine) copy(n + S, slot);
+            commit();
+            slot = slot + 1 == S ? 0 : slot + 1;
         }
 
         // ---- the warps' parts meet ----------------------------------------------------------------------------------------------------------------
         const int active = min(kWarps, count);
+        __syncthreads();
         if (mine > 0) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -570,6 +602,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
                 *reinterpret_cast<float2*>(part + 2 * NC + col * D + d) = make_float2(x, y);
             }
         }
+        if (begins && !whole && tid == 0) {
+            const long long share = f1 - f0;                  // (a share that another one follows is a whole one)
+            a.begun[blockIdx.x] = make_int4(b, h, rt, (int)(1 + (tiles - count + share - 1) / share));
+            recorded = true;
+        }
         __syncthreads();
         f += count;
         if (f - before == (long long)tiles * each) {
@@ -577,53 +614,98 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) attn_decode_kernel(
             ++b;
         }
     }
+    if (tid == 0 && !recorded) a.begun[blockIdx.x] = make_int4(0, 0, 0, 0);
 }
 
-// Joins the parts of the segments that several shares hold, in their order; columns that see nothing get zeros.  A block per (segment, query row), a thread per dimension.
-template <int D, int TT, int NT>
-__global__ void __launch_bounds__(D) attn_join_kernel(const DecodeArgs a, int ctas) {
-    constexpr int NC = 8 * NT;
-    __shared__ long long s_scan[2 * (D / 32)];
+// Joins the parts of the segments that several shares hold, in their order.  A block for each share in which such a segment begins, and for `cols` of its query rows: a warp to a
+// row and to every `split`-th part, a lane to D / 32 dimensions; `split` warps join through shared memory.
+template <int D, int NT>
+__global__ void __launch_bounds__(256) attn_join_kernel(const DecodeArgs a, int split) {
+    constexpr int NC = 8 * NT, SIZE = NC * (D + 2), W = D / 32;
+    __shared__ float s_low[8], s_sum[8], s_x[8][D];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cols = 8 / split;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int row = blockIdx.x % a.rows, seg_all = blockIdx.x / a.rows, h = seg_all % a.c.heads, b = seg_all / a.c.heads;
-    const int rt = row / NC, col = row - rt * NC, d = threadIdx.x;
-    long long before, total;
-    count_units<TT>(a, b, before, total, s_scan);
-    const int tiles = tiles_of<TT>(length_of(a, b));
+    const int4 seg = a.begun[blockIdx.x];                     // sequence, key head, tile of rows, parts
+    const int b = seg.x, h = seg.y, rt = seg.z, parts = seg.w;
+    const int col = blockIdx.y * cols + warp / split, row = rt * NC + col, first = warp % split;
+    if (parts == 0) return;                                   // (the whole block)
+    const bool some = col < NC && row < a.rows;
+    // part 0 is the share's second place, the others are the first places of the shares behind it
+    const float* p0 = a.parts + ((long long)blockIdx.x * 2 + 1) * SIZE;
+    auto part_of = [&](int i) { return i == 0 ? p0 : p0 + (long long)(2 * i - 1) * SIZE; };
+    float low = kNone, sum = 0.0f, x[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = 0.0f;
+    if (some) {
+        for (int i0 = first; i0 < parts; i0 += 4 * split) {   // four parts on their way
+            float off[4], s[4], v[4][W];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = i0 + k * split;
+                off[k] = kNone;
+                s[k] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < W; ++e) v[k][e] = 0.0f;
+                if (i < parts) {
+                    const float* p = part_of(i);
+                    off[k] = p[col];
+                    s[k] = p[NC + col];
+#pragma unroll
+                    for (int e = 0; e < W / 2; ++e) {
+                        const float2 two = *reinterpret_cast<const float2*>(p + 2 * NC + col * D + lane * W + 2 * e);
+                        v[k][2 * e] = two.x;
+                        v[k][2 * e + 1] = two.y;
+                    }
+                }
+            }
+            const float to = fminf(fminf(fminf(off[0], off[1]), fminf(off[2], off[3])), low), by = exp2_approx(to - low);
+            low = to;
+            sum *= by;
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[e] *= by;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float w = exp2_approx(to - off[k]);
+                sum = fmaf(s[k], w, sum);
+#pragma unroll
+                for (int e = 0; e < W; ++e) x[e] = fmaf(v[k][e], w, x[e]);
+            }
+        }
+    }
+    if (split > 1) {
+        if (lane == 0) {
+            s_low[warp] = low;
+            s_sum[warp] = sum;
+        }
+#pragma unroll
+        for (int e = 0; e < W; ++e) s_x[warp][lane * W + e] = x[e];
+        __syncthreads();
+        if (first != 0) return;
+        for (int w = warp + 1; w < warp + split; ++w) {
+            const float to = fminf(low, s_low[w]), mine = exp2_approx(to - low), other = exp2_approx(to - s_low[w]);
+            low = to;
+            sum = fmaf(s_sum[w], other, sum * mine);
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[e] = fmaf(s_x[w][lane * W + e], other, x[e] * mine);
+        }
+    }
+    if (!some) return;
+    const float r = sum == 0.0f ? 0.0f : (a.c.vf == nullptr ? 1.0f : __ldg(a.c.vf + h)) / sum;
     const int tok = row / a.group, head = h * a.group + (row - tok * a.group);
-    uint8_t* out = a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D + d);
-    if (tiles == 0) {
-        *reinterpret_cast<uint16_t*>(out) = 0;
-        return;
-    }
-    const long long share = share_of(total, ctas);
-    const long long first = before + (long long)(h * a.row_tiles + rt) * tiles, last = first + tiles - 1;
-    const int c0 = (int)(first / share), c1 = (int)(last / share);
-    if (c0 == c1) return;
-    constexpr int SIZE = NC * (D + 2);
-    auto part_of = [&](int c) { return a.parts + ((long long)c * 2 + (c == c0 ? 1 : 0)) * SIZE; };
-    float low = kNone;
-    for (int c = c0; c <= c1; ++c) low = fminf(low, part_of(c)[col]);
-    float sum = 0.0f, x = 0.0f;
-    for (int c = c0; c <= c1; ++c) {
-        const float* p = part_of(c);
-        const float by = exp2_approx(low - p[col]);
-        sum = fmaf(p[NC + col], by, sum);
-        x = fmaf(p[2 * NC + col * D + d], by, x);
-    }
-    x *= sum == 0.0f ? 0.0f : (a.c.vf == nullptr ? 1.0f : __ldg(a.c.vf + h)) / sum;
-    const uint32_t v = a.type == ELUTQ_TYPE_F16 ? pack<false>(x, 0.0f) : pack<true>(x, 0.0f);
-    *reinterpret_cast<uint16_t*>(out) = (uint16_t)v;
+    uint32_t* out = reinterpret_cast<uint32_t*>(a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D)) + lane * (W / 2);
+#pragma unroll
+    for (int e = 0; e < W / 2; ++e) out[e] = a.type == ELUTQ_TYPE_F16 ? pack<false>(x[2 * e] * r, x[2 * e + 1] * r) : pack<true>(x[2 * e] * r, x[2 * e + 1] * r);
 }
 
-// CTAs of a launch: as many as are resident at once
-inline int ctas_of(int nt) { return device_sm_count() * (nt == 1 ? 3 : 2); }
+// CTAs of a launch: as many as are resident at once.  (The workspace is as large as any format wants it.)
+inline int ctas_of(int per_sm) { return device_sm_count() * per_sm; }
 inline int columns_of(int rows) { return rows <= 8 ? 1 : 2; }
 
-int launch_one(const void* kernel, int grid, int block, void** args, cudaStream_t stream) {
+int launch_one(const void* kernel, dim3 grid, int block, int smem, void** args, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.dynamicSmemBytes = smem;
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)block);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -638,11 +720,28 @@ int launch_one(const void* kernel, int grid, int block, void** args, cudaStream_
 
 template <int D, int FMT, bool BF16, int NT>
 int launch_decode(DecodeArgs a, cudaStream_t stream) {
-    int ctas = ctas_of(NT);
-    void* args[] = {&a, &ctas};
-    const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, ctas, kThreads, args, stream);
+    constexpr int kRings = kWarps * stages_of(FMT, D) * stage_bytes(FMT, D), kParts = kWarps * 8 * NT * (D + 4) * 4, kSmem = kRings > kParts ? kRings : kParts;
+    // once for each device (a call would take half a microsecond of the host's time)
+    static std::atomic<unsigned long long> ready{0};
+    int dev = 0;
+    cudaError_t ce = cudaGetDevice(&dev);
+    if (ce != cudaSuccess) return (int)ce;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(ready.load(std::memory_order_acquire) & bit)) {
+        ce = cudaFuncSetAttribute(attn_decode_kernel<D, FMT, BF16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (ce != cudaSuccess) return (int)ce;
+        ready.fetch_or(bit, std::memory_order_release);
+    }
+    int ctas = ctas_of(resident(FMT, D, NT));
+    void* args[] = {&a};
+    const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3(ctas), kThreads, kSmem, args, stream);
     if (e != 0) return e;
-    return launch_one((const void*)attn_join_kernel<D, tile_tokens(FMT, D), NT>, a.B * a.c.heads * a.rows, D, args, stream);
+    // few segments have many parts each: more warps to a row
+    const long long parts = ctas / ((long long)a.B * a.c.heads * a.row_tiles);
+    int split = parts >= 32 ? 8 : parts >= 8 ? 4 : parts >= 4 ? 2 : 1;
+    void* join[] = {&a, &split};
+    const int cols = 8 / split, wide = a.rows < 8 * NT ? a.rows : 8 * NT;
+    return launch_one((const void*)attn_join_kernel<D, NT>, dim3(ctas, (wide + cols - 1) / cols), 256, 0, join, stream);
 }
 template <int D, int FMT, bool BF16>
 int launch_decode(const DecodeArgs& a, cudaStream_t stream) {
@@ -665,7 +764,7 @@ extern "C" int elutq_attn_decode_workspace_bytes(int n_q_heads, int heads, int h
     if (head_dim != 64 && head_dim != 128) return ELUTQ_ERR_UNSUPPORTED;
     if (n_q_heads % heads != 0 || (long long)n_q_heads / heads * new_tokens > 0xffff) return ELUTQ_ERR_SHAPE;
     const int nt = columns_of(n_q_heads / heads * new_tokens);
-    *bytes = (size_t)ctas_of(nt) * 2 * (8 * nt) * (head_dim + 2) * sizeof(float);
+    *bytes = (size_t)ctas_of(4) * (2 * (8 * nt) * (head_dim + 2) * sizeof(float) + sizeof(int4));
     return ELUTQ_OK;
 }
 
@@ -698,10 +797,10 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     a.row_tiles = (a.rows + nc - 1) / nc;
     a.type = cache->type;
     a.scale = scale * 1.44269504088896340736f;
-    a.parts = (float*)workspace;
+    a.begun = (int4*)workspace;
+    a.parts = (float*)(a.begun + ctas_of(4));
     a.cap = (long long)pages * cache->page_size;
     if (a.cap > 0x7fff0000LL) a.cap = 0x7fff0000LL;               // (token numbers a little behind the last one are formed)
-    if ((long long)B * n_q_heads * new_tokens > 0x7fffffffLL) return ELUTQ_ERR_SHAPE;      // (blocks of a launch)
     const int ce = D == 128 ? launch_decode<128>(a, cache->format, (cudaStream_t)stream) : launch_decode<64>(a, cache->format, (cudaStream_t)stream);
     if (ce == 0) return ELUTQ_OK;
     note_cuda_error(ce);
