@@ -9,9 +9,10 @@
 //            (movmatrix) and of pairs of V rows (byte permutes, on the codes).
 // loads      Every warp has a ring of stages of its own in shared memory, filled by asynchronous copies of 16 bytes to a lane, so a warp never waits for another within a
 //            segment.  Pieces are placed so that the fragments' reads meet no bank twice.  Rows behind a sequence and on pages that do not exist come as zeros.
-// split      All (sequence, key head, rows) segments laid behind one another, in tiles, are cut into equal shares, one for each CTA that the GPU holds: lengths may
-//            be as ragged as they like.  The warps of a CTA take the tiles of a segment in turn and join through shared memory; a segment that lies within one share
-//            is finished there, the parts of others go to the workspace and a second kernel joins them in their order.
+// split      All (sequence, key head, rows) segments laid behind one another, in tiles, are cut into equal shares, one for each warp that the GPU holds: lengths may
+//            be as ragged as they like.  A segment counts kLead tiles more, for what it costs to begin one.  A segment that lies within one share is finished there, the
+//            parts of others go to the workspace and a second kernel joins them in their order.  Where all shares of a CTA are of one segment they are joined
+//            in shared memory first.
 // softmax    One running maximum for all lanes of a column, moved only when a tile rises more than 2^10 above it (then everything is scaled): P stays below
 //            2^14, in 16 bits whatever the type.  Maximum, sum and result are fp32.
 // codes      E4M3 and E2M1 values, also times an E4M3 block scale, are exact in fp16, so both products are fp16 ones, with q brought to fp16 by a power of two for each row.
@@ -30,6 +31,7 @@ namespace elutq {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kLead = 4;
 constexpr float kNone = 1e30f;               // offset of a column that has seen no token: any score rises above it
 constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
 
@@ -46,7 +48,9 @@ struct DecodeArgs {
     int type;
     float scale;               // times log2(e)
     float* parts;
-    int4* begun;               // of each share, the segment that begins in it and goes on in the next ones: sequence, key head, tile of rows, parts (0: none)
+    int4* begun;               // segments that begin in a share and go on in the next ones: sequence, key head and tile of rows, worker, where its parts are (0: none).  For each
+                               // segment, or, where there are more of them than shares, for each share
+    int by_segment;
     long long cap;             // wide * page_size: tokens that the table has room for
 };
 
@@ -56,7 +60,7 @@ __host__ __device__ constexpr int tile_tokens(int format, int D) { return row_by
 __host__ __device__ constexpr int stage_bytes(int format, int D) { return tile_tokens(format, D) * 2 * (row_bytes(format, D) + (format == ELUTQ_KV_NVFP4 ? D / 16 : 0)); }
 __host__ __device__ constexpr int stages_of(int format, int D) { return stage_bytes(format, D) > 4608 ? 2 : 13824 / stage_bytes(format, D); }
 // CTAs that an SM holds: by shared memory, and by the registers that the results take
-__host__ __device__ constexpr int resident(int format, int D, int nt) { return format == ELUTQ_KV_NVFP4 ? 3 - (nt == 2 && D == 128) : nt == 2 && D == 128 ? 2 : stage_bytes(format, D) > 4608 ? 3 : nt == 2 ? 3 : 4; }
+__host__ __device__ constexpr int resident(int format, int D, int nt) { return nt == 2 && D == 128 ? 2 : 3; }
 
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
     const long long n = __ldg(a.lens + b);
@@ -131,21 +135,22 @@ __device__ __forceinline__ uint32_t read_shared_u16(uint32_t addr) {
 template <int TT>
 __device__ __forceinline__ int tiles_of(int len) { return (len + TT - 1) / TT; }
 
-// Units (tiles of segments) of all sequences, by a warp.
+// Units of a segment: its tiles and kLead more; none without a token
+template <int TT>
+__device__ __forceinline__ int units_of(int len) { return len == 0 ? 0 : tiles_of<TT>(len) + kLead; }
+// Units of all sequences, by a warp.
 template <int TT>
 __device__ __forceinline__ long long count_units(const DecodeArgs& a) {
     long long total = 0;
-    for (int b = threadIdx.x & 31; b < a.B; b += 32) total += tiles_of<TT>(length_of(a, b));
+    for (int b = threadIdx.x & 31; b < a.B; b += 32) total += units_of<TT>(length_of(a, b));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     return total * a.c.heads * a.row_tiles;
 }
-// Units of a share: all CTAs take the same, at least one tile for each warp.
-__device__ __forceinline__ long long share_of(long long total, int ctas) {
-    const long long n = (total + ctas - 1) / ctas;
-    return n < kWarps ? kWarps : n;
+// a / b, a below 2^63: mostly a 32-bit division, a tenth of a 64-bit one's instructions
+__device__ __forceinline__ long long quotient_of(long long a, int b) {
+    return a >> 32 == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-
 template <int D, int FMT, bool BF16, int NT>
 __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_kernel(const DecodeArgs a) {
     constexpr int TT = tile_tokens(FMT, D), SUB = TT / 16, NC = 8 * NT, S = stages_of(FMT, D), STAGE = stage_bytes(FMT, D);
@@ -167,45 +172,50 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // ---- this CTA's share -----------------------------------------------------------------------------------------------------------------------
-    const int each = a.c.heads * a.row_tiles;
-    long long before = 0, f0, f1;
-    int b = 0;
-    {
-        const long long total = count_units<TT>(a);
-        const long long share = share_of(total, gridDim.x);
-        f0 = blockIdx.x * share;
-        f1 = f0 + share < total ? f0 + share : total;
-        // sequences without a token: zeros
-        for (int e = blockIdx.x; e < a.B; e += gridDim.x)
-            if (length_of(a, e) == 0)
-                for (long long i = tid; i < (long long)a.fresh * a.c.heads * a.group * (D / 8); i += kThreads) {
-                    const long long tok = i / (a.c.heads * a.group * (D / 8));
-                    reinterpret_cast<uint4*>(a.out + 2 * ((long long)e * a.fresh + tok) * a.ldo)[i - tok * (a.c.heads * a.group * (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
-                }
-        if (f0 >= f1) {                                       // (the whole CTA)
-            if (tid == 0) a.begun[blockIdx.x] = make_int4(0, 0, 0, 0);
-            return;
-        }
-        // the sequence that the first unit belongs to: 32 at a time
-        for (;; b += 32) {
-            const long long mine = b + lane < a.B ? (long long)tiles_of<TT>(length_of(a, b + lane)) * each : 0;
-            long long incl = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += v;
+    // ---- this warp's share: units [f0, f1) of [0, total) ----------------------------------------------------------------------------------------
+    const int each = a.c.heads * a.row_tiles, worker = blockIdx.x * kWarps + warp;
+    const long long total = count_units<TT>(a), share = quotient_of(total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
+    const long long cta0 = blockIdx.x * kWarps * share, cta1 = cta0 + kWarps * share < total ? cta0 + kWarps * share : total;
+    // sequences without a token: zeros
+    for (int e = blockIdx.x; e < a.B; e += gridDim.x)
+        if (length_of(a, e) == 0) {
+            if (a.by_segment)
+                for (int i = tid; i < each; i += kThreads) a.begun[e * each + i] = make_int4(0, 0, 0, 0);
+            for (long long i = tid; i < (long long)a.fresh * a.c.heads * a.group * (D / 8); i += kThreads) {
+                const long long tok = i / (a.c.heads * a.group * (D / 8));
+                reinterpret_cast<uint4*>(a.out + 2 * ((long long)e * a.fresh + tok) * a.ldo)[i - tok * (a.c.heads * a.group * (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
             }
-            const uint32_t behind = __ballot_sync(0xffffffffu, before + incl > f0);
-            if (behind != 0) {
-                const int l = __ffs(behind) - 1;
-                before += __shfl_sync(0xffffffffu, incl - mine, l);
-                b += l;
-                break;
-            }
-            before += __shfl_sync(0xffffffffu, incl, 31);
         }
+    if (cta0 >= cta1) {                                       // (the whole CTA)
+        if (lane == 0 && !a.by_segment) a.begun[worker] = make_int4(0, 0, 0, 0);
+        return;
     }
+    // the sequence that the CTA's first unit belongs to: 32 at a time
+    int b = 0;
+    long long before = 0;                                     // units in front of the sequence
+    for (;; b += 32) {
+        const long long mine = b + lane < a.B ? (long long)units_of<TT>(length_of(a, b + lane)) * each : 0;
+        long long incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        const uint32_t behind = __ballot_sync(0xffffffffu, before + incl > cta0);
+        if (behind != 0) {
+            const int l = __ffs(behind) - 1;
+            before += __shfl_sync(0xffffffffu, incl - mine, l);
+            b += l;
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    bool joint;                                               // all of the CTA's units are of one segment
+    {
+        const int units = units_of<TT>(length_of(a, b));
+        joint = cta1 <= before + (quotient_of(cta0 - before, units) + 1) * units;
+    }
+    const long long f0 = cta0 + warp * share, f1 = f0 + share < cta1 ? f0 + share : cta1;
 
     // where a lane copies to and reads from.  A piece's place in its row is its number with some bits of the row's number turned: the eight lanes that are served together
     // read two K rows, or four V rows, of which every second.
@@ -213,63 +223,75 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
     auto v_turn = [](int r) { return PIECES >= 8 ? (r >> 1 & 3) << 1 : PIECES == 4 ? r >> 1 & 3 : 0; };
     constexpr int ROWS = 32 / PIECES;                         // rows of a copy of the warp
     const int cr = lane / PIECES, cc = lane % PIECES;
+    // (in the 512 bytes of one; after TURNS of them the rows' turns are the first one's again)
+    constexpr int TURNS = PIECES == 16 ? 4 : PIECES == 8 ? 2 : 1;
+    const uint32_t k_to = cr * ROW + 16 * (cc ^ k_turn(cr));
+    uint32_t v_to[TURNS];
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) v_to[i] = cr * ROW + 16 * (cc ^ v_turn(i * ROWS + cr));
     const uint32_t k_read = ring + g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
     const uint32_t v_read = ring + V0 + 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g);
 
     bool recorded = false;
-    for (long long f = f0; f < f1;) {
-        const int len = length_of(a, b), tiles = tiles_of<TT>(len);
-        if (tiles == 0) { ++b; continue; }
-        const long long local = f - before;
-        const int seg = (int)(local / tiles), tile0 = (int)(local - (long long)seg * tiles);
+    // (joint: every warp once, with or without tiles)
+    for (long long f = f0; f < f1 || joint;) {
+        const int len = length_of(a, b), tiles = tiles_of<TT>(len), units = units_of<TT>(len);
+        if (!joint && f - before >= (long long)units * each) {
+            before += (long long)units * each;
+            ++b;
+            continue;
+        }
+        const long long at_most = f1 - f, local = (f < cta1 ? f : cta1 - 1) - before;
+        const int seg = (int)quotient_of(local, units);
+        const long long seg0 = before + (long long)seg * units;             // the segment's first unit
+        const int unit0 = (int)(local - (long long)seg * units), unit1 = (int)(at_most < units - unit0 ? (at_most < 0 ? unit0 : unit0 + at_most) : units);
+        const int tile0 = max(0, unit0 - kLead), mine = max(0, unit1 - kLead) - tile0;      // this warp's tiles
         const int h = seg / a.row_tiles, rt = seg - h * a.row_tiles;
-        const int count = (int)(f1 - f < tiles - tile0 ? f1 - f : tiles - tile0);
+        if (!joint && mine == 0) {
+            f += unit1 - unit0;
+            continue;
+        }
         const int* pages = a.table + b * a.ld_table;
         const int least = len - a.fresh + 1;                  // tokens that the first of the new tokens sees
-        const int mine = warp < count ? (count - warp + kWarps - 1) / kWarps : 0;        // this warp's tiles: tile0 + warp + n kWarps
 
         // ---- copies ----------------------------------------------------------------------------------------------------------------------------
         uint32_t there = 0;                                   // a bit for each 16 tokens of the stages: their page exists
-        int ids = -1;                                         // lane i: page of the i-th of 32 16-token pieces of this warp's tiles
+        long long first_row = -1;                             // lane i: first row of the cache of the i-th of 32 pieces of 16 tokens of this warp's tiles; below 0: no page
         auto copy = [&](int n, int slot) {
             if (((n * SUB) & 31) == 0) {
-                const int tok = (tile0 + warp + (n + lane / SUB) * kWarps) * TT + (lane % SUB) * 16;
-                ids = -1;
-                if (n + lane / SUB < mine && tok < len) ids = __ldg(pages + a.c.page.of(tok));
-                if (ids >= a.c.n_pages) ids = -1;
+                const int tok = (tile0 + n + lane / SUB) * TT + (lane % SUB) * 16;
+                first_row = -1;
+                if (n + lane / SUB < mine && tok < len) {
+                    const int number = a.c.page.of(tok), page = __ldg(pages + number);
+                    if (page >= 0 && page < a.c.n_pages) first_row = ((long long)page * a.c.heads + h) * a.c.page_size + (tok - number * a.c.page_size);
+                }
             }
-            const int tok0 = (tile0 + warp + n * kWarps) * TT;
+            const int left = len - (tile0 + n) * TT;        // tokens from the stage's first on
             const uint32_t at = ring + slot * STAGE;
-            [[maybe_unused]] long long rows[SUB];
-            there &= ~(((1u << SUB) - 1u) << (slot * SUB));
+            uint32_t have = 0;
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
-                const int tok = tok0 + 16 * s, id = __shfl_sync(0xffffffffu, ids, (n * SUB + s) & 31);
-                there |= (uint32_t)(id >= 0) << (slot * SUB + s);
-                const long long row = ((long long)max(id, 0) * a.c.heads + h) * a.c.page_size + (tok - a.c.page.of(tok) * a.c.page_size);
-                rows[s] = row;
-                const int some = id >= 0 ? min(len - tok, 16) : 0;
-                const uint8_t *ksrc = a.c.k + row * ROW + lane * 16, *vsrc = a.c.v + row * ROW + lane * 16;
+                const long long row = __shfl_sync(0xffffffffu, first_row, (n * SUB + s) & 31);
+                const long long from = (row < 0 ? 0 : row) * ROW + lane * 16;
+                have |= (uint32_t)(row >= 0) << s;
+                const uint8_t *ksrc = a.c.k + from, *vsrc = a.c.v + from;
+                const int some = row < 0 ? 0 : left - 16 * s;
 #pragma unroll
                 for (int i = 0; i < 16 / ROWS; ++i) {
                     const int r = i * ROWS + cr;
-                    copy16(at + (16 * s + r) * ROW + 16 * (cc ^ k_turn(r)), ksrc + i * 512, r < some);
-                    copy16(at + V0 + (16 * s + r) * ROW + 16 * (cc ^ v_turn(r)), vsrc + i * 512, r < some);
+                    const uint32_t to = at + 16 * s * ROW + i * 512;
+                    copy16(to + k_to, ksrc + i * 512, r < some);
+                    copy16(to + V0 + v_to[i % TURNS], vsrc + i * 512, r < some);
                 }
             }
+            there = (there & ~(((1u << SUB) - 1u) << (slot * SUB))) | have << (slot * SUB);
             if constexpr (SCALED) {
-                // 16 tokens' scales are 128 or 64 bytes; a lane takes the same 16 of K and of V
-                constexpr int LANES = D / 16;             // of 16 tokens
-                if (lane < SUB * LANES) {
-                    const int s = lane / LANES, part = lane % LANES;
-                    long long row = rows[0];
-#pragma unroll
-                    for (int i = 1; i < SUB; ++i) row = s == i ? rows[i] : row;
-                    const bool ok = there >> (slot * SUB + s) & 1u;
-                    // (rows behind the sequence too: within the page, finite or not, they meet codes of zero; a NaN is taken out where they are used)
-                    copy16(at + KS0 + lane * 16, a.c.ks + row * (D / 16) + part * 16, ok);
-                    copy16(at + VS0 + lane * 16, a.c.vs + row * (D / 16) + part * 16, ok);
-                }
+                // 16 tokens' scales are D bytes, D / 16 lanes'; half of the lanes copy K's and half V's.  (Rows behind the sequence too: within the page, they meet codes of zero; a
+                // NaN among them is taken out where they are used.)
+                constexpr int LANES = D / 16;
+                const int l = lane & 15, s = l / LANES;
+                const long long row = __shfl_sync(0xffffffffu, first_row, (n * SUB + (s < SUB ? s : 0)) & 31);
+                if (s < SUB) copy16(at + (lane < 16 ? KS0 : VS0) + l * 16, (lane < 16 ? a.c.ks : a.c.vs) + (row < 0 ? 0 : row) * (D / 16) + l % LANES * 16, row >= 0);
             }
         };
         auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
@@ -338,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                 for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.0f;
 
         for (int n = 0, slot = 0; n < mine; ++n) {
-            const int tok0 = (tile0 + warp + n * kWarps) * TT;
+            const int tok0 = (tile0 + n) * TT;
             const uint32_t at = slot * STAGE;
             asm volatile("cp.async.wait_group %0;" :: "n"(S - 1) : "memory");
             __syncwarp();
@@ -548,76 +570,123 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             slot = slot + 1 == S ? 0 : slot + 1;
         }
 
-        // ---- the warps' parts meet ----------------------------------------------------------------------------------------------------------------
-        const int active = min(kWarps, count);
-        __syncthreads();
-        if (mine > 0) {
+        // ---- the end of a segment, or of the share ------------------------------------------------------------------------------------------------------
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], d);
+        // dimension of word m of this lane's pieces of V rows
+        auto dim_of = [&](int m) {
+            constexpr int PIECE = VC * PER_WORD;
+            return PIECE * (g + 8 * (2 * m / PIECE)) + 2 * m % PIECE;
+        };
+        auto part_of = [&](int w, int place) { return a.parts + ((long long)w * 2 + place) * (NC * (D + 2)); };
+        // The segment begins in worker w's share and ends in another's.  Its other parts: of `near` workers behind w in this CTA, one of each of `whole` CTAs that have units of no
+        // other segment, and of the first `last` workers of the CTA behind those.
+        auto record = [&](int w) {
+            const int end = (int)quotient_of(seg0 + units - 1, share), cta = end / kWarps;
+            const long long stop = (long long)(cta + 1) * kWarps * share;
+            const bool all = (stop < total ? stop : total) <= seg0 + units;        // the last CTA has units of no other segment
+            const int near = joint ? 0 : min(end, blockIdx.x * kWarps + kWarps - 1) - w;
+            const int whole = cta > blockIdx.x ? cta - blockIdx.x - (all ? 0 : 1) : 0, last = cta > blockIdx.x && !all ? end - cta * kWarps + 1 : 0;
+            a.begun[a.by_segment ? b * each + seg : w] = make_int4(b, seg, w, 1 + (near << 1) + (last << 3) + (whole << 6));
+        };
+        const float vf = a.c.vf == nullptr ? 1.0f : __ldg(a.c.vf + h);
+        if (!joint) {
+            const bool begins = tile0 == 0, whole = begins && mine == tiles;
+            float* part = part_of(worker, begins ? 1 : 0);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    const int col = nt * 8 + 2 * t + j, rr = rt * NC + col;
+                    if (rr >= a.rows) continue;
+                    if (whole) {
+                        const float r = sum[nt][j] == 0.0f ? 0.0f : vf / sum[nt][j];
+                        const int tok = rr / a.group, head = h * a.group + (rr - tok * a.group);
+                        uint8_t* p = a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D);
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], d);
-                    const int col = nt * 8 + 2 * t + j;
-                    if (g == 0) {
-                        s_off[warp][col] = off[nt][j];
-                        s_sum[warp][col] = sum[nt][j];
-                    }
+                        for (int m = 0; m < STEPS; ++m) {
+                            const float x = o[m][nt][j] * r, y = o[m][nt][j + 2] * r;
+                            *reinterpret_cast<uint32_t*>(p + 2 * dim_of(m)) = a.type == ELUTQ_TYPE_F16 ? pack<false>(x, y) : pack<true>(x, y);
+                        }
+                    } else {
+                        if (g == 0) {
+                            part[col] = off[nt][j];
+                            part[NC + col] = sum[nt][j];
+                        }
 #pragma unroll
-                    for (int m = 0; m < STEPS; ++m) {
-                        // dimension of word m of this lane's pieces of V rows
-                        constexpr int PIECE = VC * PER_WORD;
-                        const int d = PIECE * (g + 8 * (2 * m / PIECE)) + 2 * m % PIECE;
-                        *reinterpret_cast<float2*>(&s_o[warp][col][d]) = make_float2(o[m][nt][j], o[m][nt][j + 2]);
+                        for (int m = 0; m < STEPS; ++m) *reinterpret_cast<float2*>(part + 2 * NC + col * D + dim_of(m)) = make_float2(o[m][nt][j], o[m][nt][j + 2]);
                     }
                 }
+            if (begins && !whole) {
+                if (lane == 0) record(worker);
+                recorded = true;
+            }
+            if (whole && a.by_segment && lane == 0) a.begun[b * each + seg] = make_int4(0, 0, 0, 0);
+            f += unit1 - unit0;
+            continue;
         }
         __syncthreads();
-        const bool begins = tile0 == 0, whole = begins && count == tiles;
-        const int used = min(NC, a.rows - rt * NC);
-        const float vf = a.c.vf == nullptr ? 1.0f : __ldg(a.c.vf + h);
-        float* part = a.parts + ((long long)blockIdx.x * 2 + (begins ? 1 : 0)) * (NC * (D + 2));
-        for (int i = tid; i < used * (D / 2); i += kThreads) {
-            const int col = i / (D / 2), d = 2 * (i - col * (D / 2));
-            float low = kNone;
-            for (int w = 0; w < active; ++w) low = fminf(low, s_off[w][col]);
-            float total = 0.0f, x = 0.0f, y = 0.0f;
-            for (int w = 0; w < active; ++w) {
-                const float by = exp2_approx(low - s_off[w][col]);
-                const float2 v = *reinterpret_cast<const float2*>(&s_o[w][col][d]);
-                total = fmaf(s_sum[w][col], by, total);
-                x = fmaf(v.x, by, x);
-                y = fmaf(v.y, by, y);
-            }
-            if (whole) {
-                const float r = total == 0.0f ? 0.0f : vf / total;
-                const int rr = rt * NC + col, tok = rr / a.group, head = h * a.group + (rr - tok * a.group);
-                uint8_t* p = a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D + d);
-                *reinterpret_cast<uint32_t*>(p) = a.type == ELUTQ_TYPE_F16 ? pack<false>(x * r, y * r) : pack<true>(x * r, y * r);
-            } else {
-                if (d == 0) {
-                    part[col] = low;
-                    part[NC + col] = total;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int col = nt * 8 + 2 * t + j;
+                if (g == 0) {
+                    s_off[warp][col] = off[nt][j];
+                    s_sum[warp][col] = sum[nt][j];
                 }
-                *reinterpret_cast<float2*>(part + 2 * NC + col * D + d) = make_float2(x, y);
+#pragma unroll
+                for (int m = 0; m < STEPS; ++m) *reinterpret_cast<float2*>(&s_o[warp][col][dim_of(m)]) = make_float2(o[m][nt][j], o[m][nt][j + 2]);
             }
-        }
-        if (begins && !whole && tid == 0) {
-            const long long share = f1 - f0;                  // (a share that another one follows is a whole one)
-            a.begun[blockIdx.x] = make_int4(b, h, rt, (int)(1 + (tiles - count + share - 1) / share));
-            recorded = true;
-        }
         __syncthreads();
-        f += count;
-        if (f - before == (long long)tiles * each) {
-            before = f;
-            ++b;
+        const bool begins = cta0 <= seg0 + kLead, whole = begins && cta1 >= seg0 + units;
+        if (cta1 > seg0 + kLead) {                            // (there are tiles)
+            const int first = begins ? (int)quotient_of(seg0 + kLead, share) : blockIdx.x * kWarps;      // the worker whose part it is
+            const int used = min(NC, a.rows - rt * NC);
+            float* part = part_of(first, begins ? 1 : 0);
+            for (int i = tid; i < used * (D / 2); i += kThreads) {
+                const int col = i / (D / 2), d = 2 * (i - col * (D / 2));
+                float low = kNone;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) low = fminf(low, s_off[w][col]);
+                float all = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float by = exp2_approx(low - s_off[w][col]);
+                    const float2 v = *reinterpret_cast<const float2*>(&s_o[w][col][d]);
+                    all = fmaf(s_sum[w][col], by, all);
+                    x = fmaf(v.x, by, x);
+                    y = fmaf(v.y, by, y);
+                }
+                if (whole) {
+                    const float r = all == 0.0f ? 0.0f : vf / all;
+                    const int rr = rt * NC + col, tok = rr / a.group, head = h * a.group + (rr - tok * a.group);
+                    uint8_t* p = a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D + d);
+                    *reinterpret_cast<uint32_t*>(p) = a.type == ELUTQ_TYPE_F16 ? pack<false>(x * r, y * r) : pack<true>(x * r, y * r);
+                } else {
+                    if (d == 0) {
+                        part[col] = low;
+                        part[NC + col] = all;
+                    }
+                    *reinterpret_cast<float2*>(part + 2 * NC + col * D + d) = make_float2(x, y);
+                }
+            }
+            if (begins && !whole && worker == first) {
+                if (lane == 0) record(worker);
+                recorded = true;
+            }
+            if (whole && a.by_segment && tid == 0) a.begun[b * each + seg] = make_int4(0, 0, 0, 0);
         }
+        break;
     }
-    if (tid == 0 && !recorded) a.begun[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (lane == 0 && !recorded && !a.by_segment) a.begun[worker] = make_int4(0, 0, 0, 0);
 }
 
-// Joins the parts of the segments that several shares hold, in their order.  A block for each share in which such a segment begins, and for `cols` of its query rows: a warp to a
+// Joins the parts of the segments that several shares hold, in their order.  A block for each segment, or for each share in which one may begin, and for `cols` query rows: a warp to a
 // row and to every `split`-th part, a lane to D / 32 dimensions; `split` warps join through shared memory.
 template <int D, int NT>
 __global__ void __launch_bounds__(256) attn_join_kernel(const DecodeArgs a, int split) {
@@ -626,14 +695,16 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const DecodeArgs a, int 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cols = 8 / split;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int4 seg = a.begun[blockIdx.x];                     // sequence, key head, tile of rows, parts
-    const int b = seg.x, h = seg.y, rt = seg.z, parts = seg.w;
+    const int4 seg = a.begun[blockIdx.x];                     // sequence, key head and tile of rows, worker, where its parts are
+    const int b = seg.x, h = seg.y / a.row_tiles, rt = seg.y - h * a.row_tiles, worker = seg.z, near = seg.w >> 1 & 3, whole = seg.w >> 6, parts = seg.w == 0 ? 0 : 1 + near + whole + (seg.w >> 3 & 7);
     const int col = blockIdx.y * cols + warp / split, row = rt * NC + col, first = warp % split;
     if (parts == 0) return;                                   // (the whole block)
     const bool some = col < NC && row < a.rows;
-    // part 0 is the share's second place, the others are the first places of the shares behind it
-    const float* p0 = a.parts + ((long long)blockIdx.x * 2 + 1) * SIZE;
-    auto part_of = [&](int i) { return i == 0 ? p0 : p0 + (long long)(2 * i - 1) * SIZE; };
+    // part 0 is the share's second place, the others are first places
+    auto part_of = [&](int i) {
+        const int cta = worker / kWarps, w = i <= near ? worker + i : i <= near + whole ? (cta + i - near) * kWarps : (cta + whole + 1) * kWarps + (i - near - whole - 1);
+        return a.parts + ((long long)w * 2 + (i == 0 ? 1 : 0)) * SIZE;
+    };
     float low = kNone, sum = 0.0f, x[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) x[i] = 0.0f;
@@ -732,16 +803,18 @@ int launch_decode(DecodeArgs a, cudaStream_t stream) {
         if (ce != cudaSuccess) return (int)ce;
         ready.fetch_or(bit, std::memory_order_release);
     }
-    int ctas = ctas_of(resident(FMT, D, NT));
+    const int ctas = ctas_of(resident(FMT, D, NT));
+    const long long segments = (long long)a.B * a.c.heads * a.row_tiles;
+    a.by_segment = segments <= ctas * kWarps;
     void* args[] = {&a};
     const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3(ctas), kThreads, kSmem, args, stream);
     if (e != 0) return e;
     // few segments have many parts each: more warps to a row
-    const long long parts = ctas / ((long long)a.B * a.c.heads * a.row_tiles);
+    const long long parts = ctas / segments;
     int split = parts >= 32 ? 8 : parts >= 8 ? 4 : parts >= 4 ? 2 : 1;
     void* join[] = {&a, &split};
     const int cols = 8 / split, wide = a.rows < 8 * NT ? a.rows : 8 * NT;
-    return launch_one((const void*)attn_join_kernel<D, NT>, dim3(ctas, (wide + cols - 1) / cols), 256, 0, join, stream);
+    return launch_one((const void*)attn_join_kernel<D, NT>, dim3(a.by_segment ? (unsigned)segments : ctas * kWarps, (wide + cols - 1) / cols), 256, 0, join, stream);
 }
 template <int D, int FMT, bool BF16>
 int launch_decode(const DecodeArgs& a, cudaStream_t stream) {
@@ -764,7 +837,7 @@ extern "C" int elutq_attn_decode_workspace_bytes(int n_q_heads, int heads, int h
     if (head_dim != 64 && head_dim != 128) return ELUTQ_ERR_UNSUPPORTED;
     if (n_q_heads % heads != 0 || (long long)n_q_heads / heads * new_tokens > 0xffff) return ELUTQ_ERR_SHAPE;
     const int nt = columns_of(n_q_heads / heads * new_tokens);
-    *bytes = (size_t)ctas_of(4) * (2 * (8 * nt) * (head_dim + 2) * sizeof(float) + sizeof(int4));
+    *bytes = (size_t)ctas_of(4) * kWarps * (2 * (8 * nt) * (head_dim + 2) * sizeof(float) + sizeof(int4));
     return ELUTQ_OK;
 }
 
@@ -798,7 +871,7 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     a.type = cache->type;
     a.scale = scale * 1.44269504088896340736f;
     a.begun = (int4*)workspace;
-    a.parts = (float*)(a.begun + ctas_of(4));
+    a.parts = (float*)(a.begun + ctas_of(4) * kWarps);
     a.cap = (long long)pages * cache->page_size;
     if (a.cap > 0x7fff0000LL) a.cap = 0x7fff0000LL;               // (token numbers a little behind the last one are formed)
     const int ce = D == 128 ? launch_decode<128>(a, cache->format, (cudaStream_t)stream) : launch_decode<64>(a, cache->format, (cudaStream_t)stream);
