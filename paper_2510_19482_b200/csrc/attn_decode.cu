@@ -70,11 +70,21 @@ __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
 template <bool BF16>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if constexpr (BF16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same without a sum in front
+template <bool BF16>
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
     uint32_t d;
@@ -111,25 +121,26 @@ __device__ __forceinline__ void e2m1_pairs(uint32_t (&h)[4], uint32_t w) {
     asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
-// 16 bytes to shared memory, or zeros
+// 16 bytes to shared memory
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
+}
+// ... or zeros
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, bool some) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
 }
+// (plain loads: the compiler may move them, but not over the wait for the copies)
 template <int BYTES>
-__device__ __forceinline__ void read_shared(uint32_t* w, uint32_t addr) {
-    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
-    else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
-    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
-}
-__device__ __forceinline__ uint32_t read_shared_u8(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ uint32_t read_shared_u16(uint32_t addr) {
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
-    return v;
+__device__ __forceinline__ void read_shared(uint32_t* w, const uint8_t* p) {
+    if constexpr (BYTES == 16) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (BYTES == 8) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
 }
 
 template <int TT>
@@ -229,8 +240,12 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
     uint32_t v_to[TURNS];
 #pragma unroll
     for (int i = 0; i < TURNS; ++i) v_to[i] = cr * ROW + 16 * (cc ^ v_turn(i * ROWS + cr));
-    const uint32_t k_read = ring + g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
-    const uint32_t v_read = ring + V0 + 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g);
+    const uint8_t *k_lane = a.c.k + lane * 16, *v_lane = a.c.v + lane * 16;
+    [[maybe_unused]] const uint8_t* s_lane = (lane < 16 ? a.c.ks : a.c.vs) + (lane & 15) % (D / 16) * 16;
+    [[maybe_unused]] const uint32_t s_to = (lane < 16 ? KS0 : VS0) + (lane & 15) * 16;
+    const uint8_t* own = smem + warp * (S * STAGE);
+    const uint32_t k_read = g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
+    const uint32_t v_read = V0 + 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g);
 
     bool recorded = false;
     // (joint: every warp once, with or without tiles)
@@ -255,43 +270,60 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
         const int least = len - a.fresh + 1;                  // tokens that the first of the new tokens sees
 
         // ---- copies ----------------------------------------------------------------------------------------------------------------------------
-        uint32_t there = 0;                                   // a bit for each 16 tokens of the stages: their page exists
-        long long first_row = -1;                             // lane i: first row of the cache of the i-th of 32 pieces of 16 tokens of this warp's tiles; below 0: no page
+        uint32_t gone = 0;                                    // a bit for each 16 tokens of the stages: their page does not exist
+        long long from = -1;                                  // lane i: where the i-th of 32 pieces of 16 tokens of this warp's tiles begins in the cache, in bytes of K; below 0: nowhere
+        int page = -1;                                        // the same of the next 32 pieces: their page
+        auto look_up = [&](int n) {
+            const int tok = (tile0 + n + lane / SUB) * TT + (lane % SUB) * 16;
+            page = n + lane / SUB < mine && tok < len ? __ldg(pages + a.c.page.of(tok)) : -1;
+        };
+        look_up(0);
         auto copy = [&](int n, int slot) {
-            if (((n * SUB) & 31) == 0) {
+            const int piece = n * SUB & 31;
+            if (piece == 0) {
                 const int tok = (tile0 + n + lane / SUB) * TT + (lane % SUB) * 16;
-                first_row = -1;
-                if (n + lane / SUB < mine && tok < len) {
-                    const int number = a.c.page.of(tok), page = __ldg(pages + number);
-                    if (page >= 0 && page < a.c.n_pages) first_row = ((long long)page * a.c.heads + h) * a.c.page_size + (tok - number * a.c.page_size);
-                }
+                from = page < 0 || page >= a.c.n_pages ? -1 : (((long long)page * a.c.heads + h) * a.c.page_size + (tok - a.c.page.of(tok) * a.c.page_size)) * ROW;
+                look_up(n + 32 / SUB);
             }
-            const int left = len - (tile0 + n) * TT;        // tokens from the stage's first on
-            const uint32_t at = ring + slot * STAGE;
-            uint32_t have = 0;
+            const int left = len - (tile0 + n) * TT;          // tokens from the stage's first on
+            const uint32_t at = ring + slot * STAGE, kt = at + k_to;
+            long long src[SUB];
+            bool all = left >= TT;
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
-                const long long row = __shfl_sync(0xffffffffu, first_row, (n * SUB + s) & 31);
-                const long long from = (row < 0 ? 0 : row) * ROW + lane * 16;
-                have |= (uint32_t)(row >= 0) << s;
-                const uint8_t *ksrc = a.c.k + from, *vsrc = a.c.v + from;
-                const int some = row < 0 ? 0 : left - 16 * s;
+                src[s] = __shfl_sync(0xffffffffu, from, piece + s);
+                all &= src[s] >= 0;
+            }
+            if (gone != 0) gone &= ~(((1u << SUB) - 1u) << (slot * SUB));
+            if (all) {
 #pragma unroll
-                for (int i = 0; i < 16 / ROWS; ++i) {
-                    const int r = i * ROWS + cr;
-                    const uint32_t to = at + 16 * s * ROW + i * 512;
-                    copy16(to + k_to, ksrc + i * 512, r < some);
-                    copy16(to + V0 + v_to[i % TURNS], vsrc + i * 512, r < some);
+                for (int s = 0; s < SUB; ++s) {
+                    const uint8_t *k = k_lane + src[s], *v = v_lane + src[s];
+#pragma unroll
+                    for (int i = 0; i < 16 / ROWS; ++i) copy16(kt + 16 * s * ROW + i * 512, k + i * 512);
+#pragma unroll
+                    for (int i = 0; i < 16 / ROWS; ++i) copy16(at + v_to[i % TURNS] + (V0 + 16 * s * ROW + i * 512), v + i * 512);
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) {
+                    const long long start = src[s] < 0 ? 0 : src[s];
+                    const int some = src[s] < 0 ? 0 : left - 16 * s;
+                    gone |= (uint32_t)(src[s] < 0) << (slot * SUB + s);
+#pragma unroll
+                    for (int i = 0; i < 16 / ROWS; ++i) {
+                        copy16(kt + 16 * s * ROW + i * 512, k_lane + start + i * 512, i * ROWS + cr < some);
+                        copy16(at + v_to[i % TURNS] + (V0 + 16 * s * ROW + i * 512), v_lane + start + i * 512, i * ROWS + cr < some);
+                    }
                 }
             }
-            there = (there & ~(((1u << SUB) - 1u) << (slot * SUB))) | have << (slot * SUB);
             if constexpr (SCALED) {
-                // 16 tokens' scales are D bytes, D / 16 lanes'; half of the lanes copy K's and half V's.  (Rows behind the sequence too: within the page, they meet codes of zero; a
-                // NaN among them is taken out where they are used.)
+                // 16 tokens' scales are D bytes, D / 16 lanes', an eighth of their codes; half of the lanes copy K's and half V's.  (Rows behind the sequence too: within the page,
+                // they meet codes of zero; a NaN among them is taken out where they are used.)
                 constexpr int LANES = D / 16;
                 const int l = lane & 15, s = l / LANES;
-                const long long row = __shfl_sync(0xffffffffu, first_row, (n * SUB + (s < SUB ? s : 0)) & 31);
-                if (s < SUB) copy16(at + (lane < 16 ? KS0 : VS0) + l * 16, (lane < 16 ? a.c.ks : a.c.vs) + (row < 0 ? 0 : row) * (D / 16) + l % LANES * 16, row >= 0);
+                const long long start = __shfl_sync(0xffffffffu, from, piece + (s < SUB ? s : 0));
+                if (s < SUB) copy16(at + s_to, s_lane + ((start < 0 ? 0 : start) >> 3), start >= 0);
             }
         };
         auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
@@ -366,57 +398,56 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             __syncwarp();
             // ---- scores ----------------------------------------------------------------------------------------------------------------------
             float sc[SUB][NT][4];
+            uint32_t kr[SUB][2][KW];
+            [[maybe_unused]] uint32_t blk[SUB][2];            // [row]: the scales of this lane's blocks
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int r = 0; r < 2; ++r) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[s][nt][i] = 0.0f;
-                uint32_t kr[2][KW];
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int i = 0; i < KW / KC; ++i) read_shared<4 * KC>(&kr[r][i * KC], (k_read ^ (i * 64)) + at + (16 * s + 8 * r) * ROW);
-                [[maybe_unused]] uint32_t blk[2][2];          // [row][block of this lane]: scale, in both halves
-                if constexpr (SCALED) {
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const uint32_t p = ring + at + KS0 + (16 * s + g + 8 * r) * (D / 16);
-                        const uint32_t two = e4m3_pair(D == 128 ? read_shared_u16(p + 2 * t) : read_shared_u8(p + t));
-                        blk[r][0] = prmt(two, two, 0x1010);
-                        blk[r][1] = prmt(two, two, 0x3232);
+                    for (int i = 0; i < KW / KC; ++i) read_shared<4 * KC>(&kr[s][r][i * KC], own + ((k_read ^ (i * 64)) + at + (16 * s + 8 * r) * ROW));
+                    if constexpr (SCALED) {
+                        const uint8_t* p = own + at + KS0 + (16 * s + g + 8 * r) * (D / 16);
+                        blk[s][r] = e4m3_pair(D == 128 ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[t] : (uint32_t)p[t]);
                     }
                 }
+            }
+            auto product = [&](float (&d)[4], int step, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, int nt) {
+                if (step == 0) mma_first<BF16>(d, a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
+                else mma<BF16>(d, a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
+            };
 #pragma unroll
-                for (int w = 0; w < KW; ++w) {                // a word of both rows: PER_WORD / 4 steps
+            for (int w = 0; w < KW; ++w)                      // a word of both rows: PER_WORD / 4 steps
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) {
                     if constexpr (FMT == ELUTQ_KV_16) {
                         if (w % 2 == 1) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma<BF16>(sc[s][nt], kr[0][w - 1], kr[1][w - 1], kr[0][w], kr[1][w], qf[nt][w / 2][0], qf[nt][w / 2][1]);
+                            for (int nt = 0; nt < NT; ++nt) product(sc[s][nt], w / 2, kr[s][0][w - 1], kr[s][1][w - 1], kr[s][0][w], kr[s][1][w], nt);
                         }
                     } else {
                         uint32_t x[2][PER_WORD / 2];
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             if constexpr (FMT == ELUTQ_KV_E4M3) {
-                                e4m3_pairs(x[r], kr[r][w]);
+                                e4m3_pairs(x[r], kr[s][r][w]);
                             } else {
-                                e2m1_pairs(x[r], kr[r][w]);
+                                const uint32_t scale = prmt(blk[s][r], blk[s][r], w < 2 ? 0x1010 : 0x3232);
+                                e2m1_pairs(x[r], kr[s][r][w]);
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) x[r][i] = hmul2(x[r][i], blk[r][w / 2]);
+                                for (int i = 0; i < 4; ++i) x[r][i] = hmul2(x[r][i], scale);
                             }
                         }
 #pragma unroll
                         for (int i = 0; i < PER_WORD / 4; ++i)
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
-                                mma<BF16>(sc[s][nt], x[0][2 * i], x[1][2 * i], x[0][2 * i + 1], x[1][2 * i + 1], qf[nt][w * (PER_WORD / 4) + i][0], qf[nt][w * (PER_WORD / 4) + i][1]);
+                                product(sc[s][nt], w * (PER_WORD / 4) + i, x[0][2 * i], x[1][2 * i], x[0][2 * i + 1], x[1][2 * i + 1], nt);
                     }
                 }
-            }
-            const uint32_t pages_there = there >> (slot * SUB) & ((1u << SUB) - 1u);
             const bool last = tok0 + TT > least;              // some column may not see all of the tile
-            if (last || pages_there != (1u << SUB) - 1u) {
+            if (last || gone != 0) {
+                const uint32_t none = gone >> (slot * SUB);
 #pragma unroll
                 for (int s = 0; s < SUB; ++s)
 #pragma unroll
@@ -424,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int tok = tok0 + 16 * s + g + 8 * (i >> 1);
-                            if (tok >= limit[nt][i & 1] || !(pages_there >> s & 1u)) sc[s][nt][i] = -INFINITY;
+                            if (tok >= limit[nt][i & 1] || (none >> s & 1u)) sc[s][nt][i] = -INFINITY;
                         }
             }
             // ---- softmax: P of this tile ---------------------------------------------------------------------------------------------------------
@@ -481,13 +512,13 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int i = 0; i < VW / VC; ++i) read_shared<4 * VC>(&vr[r][i * VC], v_read + at + (16 * s + (r & 1) + 8 * (r >> 1)) * ROW + i * 128);
+                    for (int i = 0; i < VW / VC; ++i) read_shared<4 * VC>(&vr[r][i * VC], own + (v_read + at + (16 * s + (r & 1) + 8 * (r >> 1)) * ROW + i * 128));
                 if constexpr (SCALED) {
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         const int tok = 16 * s + 2 * t + 8 * p;
-                        const uint32_t q = ring + at + VS0 + tok * (D / 16) + (D == 128 ? g : g / 2);
-                        uint32_t bytes = read_shared_u8(q) | read_shared_u8(q + D / 16) << 8;
+                        const uint8_t* q = own + at + VS0 + tok * (D / 16) + (D == 128 ? g : g / 2);
+                        uint32_t bytes = (uint32_t)q[0] | (uint32_t)q[D / 16] << 8;
                         if (tok0 + TT > len) bytes &= (tok0 + tok < len ? 0xffu : 0u) | (tok0 + tok + 1 < len ? 0xff00u : 0u);
                         vsc[p] = e4m3_pair(bytes);
                     }
@@ -554,8 +585,8 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                             for (int m = 0; m < MS; ++m)
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
-                                    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                                    mma<BF16>(part, x[m][0] & lo, x[m][1] & lo, x[m][2] & hi, x[m][3] & hi, pf[s][nt][0], pf[s][nt][1]);
+                                    float part[4];
+                                    mma_first<BF16>(part, x[m][0] & lo, x[m][1] & lo, x[m][2] & hi, x[m][3] & hi, pf[s][nt][0], pf[s][nt][1]);
 #pragma unroll
                                     for (int i = 0; i < 4; ++i)
                                         if (limit[nt][i & 1] == sees) o[w * MS + m][nt][i] += part[i];
