@@ -125,9 +125,9 @@ __device__ __forceinline__ void e2m1_pairs(uint32_t (&h)[4], uint32_t w) {
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
 }
-// ... or zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, bool some) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
+// ... the first `bytes` of them and zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // (plain loads: the compiler may move them, but not over the wait for the copies)
 template <int BYTES>
@@ -141,6 +141,13 @@ __device__ __forceinline__ void read_shared(uint32_t* w, const uint8_t* p) {
     } else {
         w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
+}
+
+// Four 8 x 8 matrices of 16 bits, as they are or turned; a lane gives the address of a row
+template <bool TURNED>
+__device__ __forceinline__ void read_matrices(uint32_t (&x)[4], uint32_t addr) {
+    if constexpr (TURNED) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+    else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
 }
 
 template <int TT>
@@ -228,24 +235,28 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
     }
     const long long f0 = cta0 + warp * share, f1 = f0 + share < cta1 ? f0 + share : cta1;
 
-    // where a lane copies to and reads from.  A piece's place in its row is its number with some bits of the row's number turned: the eight lanes that are served together
-    // read two K rows, or four V rows, of which every second.
-    auto k_turn = [](int r) { return PIECES >= 8 ? (r & 1) << 2 : 0; };
-    auto v_turn = [](int r) { return PIECES >= 8 ? (r >> 1 & 3) << 1 : PIECES == 4 ? r >> 1 & 3 : 0; };
+    // where a lane copies to and reads from.  A piece's place in its row is its number with some bits of the row's number turned, so that the lanes that are served together
+    // meet different banks: 16 bits, the same piece of eight rows (ldmatrix); codes, two K rows, or four V rows, of which every second.
+    auto k_turn = [](int r) { return FMT == ELUTQ_KV_16 ? r & 7 : PIECES >= 8 ? (r & 1) << 2 : 0; };
+    auto v_turn = [](int r) { return FMT == ELUTQ_KV_16 ? r & 7 : PIECES >= 8 ? (r >> 1 & 3) << 1 : PIECES == 4 ? r >> 1 & 3 : 0; };
     constexpr int ROWS = 32 / PIECES;                         // rows of a copy of the warp
     const int cr = lane / PIECES, cc = lane % PIECES;
     // (in the 512 bytes of one; after TURNS of them the rows' turns are the first one's again)
-    constexpr int TURNS = PIECES == 16 ? 4 : PIECES == 8 ? 2 : 1;
-    const uint32_t k_to = cr * ROW + 16 * (cc ^ k_turn(cr));
-    uint32_t v_to[TURNS];
+    constexpr int TURNS = PIECES >= 8 ? PIECES / 4 : 1;
+    uint32_t k_to[TURNS], v_to[TURNS];
 #pragma unroll
-    for (int i = 0; i < TURNS; ++i) v_to[i] = cr * ROW + 16 * (cc ^ v_turn(i * ROWS + cr));
+    for (int i = 0; i < TURNS; ++i) {
+        k_to[i] = cr * ROW + 16 * (cc ^ k_turn(i * ROWS + cr));
+        v_to[i] = cr * ROW + 16 * (cc ^ v_turn(i * ROWS + cr));
+    }
     const uint8_t *k_lane = a.c.k + lane * 16, *v_lane = a.c.v + lane * 16;
     [[maybe_unused]] const uint8_t* s_lane = (lane < 16 ? a.c.ks : a.c.vs) + (lane & 15) % (D / 16) * 16;
     [[maybe_unused]] const uint32_t s_to = (lane < 16 ? KS0 : VS0) + (lane & 15) * 16;
     const uint8_t* own = smem + warp * (S * STAGE);
-    const uint32_t k_read = g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
-    const uint32_t v_read = V0 + 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g);
+    const uint32_t k_read = FMT == ELUTQ_KV_16 ? (lane & 15) * ROW + 16 * (lane >> 4 ^ (lane & 7))
+                                               : g * ROW + (KC == 4 ? 16 * (t ^ k_turn(g)) : 4 * KC * t);
+    const uint32_t v_read = V0 + (FMT == ELUTQ_KV_16 ? ((lane & 7) + (lane >> 4) * 8) * ROW + 16 * ((lane >> 3 & 1) ^ (lane & 7))
+                                                     : 2 * t * ROW + (VC == 4 ? 16 * (g ^ v_turn(2 * t)) : VC == 2 ? 16 * ((g >> 1) ^ v_turn(2 * t)) + 8 * (g & 1) : 4 * g));
 
     bool recorded = false;
     // (joint: every warp once, with or without tiles)
@@ -286,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                 look_up(n + 32 / SUB);
             }
             const int left = len - (tile0 + n) * TT;          // tokens from the stage's first on
-            const uint32_t at = ring + slot * STAGE, kt = at + k_to;
+            const uint32_t at = ring + slot * STAGE;
             long long src[SUB];
             bool all = left >= TT;
 #pragma unroll
@@ -300,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                 for (int s = 0; s < SUB; ++s) {
                     const uint8_t *k = k_lane + src[s], *v = v_lane + src[s];
 #pragma unroll
-                    for (int i = 0; i < 16 / ROWS; ++i) copy16(kt + 16 * s * ROW + i * 512, k + i * 512);
+                    for (int i = 0; i < 16 / ROWS; ++i) copy16(at + k_to[i % TURNS] + (16 * s * ROW + i * 512), k + i * 512);
 #pragma unroll
                     for (int i = 0; i < 16 / ROWS; ++i) copy16(at + v_to[i % TURNS] + (V0 + 16 * s * ROW + i * 512), v + i * 512);
                 }
@@ -312,18 +323,20 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                     gone |= (uint32_t)(src[s] < 0) << (slot * SUB + s);
 #pragma unroll
                     for (int i = 0; i < 16 / ROWS; ++i) {
-                        copy16(kt + 16 * s * ROW + i * 512, k_lane + start + i * 512, i * ROWS + cr < some);
-                        copy16(at + v_to[i % TURNS] + (V0 + 16 * s * ROW + i * 512), v_lane + start + i * 512, i * ROWS + cr < some);
+                        copy16(at + k_to[i % TURNS] + (16 * s * ROW + i * 512), k_lane + start + i * 512, i * ROWS + cr < some ? 16 : 0);
+                        copy16(at + v_to[i % TURNS] + (V0 + 16 * s * ROW + i * 512), v_lane + start + i * 512, i * ROWS + cr < some ? 16 : 0);
                     }
                 }
             }
             if constexpr (SCALED) {
-                // 16 tokens' scales are D bytes, D / 16 lanes', an eighth of their codes; half of the lanes copy K's and half V's.  (Rows behind the sequence too: within the page,
-                // they meet codes of zero; a NaN among them is taken out where they are used.)
+                // 16 tokens' scales are D bytes, D / 16 lanes', an eighth of their codes; half of the lanes copy K's and half V's
                 constexpr int LANES = D / 16;
                 const int l = lane & 15, s = l / LANES;
                 const long long start = __shfl_sync(0xffffffffu, from, piece + (s < SUB ? s : 0));
-                if (s < SUB) copy16(at + s_to, s_lane + ((start < 0 ? 0 : start) >> 3), start >= 0);
+                if (s < SUB) {
+                    if (all) copy16(at + s_to, s_lane + (start >> 3));
+                    else copy16(at + s_to, s_lane + ((start < 0 ? 0 : start) >> 3), start < 0 ? 0 : min(max((left - 16 * s) * (D / 16) - l % LANES * 16, 0), 16));
+                }
             }
         };
         auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
@@ -343,17 +356,24 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             const int r = rt * NC + nt * 8 + g;
             const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
             const uint8_t* p = a.q + 2 * (((long long)b * a.fresh + tok) * a.ldq + (long long)head * D);
-            constexpr int PIECE = KC * PER_WORD;              // head dimensions of a piece of K
+            if constexpr (FMT == ELUTQ_KV_16) {
 #pragma unroll
-            for (int i = 0; i < KW / KC; ++i)
+                for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-                for (int j = 0; j < PIECE / 8; ++j) {
-                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                    if (r < a.rows) v = __ldg(reinterpret_cast<const uint4*>(p + 2 * (PIECE * (t + 4 * i) + 8 * j)));
-                    const int step = (i * PIECE + 8 * j) / 4;
-                    qf[nt][step][0] = v.x; qf[nt][step][1] = v.y;
-                    qf[nt][step + 1][0] = v.z; qf[nt][step + 1][1] = v.w;
-                }
+                    for (int i = 0; i < 2; ++i) qf[nt][k][i] = r < a.rows ? __ldg(reinterpret_cast<const uint32_t*>(p) + 8 * k + 4 * i + t) : 0u;
+            } else {
+                constexpr int PIECE = KC * PER_WORD;          // head dimensions of a piece of K
+#pragma unroll
+                for (int i = 0; i < KW / KC; ++i)
+#pragma unroll
+                    for (int j = 0; j < PIECE / 8; ++j) {
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        if (r < a.rows) v = __ldg(reinterpret_cast<const uint4*>(p + 2 * (PIECE * (t + 4 * i) + 8 * j)));
+                        const int step = (i * PIECE + 8 * j) / 4;
+                        qf[nt][step][0] = v.x; qf[nt][step][1] = v.y;
+                        qf[nt][step + 1][0] = v.z; qf[nt][step + 1][1] = v.w;
+                    }
+            }
             float up = 1.0f;                                  // what brings a row's scores back
             if (FMT != ELUTQ_KV_16 && a.type == ELUTQ_TYPE_BF16) {
                 // bf16 to fp16: the row times a power of two, its largest magnitude in [1, 2).  What is less than 2^-24 of that is cut off, as it would be from the sum.
@@ -391,83 +411,87 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.0f;
 
-        for (int n = 0, slot = 0; n < mine; ++n) {
-            const int tok0 = (tile0 + n) * TT;
-            const uint32_t at = slot * STAGE;
-            asm volatile("cp.async.wait_group %0;" :: "n"(S - 1) : "memory");
-            __syncwarp();
-            // ---- scores ----------------------------------------------------------------------------------------------------------------------
-            float sc[SUB][NT][4];
-            uint32_t kr[SUB][2][KW];
-            [[maybe_unused]] uint32_t blk[SUB][2];            // [row]: the scales of this lane's blocks
-#pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-#pragma unroll
-                    for (int i = 0; i < KW / KC; ++i) read_shared<4 * KC>(&kr[s][r][i * KC], own + ((k_read ^ (i * 64)) + at + (16 * s + 8 * r) * ROW));
-                    if constexpr (SCALED) {
-                        const uint8_t* p = own + at + KS0 + (16 * s + g + 8 * r) * (D / 16);
-                        blk[s][r] = e4m3_pair(D == 128 ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[t] : (uint32_t)p[t]);
-                    }
-                }
+        // 16 tokens at a time, NVFP4 a stage's 32 (the vote on the maximum and its like are then paid for once: 64 sequences of 4 to 16 K tokens 186 -> 169 us)
+        constexpr int U = SCALED ? SUB : 1, TURN = SUB / U;
+        int slot = 0;
+        for (int n = 0; n < mine * TURN; ++n) {
+            if (n % TURN == 0) {
+                asm volatile("cp.async.wait_group %0;" :: "n"(S - 1) : "memory");
+                __syncwarp();
             }
-            auto product = [&](float (&d)[4], int step, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, int nt) {
-                if (step == 0) mma_first<BF16>(d, a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
-                else mma<BF16>(d, a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
+            const int tok0 = tile0 * TT + 16 * U * n;
+            const uint32_t at = slot * STAGE + n % TURN * 16 * U * ROW;
+            [[maybe_unused]] const uint8_t* scales = own + slot * STAGE;
+            // ---- scores ----------------------------------------------------------------------------------------------------------------------
+            float sc[U][NT][4];
+            auto product = [&](int u, int step, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                    if (step == 0) mma_first<BF16>(sc[u][nt], a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
+                    else mma<BF16>(sc[u][nt], a0, a1, a2, a3, qf[nt][step][0], qf[nt][step][1]);
             };
+            if constexpr (FMT == ELUTQ_KV_16) {
 #pragma unroll
-            for (int w = 0; w < KW; ++w)                      // a word of both rows: PER_WORD / 4 steps
+                for (int k = 0; k < STEPS; ++k) {
+                    uint32_t x[4];
+                    read_matrices<false>(x, ring + at + (k_read ^ (k * 32)));
+                    product(0, k, x[0], x[1], x[2], x[3]);
+                }
+            } else {
+                uint32_t kr[U][2][KW];
+                [[maybe_unused]] uint32_t blk[U][2];          // [row]: the scales of this lane's blocks
 #pragma unroll
-                for (int s = 0; s < SUB; ++s) {
-                    if constexpr (FMT == ELUTQ_KV_16) {
-                        if (w % 2 == 1) {
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) product(sc[s][nt], w / 2, kr[s][0][w - 1], kr[s][1][w - 1], kr[s][0][w], kr[s][1][w], nt);
+                    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                        for (int i = 0; i < KW / KC; ++i) read_shared<4 * KC>(&kr[u][r][i * KC], own + ((k_read ^ (i * 64)) + at + (16 * u + 8 * r) * ROW));
+                        if constexpr (SCALED) {
+                            const uint8_t* p = scales + KS0 + (g + 16 * u + 8 * r) * (D / 16);
+                            blk[u][r] = e4m3_pair(D == 128 ? (uint32_t)reinterpret_cast<const uint16_t*>(p)[t] : (uint32_t)p[t]);
                         }
-                    } else {
+                    }
+#pragma unroll
+                for (int w = 0; w < KW; ++w)                  // a word of both rows: PER_WORD / 4 steps
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
                         uint32_t x[2][PER_WORD / 2];
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             if constexpr (FMT == ELUTQ_KV_E4M3) {
-                                e4m3_pairs(x[r], kr[s][r][w]);
+                                e4m3_pairs(x[r], kr[u][r][w]);
                             } else {
-                                const uint32_t scale = prmt(blk[s][r], blk[s][r], w < 2 ? 0x1010 : 0x3232);
-                                e2m1_pairs(x[r], kr[s][r][w]);
+                                const uint32_t scale = prmt(blk[u][r], blk[u][r], w < 2 ? 0x1010 : 0x3232);
+                                e2m1_pairs(x[r], kr[u][r][w]);
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) x[r][i] = hmul2(x[r][i], scale);
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < PER_WORD / 4; ++i)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                product(sc[s][nt], w * (PER_WORD / 4) + i, x[0][2 * i], x[1][2 * i], x[0][2 * i + 1], x[1][2 * i + 1], nt);
+                        for (int i = 0; i < PER_WORD / 4; ++i) product(u, w * (PER_WORD / 4) + i, x[0][2 * i], x[1][2 * i], x[0][2 * i + 1], x[1][2 * i + 1]);
                     }
-                }
-            const bool last = tok0 + TT > least;              // some column may not see all of the tile
+            }
+            const bool last = tok0 + 16 * U > least;              // some column may not see all of them
             if (last || gone != 0) {
-                const uint32_t none = gone >> (slot * SUB);
+                const uint32_t none = gone >> (slot * SUB + n % TURN * U);
 #pragma unroll
-                for (int s = 0; s < SUB; ++s)
+                for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int tok = tok0 + 16 * s + g + 8 * (i >> 1);
-                            if (tok >= limit[nt][i & 1] || (none >> s & 1u)) sc[s][nt][i] = -INFINITY;
-                        }
+                        for (int i = 0; i < 4; ++i)
+                            if (tok0 + 16 * u + g + 8 * (i >> 1) >= limit[nt][i & 1] || (none >> u & 1u)) sc[u][nt][i] = -INFINITY;
             }
-            // ---- softmax: P of this tile ---------------------------------------------------------------------------------------------------------
+            // ---- softmax: P of these tokens --------------------------------------------------------------------------------------------------------
             float top[NT][2];
             bool rises = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    top[nt][j] = -INFINITY;
+                    top[nt][j] = fmaxf(sc[0][nt][j], sc[0][nt][j + 2]);
 #pragma unroll
-                    for (int s = 0; s < SUB; ++s) top[nt][j] = fmaxf(top[nt][j], fmaxf(sc[s][nt][j], sc[s][nt][j + 2]));
+                    for (int u = 1; u < U; ++u) top[nt][j] = fmaxf(top[nt][j], fmaxf(sc[u][nt][j], sc[u][nt][j + 2]));
                     rises |= fmaf(top[nt][j], cs[nt][j], off[nt][j]) > kRise;
                 }
             if (__any_sync(0xffffffffu, rises)) {
@@ -489,116 +513,110 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                         }
                     }
             }
-            uint32_t pf[SUB][NT][2];
+            uint32_t pf[U][NT][2];
 #pragma unroll
-            for (int s = 0; s < SUB; ++s)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        p[i] = exp2_approx(fmaf(sc[s][nt][i], cs[nt][i & 1], off[nt][i & 1]));
+                        p[i] = exp2_approx(fmaf(sc[u][nt][i], cs[nt][i & 1], off[nt][i & 1]));
                         sum[nt][i & 1] += p[i];
                     }
-                    pf[s][nt][0] = transposed(pack<BF16>(p[0], p[1]));
-                    pf[s][nt][1] = transposed(pack<BF16>(p[2], p[3]));
+                    pf[u][nt][0] = transposed(pack<BF16>(p[0], p[1]));
+                    pf[u][nt][1] = transposed(pack<BF16>(p[2], p[3]));
                 }
-            // ---- P V ---------------------------------------------------------------------------------------------------------------------------
-            // V rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of 16 tokens as fragments.  Tile m of the result: dimensions 2 m and 2 m + 1 of this lane's, the two tokens of a pair side by side.
-            // Codes are brought side by side before they are converted.
-            uint32_t vr[4][VW];
-            uint32_t vsc[2];
-            auto read_v = [&](int s) {
+            // ---- P V: fragments of V rows, and what is done with each of them (a tile of 16 dimensions of the result) -----------------------------------------------
+            // 16 bits: dimensions 16 m + g and 8 more.  Codes: V rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9; tile m has dimensions 2 m and 2 m + 1 of this lane's, the two tokens of a pair side by
+            // side.  They are brought there before they are converted.
+            auto with_v = [&](int u, auto&& use) {
+                if constexpr (FMT == ELUTQ_KV_16) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int i = 0; i < VW / VC; ++i) read_shared<4 * VC>(&vr[r][i * VC], own + (v_read + at + (16 * s + (r & 1) + 8 * (r >> 1)) * ROW + i * 128));
-                if constexpr (SCALED) {
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const int tok = 16 * s + 2 * t + 8 * p;
-                        const uint8_t* q = own + at + VS0 + tok * (D / 16) + (D == 128 ? g : g / 2);
-                        uint32_t bytes = (uint32_t)q[0] | (uint32_t)q[D / 16] << 8;
-                        if (tok0 + TT > len) bytes &= (tok0 + tok < len ? 0xffu : 0u) | (tok0 + tok + 1 < len ? 0xff00u : 0u);
-                        vsc[p] = e4m3_pair(bytes);
+                    for (int m = 0; m < STEPS; ++m) {
+                        uint32_t x[4];
+                        read_matrices<true>(x, ring + at + (v_read ^ (m * 32)));
+                        use(m, x[0], x[1], x[2], x[3]);
                     }
-                }
-            };
-            constexpr int MS = FMT == ELUTQ_KV_16 ? 1 : FMT == ELUTQ_KV_E4M3 ? 2 : 4;      // tiles of the result from a word of the four rows
-            auto v_fragments = [&](int w, uint32_t (&x)[MS][4]) {
+                } else {
+                    uint32_t vr[4][VW];
+                    [[maybe_unused]] uint32_t vsc[2];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const uint32_t v0 = vr[2 * p][w], v1 = vr[2 * p + 1][w];
-                    if constexpr (FMT == ELUTQ_KV_16) {
-                        x[0][2 * p] = prmt(v0, v1, 0x5410);
-                        x[0][2 * p + 1] = prmt(v0, v1, 0x7632);
-                    } else if constexpr (FMT == ELUTQ_KV_E4M3) {
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            uint32_t h[2];
-                            e4m3_pairs(h, prmt(v0, v1, i == 0 ? 0x5140 : 0x7362));
-                            x[i][2 * p] = h[0];
-                            x[i][2 * p + 1] = h[1];
+                        for (int i = 0; i < VW / VC; ++i) read_shared<4 * VC>(&vr[r][i * VC], own + (v_read + at + (16 * u + (r & 1) + 8 * (r >> 1)) * ROW + i * 128));
+                    if constexpr (SCALED) {
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            const uint8_t* q = scales + VS0 + (16 * u + 2 * t + 8 * p) * (D / 16) + (D == 128 ? g : g / 2);
+                            vsc[p] = e4m3_pair((uint32_t)q[0] | (uint32_t)q[D / 16] << 8);
                         }
-                    } else {
-                        uint32_t lo[4], hi[4];
-                        e2m1_pairs(lo, (v0 & 0x0f0f0f0fu) | (v1 << 4 & 0xf0f0f0f0u));
-                        e2m1_pairs(hi, (v0 >> 4 & 0x0f0f0f0fu) | (v1 & 0xf0f0f0f0u));
+                    }
+                    constexpr int MS = FMT == ELUTQ_KV_E4M3 ? 2 : 4;           // tiles of the result from a word of the four rows
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            x[i][2 * p] = hmul2(lo[i], vsc[p]);
-                            x[i][2 * p + 1] = hmul2(hi[i], vsc[p]);
+                    for (int w = 0; w < VW; ++w) {
+                        uint32_t x[MS][4];
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            const uint32_t v0 = vr[2 * p][w], v1 = vr[2 * p + 1][w];
+                            if constexpr (FMT == ELUTQ_KV_E4M3) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    uint32_t h[2];
+                                    e4m3_pairs(h, prmt(v0, v1, i == 0 ? 0x5140 : 0x7362));
+                                    x[i][2 * p] = h[0];
+                                    x[i][2 * p + 1] = h[1];
+                                }
+                            } else {
+                                uint32_t lo[4], hi[4];
+                                e2m1_pairs(lo, (v0 & 0x0f0f0f0fu) | (v1 << 4 & 0xf0f0f0f0u));
+                                e2m1_pairs(hi, (v0 >> 4 & 0x0f0f0f0fu) | (v1 & 0xf0f0f0f0u));
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    x[i][2 * p] = hmul2(lo[i], vsc[p]);
+                                    x[i][2 * p + 1] = hmul2(hi[i], vsc[p]);
+                                }
+                            }
                         }
+#pragma unroll
+                        for (int i = 0; i < MS; ++i) use(w * MS + i, x[i][0], x[i][1], x[i][2], x[i][3]);
                     }
                 }
             };
             if (!last || a.fresh == 1) {
 #pragma unroll
-                for (int s = 0; s < SUB; ++s) {
-                    read_v(s);
+                for (int u = 0; u < U; ++u)
+                    with_v(u, [&](int m, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
 #pragma unroll
-                    for (int w = 0; w < VW; ++w) {
-                        uint32_t x[MS][4];
-                        v_fragments(w, x);
-#pragma unroll
-                        for (int i = 0; i < MS; ++i)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma<BF16>(o[w * MS + i][nt], x[i][0], x[i][1], x[i][2], x[i][3], pf[s][nt][0], pf[s][nt][1]);
-                    }
-                }
+                        for (int nt = 0; nt < NT; ++nt) mma<BF16>(o[m][nt], x0, x1, x2, x3, pf[u][nt][0], pf[u][nt][1]);
+                    });
             } else {
                 // each new token's columns by themselves, with V rows that it does not see replaced by zeros
                 const int first = rt * NC / a.group, end = min(a.fresh, (rt * NC + NC - 1) / a.group + 1);
-                for (int nw = first; nw < end; ++nw) {
-                    const int sees = least + nw;
+                for (int nw = first; nw < end; ++nw)
 #pragma unroll
-                    for (int s = 0; s < SUB; ++s) {
-                        read_v(s);
-                        const int tok = tok0 + 16 * s + 2 * t;
+                    for (int u = 0; u < U; ++u) {
+                        const int sees = least + nw, tok = tok0 + 16 * u + 2 * t;
                         const uint32_t lo = (tok < sees ? 0xffffu : 0u) | (tok + 1 < sees ? 0xffff0000u : 0u);
                         const uint32_t hi = (tok + 8 < sees ? 0xffffu : 0u) | (tok + 9 < sees ? 0xffff0000u : 0u);
+                        with_v(u, [&](int m, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
 #pragma unroll
-                        for (int w = 0; w < VW; ++w) {
-                            uint32_t x[MS][4];
-                            v_fragments(w, x);
+                            for (int nt = 0; nt < NT; ++nt) {
+                                float part[4];
+                                mma_first<BF16>(part, x0 & lo, x1 & lo, x2 & hi, x3 & hi, pf[u][nt][0], pf[u][nt][1]);
 #pragma unroll
-                            for (int m = 0; m < MS; ++m)
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) {
-                                    float part[4];
-                                    mma_first<BF16>(part, x[m][0] & lo, x[m][1] & lo, x[m][2] & hi, x[m][3] & hi, pf[s][nt][0], pf[s][nt][1]);
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i)
-                                        if (limit[nt][i & 1] == sees) o[w * MS + m][nt][i] += part[i];
-                                }
-                        }
+                                for (int i = 0; i < 4; ++i)
+                                    if (limit[nt][i & 1] == sees) o[m][nt][i] += part[i];
+                            }
+                        });
                     }
-                }
             }
-            __syncwarp();
-            if (n + S < mine) copy(n + S, slot);
-            commit();
-            slot = slot + 1 == S ? 0 : slot + 1;
+            if (n % TURN == TURN - 1) {
+                __syncwarp();
+                if (n / TURN + S < mine) copy(n / TURN + S, slot);
+                commit();
+                slot = slot + 1 == S ? 0 : slot + 1;
+            }
         }
 
         // ---- the end of a segment, or of the share ------------------------------------------------------------------------------------------------------
@@ -608,10 +626,19 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) sum[nt][j] += __shfl_xor_sync(0xffffffffu, sum[nt][j], d);
-        // dimension of word m of this lane's pieces of V rows
+        // this lane's two dimensions of tile m of the result: the first, and how far the other one is
+        constexpr int APART = FMT == ELUTQ_KV_16 ? 8 : 1;
         auto dim_of = [&](int m) {
             constexpr int PIECE = VC * PER_WORD;
-            return PIECE * (g + 8 * (2 * m / PIECE)) + 2 * m % PIECE;
+            return FMT == ELUTQ_KV_16 ? 16 * m + g : PIECE * (g + 8 * (2 * m / PIECE)) + 2 * m % PIECE;
+        };
+        auto put = [&](float* row, int m, float x, float y) {
+            if constexpr (APART == 1) {
+                *reinterpret_cast<float2*>(row + dim_of(m)) = make_float2(x, y);
+            } else {
+                row[dim_of(m)] = x;
+                row[dim_of(m) + APART] = y;
+            }
         };
         auto part_of = [&](int w, int place) { return a.parts + ((long long)w * 2 + place) * (NC * (D + 2)); };
         // The segment begins in worker w's share and ends in another's.  Its other parts: of `near` workers behind w in this CTA, one of each of `whole` CTAs that have units of no
@@ -641,7 +668,13 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
 #pragma unroll
                         for (int m = 0; m < STEPS; ++m) {
                             const float x = o[m][nt][j] * r, y = o[m][nt][j + 2] * r;
-                            *reinterpret_cast<uint32_t*>(p + 2 * dim_of(m)) = a.type == ELUTQ_TYPE_F16 ? pack<false>(x, y) : pack<true>(x, y);
+                            const uint32_t two = a.type == ELUTQ_TYPE_F16 ? pack<false>(x, y) : pack<true>(x, y);
+                            if constexpr (APART == 1) {
+                                *reinterpret_cast<uint32_t*>(p + 2 * dim_of(m)) = two;
+                            } else {
+                                reinterpret_cast<uint16_t*>(p)[dim_of(m)] = (uint16_t)two;
+                                reinterpret_cast<uint16_t*>(p)[dim_of(m) + APART] = (uint16_t)(two >> 16);
+                            }
                         }
                     } else {
                         if (g == 0) {
@@ -649,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                             part[NC + col] = sum[nt][j];
                         }
 #pragma unroll
-                        for (int m = 0; m < STEPS; ++m) *reinterpret_cast<float2*>(part + 2 * NC + col * D + dim_of(m)) = make_float2(o[m][nt][j], o[m][nt][j + 2]);
+                        for (int m = 0; m < STEPS; ++m) put(part + 2 * NC + col * D, m, o[m][nt][j], o[m][nt][j + 2]);
                     }
                 }
             if (begins && !whole) {
@@ -671,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                     s_sum[warp][col] = sum[nt][j];
                 }
 #pragma unroll
-                for (int m = 0; m < STEPS; ++m) *reinterpret_cast<float2*>(&s_o[warp][col][dim_of(m)]) = make_float2(o[m][nt][j], o[m][nt][j + 2]);
+                for (int m = 0; m < STEPS; ++m) put(s_o[warp][col], m, o[m][nt][j], o[m][nt][j + 2]);
             }
         __syncthreads();
         const bool begins = cta0 <= seg0 + kLead, whole = begins && cta1 >= seg0 + units;
