@@ -4,10 +4,11 @@
 //
 // work       A CTA takes two tiles of 128 query rows that share keys: neighbouring (row block, query head) pairs of one key head, so the heads of a group on the same rows
 //            where a group is even.  Keys and values come in tiles of 128 by TMA (128-byte swizzle) into one ring; the two query tiles use each of them once.
-//            The longest row blocks come first in the grid.
+//            One CTA to an SM goes through every n-th of such pairs of tiles, those with the longest rows first, each other round backwards.
 // roles      A warpgroup for each query tile: a thread owns a row, reads its 128 scores from tensor memory, forms the weights and writes them back as 16-bit values
-//            over the scores, where the tensor core takes them as the first operand of P V.  One thread issues all MMAs: while one tile's scores are with
-//            its warpgroup, the other tile's products run.  One warp loads.
+//            over the scores, where the tensor core takes them as the first operand of P V, a half at a time.  One thread issues all MMAs: while one tile's scores are with
+//            its warpgroup, the other tile's products run.  One warp finds the next pair of tiles and loads, while the last one is still being worked on; one replaces what lies
+//            behind a sequence by zeros.
 // memory     Tensor memory: scores / weights and results of both tiles, 4 x 128 columns.
 // softmax    A row's maximum moves only when a tile rises more than 2^10 above it; the warp then scales its results in tensor memory.  Weights stay below 2^14.  Maximum, sum
 //            and results are fp32.
@@ -27,7 +28,8 @@ namespace {
 
 constexpr int kTile = 128;                 // query rows of a tile, keys of a tile
 constexpr int kRing = 5;                   // tiles of keys and values on their way
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kTailWarp = 10;
+constexpr int kItems = 2;                  // pairs of tiles that the roles know of at once
 constexpr int kThreads = 384;
 // Registers of a thread: of the launch's 168 the two warpgroups of the softmax get more, the third less (2 x 208 + 80 is below 3 x 168).
 constexpr int kRowRegs = 208, kOtherRegs = 80;
@@ -43,7 +45,7 @@ struct PrefillArgs {
     const uint8_t *q, *k, *v;
     uint8_t* out;
     long long ldq, ldk, ldv, ldo;          // elements between tokens
-    int total_q, total_k;
+    int B, max_q, total_q, total_k;
     int heads, group;                      // key heads; query heads of each
     int causal, type;
     float scale;                           // times log2(e)
@@ -51,12 +53,25 @@ struct PrefillArgs {
     uint32_t wait_limit;                   // polls (tests); a wait of a second runs out whatever this is
 };
 
-enum { kBarQ = 0, kBarFull = 2, kBarEmpty = kBarFull + kRing, kBarScores = kBarEmpty + kRing, kBarWeights = kBarScores + 2, kBarDone = kBarWeights + 2, kBarTail = kBarDone + 2, kBarDrain, kNumBars };
+enum { kBarQ = 0, kBarQFree = 2, kBarFull = 4, kBarEmpty = kBarFull + kRing, kBarScores = kBarEmpty + kRing, kBarWeights = kBarScores + 2, kBarDone = kBarWeights + 4,
+       kBarResults = kBarDone + 2, kBarTail = kBarResults + 2, kBarItem = kBarTail + kRing, kBarItemFree = kBarItem + kItems, kBarDrain = kBarItemFree + kItems, kNumBars };
+
+struct Tile {
+    int head, row0, tiles;                 // query head, first row in the sequence, tiles of keys
+};
+// A pair of query tiles
+struct Item {
+    int q0, nq, k0, nk;                    // the sequence's queries and keys; nq < 0: there are no more
+    int h, kv0;                            // key head; how many tiles of keys and values were loaded before
+    Tile t[2];
+    __device__ __forceinline__ int most() const { return max(t[0].tiles, t[1].tiles); }
+    __device__ __forceinline__ bool tail() const { return most() > 0 && most() * kTile > nk; }       // the last tile of keys reaches behind the sequence
+};
 
 template <int D>
 constexpr int kTileBytes = kTile * D * 2;
 template <int D>
-constexpr int kSmem = (2 + kRing) * kTileBytes<D> + kNumBars * 8 + 16;
+constexpr int kSmem = (2 + kRing) * kTileBytes<D> + kNumBars * 8 + 16 + kItems * (int)sizeof(Item);
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
@@ -73,17 +88,24 @@ __device__ __forceinline__ unsigned long long now_ns() {
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).
+// Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).  gave_up[1] counts what rows formed one by one have seen: the
+// time begins again while it moves.
 __device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile const uint32_t* gave_up, uint32_t limit) {
     if (try_wait(bar, parity)) return true;
     unsigned long long since = 0;
+    uint32_t seen = 0;
     for (uint32_t i = 1; i < limit; ++i) {
         if (try_wait(bar, parity)) return true;
         if ((i & 15u) == 0u) {
             if (gave_up != nullptr && *gave_up) return false;
             const unsigned long long t = now_ns();
-            if (since == 0) since = t;
-            else if (t - since > kWaitNs) return false;
+            const uint32_t now = gave_up != nullptr ? gave_up[1] : 0u;
+            if (since == 0 || now != seen) {
+                since = t;
+                seen = now;
+            } else if (t - since > kWaitNs) {
+                return false;
+            }
         }
     }
     return false;
@@ -171,10 +193,10 @@ __device__ __forceinline__ float2 unpack(uint32_t v) {
     return make_float2(y[0], y[1]);
 }
 
-// One row by a warp, from the first `sees` keys: a lane takes D / 32 dimensions.
+// One row by a warp, from the first `sees` keys: a lane takes D / 32 dimensions, four keys on their way.
 template <int D, bool BF16>
-__device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const uint8_t* v, long long ldk, long long ldv, int sees, float scale, uint8_t* out) {
-    constexpr int W = D / 64;              // words of a lane
+__device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const uint8_t* v, long long ldk, long long ldv, int sees, float scale, uint8_t* out, volatile uint32_t* seen) {
+    constexpr int W = D / 64, AT_ONCE = 4;             // words of a lane
     const int lane = threadIdx.x & 31;
     float x[2 * W], o[2 * W];
 #pragma unroll
@@ -184,35 +206,107 @@ __device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const
         o[2 * i] = o[2 * i + 1] = 0.0f;
     }
     float top = -INFINITY, sum = 0.0f;
-    for (int j = 0; j < sees; ++j) {
-        float s = 0.0f;
+    for (int j0 = 0; j0 < sees; j0 += AT_ONCE) {
+        float s[AT_ONCE];
+        uint32_t vw[AT_ONCE][W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float2 t = unpack<BF16>(__ldg(reinterpret_cast<const uint32_t*>(k + 2 * j * ldk) + lane * W + i));
-            s = fmaf(x[2 * i], t.x, fmaf(x[2 * i + 1], t.y, s));
+        for (int n = 0; n < AT_ONCE; ++n) {
+            const long long j = min(j0 + n, sees - 1);
+            s[n] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float2 t = unpack<BF16>(__ldg(reinterpret_cast<const uint32_t*>(k + 2 * j * ldk) + lane * W + i));
+                vw[n][i] = __ldg(reinterpret_cast<const uint32_t*>(v + 2 * j * ldv) + lane * W + i);
+                s[n] = fmaf(x[2 * i], t.x, fmaf(x[2 * i + 1], t.y, s[n]));
+            }
         }
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        s *= scale;
-        const float m = fmaxf(top, s);     // (a NaN does not move it, and reaches the sum below)
-        const float by = top == m ? 1.0f : exp2f(top - m), p = s == -INFINITY ? 0.0f : exp2f(s - m);
-        top = m;
-        sum = fmaf(sum, by, p);
+        for (int d = 16; d > 0; d >>= 1)
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float2 t = unpack<BF16>(__ldg(reinterpret_cast<const uint32_t*>(v + 2 * j * ldv) + lane * W + i));
-            o[2 * i] = fmaf(o[2 * i], by, p * t.x);
-            o[2 * i + 1] = fmaf(o[2 * i + 1], by, p * t.y);
+            for (int n = 0; n < AT_ONCE; ++n) s[n] += __shfl_xor_sync(0xffffffffu, s[n], d);
+#pragma unroll
+        for (int n = 0; n < AT_ONCE; ++n) {
+            if (j0 + n >= sees) break;
+            s[n] *= scale;
+            const float m = fmaxf(top, s[n]);  // (a NaN does not move it, and reaches the sum below)
+            const float by = top == m ? 1.0f : exp2f(top - m), p = s[n] == -INFINITY ? 0.0f : exp2f(s[n] - m);
+            top = m;
+            sum = fmaf(sum, by, p);
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float2 t = unpack<BF16>(vw[n][i]);
+                o[2 * i] = fmaf(o[2 * i], by, p * t.x);
+                o[2 * i + 1] = fmaf(o[2 * i + 1], by, p * t.y);
+            }
         }
+        if ((j0 & 0xfff) == 0 && lane == 0) *seen = *seen + 1;
     }
     const float r = 1.0f / sum;
 #pragma unroll
     for (int i = 0; i < W; ++i) reinterpret_cast<uint32_t*>(out)[lane * W + i] = sum == 0.0f ? 0u : pack<BF16>(o[2 * i] * r, o[2 * i + 1] * r);
 }
 
-struct Tile {
-    int head, row0, tiles;                 // query head, first row in the sequence, tiles of keys
+// The n-th pair of tiles of all, level by level: level l holds the pairs l of all sequences that have so many, the highest level first.
+struct Walk {
+    int level, before, here;               // the level, pairs above it, pairs of it
+    __device__ __forceinline__ int pairs_of(const PrefillArgs& a, int b) const {
+        const int q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q), nq = min(max(__ldg(a.cu_q + b + 1), q0), a.total_q) - q0;
+        return ((min(nq, a.max_q) + kTile - 1) / kTile * a.group + 1) / 2;
+    }
+    // by a whole warp; false: there are no more
+    __device__ bool find(const PrefillArgs& a, int n, int& b, int& h) {
+        const int lane = threadIdx.x & 31;
+        while (n >= before + here) {
+            if (level == 0) return false;
+            before += here;
+            --level;
+            int count = 0;
+            for (int b0 = 0; b0 < a.B; b0 += 32) count += __popc(__ballot_sync(0xffffffffu, b0 + lane < a.B && pairs_of(a, b0 + lane) > level));
+            here = count * a.heads;
+        }
+        const int left = n - before;
+        int which = left / a.heads;        // of the sequences that have this level
+        h = left - which * a.heads;
+        for (int b0 = 0;; b0 += 32) {
+            const uint32_t some = __ballot_sync(0xffffffffu, b0 + lane < a.B && pairs_of(a, b0 + lane) > level);
+            if (which < __popc(some)) {
+                b = b0 + __fns(some, 0, which + 1);
+                return true;
+            }
+            which -= __popc(some);
+        }
+    }
 };
+// A role's way through the items: its slot in the queue and the parity of its use
+struct Queue {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == kItems) { slot = 0; phase ^= 1u; }
+    }
+};
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Two fp32 values in a register pair
+__device__ __forceinline__ unsigned long long pair_of(float x, float y) {
+    unsigned long long d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+    return d;
+}
+__device__ __forceinline__ void halves(unsigned long long v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constant__ CUtensorMap km, const __grid_constant__ CUtensorMap vm,
@@ -222,39 +316,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (2 + kRing) * BYTES);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
     volatile uint32_t* gave_up = tmem_slot + 1;
+    volatile Item* items = reinterpret_cast<volatile Item*>(tmem_slot + 4);
     const uint32_t bar0 = smem_u32(bars), smem0 = smem_u32(smem);
     auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
+    if (tid == 0) {
+        auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
+        // (weights and results: a warpgroup's four warps; items: the MMA thread, the tail's warp and both warpgroups)
+        for (int i = 0; i < kNumBars; ++i) init(i, (i >= kBarWeights && i < kBarDone) || (i >= kBarResults && i < kBarTail) ? 4 : i >= kBarItemFree && i < kBarDrain ? 10 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        gave_up[0] = gave_up[1] = 0;
+    }
     grid_dependency_wait();
-    // ---- this CTA's tiles ----------------------------------------------------------------------------------------------------------------------
-    const int b = blockIdx.x / a.heads, h = blockIdx.x - b * a.heads, pair = gridDim.y - 1 - blockIdx.y;
-    const int q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q), nq = min(max(__ldg(a.cu_q + b + 1), q0), a.total_q) - q0;
-    const int k0 = min(max(__ldg(a.cu_k + b), 0), a.total_k), nk = min(max(__ldg(a.cu_k + b + 1), k0), a.total_k) - k0;
-    const int shift = nk - nq, count = (nq + kTile - 1) / kTile * a.group;
-    if (2 * pair >= count) return;
-    auto tile_of = [&](int i) {
-        Tile t;
-        const int n = 2 * pair + i, blk = n / a.group;
-        t.head = h * a.group + (n - blk * a.group);
-        t.row0 = blk * kTile;
-        const int sees = a.causal ? min(nk, min(t.row0 + kTile, nq) + shift) : nk;
-        t.tiles = n < count ? (max(sees, 0) + kTile - 1) / kTile : 0;
-        return t;
-    };
-    const Tile ta = tile_of(0), tb = tile_of(1);
-    const int most = max(ta.tiles, tb.tiles);
-    const bool tail = most > 0 && most * kTile > nk;          // the last tile of keys reaches behind the sequence
-
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(tmem_slot)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    if (tid == 0) {
-        auto init = [&](int i, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar(i)), "r"(n) : "memory"); };
-        for (int i = 0; i < kNumBars; ++i) init(i, i == kBarWeights || i == kBarWeights + 1 ? 4 : 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        *gave_up = 0;
     }
     fence_before();
     __syncthreads();
@@ -262,48 +339,118 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
     grid_launch_dependents();              // (with tensor memory in hand: a kernel that waits for this one may want some too)
     const uint32_t tmem = *tmem_slot;
     const uint32_t limit = a.wait_limit;
+    auto item_at = [&](int slot) {
+        Item it;
+        const volatile int* from = reinterpret_cast<const volatile int*>(items + slot);
+        int* to = reinterpret_cast<int*>(&it);
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) to[i] = from[i];
+        return it;
+    };
 
     if (warp >= kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
         if (warp == kLoadWarp) {
-            // ---- loads: the query tiles, then keys and values of tile after tile ---------------------------------------------------------------------------
-            int issued = 0;
+            // ---- items and loads: keys 0, the query tiles, values 0, keys 1, .. ----------------------------------------------------------------------------
+            Queue queue;
+            Walk walk;
+            walk.before = walk.here = 0;
+            walk.level = ((min(a.max_q, a.total_q) + kTile - 1) / kTile * a.group + 1) / 2;
+            int kv = 0, used[2] = {0, 0};                     // tiles of keys and values; items that had the query tile
+            uint32_t tails = 0, parity = 0;                   // a bit for each slot: its last load was announced to the tail's warp; the parity of such uses
             bool ok = true;
-            if (lane == 0 && !a.test) {
-                for (int i = 0; i < 2; ++i) {
-                    const Tile& t = i == 0 ? ta : tb;
-                    if (t.tiles == 0) continue;
-                    expect(bar(kBarQ + i), BYTES);
-                    for (int s = 0; s < HALVES; ++s) tma_load(smem0 + i * BYTES + s * (kTile * 128), &qm, 64 * s, t.head, q0 + t.row0, bar(kBarQ + i));
+            for (int round = 0; ok; ++round) {
+                const int n = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+                Item it;
+                int b = 0, h = 0;
+                const bool some = walk.find(a, n, b, h);
+                if (some) {
+                    it.q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q);
+                    it.nq = min(max(__ldg(a.cu_q + b + 1), it.q0), a.total_q) - it.q0;
+                    it.k0 = min(max(__ldg(a.cu_k + b), 0), a.total_k);
+                    it.nk = min(max(__ldg(a.cu_k + b + 1), it.k0), a.total_k) - it.k0;
+                    it.h = h;
+                    it.kv0 = kv;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int count = (min(it.nq, a.max_q) + kTile - 1) / kTile * a.group, at = 2 * walk.level + i, blk = at / a.group;
+                        it.t[i].head = at < count ? h * a.group + (at - blk * a.group) : -1;
+                        it.t[i].row0 = blk * kTile;
+                        const int sees = a.causal ? min(it.nk, min(it.t[i].row0 + kTile, it.nq) + it.nk - it.nq) : it.nk;
+                        it.t[i].tiles = at < count ? (max(sees, 0) + kTile - 1) / kTile : 0;
+                    }
+                } else {
+                    it.q0 = it.k0 = it.nk = it.h = it.kv0 = 0;
+                    it.nq = -1;
+                    it.t[0].head = it.t[0].row0 = it.t[0].tiles = it.t[1].head = it.t[1].row0 = it.t[1].tiles = 0;
                 }
-                for (int n = 0; n < 2 * most && ok; ++n) {
-                    const int slot = n % kRing;
-                    ok = wait_alone(bar(kBarEmpty + slot), (uint32_t)(n / kRing & 1) ^ 1u, gave_up, limit);
-                    if (!ok) break;
-                    expect(bar(kBarFull + slot), BYTES);
-                    for (int s = 0; s < HALVES; ++s)
-                        tma_load(smem0 + (2 + slot) * BYTES + s * (kTile * 128), n & 1 ? &vm : &km, 64 * s, h, k0 + (n >> 1) * kTile, bar(kBarFull + slot));
-                    ++issued;
+                ok = wait_warp(bar(kBarItemFree + queue.slot), queue.phase ^ 1u, gave_up, limit);
+                if (!ok) break;
+                if (lane == 0) {
+                    volatile int* to = reinterpret_cast<volatile int*>(items + queue.slot);
+                    const int* from = reinterpret_cast<const int*>(&it);
+#pragma unroll
+                    for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) to[i] = from[i];
+                    arrive(bar(kBarItem + queue.slot));
                 }
+                queue.next();
+                if (!some) break;
+                const int most = it.most();
+                if (lane == 0 && !a.test) {
+                    auto load_q = [&](int i) {
+                        if (it.t[i].tiles == 0) return true;
+                        if (!wait_alone(bar(kBarQFree + i), (uint32_t)(used[i] & 1) ^ 1u, gave_up, limit)) return false;
+                        ++used[i];
+                        expect(bar(kBarQ + i), BYTES);
+                        for (int s = 0; s < HALVES; ++s) tma_load(smem0 + i * BYTES + s * (kTile * 128), &qm, 64 * s, it.t[i].head, it.q0 + it.t[i].row0, bar(kBarQ + i));
+                        return true;
+                    };
+                    for (int m = 0; m < 2 * most && ok; ++m) {
+                        if (m == 1) ok = load_q(0) && load_q(1);
+                        const int slot = kv % kRing;
+                        if (ok) ok = wait_alone(bar(kBarEmpty + slot), (uint32_t)(kv / kRing & 1) ^ 1u, gave_up, limit);
+                        if (!ok) break;
+                        const bool tail = m == 2 * most - 1 && it.tail();
+                        const int to = tail ? kBarTail + slot : kBarFull + slot;
+                        expect(bar(to), BYTES);
+                        for (int s = 0; s < HALVES; ++s) tma_load(smem0 + (2 + slot) * BYTES + s * (kTile * 128), m & 1 ? &vm : &km, 64 * s, it.h, it.k0 + (m >> 1) * kTile, bar(to));
+                        tails = tail ? tails | 1u << slot : tails & ~(1u << slot);
+                        parity ^= (uint32_t)tail << slot;
+                        ++kv;
+                    }
+                }
+                kv = __shfl_sync(0xffffffffu, kv, 0);
+                ok = __all_sync(0xffffffffu, ok);
             }
-            ok = __all_sync(0xffffffffu, ok);
-            issued = __shfl_sync(0xffffffffu, issued, 0);
-            if (ok && tail && !a.test) {
-                // V rows behind the sequence: zeros
-                const int n = 2 * most - 1, slot = n % kRing;
-                if (wait_warp(bar(kBarFull + slot), (uint32_t)(n / kRing) & 1u, gave_up, limit)) {
-                    for (int i = (nk - (most - 1) * kTile) * 8 + lane; i < kTile * 8; i += 32)
-                        for (int s = 0; s < HALVES; ++s) *reinterpret_cast<uint4*>(smem + (2 + slot) * BYTES + s * (kTile * 128) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive(bar(kBarTail));
-                }
-            }
-            if (*gave_up) {
+            if (*gave_up && lane == 0) {
                 // what is on its way lands before the CTA leaves
                 for (int i = 0; i < 2; ++i)
-                    if ((i == 0 ? ta : tb).tiles != 0 && !a.test) poll(bar(kBarQ + i), 0, nullptr, 0xffffffffu);
-                for (int n = max(0, issued - kRing); n < issued; ++n) poll(bar(kBarFull + n % kRing), (uint32_t)(n / kRing) & 1u, nullptr, 0xffffffffu);
+                    if (used[i] > 0) poll(bar(kBarQ + i), (uint32_t)(used[i] - 1) & 1u, nullptr, 0xffffffffu);
+                for (int n = max(0, kv - kRing); n < kv; ++n) {
+                    const int slot = n % kRing;
+                    if (tails >> slot & 1u) poll(bar(kBarTail + slot), (parity >> slot & 1u) ^ 1u, nullptr, 0xffffffffu);
+                    else poll(bar(kBarFull + slot), (uint32_t)(n / kRing) & 1u, nullptr, 0xffffffffu);
+                }
+            }
+            __syncwarp();
+        } else if (warp == kTailWarp) {
+            // ---- V rows behind a sequence: zeros.  Such a tile is announced to this warp, which then announces it to the MMAs --------------------------------------
+            uint32_t parity = 0;                              // a bit for each slot
+            for (Queue queue;; queue.next()) {
+                if (!wait_warp(bar(kBarItem + queue.slot), queue.phase, gave_up, limit)) break;
+                const Item it = item_at(queue.slot);
+                __syncwarp();
+                if (lane == 0) arrive(bar(kBarItemFree + queue.slot));
+                if (it.nq < 0) break;
+                if (!it.tail()) continue;
+                const int n = it.kv0 + 2 * it.most() - 1, slot = n % kRing;
+                if (!wait_warp(bar(kBarTail + slot), parity >> slot & 1u, gave_up, limit)) break;
+                parity ^= 1u << slot;
+                for (int i = (it.nk - (it.most() - 1) * kTile) * 8 + lane; i < kTile * 8; i += 32)
+                    for (int s = 0; s < HALVES; ++s) *reinterpret_cast<uint4*>(smem + (2 + slot) * BYTES + s * (kTile * 128) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive(bar(kBarFull + slot));
             }
         } else if (warp == kMmaWarp) {
             // ---- MMAs ------------------------------------------------------------------------------------------------------------------------------
@@ -311,9 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 constexpr uint32_t kTypes = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u);
                 constexpr uint32_t kQK = kTypes | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
                 constexpr uint32_t kPV = kTypes | (1u << 16) | (uint32_t)(D >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
-                bool ok = true;
-                auto scores = [&](int i, int j) {                 // tile i times keys j
-                    const int slot = 2 * j % kRing;
+                auto scores = [&](int i, int slot) {          // query tile i times the keys of a slot
                     const uint64_t q = rows_desc(smem0 + i * BYTES), k = rows_desc(smem0 + (2 + slot) * BYTES);
 #pragma unroll
                     for (int s = 0; s < D / 16; ++s) {
@@ -322,44 +467,62 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                     }
                     commit(bar(kBarScores + i));
                 };
-                auto products = [&](int i, int j) {
-                    const int slot = (2 * j + 1) % kRing;
+                auto products = [&](int i, int slot, int half, bool first) {
                     const uint64_t v = columns_desc(smem0 + (2 + slot) * BYTES);
 #pragma unroll
-                    for (int s = 0; s < kTile / 16; ++s)
-                        mma_ts(tmem + kResults + i * kTile, tmem + kScores + i * kTile + 8 * s, v + (uint64_t)(s * (2048 >> 4)), kPV, j != 0 || s != 0);
+                    for (int s = 0; s < kTile / 32; ++s) {
+                        const int at = half * (kTile / 32) + s;
+                        mma_ts(tmem + kResults + i * kTile, tmem + kScores + i * kTile + 8 * at, v + (uint64_t)(at * (2048 >> 4)), kPV, !first || s != 0);
+                    }
                 };
                 auto full = [&](int n) { return wait_alone(bar(kBarFull + n % kRing), (uint32_t)(n / kRing) & 1u, gave_up, limit); };
-                if (most > 0) {
-                    ok = full(0);
-                    for (int i = 0; i < 2 && ok; ++i) {
-                        if ((i == 0 ? ta : tb).tiles == 0) continue;
-                        ok = wait_alone(bar(kBarQ + i), 0, gave_up, limit);
-                        fence_after();
-                        if (ok) scores(i, 0);
-                    }
-                    if (ok) commit(bar(kBarEmpty));
-                }
-                for (int j = 0; j < most && ok; ++j) {
-                    for (int i = 0; i < 2 && ok; ++i) {
-                        const int tiles = (i == 0 ? ta : tb).tiles;
-                        if (j >= tiles) continue;
-                        ok = full(2 * j + 1);
-                        if (ok && tail && j == most - 1) ok = wait_alone(bar(kBarTail), 0, gave_up, limit);
-                        if (ok) ok = wait_alone(bar(kBarWeights + i), (uint32_t)j & 1u, gave_up, limit);
-                        if (!ok) break;
-                        fence_after();
-                        products(i, j);
-                        if (j + 1 == tiles) {
-                            commit(bar(kBarDone + i));
-                        } else {
-                            ok = full(2 * j + 2);
-                            if (ok) scores(i, j + 1);
-                        }
-                    }
+                int used[2] = {0, 0}, done[2] = {0, 0};       // items that had the query tile, tiles of weights taken
+                bool ok = true;
+                for (Queue queue; ok; queue.next()) {
+                    ok = wait_alone(bar(kBarItem + queue.slot), queue.phase, gave_up, limit);
                     if (!ok) break;
-                    commit(bar(kBarEmpty + (2 * j + 1) % kRing));
-                    if (j + 1 < most) commit(bar(kBarEmpty + (2 * j + 2) % kRing));
+                    const Item it = item_at(queue.slot);
+                    arrive(bar(kBarItemFree + queue.slot));
+                    if (it.nq < 0) break;
+                    const int most = it.most();
+                    if (most == 0) continue;
+                    ok = full(it.kv0);
+                    for (int i = 0; i < 2 && ok; ++i) {
+                        if (it.t[i].tiles == 0) continue;
+                        ok = wait_alone(bar(kBarQ + i), (uint32_t)used[i] & 1u, gave_up, limit);
+                        fence_after();
+                        if (ok) scores(i, it.kv0 % kRing);
+                        if (it.t[i].tiles == 1) commit(bar(kBarQFree + i));
+                    }
+                    if (ok) commit(bar(kBarEmpty + it.kv0 % kRing));
+                    for (int j = 0; j < most && ok; ++j) {
+                        const int v = it.kv0 + 2 * j + 1;
+                        for (int i = 0; i < 2 && ok; ++i) {
+                            const int tiles = it.t[i].tiles;
+                            if (j >= tiles) continue;
+                            ok = full(v);
+                            // (the results of the item before have been read)
+                            if (ok && j == 0) ok = wait_alone(bar(kBarResults + i), (uint32_t)(used[i] & 1) ^ 1u, gave_up, limit);
+                            for (int half = 0; half < 2 && ok; ++half) {
+                                ok = wait_alone(bar(kBarWeights + 2 * i + half), (uint32_t)done[i] & 1u, gave_up, limit);
+                                fence_after();
+                                if (ok) products(i, v % kRing, half, j == 0 && half == 0);
+                            }
+                            if (!ok) break;
+                            ++done[i];
+                            if (j + 1 == tiles) {
+                                commit(bar(kBarDone + i));
+                            } else {
+                                ok = full(v + 1);
+                                if (ok) scores(i, (v + 1) % kRing);
+                                if (j + 2 == tiles) commit(bar(kBarQFree + i));
+                            }
+                        }
+                        if (!ok) break;
+                        commit(bar(kBarEmpty + v % kRing));
+                        if (j + 1 < most) commit(bar(kBarEmpty + (v + 1) % kRing));
+                    }
+                    for (int i = 0; i < 2; ++i) used[i] += it.t[i].tiles != 0;
                 }
                 // (MMAs in flight read shared memory, and their commits arrive there)
                 commit(bar(kBarDrain));
@@ -371,103 +534,126 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRowRegs));
         // ---- softmax: a thread to a row -------------------------------------------------------------------------------------------------------------
         const int i = warp >> 2;
-        const Tile t = i == 0 ? ta : tb;
-        const int row = t.row0 + (tid & 127);
-        const int sees = a.causal ? max(min(nk, row + 1 + shift), 0) : nk;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, sc = tmem + lanes + kScores + i * kTile, res = tmem + lanes + kResults + i * kTile;
-        float off = kNone, sum = 0.0f;
-        bool ok = true;
-        for (int j = 0; j < t.tiles; ++j) {
-            ok = wait_warp(bar(kBarScores + i), (uint32_t)j & 1u, gave_up, limit);
-            if (!ok) break;
-            fence_after();
-            uint32_t s[kTile];
+        const unsigned long long scale2 = pair_of(a.scale, a.scale);
+        int done = 0, used = 0;                               // tiles of scores, items
+        for (Queue queue;; queue.next()) {
+            if (!wait_warp(bar(kBarItem + queue.slot), queue.phase, gave_up, limit)) break;
+            const int q0 = items[queue.slot].q0, nq = items[queue.slot].nq, k0 = items[queue.slot].k0, nk = items[queue.slot].nk, h = items[queue.slot].h;
+            const int head = items[queue.slot].t[i].head, row0 = items[queue.slot].t[i].row0, tiles = items[queue.slot].t[i].tiles;
+            __syncwarp();
+            if (lane == 0) arrive(bar(kBarItemFree + queue.slot));
+            if (nq < 0) break;
+            if (head < 0) continue;
+            const int row = row0 + (tid & 127), shift = nk - nq;
+            const int sees = a.causal ? max(min(nk, row + 1 + shift), 0) : nk;
+            float off = kNone;
+            unsigned long long sums[2] = {0ull, 0ull};
+            bool ok = true;
+            for (int j = 0; j < tiles; ++j, ++done) {
+                ok = wait_warp(bar(kBarScores + i), (uint32_t)done & 1u, gave_up, limit);
+                if (!ok) break;
+                fence_after();
+                uint32_t s[kTile];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, sc + 32 * c);
+                for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, sc + 32 * c);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
-            const int left = sees - j * kTile;
-            if (__any_sync(0xffffffffu, left < kTile)) {
+                for (int c = 0; c < 4; ++c) tmem_ld_wait32(s + 32 * c);
+                const int left = sees - j * kTile;
+                if (__any_sync(0xffffffffu, left < kTile)) {
 #pragma unroll
-                for (int c = 0; c < kTile; ++c)
-                    if (c >= left) s[c] = 0xff800000u;
-            }
-            float top = -INFINITY;
+                    for (int c = 0; c < kTile; ++c)
+                        if (c >= left) s[c] = 0xff800000u;
+                }
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < kTile; ++c) top = fmaxf(top, __uint_as_float(s[c]));
-            if (__any_sync(0xffffffffu, fmaf(top, a.scale, off) > kRise)) {
-                const float to = top == -INFINITY ? off : fminf(off, kBase - top * a.scale);
-                const float by = exp2_approx(to - off);
-                off = to;
-                sum *= by;
-                if (j > 0) {                                  // (the products so far are done: the scores came behind them)
+                for (int c = 0; c < kTile; c += 2) tops[c / 2 % 4] = max3(tops[c / 2 % 4], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+                const float top = max3(fmaxf(tops[0], tops[1]), tops[2], tops[3]);
+                if (__any_sync(0xffffffffu, fmaf(top, a.scale, off) > kRise)) {
+                    const float to = top == -INFINITY ? off : fminf(off, kBase - top * a.scale);
+                    const float by = exp2_approx(to - off);
+                    off = to;
+                    const unsigned long long by2 = pair_of(by, by);
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32(o, res + 32 * c);
-                        tmem_ld_wait32(o);
+                    for (int k = 0; k < 2; ++k) sums[k] = fma2(sums[k], by2, 0ull);
+                    if (j > 0) {                              // (the products so far are done: the scores came behind them)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                        tmem_st32(res + 32 * c, o);
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32(o, res + 32 * c);
+                            tmem_ld_wait32(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                            tmem_st32(res + 32 * c, o);
+                        }
                     }
                 }
-            }
+                const unsigned long long off2 = pair_of(off, off);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t w[32];
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t w[32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float lo = exp2_approx(fmaf(__uint_as_float(s[64 * c + 2 * e]), a.scale, off)), hi = exp2_approx(fmaf(__uint_as_float(s[64 * c + 2 * e + 1]), a.scale, off));
-                    sum += lo + hi;
-                    w[e] = pack<BF16>(lo, hi);
+                    for (int e = 0; e < 32; ++e) {
+                        float lo, hi;
+                        halves(fma2(pair_of(__uint_as_float(s[64 * c + 2 * e]), __uint_as_float(s[64 * c + 2 * e + 1])), scale2, off2), lo, hi);
+                        lo = exp2_approx(lo);
+                        hi = exp2_approx(hi);
+                        sums[e & 1] = add2(sums[e & 1], pair_of(lo, hi));
+                        w[e] = pack<BF16>(lo, hi);
+                    }
+                    tmem_st32(sc + 32 * c, w);
+                    tmem_st_wait();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive(bar(kBarWeights + 2 * i + c));
                 }
-                tmem_st32(sc + 32 * c, w);
             }
-            tmem_st_wait();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive(bar(kBarWeights + i));
-        }
-        if (2 * pair + i < count && ok) {
-            uint8_t* out = a.out + 2 * ((long long)(q0 + row) * a.ldo + (long long)t.head * D);
-            const float r = sum == 0.0f ? 0.0f : 1.0f / sum;
+            if (!ok) break;
+            float x, y;
+            halves(add2(sums[0], sums[1]), x, y);
+            const float sum = x + y, r = sum == 0.0f ? 0.0f : 1.0f / sum;
+            uint8_t* out = a.out + 2 * ((long long)(q0 + row) * a.ldo + (long long)head * D);
             float check = 0.0f;
-            if (t.tiles > 0) {
-                ok = wait_warp(bar(kBarDone + i), 0, gave_up, limit);
+            if (tiles > 0) {
+                if (!wait_warp(bar(kBarDone + i), (uint32_t)used & 1u, gave_up, limit)) break;
+                ++used;
                 fence_after();
             }
-            if (ok) {
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    if (t.tiles > 0) {
-                        tmem_ld32(o, res + 32 * c);
-                        tmem_ld_wait32(o);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = 0u;
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                if (tiles > 0) {
+                    tmem_ld32(o, res + 32 * c);
+                    tmem_ld_wait32(o);
+                    if (c == D / 32 - 1) {                    // the next item's products may come
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive(bar(kBarResults + i));
                     }
+                } else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float lo = __uint_as_float(o[2 * e]) * r, hi = __uint_as_float(o[2 * e + 1]) * r;
-                        check = fmaf(0.0f, lo, fmaf(0.0f, hi, check));
-                        o[e] = pack<BF16>(lo, hi);
-                    }
-                    if (row < nq) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out)[4 * c + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                    }
+                    for (int e = 0; e < 32; ++e) o[e] = 0u;
                 }
-                uint32_t again = __ballot_sync(0xffffffffu, check != 0.0f && row < nq);      // (NaN: something was not finite)
-                while (again != 0) {
-                    const int l = __ffs(again) - 1;
-                    again &= again - 1;
-                    const int rr = t.row0 + 32 * (warp & 3) + l;
-                    __syncwarp();                             // (the row's own stores come first)
-                    row_alone<D, BF16>(a.q + 2 * ((long long)(q0 + rr) * a.ldq + (long long)t.head * D), a.k + 2 * ((long long)k0 * a.ldk + (long long)h * D),
-                                       a.v + 2 * ((long long)k0 * a.ldv + (long long)h * D), a.ldk, a.ldv, a.causal ? max(min(nk, rr + 1 + shift), 0) : nk, a.scale,
-                                       a.out + 2 * ((long long)(q0 + rr) * a.ldo + (long long)t.head * D));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float lo = __uint_as_float(o[2 * e]) * r, hi = __uint_as_float(o[2 * e + 1]) * r;
+                    check = fmaf(0.0f, lo, fmaf(0.0f, hi, check));
+                    o[e] = pack<BF16>(lo, hi);
                 }
+                if (row < nq) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(out)[4 * c + e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                }
+            }
+            uint32_t again = __ballot_sync(0xffffffffu, check != 0.0f && row < nq);          // (NaN: something was not finite)
+            while (again != 0) {
+                const int l = __ffs(again) - 1;
+                again &= again - 1;
+                const int rr = row0 + 32 * (warp & 3) + l;
+                __syncwarp();                                 // (the row's own stores come first)
+                row_alone<D, BF16>(a.q + 2 * ((long long)(q0 + rr) * a.ldq + (long long)head * D), a.k + 2 * ((long long)k0 * a.ldk + (long long)h * D),
+                                   a.v + 2 * ((long long)k0 * a.ldv + (long long)h * D), a.ldk, a.ldv, a.causal ? max(min(nk, rr + 1 + shift), 0) : nk, a.scale,
+                                   a.out + 2 * ((long long)(q0 + rr) * a.ldo + (long long)head * D), gave_up + 1);
             }
         }
     }
@@ -533,13 +719,17 @@ int run_prefill(const void* q, long long ldq, const void* k, long long ldk, cons
     // strides of a tensor map are below 2^40 bytes; coordinates and row numbers 32 bits; blocks of a launch
     const long long most_ld = 1LL << 38;
     const int group = n_q_heads / heads;
-    const long long pairs = (((long long)max_q + kTile - 1) / kTile * group + 1) / 2;
-    if (ldq > most_ld || ldk > most_ld || ldv > most_ld || total_q > 0x3fffffff || total_k > 0x3fffffff || pairs > 0xffff || (long long)B * heads > 0x7fffffffLL) return ELUTQ_ERR_SHAPE;
+    // (items are counted in 32 bits: at most one more for each sequence than the queries' tiles have pairs)
+    const long long blocks = ((long long)(max_q < total_q ? max_q : total_q) + kTile - 1) / kTile, pairs = (blocks * group + 1) / 2;
+    const long long total_items = (((long long)total_q / kTile + B) * group / 2 + B) * heads;
+    if (ldq > most_ld || ldk > most_ld || ldv > most_ld || total_q > 0x3fffffff || total_k > 0x3fffffff || total_items > 0x3fffffffLL || total_items < 0) return ELUTQ_ERR_SHAPE;
     PrefillArgs a;
     a.cu_q = cu_q; a.cu_k = cu_k;
     a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v;
     a.out = (uint8_t*)out;
     a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
+    a.B = B;
+    a.max_q = (int)((((long long)max_q + kTile - 1) / kTile * kTile < 0x7fffff00LL) ? ((long long)max_q + kTile - 1) / kTile * kTile : 0x7fffff00LL);
     a.total_q = total_q; a.total_k = total_k;
     a.heads = heads;
     a.group = group;
@@ -553,7 +743,8 @@ int run_prefill(const void* q, long long ldq, const void* k, long long ldk, cons
     int ce = rows_map(&qm, q, total_q, n_q_heads, D, ldq, bf16);
     if (ce == 0) ce = rows_map(&km, k, total_k, heads, D, ldk, bf16);
     if (ce == 0) ce = rows_map(&vm, v, total_k, heads, D, ldv, bf16);
-    const dim3 grid((unsigned)(B * heads), (unsigned)pairs);
+    const long long items = pairs * B * heads;
+    const dim3 grid((unsigned)(items < device_sm_count() ? items : device_sm_count()));
     if (ce == 0)
         ce = D == 128 ? (bf16 ? launch_prefill<128, true>(qm, km, vm, a, grid, (cudaStream_t)stream) : launch_prefill<128, false>(qm, km, vm, a, grid, (cudaStream_t)stream))
                       : (bf16 ? launch_prefill<64, true>(qm, km, vm, a, grid, (cudaStream_t)stream) : launch_prefill<64, false>(qm, km, vm, a, grid, (cudaStream_t)stream));

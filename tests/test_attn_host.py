@@ -117,7 +117,7 @@ def test_arguments_of_a_prompt(entry, more):
                dict(flags=2), dict(scale=0.0), dict(scale=float("nan"))):
         assert prefill(entry, more, **kw) == -1, kw
     assert prefill(entry, more, D=96) == -5
-    for kw in (dict(n=5, ldq=1024, ldo=1024), dict(ldq=504), dict(ldk=248), dict(ldv=128), dict(ldo=504), dict(total_q=1 << 30), dict(ldk=1 << 39), dict(max_q=2 ** 31 - 1)):
+    for kw in (dict(n=5, ldq=1024, ldo=1024), dict(ldq=504), dict(ldk=248), dict(ldv=128), dict(ldo=504), dict(total_q=1 << 30), dict(ldk=1 << 39), dict(B=1 << 30)):
         assert prefill(entry, more, **kw) == -2, kw
     for kw in (dict(q=72), dict(ldq=516), dict(k=130), dict(ldk=257), dict(v=264), dict(out=520), dict(cu_q=9), dict(cu_k=18)):
         assert prefill(entry, more, **kw) == -3, kw
