@@ -539,9 +539,10 @@ int elutq_kv_read(const elutq_kv_cache* cache, const int* table, long long ld_ta
  * out = softmax(scale * q K^T) V; new token i sees tokens 0 .. lens[b] - new_tokens + i.  A row that sees nothing is zeros.  What lies in pages behind that is not
  * looked at, whatever it is; tokens on a page outside the cache count as masked.  scale > 0.  Products of 16-bit values, fp32 sums; the weights of a row are rounded to
  * 16 bits (relative to 2^14 times the least that still counts) for the product with V.
- * The workspace belongs to one call at a time (calls of one stream follow one another) and needs no initialisation.  Results are the same bit for bit in every call.
+ * The workspace belongs to one call at a time (calls of one stream follow one another) and needs no initialisation; short tables need none (0 bytes: it may be NULL).
+ * Results are the same bit for bit in every call of the same sizes.
  */
-int elutq_attn_decode_workspace_bytes(int n_q_heads, int heads, int head_dim, int new_tokens, size_t* bytes);
+int elutq_attn_decode_workspace_bytes(const elutq_kv_cache* cache, int pages, int B, int new_tokens, int n_q_heads, size_t* bytes);
 int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq, void* out, long long ldo, const int* table, long long ld_table, int pages,
                       const int* lens, int B, int new_tokens, int n_q_heads, float scale, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -93,7 +93,7 @@ _SIGNATURES = {
     "elutq_kv_write": (c_int, [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int,
                                c_void_p, c_void_p, c_void_p, c_int, c_int, c_uint, c_void_p]),
     "elutq_kv_read": (c_int, [c_void_p, c_void_p, c_longlong, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p]),
-    "elutq_attn_decode_workspace_bytes": (c_int, [c_int, c_int, c_int, c_int, ctypes.POINTER(c_size_t)]),
+    "elutq_attn_decode_workspace_bytes": (c_int, [c_void_p, c_int, c_int, c_int, c_int, c_void_p]),
     "elutq_attn_decode": (c_int, [c_void_p, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_int, c_int, c_int, c_float,
                                   c_void_p, c_size_t, c_void_p]),
     "elutq_attn_prefill": (c_int, [c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_void_p, c_longlong, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_float, c_uint,
@@ -456,34 +456,44 @@ def elutq_rope_table(n_pos: int, rot_dim: int, theta: float = 10000.0, scaling: 
     return table
 
 
-def _rows(where: str, name: str, t, n: int, D: int, dtype, device: int, rows: int = -1) -> int:
+_ATTENTION = None
+
+
+def _attention():
+    """What a call of these entries needs, looked up once: torch, the current device, a device's current stream, and the C functions."""
+    global _ATTENTION
+    if _ATTENTION is None:
+        torch, _, current, raw = _torch()
+        L = lib()
+        _ATTENTION = (torch, torch.int32, torch.float32, current, raw, L.elutq_kv_write, L.elutq_kv_read, L.elutq_attn_decode, L.elutq_attn_decode_workspace_bytes)
+    return _ATTENTION
+
+
+def _rows(where: str, name: str, t, n: int, D: int, dtype, device: int, rows: int) -> int:
     """Distance between the tokens of [rows, n, D] with heads side by side, in elements."""
-    shape = t.shape
-    if len(shape) != 3 or shape[1] != n or shape[2] != D or t.dtype is not dtype or t.get_device() != device or (rows >= 0 and shape[0] != rows):
-        _refuse(where, f"{name}: {'' if rows < 0 else rows} tokens of {n} heads of {D} values of {dtype} wanted", t)
-    ld, head, one = t.stride()
-    if one != 1 or (n > 1 and head != D):
-        _refuse(where, f"{name}: the heads of a token side by side wanted", t)
-    return ld if shape[0] > 1 else n * D
+    ld, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != (rows, n, D) or t.dtype is not dtype or t.get_device() != device or one != 1 or (head != D and n > 1):
+        _refuse(where, f"{name}: {rows} tokens of {n} heads of {D} values of {dtype}, the heads of a token side by side, wanted", t)
+    return ld if rows > 1 else n * D
 
 
-def _table(where: str, table, B: int, device: int) -> int:
-    """Distance between the rows of a table of pages int32 [B, pages]."""
-    shape = table.shape
-    if len(shape) != 2 or shape[0] != B or table.dtype is not _TORCH[0].int32 or table.get_device() != device or (shape[1] > 1 and table.stride(1) != 1):
-        _refuse(where, f"table: int32, {B} rows of pages wanted", table)
-    return table.stride(0) if B > 1 else shape[1]
+def _pages(where: str, table, device: int):
+    """(sequences, pages, distance between the rows) of a table of pages int32 [B, pages]."""
+    B, pages = table.shape if table.dim() == 2 else (0, 0)
+    if B < 1 or table.dtype is not _TORCH[0].int32 or table.get_device() != device or (pages > 1 and table.stride(1) != 1):
+        _refuse(where, "table: int32, a row of pages for each sequence wanted", table)
+    return B, pages, table.stride(0) if B > 1 else pages
 
 
 def elutq_kv_write(cache: KvCache, k, v, slots, q=None, q_out=None, positions=None, rope=None, flags: int = 0, k_out=None, stream=None) -> None:
     """k, v [tokens, heads, head_dim] into the cache, q and k rotated; slots, positions int32 [tokens], rope fp32 [n_pos, rot_dim].
     q [tokens, query heads, head_dim] -> q_out; the rotated keys -> k_out, if given."""
     where = "elutq_kv_write"
-    torch, _, current, raw = _torch()
+    _, int32, float32, current, raw, write, _, _, _ = _ATTENTION or _attention()
     d, H, D, dtype, rows = cache.device, cache.heads, cache.head_dim, cache.dtype, k.shape[0]
     if d != current() or (q is None) != (q_out is None) or (rope is not None and (positions is None or rope.dim() != 2)):
         _refuse(where, "q with q_out, and rope [n_pos, rot_dim] with positions wanted", k, q, q_out, rope, positions)
-    ldk, ldv = _rows(where, "k", k, H, D, dtype, d), _rows(where, "v", v, H, D, dtype, d, rows)
+    ldk, ldv = _rows(where, "k", k, H, D, dtype, d, rows), _rows(where, "v", v, H, D, dtype, d, rows)
     n = ldq = ldqo = ldko = n_pos = rot = 0
     if q is not None:
         n = q.shape[1] if q.dim() == 3 else -1
@@ -492,52 +502,66 @@ def elutq_kv_write(cache: KvCache, k, v, slots, q=None, q_out=None, positions=No
         ldko = _rows(where, "k_out", k_out, H, D, dtype, d, rows)
     if rope is not None:
         n_pos, rot = rope.shape
-    _check(lib().elutq_kv_write(cache.address, _ptr(q), ldq, _ptr(q_out), ldqo, n, k.data_ptr(), ldk, _ptr(k_out), ldko, v.data_ptr(), ldv, rows,
-                                _small(where, "slots", slots, torch.int32, rows, d), _small(where, "positions", positions, torch.int32, rows, d),
-                                _small(where, "rope", rope, torch.float32, n_pos * rot, d), n_pos, rot, flags, raw(d) if stream is None else _stream(stream)), where)
+    status = write(cache.address, 0 if q is None else q.data_ptr(), ldq, 0 if q is None else q_out.data_ptr(), ldqo, n, k.data_ptr(), ldk, 0 if k_out is None else k_out.data_ptr(), ldko,
+                   v.data_ptr(), ldv, rows, _small(where, "slots", slots, int32, rows, d), _small(where, "positions", positions, int32, rows, d),
+                   _small(where, "rope", rope, float32, n_pos * rot, d), n_pos, rot, flags, raw(d) if stream is None else _stream(stream))
+    if status != 0:
+        raise ElutqError(status, where)
 
 
 def elutq_kv_read(cache: KvCache, table, first, cu, k_out, v_out, stream=None) -> None:
     """Tokens first[b] .. of every sequence to rows cu[b] .. cu[b+1] of k_out, v_out [rows, heads, head_dim]; table int32 [B, pages], first int32 [B] or None,
     cu int32 [B + 1]."""
     where = "elutq_kv_read"
-    torch, _, current, raw = _torch()
-    d, H, D, dtype, B, rows = cache.device, cache.heads, cache.head_dim, cache.dtype, table.shape[0], k_out.shape[0]
+    _, int32, _, current, raw, _, read, _, _ = _ATTENTION or _attention()
+    d, H, D, dtype, rows = cache.device, cache.heads, cache.head_dim, cache.dtype, k_out.shape[0]
     if d != current():
         _refuse(where, f"a cache on the current device wanted, cuda:{d} given", k_out)
-    ldk, ldv = _rows(where, "k_out", k_out, H, D, dtype, d), _rows(where, "v_out", v_out, H, D, dtype, d, rows)
-    ld = _table(where, table, B, d)
-    _check(lib().elutq_kv_read(cache.address, table.data_ptr(), ld, table.shape[1], _small(where, "first", first, torch.int32, B, d),
-                               _small(where, "cu", cu, torch.int32, B + 1, d), B, rows, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv,
-                               raw(d) if stream is None else _stream(stream)), where)
+    ldk, ldv = _rows(where, "k_out", k_out, H, D, dtype, d, rows), _rows(where, "v_out", v_out, H, D, dtype, d, rows)
+    B, pages, ld = _pages(where, table, d)
+    status = read(cache.address, table.data_ptr(), ld, pages, _small(where, "first", first, int32, B, d), _small(where, "cu", cu, int32, B + 1, d), B, rows,
+                  k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, raw(d) if stream is None else _stream(stream))
+    if status != 0:
+        raise ElutqError(status, where)
 
 
-def elutq_attn_decode_workspace_bytes(n_q_heads: int, heads: int, head_dim: int, new_tokens: int = 1) -> int:
+def elutq_attn_decode_workspace_bytes(cache: KvCache, pages: int, B: int, new_tokens: int, n_q_heads: int) -> int:
     out = c_size_t(0)
-    _check(lib().elutq_attn_decode_workspace_bytes(n_q_heads, heads, head_dim, new_tokens, ctypes.byref(out)), "elutq_attn_decode_workspace_bytes")
+    _check(lib().elutq_attn_decode_workspace_bytes(cache.address, pages, B, new_tokens, n_q_heads, ctypes.addressof(out)), "elutq_attn_decode_workspace_bytes")
     return out.value
 
 
 def elutq_attn_decode(cache: KvCache, q, out, table, lens, new_tokens: int = 1, scale=None, workspace=None, stream=None) -> None:
     """out = attention of q [B * new_tokens, query heads, head_dim], the last tokens of the sequences, over the cache; table int32 [B, pages], lens int32 [B].
-    scale None: head_dim ** -0.5.  workspace None: taken from torch's allocator (give one with a stream that is not torch's current one)."""
+    scale None: head_dim ** -0.5.  workspace None: taken from torch's allocator, if one is needed (give one with a stream that is not torch's current one)."""
     where = "elutq_attn_decode"
-    torch, _, current, raw = _torch()
-    d, D, dtype, B = cache.device, cache.head_dim, cache.dtype, table.shape[0]
+    torch, int32, _, current, raw, _, _, decode, size = _ATTENTION or _attention()
+    d, D, dtype = cache.device, cache.head_dim, cache.dtype
     if d != current() or q.dim() != 3:
         _refuse(where, f"a cache on the current device (cuda:{d} given) and q [tokens, heads, head_dim] wanted", q)
-    n = q.shape[1]
-    ldq, ldo = _rows(where, "q", q, n, D, dtype, d, B * new_tokens), _rows(where, "out", out, n, D, dtype, d, B * new_tokens)
-    ld = _table(where, table, B, d)
+    B, pages, ld = _pages(where, table, d)
+    n, rows = q.shape[1], B * new_tokens
+    ldq, ldo = _rows(where, "q", q, n, D, dtype, d, rows), _rows(where, "out", out, n, D, dtype, d, rows)
+    address = nbytes = 0
     if workspace is None:
-        if stream is not None:
-            _refuse(where, "a stream of one's own needs a workspace of its own", q)
-        workspace = q.new_empty(elutq_attn_decode_workspace_bytes(n, cache.heads, D, new_tokens), dtype=torch.uint8)
+        need = c_size_t(0)
+        status = size(cache.address, pages, B, new_tokens, n, ctypes.byref(need))
+        if status != 0:
+            raise ElutqError(status, where)
+        nbytes = need.value
+        if nbytes != 0:
+            if stream is not None:
+                _refuse(where, f"a stream of one's own needs a workspace of its own: {nbytes} bytes")
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
+            address = workspace.data_ptr()
     elif not workspace.is_contiguous() or workspace.get_device() != d:
         _refuse(where, "workspace wanted", workspace)
-    _check(lib().elutq_attn_decode(cache.address, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, table.shape[1], _small(where, "lens", lens, torch.int32, B, d),
-                                   B, new_tokens, n, D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.nbytes,
-                                   raw(d) if stream is None else _stream(stream)), where)
+    else:
+        address, nbytes = workspace.data_ptr(), workspace.nbytes
+    status = decode(cache.address, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, pages, _small(where, "lens", lens, int32, B, d), B, new_tokens, n,
+                    D ** -0.5 if scale is None else scale, address, nbytes, raw(d) if stream is None else _stream(stream))
+    if status != 0:
+        raise ElutqError(status, where)
 
 
 def _prefill(where: str, q, k, v, out, cu_q, cu_k, max_q, scale, causal, stream, *more) -> None:
@@ -547,7 +571,7 @@ def _prefill(where: str, q, k, v, out, cu_q, cu_k, max_q, scale, causal, stream,
         _refuse(where, "q, k [tokens, heads, head_dim] wanted", q, k)
     (rows, n, D), (keys, H, _) = q.shape, k.shape
     B = cu_q.numel() - 1
-    _check(getattr(lib(), where)(q.data_ptr(), _rows(where, "q", q, n, D, dtype, d), k.data_ptr(), _rows(where, "k", k, H, D, dtype, d), v.data_ptr(), _rows(where, "v", v, H, D, dtype, d, keys),
+    _check(getattr(lib(), where)(q.data_ptr(), _rows(where, "q", q, n, D, dtype, d, rows), k.data_ptr(), _rows(where, "k", k, H, D, dtype, d, keys), v.data_ptr(), _rows(where, "v", v, H, D, dtype, d, keys),
                                  out.data_ptr(), _rows(where, "out", out, n, D, dtype, d, rows), types.get(dtype, -1), _small(where, "cu_q", cu_q, torch.int32, B + 1, d),
                                  _small(where, "cu_k", cu_k, torch.int32, B + 1, d), B, max_q, rows, keys, n, H, D, D ** -0.5 if scale is None else scale,
                                  0 if causal else ATTN_ALL_KEYS, *more, raw(d) if stream is None else _stream(stream)), where)

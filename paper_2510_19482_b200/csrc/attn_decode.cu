@@ -32,6 +32,8 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kLead = 4;
+constexpr long long kMostTokens = 0x7fff0000LL;      // of a sequence (numbers a little behind the last one are formed)
+constexpr int kShortTokens = 128;            // of a warp
 constexpr float kNone = 1e30f;               // offset of a column that has seen no token: any score rises above it
 constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
 
@@ -51,6 +53,7 @@ struct DecodeArgs {
     int4* begun;               // segments that begin in a share and go on in the next ones: sequence, key head and tile of rows, worker, where its parts are (0: none).  For each
                                // segment, or, where there are more of them than shares, for each share
     int by_segment;
+    int split;                 // CTAs of a cluster that have a segment to themselves; 0: shares of the whole
     long long cap;             // wide * page_size: tokens that the table has room for
 };
 
@@ -183,57 +186,63 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
     extern __shared__ __align__(1024) uint8_t smem[];
     // (the warps' parts lie over their rings, which are empty by then)
     float (*s_o)[NC][PAD] = reinterpret_cast<float (*)[NC][PAD]>(smem);
-    __shared__ float s_off[kWarps][NC], s_sum[kWarps][NC];
+    __shared__ float s_off[kWarps][NC], s_sum[kWarps][NC], s_all[2][NC];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * STAGE);
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // ---- this warp's share: units [f0, f1) of [0, total) ----------------------------------------------------------------------------------------
+    // ---- this warp's share: units [f0, f1) of [0, total), or a part of the segment that the cluster has ---------------------------------------------------
     const int each = a.c.heads * a.row_tiles, worker = blockIdx.x * kWarps + warp;
-    const long long total = count_units<TT>(a), share = quotient_of(total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
-    const long long cta0 = blockIdx.x * kWarps * share, cta1 = cta0 + kWarps * share < total ? cta0 + kWarps * share : total;
-    // sequences without a token: zeros
-    for (int e = blockIdx.x; e < a.B; e += gridDim.x)
-        if (length_of(a, e) == 0) {
-            if (a.by_segment)
-                for (int i = tid; i < each; i += kThreads) a.begun[e * each + i] = make_int4(0, 0, 0, 0);
-            for (long long i = tid; i < (long long)a.fresh * a.c.heads * a.group * (D / 8); i += kThreads) {
-                const long long tok = i / (a.c.heads * a.group * (D / 8));
-                reinterpret_cast<uint4*>(a.out + 2 * ((long long)e * a.fresh + tok) * a.ldo)[i - tok * (a.c.heads * a.group * (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
-            }
-        }
-    if (cta0 >= cta1) {                                       // (the whole CTA)
-        if (lane == 0 && !a.by_segment) a.begun[worker] = make_int4(0, 0, 0, 0);
-        return;
-    }
-    // the sequence that the CTA's first unit belongs to: 32 at a time
     int b = 0;
+    long long total = 0, share = 0, cta0 = 0, cta1 = 0, f0 = 0, f1 = 0;
     long long before = 0;                                     // units in front of the sequence
-    for (;; b += 32) {
-        const long long mine = b + lane < a.B ? (long long)units_of<TT>(length_of(a, b + lane)) * each : 0;
-        long long incl = mine;
+    bool joint = true;                                        // all of the CTA's units are of one segment
+    if (a.split != 0) {
+        b = blockIdx.x / a.split / each;
+    } else {
+        total = count_units<TT>(a);
+        share = quotient_of(total + gridDim.x * kWarps - 1, gridDim.x * kWarps);
+        cta0 = blockIdx.x * kWarps * share;
+        cta1 = cta0 + kWarps * share < total ? cta0 + kWarps * share : total;
+        // sequences without a token: zeros
+        for (int e = blockIdx.x; e < a.B; e += gridDim.x)
+            if (length_of(a, e) == 0) {
+                if (a.by_segment)
+                    for (int i = tid; i < each; i += kThreads) a.begun[e * each + i] = make_int4(0, 0, 0, 0);
+                for (long long i = tid; i < (long long)a.fresh * a.c.heads * a.group * (D / 8); i += kThreads) {
+                    const long long tok = i / (a.c.heads * a.group * (D / 8));
+                    reinterpret_cast<uint4*>(a.out + 2 * ((long long)e * a.fresh + tok) * a.ldo)[i - tok * (a.c.heads * a.group * (D / 8))] = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+        if (cta0 >= cta1) {                                   // (the whole CTA)
+            if (lane == 0 && !a.by_segment) a.begun[worker] = make_int4(0, 0, 0, 0);
+            return;
+        }
+        // the sequence that the CTA's first unit belongs to: 32 at a time
+        for (;; b += 32) {
+            const long long mine = b + lane < a.B ? (long long)units_of<TT>(length_of(a, b + lane)) * each : 0;
+            long long incl = mine;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            const uint32_t behind = __ballot_sync(0xffffffffu, before + incl > cta0);
+            if (behind != 0) {
+                const int l = __ffs(behind) - 1;
+                before += __shfl_sync(0xffffffffu, incl - mine, l);
+                b += l;
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
         }
-        const uint32_t behind = __ballot_sync(0xffffffffu, before + incl > cta0);
-        if (behind != 0) {
-            const int l = __ffs(behind) - 1;
-            before += __shfl_sync(0xffffffffu, incl - mine, l);
-            b += l;
-            break;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    bool joint;                                               // all of the CTA's units are of one segment
-    {
         const int units = units_of<TT>(length_of(a, b));
         joint = cta1 <= before + (quotient_of(cta0 - before, units) + 1) * units;
+        f0 = cta0 + warp * share;
+        f1 = f0 + share < cta1 ? f0 + share : cta1;
     }
-    const long long f0 = cta0 + warp * share, f1 = f0 + share < cta1 ? f0 + share : cta1;
 
     // where a lane copies to and reads from.  A piece's place in its row is its number with some bits of the row's number turned, so that the lanes that are served together
     // meet different banks: 16 bits, the same piece of eight rows (ldmatrix); codes, two K rows, or four V rows, of which every second.
@@ -267,11 +276,22 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             ++b;
             continue;
         }
-        const long long at_most = f1 - f, local = (f < cta1 ? f : cta1 - 1) - before;
-        const int seg = (int)quotient_of(local, units);
-        const long long seg0 = before + (long long)seg * units;             // the segment's first unit
-        const int unit0 = (int)(local - (long long)seg * units), unit1 = (int)(at_most < units - unit0 ? (at_most < 0 ? unit0 : unit0 + at_most) : units);
-        const int tile0 = max(0, unit0 - kLead), mine = max(0, unit1 - kLead) - tile0;      // this warp's tiles
+        int seg, tile0, mine, unit0 = 0, unit1 = 0;           // the segment of the sequence; this warp's tiles
+        long long seg0 = 0;                                   // the segment's first unit
+        if (a.split != 0) {
+            const int rank = blockIdx.x % a.split, at = kWarps * rank + warp, of = kWarps * a.split;
+            seg = blockIdx.x / a.split - b * each;
+            tile0 = (int)((long long)tiles * at / of);
+            mine = (int)((long long)tiles * (at + 1) / of) - tile0;
+        } else {
+            const long long at_most = f1 - f, local = (f < cta1 ? f : cta1 - 1) - before;
+            seg = (int)quotient_of(local, units);
+            seg0 = before + (long long)seg * units;
+            unit0 = (int)(local - (long long)seg * units);
+            unit1 = (int)(at_most < units - unit0 ? (at_most < 0 ? unit0 : unit0 + at_most) : units);
+            tile0 = max(0, unit0 - kLead);
+            mine = max(0, unit1 - kLead) - tile0;
+        }
         const int h = seg / a.row_tiles, rt = seg - h * a.row_tiles;
         if (!joint && mine == 0) {
             f += unit1 - unit0;
@@ -707,10 +727,66 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                 for (int m = 0; m < STEPS; ++m) put(s_o[warp][col], m, o[m][nt][j], o[m][nt][j + 2]);
             }
         __syncthreads();
-        const bool begins = cta0 <= seg0 + kLead, whole = begins && cta1 >= seg0 + units;
-        if (cta1 > seg0 + kLead) {                            // (there are tiles)
-            const int first = begins ? (int)quotient_of(seg0 + kLead, share) : blockIdx.x * kWarps;      // the worker whose part it is
-            const int used = min(NC, a.rows - rt * NC);
+        const int used = min(NC, a.rows - rt * NC);
+        if (a.split > 1) {
+            // the CTAs' parts meet in distributed shared memory: each CTA sums up its warps', and then a share of the values over all CTAs
+            for (int i = tid; i < used * (D / 2); i += kThreads) {
+                const int col = i / (D / 2), d = 2 * (i - col * (D / 2));
+                float low = kNone;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) low = fminf(low, s_off[w][col]);
+                float all = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float by = exp2_approx(low - s_off[w][col]);
+                    const float2 v = *reinterpret_cast<const float2*>(&s_o[w][col][d]);
+                    all = fmaf(s_sum[w][col], by, all);
+                    x = fmaf(v.x, by, x);
+                    y = fmaf(v.y, by, y);
+                }
+                *reinterpret_cast<float2*>(&s_o[0][col][d]) = make_float2(x, y);
+                if (d == 0) {
+                    s_all[0][col] = low;
+                    s_all[1][col] = all;
+                }
+            }
+            cluster_barrier();
+            const int rank = blockIdx.x % a.split;
+            for (int i = tid * a.split + rank; i < used * (D / 2); i += kThreads * a.split) {
+                const int col = i / (D / 2), d = 2 * (i - col * (D / 2));
+                float lows[8], sums[8], xs[8], ys[8], low = kNone;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    lows[r] = kNone;
+                    sums[r] = xs[r] = ys[r] = 0.0f;
+                    if (r < a.split) {
+                        lows[r] = ld_cluster_f32(&s_all[0][col], r);
+                        sums[r] = ld_cluster_f32(&s_all[1][col], r);
+                        xs[r] = ld_cluster_f32(&s_o[0][col][d], r);
+                        ys[r] = ld_cluster_f32(&s_o[0][col][d + 1], r);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) low = fminf(low, lows[r]);
+                float all = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float by = exp2_approx(low - lows[r]);
+                    all = fmaf(sums[r], by, all);
+                    x = fmaf(xs[r], by, x);
+                    y = fmaf(ys[r], by, y);
+                }
+                const float r = all == 0.0f ? 0.0f : vf / all;
+                const int rr = rt * NC + col, tok = rr / a.group, head = h * a.group + (rr - tok * a.group);
+                uint8_t* p = a.out + 2 * (((long long)b * a.fresh + tok) * a.ldo + (long long)head * D + d);
+                *reinterpret_cast<uint32_t*>(p) = a.type == ELUTQ_TYPE_F16 ? pack<false>(x * r, y * r) : pack<true>(x * r, y * r);
+            }
+            cluster_barrier();                                // (nobody leaves while its memory is read)
+            return;
+        }
+        const bool begins = a.split != 0 || cta0 <= seg0 + kLead, whole = begins && (a.split != 0 || cta1 >= seg0 + units);
+        if (whole || cta1 > seg0 + kLead) {                   // (there are tiles)
+            const int first = !whole && begins ? (int)quotient_of(seg0 + kLead, share) : blockIdx.x * kWarps;      // the worker whose part it is
             float* part = part_of(first, begins ? 1 : 0);
             for (int i = tid; i < used * (D / 2); i += kThreads) {
                 const int col = i / (D / 2), d = 2 * (i - col * (D / 2));
@@ -743,11 +819,11 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                 if (lane == 0) record(worker);
                 recorded = true;
             }
-            if (whole && a.by_segment && tid == 0) a.begun[b * each + seg] = make_int4(0, 0, 0, 0);
+            if (whole && a.by_segment && a.split == 0 && tid == 0) a.begun[b * each + seg] = make_int4(0, 0, 0, 0);
         }
         break;
     }
-    if (lane == 0 && !recorded && !a.by_segment) a.begun[worker] = make_int4(0, 0, 0, 0);
+    if (lane == 0 && !recorded && !a.by_segment && a.split == 0) a.begun[worker] = make_int4(0, 0, 0, 0);
 }
 
 // Joins the parts of the segments that several shares hold, in their order.  A block for each segment, or for each share in which one may begin, and for `cols` query rows: a warp to a
@@ -833,28 +909,57 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const DecodeArgs a, int 
     for (int e = 0; e < W / 2; ++e) out[e] = a.type == ELUTQ_TYPE_F16 ? pack<false>(x[2 * e] * r, x[2 * e + 1] * r) : pack<true>(x[2 * e] * r, x[2 * e + 1] * r);
 }
 
-// CTAs of a launch: as many as are resident at once.  (The workspace is as large as any format wants it.)
+// CTAs of a launch: as many as are resident at once
 inline int ctas_of(int per_sm) { return device_sm_count() * per_sm; }
 inline int columns_of(int rows) { return rows <= 8 ? 1 : 2; }
 
-int launch_one(const void* kernel, dim3 grid, int block, int smem, void** args, cudaStream_t stream) {
+int launch_one(const void* kernel, dim3 grid, int block, int smem, void** args, cudaStream_t stream, int cluster = 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.dynamicSmemBytes = smem;
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)block);
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
     if (e == cudaSuccess) count_launch(1);
     return (int)e;
 }
 
+// Short sequences: a cluster of CTAs for each segment, joined in distributed shared memory, one launch instead of two.  How long they are only the device knows; the table says how
+// long they may be.
+int split_of(long long segments, long long cap, int ctas) {
+    if (cap > 8 * kWarps * kShortTokens || segments > 0xffffff) return 0;
+    int split = 1;
+    while (split * kWarps * kShortTokens < cap) split *= 2;
+    while (split < 8 && 2 * split * segments <= ctas && split * kWarps * 16 < cap) split *= 2;
+    return split == 1 || split * segments <= 2LL * ctas ? split : 0;
+}
+
+// What a call of a shape is: columns of a tile of query rows (in eights), CTAs that are resident at once, CTAs of a cluster (0: shares of the whole), bytes of workspace
+struct Plan {
+    int nt, ctas, split;
+    size_t bytes;
+};
+Plan plan_of(const elutq_kv_cache* c, int pages, int B, int new_tokens, int n_q_heads) {
+    Plan p;
+    const int rows = n_q_heads / c->heads * new_tokens;
+    p.nt = columns_of(rows);
+    p.ctas = ctas_of(resident(c->format, c->head_dim, p.nt));
+    const long long cap = (long long)pages * c->page_size;
+    p.split = split_of((long long)B * c->heads * ((rows + 8 * p.nt - 1) / (8 * p.nt)), cap < kMostTokens ? cap : kMostTokens, p.ctas);
+    p.bytes = p.split != 0 ? 0 : (size_t)p.ctas * kWarps * (2 * (8 * p.nt) * (c->head_dim + 2) * sizeof(float) + sizeof(int4));
+    return p;
+}
+
 template <int D, int FMT, bool BF16, int NT>
-int launch_decode(DecodeArgs a, cudaStream_t stream) {
+int launch_decode(DecodeArgs a, const Plan& plan, cudaStream_t stream) {
     constexpr int kRings = kWarps * stages_of(FMT, D) * stage_bytes(FMT, D), kParts = kWarps * 8 * NT * (D + 4) * 4, kSmem = kRings > kParts ? kRings : kParts;
     // once for each device (a call would take half a microsecond of the host's time)
     static std::atomic<unsigned long long> ready{0};
@@ -867,9 +972,14 @@ int launch_decode(DecodeArgs a, cudaStream_t stream) {
         if (ce != cudaSuccess) return (int)ce;
         ready.fetch_or(bit, std::memory_order_release);
     }
-    const int ctas = ctas_of(resident(FMT, D, NT));
+    const int ctas = plan.ctas;
     const long long segments = (long long)a.B * a.c.heads * a.row_tiles;
     a.by_segment = segments <= ctas * kWarps;
+    a.split = plan.split;
+    if (a.split != 0) {
+        void* args[] = {&a};
+        return launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3((unsigned)(segments * a.split)), kThreads, kSmem, args, stream, a.split);
+    }
     void* args[] = {&a};
     const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3(ctas), kThreads, kSmem, args, stream);
     if (e != 0) return e;
@@ -881,13 +991,22 @@ int launch_decode(DecodeArgs a, cudaStream_t stream) {
     return launch_one((const void*)attn_join_kernel<D, NT>, dim3(a.by_segment ? (unsigned)segments : ctas * kWarps, (wide + cols - 1) / cols), 256, 0, join, stream);
 }
 template <int D, int FMT, bool BF16>
-int launch_decode(const DecodeArgs& a, cudaStream_t stream) {
-    return columns_of(a.rows) == 1 ? launch_decode<D, FMT, BF16, 1>(a, stream) : launch_decode<D, FMT, BF16, 2>(a, stream);
+int launch_decode(const DecodeArgs& a, const Plan& plan, cudaStream_t stream) {
+    return plan.nt == 1 ? launch_decode<D, FMT, BF16, 1>(a, plan, stream) : launch_decode<D, FMT, BF16, 2>(a, plan, stream);
 }
 template <int D>
-int launch_decode(const DecodeArgs& a, int format, cudaStream_t stream) {
-    if (format == ELUTQ_KV_16) return a.type == ELUTQ_TYPE_BF16 ? launch_decode<D, ELUTQ_KV_16, true>(a, stream) : launch_decode<D, ELUTQ_KV_16, false>(a, stream);
-    return format == ELUTQ_KV_E4M3 ? launch_decode<D, ELUTQ_KV_E4M3, false>(a, stream) : launch_decode<D, ELUTQ_KV_NVFP4, false>(a, stream);
+int launch_decode(const DecodeArgs& a, int format, const Plan& plan, cudaStream_t stream) {
+    if (format == ELUTQ_KV_16) return a.type == ELUTQ_TYPE_BF16 ? launch_decode<D, ELUTQ_KV_16, true>(a, plan, stream) : launch_decode<D, ELUTQ_KV_16, false>(a, plan, stream);
+    return format == ELUTQ_KV_E4M3 ? launch_decode<D, ELUTQ_KV_E4M3, false>(a, plan, stream) : launch_decode<D, ELUTQ_KV_NVFP4, false>(a, plan, stream);
+}
+
+// The arguments that the size of the workspace hangs on, too
+int check_sizes(const elutq_kv_cache* c, int pages, int B, int new_tokens, int n_q_heads) {
+    const int st = kv_check(c);
+    if (st != ELUTQ_OK) return st;
+    if (pages <= 0 || B <= 0 || new_tokens <= 0 || n_q_heads <= 0) return ELUTQ_ERR_INVALID_ARG;
+    if (n_q_heads % c->heads != 0 || (long long)n_q_heads / c->heads * new_tokens > 0xffff || (long long)B * n_q_heads * new_tokens > 0x7fffffffLL) return ELUTQ_ERR_SHAPE;
+    return ELUTQ_OK;
 }
 
 }  // namespace
@@ -896,28 +1015,26 @@ int launch_decode(const DecodeArgs& a, int format, cudaStream_t stream) {
 
 using namespace elutq;
 
-extern "C" int elutq_attn_decode_workspace_bytes(int n_q_heads, int heads, int head_dim, int new_tokens, size_t* bytes) {
-    if (!bytes || n_q_heads <= 0 || heads <= 0 || new_tokens <= 0) return ELUTQ_ERR_INVALID_ARG;
-    if (head_dim != 64 && head_dim != 128) return ELUTQ_ERR_UNSUPPORTED;
-    if (n_q_heads % heads != 0 || (long long)n_q_heads / heads * new_tokens > 0xffff) return ELUTQ_ERR_SHAPE;
-    const int nt = columns_of(n_q_heads / heads * new_tokens);
-    *bytes = (size_t)ctas_of(4) * kWarps * (2 * (8 * nt) * (head_dim + 2) * sizeof(float) + sizeof(int4));
-    return ELUTQ_OK;
+extern "C" int elutq_attn_decode_workspace_bytes(const elutq_kv_cache* cache, int pages, int B, int new_tokens, int n_q_heads, size_t* bytes) {
+    if (!bytes) return ELUTQ_ERR_INVALID_ARG;
+    const int st = check_sizes(cache, pages, B, new_tokens, n_q_heads);
+    if (st == ELUTQ_OK) *bytes = plan_of(cache, pages, B, new_tokens, n_q_heads).bytes;
+    return st;
 }
 
 extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq, void* out, long long ldo, const int* table, long long ld_table, int pages,
                                  const int* lens, int B, int new_tokens, int n_q_heads, float scale, void* workspace, size_t workspace_bytes, void* stream) {
-    int st = kv_check(cache);
+    int st = check_sizes(cache, pages, B, new_tokens, n_q_heads);
     if (st != ELUTQ_OK) return st;
-    if (!q || !out || !table || !lens || !workspace || pages <= 0 || B <= 0 || new_tokens <= 0 || n_q_heads <= 0) return ELUTQ_ERR_INVALID_ARG;
+    if (!q || !out || !table || !lens) return ELUTQ_ERR_INVALID_ARG;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ELUTQ_ERR_INVALID_ARG;
     const int D = cache->head_dim, H = cache->heads;
-    size_t need = 0;
-    if ((st = elutq_attn_decode_workspace_bytes(n_q_heads, H, D, new_tokens, &need)) != ELUTQ_OK) return st;
+    const Plan plan = plan_of(cache, pages, B, new_tokens, n_q_heads);
+    if (plan.bytes != 0 && !workspace) return ELUTQ_ERR_INVALID_ARG;
     if (ld_table < pages) return ELUTQ_ERR_SHAPE;
     if ((st = kv_rows_check(q, ldq, n_q_heads, D)) != ELUTQ_OK || (st = kv_rows_check(out, ldo, n_q_heads, D)) != ELUTQ_OK) return st;
     if (!mx4_aligned(table, 4) || !mx4_aligned(lens, 4) || !mx4_aligned(workspace, 16)) return ELUTQ_ERR_ALIGN;
-    if (workspace_bytes < need) return ELUTQ_ERR_BUFFER_TOO_SMALL;
+    if (workspace_bytes < plan.bytes) return ELUTQ_ERR_BUFFER_TOO_SMALL;
     DecodeArgs a;
     a.c = kv_view(cache);
     a.q = (const uint8_t*)q;
@@ -930,15 +1047,15 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     a.fresh = new_tokens;
     a.group = n_q_heads / H;
     a.rows = a.group * new_tokens;
-    const int nc = 8 * columns_of(a.rows);
+    const int nc = 8 * plan.nt;
     a.row_tiles = (a.rows + nc - 1) / nc;
     a.type = cache->type;
     a.scale = scale * 1.44269504088896340736f;
     a.begun = (int4*)workspace;
-    a.parts = (float*)(a.begun + ctas_of(4) * kWarps);
+    a.parts = (float*)(a.begun + plan.ctas * kWarps);
     a.cap = (long long)pages * cache->page_size;
-    if (a.cap > 0x7fff0000LL) a.cap = 0x7fff0000LL;               // (token numbers a little behind the last one are formed)
-    const int ce = D == 128 ? launch_decode<128>(a, cache->format, (cudaStream_t)stream) : launch_decode<64>(a, cache->format, (cudaStream_t)stream);
+    if (a.cap > kMostTokens) a.cap = kMostTokens;
+    const int ce = D == 128 ? launch_decode<128>(a, cache->format, plan, (cudaStream_t)stream) : launch_decode<64>(a, cache->format, plan, (cudaStream_t)stream);
     if (ce == 0) return ELUTQ_OK;
     note_cuda_error(ce);
     return ELUTQ_ERR_CUDA;

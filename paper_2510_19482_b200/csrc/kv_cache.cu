@@ -25,7 +25,7 @@ struct WriteArgs {
     int n_pos, rot, interleaved;
     int n_q, heads_all;                        // query heads; all rows of a token: queries, keys, values
     long long warps;
-    int turns;                                 // warps of a token
+    int turns, batches;                        // warps of a token; batches of rows that a warp handles
 };
 
 template <int TYPE>
@@ -77,7 +77,7 @@ __device__ __forceinline__ void store_row(uint8_t* base, uint8_t* scales, const 
     }
 }
 
-// U: rows that a lane handles, their loads in flight together
+// U: rows of a batch that a lane handles, their loads in flight together
 template <int D, int FMT, int TYPE, int U>
 __global__ void __launch_bounds__(128) kv_write_kernel(const WriteArgs a) {
     constexpr int LANES = D / 8, ROWS = 32 / LANES;        // of a row; rows of a warp at a time
@@ -87,17 +87,20 @@ __global__ void __launch_bounds__(128) kv_write_kernel(const WriteArgs a) {
     if (w >= a.warps) return;
     const int lane = threadIdx.x & 31, part = lane % LANES, d0 = 8 * part;
     const long long token = w / a.turns;
-    const int first = (int)(w - token * a.turns) * (ROWS * U) + lane / LANES;
+    int first = (int)(w - token * a.turns) * a.batches * (ROWS * U) + lane / LANES;
     const int slot = __ldg(a.slots + token);
+    const uint8_t *q = a.q + 2 * token * a.ldq, *k = a.k + 2 * token * a.ldk, *v = a.v + 2 * token * a.ldv;
     uint4 x[U];
+    auto load = [&] {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int r = first + u * ROWS;
-        const int kv = r - a.n_q, h = kv < a.c.heads ? kv : kv - a.c.heads;
-        const uint8_t* src = kv < 0 ? a.q + 2 * (token * a.ldq + (long long)r * D) : kv < a.c.heads ? a.k + 2 * (token * a.ldk + (long long)h * D) : a.v + 2 * (token * a.ldv + (long long)h * D);
-        x[u] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < a.heads_all) x[u] = *(reinterpret_cast<const uint4*>(src) + part);
-    }
+        for (int u = 0; u < U; ++u) {
+            const int r = first + u * ROWS, kv = r - a.n_q;
+            const uint8_t* src = kv < 0 ? q + r * (2 * D) : kv < a.c.heads ? k + kv * (2 * D) : v + (kv - a.c.heads) * (2 * D);
+            x[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < a.heads_all) x[u] = *(reinterpret_cast<const uint4*>(src) + part);
+        }
+    };
+    load();
     float c[8], s[8];
     const int half = a.rot / 2;
     const bool turned = d0 < a.rot;
@@ -128,49 +131,54 @@ __global__ void __launch_bounds__(128) kv_write_kernel(const WriteArgs a) {
     const bool held = slot >= 0 && slot < a.c.n_pages * a.c.page_size;
     const int page = held ? a.c.page.of(slot) : 0;
     const long long row0 = (long long)page * a.c.heads * a.c.page_size + (held ? slot - page * a.c.page_size : 0);
+    for (int batch = 0;; ++batch) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int r = first + u * ROWS;
-        if (__all_sync(0xffffffffu, r >= a.heads_all)) break;
-        const int kv = r - a.n_q;
-        const bool is_v = kv >= a.c.heads;
-        float y[8];
-        word_values<TYPE>(y, x[u].x);
-        word_values<TYPE>(y + 2, x[u].y);
-        word_values<TYPE>(y + 4, x[u].z);
-        word_values<TYPE>(y + 6, x[u].w);
-        if (a.rope != nullptr) {
-            if (a.interleaved) {
-                if (turned && !is_v) {
+        for (int u = 0; u < U; ++u) {
+            const int r = first + u * ROWS;
+            if (U > 1 && __all_sync(0xffffffffu, r >= a.heads_all)) break;
+            const int kv = r - a.n_q;
+            const bool is_v = kv >= a.c.heads;
+            float y[8];
+            word_values<TYPE>(y, x[u].x);
+            word_values<TYPE>(y + 2, x[u].y);
+            word_values<TYPE>(y + 4, x[u].z);
+            word_values<TYPE>(y + 6, x[u].w);
+            if (a.rope != nullptr) {
+                if (a.interleaved) {
+                    if (turned && !is_v) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y1 = __fsub_rn(__fmul_rn(y[2 * i], c[i]), __fmul_rn(y[2 * i + 1], s[i]));
-                        y[2 * i + 1] = __fadd_rn(__fmul_rn(y[2 * i + 1], c[i]), __fmul_rn(y[2 * i], s[i]));
-                        y[2 * i] = y1;
+                        for (int i = 0; i < 4; ++i) {
+                            const float y1 = __fsub_rn(__fmul_rn(y[2 * i], c[i]), __fmul_rn(y[2 * i + 1], s[i]));
+                            y[2 * i + 1] = __fadd_rn(__fmul_rn(y[2 * i + 1], c[i]), __fmul_rn(y[2 * i], s[i]));
+                            y[2 * i] = y1;
+                        }
+                    }
+                } else {
+                    float z[8];
+                    word_values<TYPE>(z, __shfl_sync(0xffffffffu, x[u].x, other));
+                    word_values<TYPE>(z + 2, __shfl_sync(0xffffffffu, x[u].y, other));
+                    word_values<TYPE>(z + 4, __shfl_sync(0xffffffffu, x[u].z, other));
+                    word_values<TYPE>(z + 6, __shfl_sync(0xffffffffu, x[u].w, other));
+                    if (turned && !is_v) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = __fadd_rn(__fmul_rn(y[i], c[i]), __fmul_rn(z[i], s[i]));
                     }
                 }
-            } else {
-                float z[8];
-                word_values<TYPE>(z, __shfl_sync(0xffffffffu, x[u].x, other));
-                word_values<TYPE>(z + 2, __shfl_sync(0xffffffffu, x[u].y, other));
-                word_values<TYPE>(z + 4, __shfl_sync(0xffffffffu, x[u].z, other));
-                word_values<TYPE>(z + 6, __shfl_sync(0xffffffffu, x[u].w, other));
-                if (turned && !is_v) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = __fadd_rn(__fmul_rn(y[i], c[i]), __fmul_rn(z[i], s[i]));
-                }
+            }
+            const bool there = r < a.heads_all;
+            if (there && !is_v) {
+                uint8_t* out = kv < 0 ? a.q_out + 2 * (token * a.ldqo + (long long)r * D) : a.k_out == nullptr ? nullptr : a.k_out + 2 * (token * a.ldko + (long long)kv * D);
+                if (out != nullptr)
+                    reinterpret_cast<uint4*>(out)[part] = make_uint4(to_pair<TYPE>(y[0], y[1]), to_pair<TYPE>(y[2], y[3]), to_pair<TYPE>(y[4], y[5]), to_pair<TYPE>(y[6], y[7]));
+            }
+            if (__any_sync(0xffffffffu, there && kv >= 0)) {
+                const int h = is_v ? kv - a.c.heads : kv < 0 ? 0 : kv;
+                store_row<D, FMT, TYPE>(is_v ? a.c.v : a.c.k, is_v ? a.c.vs : a.c.ks, is_v ? a.c.vf : a.c.kf, row0 + (long long)h * a.c.page_size, there ? h : 0, part, y, there && kv >= 0 && held);
             }
         }
-        const bool there = r < a.heads_all;
-        if (there && !is_v) {
-            uint8_t* out = kv < 0 ? a.q_out + 2 * (token * a.ldqo + (long long)r * D) : a.k_out == nullptr ? nullptr : a.k_out + 2 * (token * a.ldko + (long long)kv * D);
-            if (out != nullptr)
-                reinterpret_cast<uint4*>(out)[part] = make_uint4(to_pair<TYPE>(y[0], y[1]), to_pair<TYPE>(y[2], y[3]), to_pair<TYPE>(y[4], y[5]), to_pair<TYPE>(y[6], y[7]));
-        }
-        if (__any_sync(0xffffffffu, there && kv >= 0)) {
-            const int h = is_v ? kv - a.c.heads : kv < 0 ? 0 : kv;
-            store_row<D, FMT, TYPE>(is_v ? a.c.v : a.c.k, is_v ? a.c.vs : a.c.ks, is_v ? a.c.vf : a.c.kf, row0 + (long long)h * a.c.page_size, there ? h : 0, part, y, there && kv >= 0 && held);
-        }
+        first += U * ROWS;
+        if (batch + 1 >= a.batches || first - lane / LANES >= a.heads_all) break;
+        load();
     }
 }
 
@@ -333,8 +341,11 @@ int launch_write(WriteArgs& a, long long tokens, cudaStream_t stream) {
     constexpr int ROWS = 32 / (D / 8);
     // few tokens: a row to a lane, so that the rows' latencies run side by side; otherwise the angles are loaded once for several
     const bool few = tokens * a.heads_all / ROWS < 16LL * device_sm_count();
-    const int rows = ROWS * (few ? 1 : kUnroll);
-    a.turns = (a.heads_all + rows - 1) / rows;
+    const int rows = ROWS * (few ? 1 : kUnroll), batches = (a.heads_all + rows - 1) / rows;
+    // ... for all of a token where there are tokens enough
+    a.turns = few ? batches : 1;
+    while (a.turns < batches && tokens * a.turns < 64LL * device_sm_count()) ++a.turns;
+    a.batches = (batches + a.turns - 1) / a.turns;
     a.warps = tokens * a.turns;
     return few ? launch(kv_write_kernel<D, FMT, TYPE, 1>, a.warps * 32, 128, stream, a) : launch(kv_write_kernel<D, FMT, TYPE, kUnroll>, a.warps * 32, 128, stream, a);
 }
@@ -406,7 +417,7 @@ extern "C" int elutq_kv_write(const elutq_kv_cache* cache, const void* q, long l
     if ((st = kv_rows_check(k, ldk, H, D)) != ELUTQ_OK || (st = kv_rows_check(v, ldv, H, D)) != ELUTQ_OK) return st;
     if (k_out != nullptr && (st = kv_rows_check(k_out, ldko, H, D)) != ELUTQ_OK) return st;
     if (!mx4_aligned(slots, 4) || !mx4_aligned(positions, 4) || !mx4_aligned(rope, 16)) return ELUTQ_ERR_ALIGN;
-    if ((long long)n_q_heads + 2LL * H > 0xffffff || (long long)tokens * (n_q_heads + 2LL * H) > (1LL << 34)) return ELUTQ_ERR_SHAPE;        // (blocks of a launch)
+    if ((long long)n_q_heads + 2LL * H > (1 << 22) || (long long)tokens * (n_q_heads + 2LL * H) > (1LL << 34)) return ELUTQ_ERR_SHAPE;        // (blocks of a launch)
     WriteArgs a;
     a.c = kv_view(cache);
     a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v;

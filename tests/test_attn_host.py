@@ -62,7 +62,7 @@ def test_arguments_of_a_read():
 
 def test_arguments_of_a_decoding_step():
     before, c = elutq.elutq_launch_count(), cache()
-    for kw in (dict(q=0), dict(out=0), dict(table=0), dict(lens=0), dict(ws=0), dict(pages=0), dict(B=0), dict(new=0), dict(n=0), dict(scale=0.0), dict(scale=-1.0),
+    for kw in (dict(q=0), dict(out=0), dict(table=0), dict(lens=0), dict(pages=0), dict(B=0), dict(new=0), dict(n=0), dict(scale=0.0), dict(scale=-1.0),
                dict(scale=float("nan")), dict(scale=float("inf"))):
         assert decode(c, **kw) == -1, kw
     assert decode(None) == -1
@@ -70,12 +70,13 @@ def test_arguments_of_a_decoding_step():
         assert decode(c, **kw) == -2, kw
     for kw in (dict(q=72), dict(out=136), dict(ldq=516), dict(table=18), dict(lens=9), dict(ws=1032)):
         assert decode(c, **kw) == -3, kw
-    out = ctypes.c_size_t(0)
-    assert elutq.lib().elutq_attn_decode_workspace_bytes(4, 2, 128, 1, ctypes.byref(out)) == 0 and out.value > 0
-    assert decode(c, size=out.value - 1) == -4
-    assert elutq.lib().elutq_attn_decode_workspace_bytes(4, 2, 96, 1, ctypes.byref(out)) == -5
-    assert elutq.lib().elutq_attn_decode_workspace_bytes(4, 3, 128, 1, ctypes.byref(out)) == -2
-    assert elutq.lib().elutq_attn_decode_workspace_bytes(4, 2, 128, 1, None) == elutq.lib().elutq_attn_decode_workspace_bytes(4, 0, 128, 1, ctypes.byref(out)) == -1
+    out, ask = ctypes.c_size_t(7), elutq.lib().elutq_attn_decode_workspace_bytes
+    assert ask(ctypes.byref(c), 5000, 2, 1, 4, ctypes.byref(out)) == 0 and out.value > 0
+    assert decode(c, pages=5000, ld=5000, size=out.value - 1) == -4 and decode(c, pages=5000, ld=5000, ws=0) == -1
+    assert ask(ctypes.byref(c), 5, 2, 1, 4, ctypes.byref(out)) == 0 and out.value == 0            # a short table: none needed
+    assert ask(ctypes.byref(c), 5, 2, 1, 5, ctypes.byref(out)) == -2 and ask(ctypes.byref(c), 5, 2, 1 << 16, 4, ctypes.byref(out)) == -2
+    assert ask(None, 5, 2, 1, 4, ctypes.byref(out)) == ask(ctypes.byref(c), 0, 2, 1, 4, ctypes.byref(out)) == ask(ctypes.byref(c), 5, 2, 1, 4, None) == -1
+    assert ask(ctypes.byref(cache(head_dim=96)), 5, 2, 1, 4, ctypes.byref(out)) == -5
     assert elutq.elutq_launch_count() == before
 
 
