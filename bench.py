@@ -897,6 +897,82 @@ def run_fit(args) -> None:
     print(json.dumps(line), flush=True)
 
 
+def run_attention(args) -> None:
+    """Decoding steps of one layer's attention half, `attention:q:FORMAT:B:L`: merged q/k/v linear at q bits, rotary positions and the write into a cache of B sequences of L tokens
+    (FORMAT 16, e4m3 or nvfp4), attention over it, o linear; LLaMA-3.1 8B shapes (32 query heads over 8 key heads of 128)."""
+    import torch
+
+    import paper_2510_19482_b200 as elutq
+
+    q_bits, name, B, L = args.workload.split(":")[1:5]
+    q_bits, B, L = int(q_bits), int(B), int(L)
+    fmt = {"16": elutq.KV_16, "e4m3": elutq.KV_E4M3, "nvfp4": elutq.KV_NVFP4}[name]
+    Hq, H, D, page, K = 32, 8, 128, 64, 4096
+    packed = []
+    for tag, (N, k) in (("qkv", workloads.LLAMA31_8B["qkv"]), ("o", workloads.LLAMA31_8B["o"])):
+        lay = workloads.hlq_layer(0, f"bench-attention/{tag}", q_bits, 128, N, k)
+        packed.append(elutq.elutq_pack(torch.from_numpy(lay.planes).cuda(), torch.from_numpy(lay.scales.view(np.int16)).cuda().view(torch.float16),
+                                       torch.from_numpy(lay.offsets.view(np.int16)).cuda().view(torch.float16), q_bits, 128, N, k))
+    pages = -(-L // page)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    row = {"16": 2 * D, "e4m3": D, "nvfp4": D // 2}[name]
+    shape = (B * pages, H, page, D if name == "16" else row)
+    # a pool of ordinary values: finite in every format
+    make = lambda: (torch.randn(shape, generator=gen, device="cuda", dtype=torch.float16) if name == "16" else  # noqa: E731
+                    torch.randint(0, 120 if name == "e4m3" else 256, shape, generator=gen, device="cuda", dtype=torch.uint8))
+    scales = [torch.randint(40, 60, (B * pages, H, page, D // 16), generator=gen, device="cuda", dtype=torch.uint8) if name == "nvfp4" else None for _ in range(2)]
+    factor = None if name == "16" else torch.full((H,), 0.05, device="cuda")
+    cache = elutq.KvCache(fmt, torch.float16, make(), make(), scales[0], scales[1], k_factor=factor, v_factor=factor)
+    table = torch.randperm(B * pages, generator=gen, device="cuda").int().view(B, pages)
+    lens = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    slots = (table[:, (L - 1) // page] * page + (L - 1) % page).contiguous()
+    rope = elutq.elutq_rope_table(L, D, 500000.0, elutq.ROPE_BANDS, factor=8.0)
+    X = torch.randn((B, K), generator=gen, device="cuda", dtype=torch.float16)
+    merged = torch.empty((B, Hq + 2 * H, D), dtype=torch.float16, device="cuda")
+    heads, Y = torch.empty((B, Hq, D), dtype=torch.float16, device="cuda"), torch.empty((B, K), dtype=torch.float16, device="cuda")
+    need = elutq.elutq_attn_decode_workspace_bytes(cache, pages, B, 1, Hq)
+    workspace = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+    positions = lens - 1
+
+    def step():
+        elutq.elutq_lut_gemm(X, packed[0], merged, B, (Hq + 2 * H) * D, K)
+        q = merged[:, :Hq]
+        elutq.elutq_kv_write(cache, merged[:, Hq : Hq + H], merged[:, Hq + H :], slots, q=q, q_out=q, positions=positions, rope=rope)
+        elutq.elutq_attn_decode(cache, q, heads, table, lens, workspace=workspace)
+        elutq.elutq_lut_gemm(heads, packed[1], Y, B, K, Hq * D)
+
+    for _ in range(args.warmup):
+        step()
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    for M, N, k in ((B, (Hq + 2 * H) * D, K), (B, K, Hq * D)):          # (nothing is allocated during a capture)
+        elutq.elutq_reserve(M, N, k, stream)
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    before = elutq.elutq_launch_count()
+    step()
+    launches = elutq.elutq_launch_count() - before
+    torch.cuda.synchronize()
+    flush = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+    times = []
+    for _ in range(args.steps):
+        flush.zero_()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        graph.replay()
+        e1.record()
+        times.append((e0, e1))
+    torch.cuda.synchronize()
+    ms = sorted(a.elapsed_time(b) for a, b in times)[len(times) // 2]
+    weights = sum(workloads.algorithmic_bytes(B, N, k, q_bits, 128) for N, k in (workloads.LLAMA31_8B["qkv"], workloads.LLAMA31_8B["o"]))
+    kept = B * L * 2 * H * (row + (D // 16 if name == "nvfp4" else 0))
+    print(json.dumps({"metric": "attention half of a decoding step", "value": (weights + kept) / (ms * 1e-3) / 1e9, "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+                      "ms_per_step": ms, "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "f16", "data": "synthetic",
+                      "config": {"workload": f"8B attention half at q={q_bits}, {B} sequences of {L} tokens, cache {name}", "weight_bytes": weights, "cache_bytes": kept,
+                                 "l2": "flushed in front of every step (median of single steps, which count the launch of a graph)"},
+                      "gpu_launches": launches * args.steps}), flush=True)
+
+
 def main() -> None:
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -904,7 +980,7 @@ def main() -> None:
     ap.add_argument("--warmup", type=int, default=None)
     ap.add_argument("--impl", default="cuda", choices=["cuda", "reference"])
     ap.add_argument("--workload", default="cfg1",
-                    help="one of %s, custom:q:N:K[:M],... (G = 128), or fit:q:G:N:K (the offline parameter fit)"
+                    help="one of %s, custom:q:N:K[:M],... (G = 128), fit:q:G:N:K (the offline parameter fit), or attention:q:FORMAT:B:L (a layer's attention half, decoding)"
                          % ", ".join(sorted(WORKLOAD_NAMES)))
     ap.add_argument("--flags", type=lambda v: int(v, 0), default=0,
                     help="ELUTQ_FLAG_* bits for every call (kernel-variant comparisons; 0 = the default path)")
@@ -920,6 +996,11 @@ def main() -> None:
         args.steps = args.steps or 5
         args.warmup = max(args.warmup or 3, 3)
         run_fit(args)
+        return
+    if args.workload.startswith("attention:"):
+        args.steps = args.steps or 200
+        args.warmup = max(args.warmup or 10, 3)
+        run_attention(args)
         return
     if args.workload not in WORKLOAD_NAMES:
         if not args.workload.startswith("custom:"):
