@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -400,39 +401,35 @@ def elutq_mx4_test_wait_expiry(x_codes, x_scales, w_codes, w_scales, Y, M: int, 
                                             types.get(Y.dtype, -1), M, N, K, fmt, wait_limit, _stream(stream)), where)
 
 
+_DESC = struct.Struct("6Q6i")       # elutq_kv_cache
+
+
 class KvCache:
     """A paged cache: k, v [n_pages, heads, page_size, row] (KV_16: values of `dtype`; KV_E4M3: bytes; KV_NVFP4: head_dim / 2 bytes of codes, with
     scales [n_pages, heads, page_size, head_dim / 16] of bytes), all dense; factors fp32 [heads] or None.  `dtype`: of queries, keys, values and results."""
 
-    __slots__ = ("desc", "address", "device", "dtype", "heads", "head_dim", "tensors")
+    __slots__ = ("desc", "device", "dtype", "heads", "head_dim", "tensors")
 
     def __init__(self, fmt: int, dtype, k, v, k_scales=None, v_scales=None, k_factor=None, v_factor=None):
-        where = "KvCache"
-        torch, types, _, _ = _torch()
-        d, shape = k.get_device(), k.shape
-        kind = types.get(dtype, -1)
-        if kind not in (TYPE_F16, TYPE_BF16) or fmt not in (KV_16, KV_E4M3, KV_NVFP4) or len(shape) != 4 or d < 0:
-            _refuse(where, "a format, torch.float16 or torch.bfloat16, and k, v of four dimensions wanted", k, v)
+        torch, types, _, _ = _TORCH or _torch()
+        d, shape, kind = k.get_device(), k.shape, types.get(dtype, TYPE_F32)
+        if (kind == TYPE_F32 or not 0 <= fmt <= 2 or len(shape) != 4 or d < 0 or v.shape != shape or v.get_device() != d or not k.is_contiguous() or not v.is_contiguous() or
+                (k.dtype is not dtype or v.dtype is not dtype if fmt == 0 else k.element_size() != 1 or v.element_size() != 1)):
+            _refuse("KvCache", "a format, torch.float16 or torch.bfloat16, and k, v of one shape [n_pages, heads, page_size, row], of that type or of bytes, wanted", k, v)
         pages, heads, page, dim = shape
-        if fmt == KV_16:
-            if k.dtype is not dtype or v.dtype is not dtype:
-                _refuse(where, f"k, v of {dtype} wanted", k, v)
-        else:
-            if k.element_size() != 1 or v.element_size() != 1:
-                _refuse(where, "k, v of bytes wanted", k, v)
-            if fmt == KV_NVFP4:
-                dim *= 2
-        if v.shape != shape or v.get_device() != d or not k.is_contiguous() or not v.is_contiguous():
-            _refuse(where, "k, v of one shape wanted", k, v)
-        addresses = [0, 0]
+        ks = vs = kf = vf = 0
         if fmt == KV_NVFP4:
-            for i, s in enumerate((k_scales, v_scales)):
-                if s is None or s.nbytes != pages * heads * page * (dim // 16) or s.element_size() != 1 or not s.is_contiguous() or s.get_device() != d:
-                    _refuse(where, f"scales: {pages * heads * page * (dim // 16)} bytes wanted", s)
-                addresses[i] = s.data_ptr()
-        self.desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), addresses[0], addresses[1], _small(where, "k_factor", k_factor, torch.float32, heads, d),
-                                _small(where, "v_factor", v_factor, torch.float32, heads, d), fmt, kind, pages, heads, page, dim)
-        self.address = ctypes.addressof(self.desc)
+            dim *= 2
+            n = pages * heads * page * (dim // 16)
+            for t in (k_scales, v_scales):
+                if t is None or t.nbytes != n or t.element_size() != 1 or not t.is_contiguous() or t.get_device() != d:
+                    _refuse("KvCache", f"scales: {n} bytes wanted", t)
+            ks, vs = k_scales.data_ptr(), v_scales.data_ptr()
+        if k_factor is not None:
+            kf = _small("KvCache", "k_factor", k_factor, torch.float32, heads, d)
+        if v_factor is not None:
+            vf = _small("KvCache", "v_factor", v_factor, torch.float32, heads, d)
+        self.desc = _DESC.pack(k.data_ptr(), v.data_ptr(), ks, vs, kf, vf, fmt, kind, pages, heads, page, dim)
         self.device, self.dtype, self.heads, self.head_dim = d, dtype, heads, dim
         self.tensors = (k, v, k_scales, v_scales, k_factor, v_factor)      # (they live as long as the descriptor names them)
 
@@ -471,10 +468,10 @@ def _attention():
 
 def _rows(where: str, name: str, t, n: int, D: int, dtype, device: int, rows: int) -> int:
     """Distance between the tokens of [rows, n, D] with heads side by side, in elements."""
-    ld, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.shape != (rows, n, D) or t.dtype is not dtype or t.get_device() != device or one != 1 or (head != D and n > 1):
+    stride = t.stride()
+    if t.shape != (rows, n, D) or stride[2] != 1 or (stride[1] != D and n > 1) or t.dtype is not dtype or t.get_device() != device:
         _refuse(where, f"{name}: {rows} tokens of {n} heads of {D} values of {dtype}, the heads of a token side by side, wanted", t)
-    return ld if rows > 1 else n * D
+    return stride[0] if rows > 1 else n * D
 
 
 def _pages(where: str, table, device: int):
@@ -502,7 +499,7 @@ def elutq_kv_write(cache: KvCache, k, v, slots, q=None, q_out=None, positions=No
         ldko = _rows(where, "k_out", k_out, H, D, dtype, d, rows)
     if rope is not None:
         n_pos, rot = rope.shape
-    status = write(cache.address, 0 if q is None else q.data_ptr(), ldq, 0 if q is None else q_out.data_ptr(), ldqo, n, k.data_ptr(), ldk, 0 if k_out is None else k_out.data_ptr(), ldko,
+    status = write(cache.desc, 0 if q is None else q.data_ptr(), ldq, 0 if q is None else q_out.data_ptr(), ldqo, n, k.data_ptr(), ldk, 0 if k_out is None else k_out.data_ptr(), ldko,
                    v.data_ptr(), ldv, rows, _small(where, "slots", slots, int32, rows, d), _small(where, "positions", positions, int32, rows, d),
                    _small(where, "rope", rope, float32, n_pos * rot, d), n_pos, rot, flags, raw(d) if stream is None else _stream(stream))
     if status != 0:
@@ -519,7 +516,7 @@ def elutq_kv_read(cache: KvCache, table, first, cu, k_out, v_out, stream=None) -
         _refuse(where, f"a cache on the current device wanted, cuda:{d} given", k_out)
     ldk, ldv = _rows(where, "k_out", k_out, H, D, dtype, d, rows), _rows(where, "v_out", v_out, H, D, dtype, d, rows)
     B, pages, ld = _pages(where, table, d)
-    status = read(cache.address, table.data_ptr(), ld, pages, _small(where, "first", first, int32, B, d), _small(where, "cu", cu, int32, B + 1, d), B, rows,
+    status = read(cache.desc, table.data_ptr(), ld, pages, _small(where, "first", first, int32, B, d), _small(where, "cu", cu, int32, B + 1, d), B, rows,
                   k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, raw(d) if stream is None else _stream(stream))
     if status != 0:
         raise ElutqError(status, where)
@@ -527,7 +524,7 @@ def elutq_kv_read(cache: KvCache, table, first, cu, k_out, v_out, stream=None) -
 
 def elutq_attn_decode_workspace_bytes(cache: KvCache, pages: int, B: int, new_tokens: int, n_q_heads: int) -> int:
     out = c_size_t(0)
-    _check(lib().elutq_attn_decode_workspace_bytes(cache.address, pages, B, new_tokens, n_q_heads, ctypes.addressof(out)), "elutq_attn_decode_workspace_bytes")
+    _check(lib().elutq_attn_decode_workspace_bytes(cache.desc, pages, B, new_tokens, n_q_heads, ctypes.addressof(out)), "elutq_attn_decode_workspace_bytes")
     return out.value
 
 
@@ -545,7 +542,7 @@ def elutq_attn_decode(cache: KvCache, q, out, table, lens, new_tokens: int = 1, 
     address = nbytes = 0
     if workspace is None:
         need = c_size_t(0)
-        status = size(cache.address, pages, B, new_tokens, n, ctypes.byref(need))
+        status = size(cache.desc, pages, B, new_tokens, n, ctypes.byref(need))
         if status != 0:
             raise ElutqError(status, where)
         nbytes = need.value
@@ -558,7 +555,7 @@ def elutq_attn_decode(cache: KvCache, q, out, table, lens, new_tokens: int = 1, 
         _refuse(where, "workspace wanted", workspace)
     else:
         address, nbytes = workspace.data_ptr(), workspace.nbytes
-    status = decode(cache.address, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, pages, _small(where, "lens", lens, int32, B, d), B, new_tokens, n,
+    status = decode(cache.desc, q.data_ptr(), ldq, out.data_ptr(), ldo, table.data_ptr(), ld, pages, _small(where, "lens", lens, int32, B, d), B, new_tokens, n,
                     D ** -0.5 if scale is None else scale, address, nbytes, raw(d) if stream is None else _stream(stream))
     if status != 0:
         raise ElutqError(status, where)
