@@ -536,7 +536,7 @@ int elutq_kv_read(const elutq_kv_cache* cache, const int* table, long long ld_ta
  * Attention of the last new_tokens tokens of every sequence over its part of the cache (which holds them already):
  *   q, out  [B * new_tokens][n_q_heads], sequence by sequence; query heads h * n_q_heads / heads .. belong to key head h
  *   lens    device int [B]: tokens of the sequence, the new ones among them; cut to what the table has room for
- * out = softmax(scale * q K^T) V; new token i sees tokens 0 .. lens[b] - new_tokens + i.  A row that sees nothing is zeros.  What lies in pages behind that is not
+ * out must not overlap q.  out = softmax(scale * q K^T) V; new token i sees tokens 0 .. lens[b] - new_tokens + i.  A row that sees nothing is zeros.  What lies in pages behind that is not
  * looked at, whatever it is; tokens on a page outside the cache count as masked.  scale > 0.  Products of 16-bit values, fp32 sums; the weights of a row are rounded to
  * 16 bits (relative to 2^14 times the least that still counts) for the product with V.
  * The workspace belongs to one call at a time (calls of one stream follow one another) and needs no initialisation; short tables need none (0 bytes: it may be NULL).
@@ -554,7 +554,7 @@ int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq,
  *   max_q       queries of the longest sequence, or more; queries of a sequence from max_q (rounded up to 128) on are left out
  *   flags       0: causal, the last query sees all keys of its sequence and every one before it one key less (so keys of an earlier part of the prompt come in
  *               front); ELUTQ_ATTN_ALL_KEYS: every query sees all keys
- * out = softmax(scale * q K^T) V; a row that sees nothing is zeros.  No row is touched by what it does not see, infinities and NaN among that.  scale > 0.  Products of 16-bit
+ * out must not overlap the inputs.  out = softmax(scale * q K^T) V; a row that sees nothing is zeros.  No row is touched by what it does not see, infinities and NaN among that.  scale > 0.  Products of 16-bit
  * values, fp32 sums; the weights of a row are rounded to `type` for the product with V.
  */
 #define ELUTQ_ATTN_ALL_KEYS 0x1u

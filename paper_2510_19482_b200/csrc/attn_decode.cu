@@ -36,7 +36,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kLead = 4;
 constexpr long long kMostTokens = 0x7fff0000LL;      // of a sequence (numbers a little behind the last one are formed)
 constexpr int kShortTokens = 128;            // of a warp
-constexpr float kNone = 1e30f;               // offset of a column that has seen no token: any score rises above it
+constexpr float kNone = 3e38f;               // offset of a column that has seen no token: any score rises above it
 constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
 
 struct DecodeArgs {
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             return;
         }
         // the sequence that the CTA's first unit belongs to: 32 at a time
-        for (;; b += 32) {
+        for (; b < a.B; b += 32) {
             const long long mine = b + lane < a.B ? (long long)units_of<TT>(length_of(a, b + lane)) * each : 0;
             long long incl = mine;
 #pragma unroll
@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
             }
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
+        if (b >= a.B) return;                                 // (only where lengths change during the call)
         const int units = units_of<TT>(length_of(a, b));
         joint = cta1 <= before + (quotient_of(cta0 - before, units) + 1) * units;
         f0 = cta0 + warp * share;
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
         const int len = length_of(a, b), tiles = tiles_of<TT>(len), units = units_of<TT>(len);
         if (!joint && f - before >= (long long)units * each) {
             before += (long long)units * each;
-            ++b;
+            if (++b >= a.B) break;
             continue;
         }
         int seg, tile0, mine, unit0 = 0, unit1 = 0;           // the segment of the sequence; this warp's tiles
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                     top[nt][j] = fmaxf(sc[0][nt][j], sc[0][nt][j + 2]);
 #pragma unroll
                     for (int u = 1; u < U; ++u) top[nt][j] = fmaxf(top[nt][j], fmaxf(sc[u][nt][j], sc[u][nt][j + 2]));
-                    rises |= fmaf(top[nt][j], cs[nt][j], off[nt][j]) > kRise;
+                    rises |= __fmul_rn(top[nt][j], cs[nt][j]) + off[nt][j] > kRise;
                 }
             if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                         float x = top[nt][j];
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-                        const float to = x == -INFINITY ? off[nt][j] : fminf(off[nt][j], kBase - x * cs[nt][j]);
+                        const float to = x == -INFINITY ? off[nt][j] : fminf(off[nt][j], kBase - __fmul_rn(x, cs[nt][j]));
                         const float by = exp2_approx(to - off[nt][j]);
                         off[nt][j] = to;
                         sum[nt][j] *= by;
@@ -543,7 +544,8 @@ __global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_ke
                     float p[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        p[i] = exp2_approx(fmaf(sc[u][nt][i], cs[nt][i & 1], off[nt][i & 1]));
+                        // (not fused: the offset comes from a rounded product, and where products are large the difference of the two would be anything)
+                        p[i] = exp2_approx(__fmul_rn(sc[u][nt][i], cs[nt][i & 1]) + off[nt][i & 1]);
                         sum[nt][i & 1] += p[i];
                     }
                     pf[u][nt][0] = transposed(pack<BF16>(p[0], p[1]));
@@ -1031,7 +1033,7 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
                                  const int* lens, int B, int new_tokens, int n_q_heads, float scale, void* workspace, size_t workspace_bytes, void* stream) {
     int st = check_sizes(cache, pages, B, new_tokens, n_q_heads);
     if (st != ELUTQ_OK) return st;
-    if (!q || !out || !table || !lens) return ELUTQ_ERR_INVALID_ARG;
+    if (!q || !out || out == q || !table || !lens) return ELUTQ_ERR_INVALID_ARG;
     if (!(scale > 0.0f) || !(scale < 1e30f)) return ELUTQ_ERR_INVALID_ARG;
     const int D = cache->head_dim, H = cache->heads;
     const Plan plan = plan_of(cache, pages, B, new_tokens, n_q_heads);

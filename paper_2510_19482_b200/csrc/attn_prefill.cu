@@ -15,7 +15,7 @@
 //            it.  A quarter of them formed by a polynomial instead brought nothing: 8192 tokens 439 -> 461 us; long runs are at the power limit.)
 // masked     Scores are selected, and V rows behind a sequence (the next one's, or whatever lies behind the last) are replaced by zeros in shared memory.  A weight of zero
 //            times a V that is not finite would still be NaN, for a row in front of such a token in the same tile: rows whose result is not finite are formed again,
-//            one by one, from what they see.  Finite inputs never come there.
+//            one by one, from what they see.  So are rows whose scores pass 2^22.  Other inputs never come there.
 //
 // Every wait is bounded: the thread whose wait runs out raises the device's status word, and all roles leave their loops.
 #include <atomic>
@@ -35,8 +35,9 @@ constexpr int kItems = 2;                  // pairs of tiles that the roles know
 constexpr int kThreads = 384;
 // Registers of a thread: of the launch's 168 the two warpgroups of the softmax get more, the third less (2 x 208 + 80 is below 3 x 168).
 constexpr int kRowRegs = 208, kOtherRegs = 80;
-constexpr float kNone = 1e30f;               // offset of a row that has seen no key: any score rises above it
+constexpr float kNone = 3e38f;               // offset of a row that has seen no key: any score rises above it
 constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
+constexpr float kLarge = 4194304.0f;         // 2^22: scores beyond it leave less than half a bit behind the point in an offset
 constexpr unsigned long long kWaitNs = 1000000000ull;
 constexpr int kFirstPart = 96;               // keys of a tile whose weights are handed over first
 constexpr int kScores = 0, kResults = 256;   // columns of tensor memory, 128 for each tile
@@ -257,6 +258,7 @@ __device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const
 struct Walk {
     int level, before, here;               // the level, pairs above it, pairs of it
     int mine;                              // pairs of sequence `lane` (the first 32 are asked for again and again)
+    int at, passed;                        // where the last pair was found (32 sequences from there on), those of the level in front of it: n only rises
     __device__ __forceinline__ uint32_t have(const PrefillArgs& a, int b0) const {          // of 32 sequences, those that have this level
         const int b = b0 + (threadIdx.x & 31);
         return __ballot_sync(0xffffffffu, (b0 == 0 ? mine : b < a.B ? pairs_of(a, b) : 0) > level);
@@ -265,27 +267,47 @@ struct Walk {
         const int q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q), nq = min(max(__ldg(a.cu_q + b + 1), q0), a.total_q) - q0;
         return ((min(nq, a.max_q) + kTile - 1) / kTile * a.group + 1) / 2;
     }
-    // by a whole warp; false: there are no more
-    __device__ bool find(const PrefillArgs& a, int n, int& b, int& h) {
+    // A long search is seen by those that wait for its result.
+    __device__ __forceinline__ void moves(int b0, volatile uint32_t* seen) const {
+        if ((b0 & 0x7fff) == 0 && (threadIdx.x & 31) == 0) *seen = *seen + 1;
+    }
+    // by a whole warp, as the next ones
+    __device__ void begin(const PrefillArgs& a, volatile uint32_t* seen) {
+        before = here = at = passed = 0;
+        const int b = threadIdx.x & 31;
+        int most = mine = b < a.B ? pairs_of(a, b) : 0;
+        for (int b0 = 32; b0 < a.B; b0 += 32) {
+            if (b0 + b < a.B) most = max(most, pairs_of(a, b0 + b));
+            moves(b0, seen);
+        }
+        level = __reduce_max_sync(0xffffffffu, most);
+    }
+    // false: there are no more
+    __device__ bool find(const PrefillArgs& a, int n, int& b, int& h, volatile uint32_t* seen) {
         while (n >= before + here) {
             if (level == 0) return false;
             before += here;
             --level;
+            at = passed = 0;
             int count = 0;
-            for (int b0 = 0; b0 < a.B; b0 += 32) count += __popc(have(a, b0));
+            for (int b0 = 0; b0 < a.B; b0 += 32) {
+                count += __popc(have(a, b0));
+                moves(b0, seen);
+            }
             here = count * a.heads;
         }
-        const int left = n - before;
-        int which = left / a.heads;        // of the sequences that have this level
+        const int left = n - before, which = left / a.heads;       // of the sequences that have this level
         h = left - which * a.heads;
-        for (int b0 = 0;; b0 += 32) {
-            const uint32_t some = have(a, b0);
-            if (which < __popc(some)) {
-                b = b0 + __fns(some, 0, which + 1);
+        for (; at < a.B; at += 32) {
+            const uint32_t some = have(a, at);
+            if (which - passed < __popc(some)) {
+                b = at + __fns(some, 0, which - passed + 1);
                 return true;
             }
-            which -= __popc(some);
+            passed += __popc(some);
+            moves(at, seen);
         }
+        return false;
     }
 };
 // A role's way through the items: its slot in the queue and the parity of its use
@@ -366,9 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
             // ---- items and loads: keys 0, the query tiles, values 0, keys 1, .. ----------------------------------------------------------------------------
             Queue queue;
             Walk walk;
-            walk.before = walk.here = 0;
-            walk.mine = lane < a.B ? walk.pairs_of(a, lane) : 0;
-            walk.level = a.B <= 32 ? __reduce_max_sync(0xffffffffu, walk.mine) : ((min(a.max_q, a.total_q) + kTile - 1) / kTile * a.group + 1) / 2;
+            walk.begin(a, gave_up + 1);
             int kv = 0, used[2] = {0, 0};                     // tiles of keys and values; items that had the query tile
             uint32_t tails = 0, parity = 0;                   // a bit for each slot: its last load was announced to the tail's warp; the parity of such uses
             bool ok = true;
@@ -376,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 const int n = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
                 Item it;
                 int b = 0, h = 0;
-                const bool some = walk.find(a, n, b, h);
+                const bool some = walk.find(a, n, b, h, gave_up + 1);
                 if (some) {
                     it.q0 = min(max(__ldg(a.cu_q + b), 0), a.total_q);
                     it.nq = min(max(__ldg(a.cu_q + b + 1), it.q0), a.total_q) - it.q0;
@@ -681,7 +701,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 }
                 __syncwarp();
             }
-            uint32_t again = __ballot_sync(0xffffffffu, check != 0.0f && row < nq);          // (NaN: something was not finite)
+            // (NaN: something was not finite.  A large offset: fmaf(x, scale, offset) has its rounding in it, which may be anything)
+            uint32_t again = __ballot_sync(0xffffffffu, (check != 0.0f || (tiles > 0 && fabsf(off) > kLarge && sees > 0)) && row < nq);
             while (again != 0) {
                 const int l = __ffs(again) - 1;
                 again &= again - 1;
@@ -743,7 +764,7 @@ int launch_prefill(const CUtensorMap& qm, const CUtensorMap& km, const CUtensorM
 
 int run_prefill(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q, const int* cu_k, int B,
                 int max_q, int total_q, int total_k, int n_q_heads, int heads, int D, float scale, unsigned flags, uint32_t test_limit, void* stream) {
-    if (!q || !k || !v || !out || !cu_q || !cu_k || B <= 0 || max_q <= 0 || total_q <= 0 || total_k <= 0 || n_q_heads <= 0 || heads <= 0) return ELUTQ_ERR_INVALID_ARG;
+    if (!q || !k || !v || !out || out == q || out == k || out == v || !cu_q || !cu_k || B <= 0 || max_q <= 0 || total_q <= 0 || total_k <= 0 || n_q_heads <= 0 || heads <= 0) return ELUTQ_ERR_INVALID_ARG;
     if ((type != ELUTQ_TYPE_F16 && type != ELUTQ_TYPE_BF16) || (flags & ~ELUTQ_ATTN_ALL_KEYS) || !(scale > 0.0f) || !(scale < 1e30f)) return ELUTQ_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return ELUTQ_ERR_UNSUPPORTED;
     if (n_q_heads % heads != 0) return ELUTQ_ERR_SHAPE;

@@ -168,3 +168,25 @@ def test_the_same_bits_every_time_in_any_batch_order():
     first = call(p, q, 1)
     for _ in range(3):
         assert np.array_equal(first, call(p, q, 1))
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+@pytest.mark.parametrize("scale", [1e3, 3e7, 1e9, 3e12, 1e28])
+def test_scores_of_any_size(fmt, scale):
+    """One key is nearest to the query by far, or two are equally near: the result is its value, or their mean, however large the scores.  Scores of fp32 are off by
+    (D + 8) 2^-23 of 1e3 at most, before the scale; the nearest is ahead by more than 10.  The weights and the result are rounded once each."""
+    rng = np.random.default_rng(fmt)
+    H, D, lens = 3, 128, [300, 700, 5000, 40]
+    k, v = data(rng, lens, H, D)
+    u = rng.choice([-1.0, 1.0], (H, D)).astype(np.float32)
+    near = [[7], [3, 600], [4000], [39]]
+    for b in range(4):
+        k[b] = k[b] * 0.01 + u * (2.0 if b % 2 else -4.0)      # (scores below zero, too)
+        k[b][near[b]] = u * (4.0 if b % 2 else -2.0)
+    p = Paged(rng, fmt, "bf16", lens, H, D, 64, k, v, factors=False)
+    q = rounded(np.tile(u, (4, 1, 1)), "bf16")
+    got = call(p, q, 1, scale=scale)
+    for b in range(4):
+        want = p.held[1][b][near[b]]
+        tol = (2 * HALF_STEP["bf16"] + 2.0 ** -16) * np.abs(want).mean(0)
+        assert (np.abs(got[b] - want.mean(0)) <= tol).all(), (b, float(np.nanmax(np.abs(got[b] - want.mean(0)))))

@@ -124,3 +124,11 @@ def test_arguments_of_a_prompt(entry, more):
         assert prefill(entry, more, **kw) == -3, kw
     assert prefill("elutq_attn_test_wait_expiry", (0,)) == -1
     assert elutq.elutq_launch_count() == before
+
+
+def test_results_in_place_of_inputs():
+    """Queries are read again after the first results are written."""
+    before = elutq.elutq_launch_count()
+    assert decode(cache(), q=128) == -1
+    assert prefill(out=64) == prefill(out=128) == prefill(out=256) == -1
+    assert elutq.elutq_launch_count() == before

@@ -160,3 +160,42 @@ def test_waits_that_run_out():
     assert elutq.elutq_device_status() == 0
     elutq.elutq_attn_prefill(q, k, v, out, cu, cu, 600)
     assert elutq.elutq_device_status() == 0 and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [1e3, 3e7, 1e9, 3e12, 1e28])
+def test_scores_of_any_size(dtype, scale):
+    """One key is nearest to all queries by far, or two are equally near: the result is its value, or their mean, however large the scores.  Scores of fp32 are off by
+    (D + 8) 2^-23 of 1e3 at most, before the scale; the nearest is ahead by more than 10.  The weights and the result are rounded once each."""
+    rng = np.random.default_rng(1)
+    H, D, lens, near = 2, 128, [200, 150], [[3], [2, 5]]
+    q, k, v = make(rng, lens, lens, H, H, D, dtype)
+    u = rng.choice([-1.0, 1.0], (H, D)).astype(np.float32)
+    q[:] = u
+    k[:200] = rounded(k[:200] * 0.01 - u * 4, dtype)           # (scores below zero)
+    k[200:] = rounded(k[200:] * 0.01 + u * 2, dtype)
+    k[3], k[202], k[205] = u * -2, u * 4, u * 4
+    got = run(q, k, v, lens, lens, dtype, scale=scale)
+    for at, n, rows in ((0, 200, near[0]), (200, 150, near[1])):
+        want = v[at : at + n][rows].astype(np.float64)
+        tol = (2 * HALF_STEP[dtype] + 2.0 ** -16) * np.abs(want).mean(0) + 2.0 ** -24
+        assert (np.abs(got[at + rows[-1] : at + n] - want.mean(0)) <= tol).all()
+
+
+@pytest.mark.parametrize("lens,max_q", [([0, 3, 40, 1, 17] * 15 + [300, 2], 400), ([2, 0, 1, 3, 0] * 300, 2 ** 30), ([1] * 33 + [600], 1024)])
+def test_many_sequences(lens, max_q):
+    """More than the 32 that are looked at together, several pairs of tiles for every CTA, longest lengths far above the true ones."""
+    rng = np.random.default_rng(len(lens))
+    q, k, v = make(rng, lens, lens, 6, 2, 64, "bf16")
+    check(run(q, k, v, lens, lens, "bf16", max_q=max_q), q, k, v, lens, lens, "bf16")
+
+
+def test_queries_beyond_the_longest_are_left_out():
+    rng = np.random.default_rng(2)
+    lens = [300, 100]
+    q, k, v = make(rng, lens, lens, 2, 1, 64, "f16")
+    got = run(q, k, v, lens, lens, "f16", max_q=101)
+    assert (got[128:300] == 77).all()
+    full = run(q, k, v, lens, lens, "f16")
+    assert np.array_equal(got[:128], full[:128]) and np.array_equal(got[300:], full[300:])
+    check(full, q, k, v, lens, lens, "f16")
