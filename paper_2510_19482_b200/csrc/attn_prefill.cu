@@ -269,7 +269,7 @@ struct Walk {
     }
     // A long search is seen by those that wait for its result.
     __device__ __forceinline__ void moves(int b0, volatile uint32_t* seen) const {
-        if ((b0 & 0x7fff) == 0 && (threadIdx.x & 31) == 0) *seen = *seen + 1;
+        if ((b0 & 0x7fff) == 0x7fe0 && (threadIdx.x & 31) == 0) *seen = *seen + 1;
     }
     // by a whole warp, as the next ones
     __device__ void begin(const PrefillArgs& a, volatile uint32_t* seen) {
