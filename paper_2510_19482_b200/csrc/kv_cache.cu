@@ -79,7 +79,7 @@ __device__ __forceinline__ void store_row(uint8_t* base, uint8_t* scales, const 
 
 // U: rows of a batch that a lane handles, their loads in flight together
 template <int D, int FMT, int TYPE, int U>
-__global__ void __launch_bounds__(128) kv_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(128, 8) kv_write_kernel(const WriteArgs a) {
     constexpr int LANES = D / 8, ROWS = 32 / LANES;        // of a row; rows of a warp at a time
     const long long w = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
     grid_dependency_wait();
@@ -344,7 +344,7 @@ int launch_write(WriteArgs& a, long long tokens, cudaStream_t stream) {
     const int rows = ROWS * (few ? 1 : kUnroll), batches = (a.heads_all + rows - 1) / rows;
     // ... for all of a token where there are tokens enough
     a.turns = few ? batches : 1;
-    while (a.turns < batches && tokens * a.turns < 64LL * device_sm_count()) ++a.turns;
+    while (a.turns < batches && tokens * a.turns < 300LL * device_sm_count()) ++a.turns;
     a.batches = (batches + a.turns - 1) / a.turns;
     a.warps = tokens * a.turns;
     return few ? launch(kv_write_kernel<D, FMT, TYPE, 1>, a.warps * 32, 128, stream, a) : launch(kv_write_kernel<D, FMT, TYPE, kUnroll>, a.warps * 32, 128, stream, a);
