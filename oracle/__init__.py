@@ -16,6 +16,8 @@ lut      the same result through the bit-serial look-up-table procedure of
 storage  bits-per-weight and model-size accounting (Tables 1 and 3 of the paper)
 fit      Algorithm 1 (alternating bit-pattern selection and least squares) that produces
          (B, s, z) from unquantised fp16 weights
+attention  rotary positions, the rows of a paged cache (16 bits, E4M3, NVFP4) and attention from
+         their definitions, with the bounds that results are held to
 layout   reference packer / unpacker for the library's device layout
          (a documented pure function; the paper fixes no device layout, so
          this part is "parity unpinned" by the paper and pinned by round trip,
