@@ -190,3 +190,24 @@ def test_scores_of_any_size(fmt, scale):
         want = p.held[1][b][near[b]]
         tol = (2 * HALF_STEP["bf16"] + 2.0 ** -16) * np.abs(want).mean(0)
         assert (np.abs(got[b] - want.mean(0)) <= tol).all(), (b, float(np.nanmax(np.abs(got[b] - want.mean(0)))))
+
+
+@pytest.mark.parametrize("fmt,D,Hq,new", [(0, 64, 8, 1), (2, 128, 32, 4), (1, 64, 16, 1)])
+@pytest.mark.parametrize("longest", [40, 1700])
+def test_more_segments_than_shares(fmt, D, Hq, new, longest):
+    """Hundreds of short sequences, some empty, one long or all short: several segments to a share, or a cluster to each."""
+    rng = np.random.default_rng(longest)
+    H = 8
+    lens = [int(x) for x in rng.integers(0, 40, 260)]
+    lens[77] = longest
+    p = Paged(rng, fmt, "f16", lens, H, D, 16, *data(rng, lens, H, D))
+    q = rounded(rng.standard_normal((260 * new, Hq, D)), "f16")
+    check(call(p, q, new), p, q, new, D ** -0.5, Hq)
+
+
+@pytest.mark.parametrize("wide", [1, 400])
+def test_all_sequences_empty(wide):
+    rng = np.random.default_rng(3)
+    p = Paged(rng, 1, "bf16", [0, 0, 0], 2, 64, 16)
+    p.table_d = ints(np.zeros((3, wide)))
+    assert (call(p, rounded(rng.standard_normal((6, 4, 64)), "bf16"), 2) == 0).all()
