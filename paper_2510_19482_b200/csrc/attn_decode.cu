@@ -64,8 +64,10 @@ __host__ __device__ constexpr int row_bytes(int format, int D) { return format =
 __host__ __device__ constexpr int tile_tokens(int format, int D) { return row_bytes(format, D) >= 128 ? 16 : 32; }
 __host__ __device__ constexpr int stage_bytes(int format, int D) { return tile_tokens(format, D) * 2 * (row_bytes(format, D) + (format == ELUTQ_KV_NVFP4 ? D / 16 : 0)); }
 __host__ __device__ constexpr int stages_of(int format, int D) { return stage_bytes(format, D) > 4608 ? 2 : 13824 / stage_bytes(format, D); }
-// CTAs that an SM holds: by shared memory, and by the registers that the results take
-__host__ __device__ constexpr int resident(int format, int D, int nt) { return nt == 2 && D == 128 ? 2 : 3; }
+// CTAs that an SM holds: by shared memory, and by the registers that the results take.  NVFP4 has its 32 tokens a turn in registers, too: 234 of them for dimension 128, 223
+// for 64 and two tiles of columns.  With three CTAs of 168 some are spilled; that is still ahead where a grid of short sequences runs in fewer rounds that way (plan_of).
+__host__ __device__ constexpr bool either(int format, int D, int nt) { return format == ELUTQ_KV_NVFP4 && (D == 128) == (nt == 1); }
+__host__ __device__ constexpr int resident(int format, int D, int nt) { return (nt == 2 && D == 128) || either(format, D, nt) ? 2 : 3; }
 
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
     const long long n = __ldg(a.lens + b);
@@ -174,8 +176,8 @@ __device__ __forceinline__ long long count_units(const DecodeArgs& a) {
 __device__ __forceinline__ long long quotient_of(long long a, int b) {
     return a >> 32 == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-template <int D, int FMT, bool BF16, int NT>
-__global__ void __launch_bounds__(kThreads, resident(FMT, D, NT)) attn_decode_kernel(const DecodeArgs a) {
+template <int D, int FMT, bool BF16, int NT, int PER>
+__global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const DecodeArgs a) {
     constexpr int TT = tile_tokens(FMT, D), SUB = TT / 16, NC = 8 * NT, S = stages_of(FMT, D), STAGE = stage_bytes(FMT, D);
     constexpr int ROW = row_bytes(FMT, D), PIECES = ROW / 16;
     constexpr int PER_WORD = FMT == ELUTQ_KV_16 ? 2 : FMT == ELUTQ_KV_E4M3 ? 4 : 8;      // values of a word
@@ -951,21 +953,29 @@ int split_of(long long segments, long long cap, int ctas) {
 
 // What a call of a shape is: columns of a tile of query rows (in eights), CTAs that are resident at once, CTAs of a cluster (0: shares of the whole), bytes of workspace
 struct Plan {
-    int nt, ctas, split;
+    int nt, per, ctas, split;
     size_t bytes;
 };
 Plan plan_of(const elutq_kv_cache* c, int pages, int B, int new_tokens, int n_q_heads) {
     Plan p;
     const int rows = n_q_heads / c->heads * new_tokens;
     p.nt = columns_of(rows);
-    p.ctas = ctas_of(resident(c->format, c->head_dim, p.nt));
+    p.per = resident(c->format, c->head_dim, p.nt);
+    p.ctas = ctas_of(p.per);
     const long long cap = (long long)pages * c->page_size;
-    p.split = split_of((long long)B * c->heads * ((rows + 8 * p.nt - 1) / (8 * p.nt)), cap < kMostTokens ? cap : kMostTokens, p.ctas);
+    const long long segments = (long long)B * c->heads * ((rows + 8 * p.nt - 1) / (8 * p.nt));
+    p.split = split_of(segments, cap < kMostTokens ? cap : kMostTokens, p.ctas);
+    // A round of three CTAs to an SM takes about 4/3 of one of two.  NVFP4, 8 key heads, dimension 128, us, two : three: 50 x 900 tokens (400 segments) 23.4 : 19.3, 64 x 1000 26.8 :
+    // 30.2, 256 x 300 46.3 : 40.8, 300 x 700 71.5 : 63.4.  Fewer CTAs, or shares: two (30 x 1000 14.0 : 17.8, 4 x 30000 36.1 : 40.2, 128 x 4000 88.0 : 90.9).
+    if (either(c->format, c->head_dim, p.nt) && p.split == 1) {
+        const long long two = device_sm_count() * 2, three = device_sm_count() * 3;
+        if (4 * ((segments + three - 1) / three) < 3 * ((segments + two - 1) / two)) p.per = 3;
+    }
     p.bytes = p.split != 0 ? 0 : (size_t)p.ctas * kWarps * (2 * (8 * p.nt) * (c->head_dim + 2) * sizeof(float) + sizeof(int4));
     return p;
 }
 
-template <int D, int FMT, bool BF16, int NT>
+template <int D, int FMT, bool BF16, int NT, int PER>
 int launch_decode(DecodeArgs a, const Plan& plan, cudaStream_t stream) {
     constexpr int kRings = kWarps * stages_of(FMT, D) * stage_bytes(FMT, D), kParts = kWarps * 8 * NT * (D + 4) * 4, kSmem = kRings > kParts ? kRings : kParts;
     // once for each device (a call would take half a microsecond of the host's time)
@@ -975,7 +985,7 @@ int launch_decode(DecodeArgs a, const Plan& plan, cudaStream_t stream) {
     if (ce != cudaSuccess) return (int)ce;
     const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
     if (!(ready.load(std::memory_order_acquire) & bit)) {
-        ce = cudaFuncSetAttribute(attn_decode_kernel<D, FMT, BF16, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        ce = cudaFuncSetAttribute(attn_decode_kernel<D, FMT, BF16, NT, PER>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (ce != cudaSuccess) return (int)ce;
         ready.fetch_or(bit, std::memory_order_release);
     }
@@ -985,10 +995,10 @@ int launch_decode(DecodeArgs a, const Plan& plan, cudaStream_t stream) {
     a.split = plan.split;
     if (a.split != 0) {
         void* args[] = {&a};
-        return launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3((unsigned)(segments * a.split)), kThreads, kSmem, args, stream, a.split);
+        return launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT, PER>, dim3((unsigned)(segments * a.split)), kThreads, kSmem, args, stream, a.split);
     }
     void* args[] = {&a};
-    const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT>, dim3(ctas), kThreads, kSmem, args, stream);
+    const int e = launch_one((const void*)attn_decode_kernel<D, FMT, BF16, NT, PER>, dim3(ctas), kThreads, kSmem, args, stream);
     if (e != 0) return e;
     // few segments have many parts each: more warps to a row
     const long long parts = ctas / segments;
@@ -996,6 +1006,14 @@ int launch_decode(DecodeArgs a, const Plan& plan, cudaStream_t stream) {
     void* join[] = {&a, &split};
     const int cols = 8 / split, wide = a.rows < 8 * NT ? a.rows : 8 * NT;
     return launch_one((const void*)attn_join_kernel<D, NT>, dim3(a.by_segment ? (unsigned)segments : ctas * kWarps, (wide + cols - 1) / cols), 256, 0, join, stream);
+}
+template <int D, int FMT, bool BF16, int NT>
+int launch_decode(const DecodeArgs& a, const Plan& plan, cudaStream_t stream) {
+    constexpr int PER = resident(FMT, D, NT);
+    if constexpr (either(FMT, D, NT)) {
+        if (plan.per == 3) return launch_decode<D, FMT, BF16, NT, 3>(a, plan, stream);
+    }
+    return launch_decode<D, FMT, BF16, NT, PER>(a, plan, stream);
 }
 template <int D, int FMT, bool BF16>
 int launch_decode(const DecodeArgs& a, const Plan& plan, cudaStream_t stream) {
