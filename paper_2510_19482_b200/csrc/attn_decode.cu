@@ -23,7 +23,7 @@
 //
 // Bound: HBM (the cache), for few tokens the latency of table, keys, joining.  Measured (32 query heads, 8 key heads, dimension 128): 16 bits, 64 sequences of 2000 to
 // 4000 tokens 128 us, 98 % of the copy rate; E4M3, 64 of 4000 to 8000 137 us, 92 %; NVFP4, 64 of 4096 to 16384 165 us, 72 %, where the instructions that turn codes into 16-bit values are
-// the bound.  One sequence of 128K tokens in NVFP4 45 us, 51 %; one of up to 1000 tokens 6.5 us.
+// the bound.  One sequence of 128K tokens in NVFP4 43 us, 54 %; one of up to 1000 tokens 6.5 us.
 #include <atomic>
 
 #include "kv.cuh"
@@ -940,9 +940,9 @@ int launch_one(const void* kernel, dim3 grid, int block, int smem, void** args, 
 
 // Short sequences: a cluster of CTAs for each segment, joined in distributed shared memory, one launch instead of two.  How long they are only the device knows; the table says how
 // long they may be.  A warp takes up to 128 tokens that way, and 256 where the clusters take more than half of the CTAs that are resident at once, so that shares of
-// the whole would not be much shorter.  Measured with 8 key heads (us, clusters : shares of the whole): 1 x 1000 NVFP4 6.5 : 8.3, 8 x 2000 NVFP4 13.5 : 15.4, 64 x 500 16 bits 28.1 :
-// 29.3, 50 x 900 NVFP4 21.1 : 26.4, 128 x 700 16 bits 60.6 : 66.1, 100 x 1000 E4M3 40.8 : 44.9; not taken: 1 x 8000 16 bits 14.9 : 12.7, 4 x 8000 NVFP4 18.5 : 17.0, and 64
-// clusters of 8, more than are resident at once, 19.5 : 13.2.
+// the whole would not be much shorter.  Measured with 8 key heads (us, clusters : shares of the whole): 1 x 1000 NVFP4 6.9 : 9.3, 8 x 2000 NVFP4 11.3 : 13.7, 16 x 2000 NVFP4 16.1 :
+// 19.2, 4 x 8000 16 bits 27.5 : 29.8, 64 x 500 16 bits 28.6 : 29.3, 128 x 700 16 bits 61 : 66, 100 x 1000 E4M3 41.0 : 44.9, at worst 64 x 1000 NVFP4 29.4 : 28.1; not
+// taken: 1 x 8000 16 bits 14.9 : 12.7, and 64 clusters of 8, more than are resident at once, 19.5 : 13.2.
 int split_of(long long segments, long long cap, int ctas) {
     if (segments > 0xffffff) return 0;
     int split = 1;
