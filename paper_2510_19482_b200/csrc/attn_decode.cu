@@ -420,8 +420,11 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                // (lane 8 t + 4 j holds column 2 t + j)
-                cs[nt][j] = a.scale * kf * __shfl_sync(0xffffffffu, up, 8 * t + 4 * j);
+                // (lane 8 t + 4 j holds column 2 t + j.  The product of the three, in an order where none leaves the range, is kept to normal numbers: a masked place is -inf times
+                // it.  Below them every score of the row vanishes, above them only the largest counts, with this factor as with the true one.)
+                const float back = __shfl_sync(0xffffffffu, up, 8 * t + 4 * j);
+                if constexpr (FMT == ELUTQ_KV_16) cs[nt][j] = a.scale;
+                else cs[nt][j] = (float)fmin(fmax((double)a.scale * kf * back, 1.17549435e-38), 3.40282347e38);
                 const int rr = rt * NC + nt * 8 + 2 * t + j;
                 limit[nt][j] = rr < a.rows ? least + rr / a.group : len;
                 off[nt][j] = kNone;

@@ -1,0 +1,47 @@
+"""Attention at the limits of its types: rows whose scores vanish, values next to the largest, a channel far above the others."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_19482_b200 as elutq
+from kv_util import HALF_STEP, TYPES, Paged, dev, ints, rounded
+from oracle import attention
+from test_attn_decode_gpu import call, check, data
+from test_attn_prefill_gpu import make, run
+
+pytestmark = pytest.mark.gpu
+
+
+def with_factors(p, kf, vf=1.0):
+    """The cache of p (made without factors), its values times these."""
+    f = [torch.full((p.heads,), float(x), device="cuda") for x in (kf, vf)]
+    p.held = [[h * float(np.float32(x)) for h in held] for held, x in zip(p.held, (kf, vf))]
+    p.cache = elutq.KvCache(p.fmt, TYPES[p.dtype], p.data[0], p.data[1], p.scales[0], p.scales[1], k_factor=f[0], v_factor=f[1])
+    return p
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 3])
+@pytest.mark.parametrize("wide", [64, 20000])
+@pytest.mark.parametrize("kf,scale", [(1e-8, None), (1.0, 1e-8), (1e-30, 1e-30), (1e-44, 1e-3)])
+def test_rows_whose_scores_vanish(fmt, dtype, new, wide, kf, scale):
+    """Queries of zeros, of the smallest magnitudes, and ordinary ones, over keys whose factor times the scale is far below what queries of such rows are brought back with: every visible
+    value counts the same, and places behind the sequence or on a missing page count nothing."""
+    rng = np.random.default_rng(fmt)
+    H, Hq, D, lens = 2, 4, 128, [17, 50, 3, 64]
+    p = with_factors(Paged(rng, fmt, dtype, lens, H, D, 16, *data(rng, lens, H, D), factors=False), kf)
+    table = np.full((4, wide // 16), -1, dtype=np.int32)
+    table[:, : p.table.shape[1]] = p.table
+    p.table_d = ints(table)
+    q = rounded(rng.standard_normal((4 * new, Hq, D)), dtype)
+    q[:, 0], q[:, 1, 1:] = 0, 0
+    q[:, 3] = rounded(q[:, 3] * 2.0 ** -130 if dtype == "bf16" else q[:, 3] * 2.0 ** -20, dtype)
+    check(call(p, q, new, scale=scale), p, q, new, D ** -0.5 if scale is None else scale, Hq)
+    p.table_d[1, 1] = -1
+    got = call(p, q, new, scale=scale)
+    keep = np.r_[0:16, 32:50]
+    p.held = [[h if b != 1 else h[keep] for b, h in enumerate(x)] for x in p.held]
+    p.lens = [17, 34, 3, 64]
+    check(got, p, q, new, D ** -0.5 if scale is None else scale, Hq)
