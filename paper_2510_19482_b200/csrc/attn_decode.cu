@@ -14,7 +14,8 @@
 //            parts of others go to the workspace and a second kernel joins them in their order.  Where all shares of a CTA are of one segment they are joined
 //            in shared memory first.
 // softmax    One running maximum for all lanes of a column, moved only when a tile rises more than 2^10 above it (then everything is scaled): P stays below
-//            2^14, in 16 bits whatever the type.  Maximum, sum and result are fp32.
+//            2^14, in fp16; in bf16, which has the range for it, below half of one over the number of tokens, so that sums of the largest values are finite.  Maximum, sum
+//            and result are fp32.
 // codes      E4M3 and E2M1 values, also times an E4M3 block scale, are exact in fp16, so both products are fp16 ones, with q brought to fp16 by a power of two for each row.
 //            The heads' factors are multiplied into the scale and into the result.
 //
@@ -37,7 +38,7 @@ constexpr int kLead = 4;
 constexpr long long kMostTokens = 0x7fff0000LL;      // of a sequence (numbers a little behind the last one are formed)
 constexpr int kShortTokens = 128;            // of a warp
 constexpr float kNone = 3e38f;               // offset of a column that has seen no token: any score rises above it
-constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
+constexpr float kRise = 14.0f, kLag = 10.0f; // 2^(x - m + 4) in fp16, m moved when that would pass 2^14
 
 struct DecodeArgs {
     KvView c;
@@ -303,6 +304,8 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
             continue;
         }
         const int* pages = a.table + b * a.ld_table;
+        // (bf16: len weights of less than half of 1 / len cannot bring the largest values beyond fp32.  It is values next to the smallest normal number that lose bits for it.)
+        const float most = FMT == ELUTQ_KV_16 && BF16 ? (float)(__clz(len) - 33) : kRise;
         const int least = len - a.fresh + 1;                  // tokens that the first of the new tokens sees
 
         // ---- copies ----------------------------------------------------------------------------------------------------------------------------
@@ -520,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
                     top[nt][j] = fmaxf(sc[0][nt][j], sc[0][nt][j + 2]);
 #pragma unroll
                     for (int u = 1; u < U; ++u) top[nt][j] = fmaxf(top[nt][j], fmaxf(sc[u][nt][j], sc[u][nt][j + 2]));
-                    rises |= __fmul_rn(top[nt][j], cs[nt][j]) + off[nt][j] > kRise;
+                    rises |= __fmul_rn(top[nt][j], cs[nt][j]) + off[nt][j] > most;
                 }
             if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
@@ -530,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
                         float x = top[nt][j];
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-                        const float to = x == -INFINITY ? off[nt][j] : fminf(off[nt][j], kBase - __fmul_rn(x, cs[nt][j]));
+                        const float to = x == -INFINITY ? off[nt][j] : fminf(off[nt][j], most - kLag - __fmul_rn(x, cs[nt][j]));
                         const float by = exp2_approx(to - off[nt][j]);
                         off[nt][j] = to;
                         sum[nt][j] *= by;

@@ -45,3 +45,26 @@ def test_rows_whose_scores_vanish(fmt, dtype, new, wide, kf, scale):
     p.held = [[h if b != 1 else h[keep] for b, h in enumerate(x)] for x in p.held]
     p.lens = [17, 34, 3, 64]
     check(got, p, q, new, D ** -0.5 if scale is None else scale, Hq)
+
+
+@pytest.mark.parametrize("new", [1, 3])
+@pytest.mark.parametrize("wide", [736, 20000])
+@pytest.mark.parametrize("size", [2e34, 1e37, 3e38, 1e-30])
+def test_values_next_to_the_largest(new, wide, size):
+    """bf16 values up to the type's largest: their means are finite, whatever the weights and however many there are, and small ones keep their bits.  In units of `size` the bound is that of
+    ordinary values; besides, n products are off by half of the smallest subnormal step, against a largest weight of 2^-(bits of n + 11) at least."""
+    rng = np.random.default_rng(1)
+    H, Hq, D, lens = 2, 6, 128, [1, 40, 700, 730]
+    k, _ = data(rng, lens, H, D)
+    v = [rng.uniform(0.3, 1.0, x.shape) * size for x in k]
+    p = Paged(rng, 0, "bf16", lens, H, D, 16, k, v)
+    table = np.full((4, wide // 16), -1, dtype=np.int32)
+    table[:, : p.table.shape[1]] = p.table
+    p.table_d = ints(table)
+    q = rounded(rng.standard_normal((4 * new, Hq, D)) * rng.choice([0.0, 0.2, 3.0], (4 * new, Hq, 1)), "bf16")
+    got = call(p, q, new) / size
+    for b, n in enumerate(lens):
+        rows = slice(b * new, (b + 1) * new)
+        out, mag, span, _ = attention.attend(q[rows], p.held[0][b], p.held[1][b] / size, D ** -0.5, n - new + 1 + np.arange(new))
+        tol = attention.tolerance(out, mag, span, np.zeros_like(span), D, n, HALF_STEP["bf16"], HALF_STEP["bf16"]) + n * 2.0 ** (n.bit_length() + 11 - 150) / size
+        assert (np.abs(got[rows] - out) <= tol).all(), (b, float((np.abs(got[rows] - out) / tol).max()))
