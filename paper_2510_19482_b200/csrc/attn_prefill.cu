@@ -201,7 +201,8 @@ __device__ __forceinline__ float2 unpack(uint32_t v) {
     return make_float2(y[0], y[1]);
 }
 
-// One row by a warp, from the first `sees` keys: a lane takes D / 32 dimensions, four keys on their way.
+// One row by a warp, from the first `sees` keys: a lane takes D / 32 dimensions, four keys on their way.  Weights are at most half of one over the number of keys, so that sums of the
+// largest values are finite.
 template <int D, bool BF16>
 __device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const uint8_t* v, long long ldk, long long ldv, int sees, float scale, uint8_t* out, volatile uint32_t* seen) {
     constexpr int W = D / 64, AT_ONCE = 4;             // words of a lane
@@ -213,6 +214,7 @@ __device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const
         x[2 * i] = t.x; x[2 * i + 1] = t.y;
         o[2 * i] = o[2 * i + 1] = 0.0f;
     }
+    const float unit = __uint_as_float((uint32_t)(94 + __clz(sees)) << 23);     // 2^-(bits of sees + 1)
     float top = -INFINITY, sum = 0.0f;
     for (int j0 = 0; j0 < sees; j0 += AT_ONCE) {
         float s[AT_ONCE];
@@ -237,7 +239,7 @@ __device__ __noinline__ void row_alone(const uint8_t* q, const uint8_t* k, const
             if (j0 + n >= sees) break;
             s[n] *= scale;
             const float m = fmaxf(top, s[n]);  // (a NaN does not move it, and reaches the sum below)
-            const float by = top == m ? 1.0f : exp2f(top - m), p = s[n] == -INFINITY ? 0.0f : exp2f(s[n] - m);
+            const float by = top == m ? 1.0f : exp2f(top - m), p = s[n] == -INFINITY ? 0.0f : exp2f(s[n] - m) * unit;
             top = m;
             sum = fmaf(sum, by, p);
 #pragma unroll

@@ -68,3 +68,22 @@ def test_values_next_to_the_largest(new, wide, size):
         out, mag, span, _ = attention.attend(q[rows], p.held[0][b], p.held[1][b] / size, D ** -0.5, n - new + 1 + np.arange(new))
         tol = attention.tolerance(out, mag, span, np.zeros_like(span), D, n, HALF_STEP["bf16"], HALF_STEP["bf16"]) + n * 2.0 ** (n.bit_length() + 11 - 150) / size
         assert (np.abs(got[rows] - out) <= tol).all(), (b, float((np.abs(got[rows] - out) / tol).max()))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [2e34, 1e37, 3e38])
+def test_values_next_to_the_largest_in_prompts(D, causal, size):
+    """The same over prompts, in units of `size`."""
+    rng = np.random.default_rng(D)
+    lens, Hq, H = [1, 40, 333], 3, 1
+    q, k, v = make(rng, lens, lens, Hq, H, D, "bf16")
+    v = rounded(rng.uniform(0.3, 1.0, v.shape) * size, "bf16")
+    got = run(q, k, v, lens, lens, "bf16", causal) / size
+    at = 0
+    for n in lens:
+        s = slice(at, at + n)
+        out, mag, span, _ = attention.attend(q[s], k[s], v[s] / size, D ** -0.5, 1 + np.arange(n) if causal else np.full(n, n))
+        tol = attention.tolerance(out, mag, span, np.zeros_like(span), D, n, HALF_STEP["bf16"], HALF_STEP["bf16"])
+        assert (np.abs(got[s] - out) <= tol).all(), (n, float((np.abs(got[s] - out) / tol).max()))
+        at += n
