@@ -538,7 +538,8 @@ int elutq_kv_read(const elutq_kv_cache* cache, const int* table, long long ld_ta
  *   lens    device int [B]: tokens of the sequence, the new ones among them; cut to what the table has room for
  * out must not overlap q.  out = softmax(scale * q K^T) V; new token i sees tokens 0 .. lens[b] - new_tokens + i.  A row that sees nothing is zeros.  What lies in pages behind that is not
  * looked at, whatever it is; tokens on a page outside the cache count as masked.  scale > 0.  Products of 16-bit values, fp32 sums; the weights of a row are rounded to
- * 16 bits (relative to 2^14 times the least that still counts) for the product with V.
+ * 16 bits (bf16 over a bf16 cache, otherwise fp16, relative to 2^14 times the least that still counts) for the product with V.  bf16 queries over E4M3 or NVFP4: a value below 2^-32 of the
+ * largest of its head is rounded to multiples of 2^-39 of that.
  * The workspace belongs to one call at a time (calls of one stream follow one another) and needs no initialisation; short tables need none (0 bytes: it may be NULL).
  * Results are the same bit for bit in every call of the same sizes.
  */

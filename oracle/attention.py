@@ -102,7 +102,7 @@ def attend(q: np.ndarray, k: np.ndarray, v: np.ndarray, scale: float, sees: np.n
 
 def tolerance(out, mag, span, big, D: int, keys: int, half_step_p: float, half_step: float, base: float = 2.0 ** -4):
     """Bound on an output's error.  Scores: fp32 sums of D exact products, each addition off by 2^-23 of the sum of magnitudes at most, a few more roundings of
-    the score itself, and a query row's values below 2^-24 of its largest may be cut off: delta = (D + 8) 2^-23 span.  A weight is then off by a factor exp(delta), in
+    the score itself: delta = (D + 8) 2^-23 span.  A weight is then off by a factor exp(delta), in
     the sum and in the numerator, and by 2^-21 in the exponential; numerators are rounded to 16 bits (half_step_p relative, or 2^-25 where fp16 runs out of exponents,
     against a sum of `1 / base` at least); the sums over keys are fp32; the result is rounded once more (half_step, or the subnormal 2^-25)."""
     delta = (D + 8) * 2.0 ** -23 * span

@@ -404,7 +404,8 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
             }
             float up = 1.0f;                                  // what brings a row's scores back
             if (FMT != ELUTQ_KV_16 && a.type == ELUTQ_TYPE_BF16) {
-                // bf16 to fp16: the row times a power of two, its largest magnitude in [1, 2).  What is less than 2^-24 of that is cut off, as it would be from the sum.
+                // bf16 to fp16: the row times a power of two, its largest magnitude in [2^15, 2^16) (65280 at most).  So values down to 2^-32 of the largest keep their bits; below, they are
+                // rounded to multiples of 2^-24, 2^-39 of it.
                 uint32_t top = 0;
 #pragma unroll
                 for (int k = 0; k < STEPS; ++k)
@@ -412,9 +413,9 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
                     for (int i = 0; i < 2; ++i) top = max(top, max(qf[nt][k][i] & 0x7fffu, qf[nt][k][i] >> 16 & 0x7fffu));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const int e = min(max((int)(top >> 7), 1), 253);           // (subnormal rows and those with infinities: as near as a normal power gets)
-                const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-                up = __uint_as_float((uint32_t)e << 23);
+                const int e = min(max((int)(top >> 7), 16), 254);          // (rows below 2^-111 and those with infinities: as near as a normal power gets)
+                const float down = __uint_as_float((uint32_t)(269 - e) << 23);
+                up = __uint_as_float((uint32_t)(e - 15) << 23);
 #pragma unroll
                 for (int k = 0; k < STEPS; ++k)
 #pragma unroll

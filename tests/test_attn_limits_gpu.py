@@ -87,3 +87,27 @@ def test_values_next_to_the_largest_in_prompts(D, causal, size):
         tol = attention.tolerance(out, mag, span, np.zeros_like(span), D, n, HALF_STEP["bf16"], HALF_STEP["bf16"])
         assert (np.abs(got[s] - out) <= tol).all(), (n, float((np.abs(got[s] - out) / tol).max()))
         at += n
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("far", [2.0 ** 16, 2.0 ** 18, 2.0 ** 22, 2.0 ** 30])
+def test_a_channel_far_above_the_others_over_keys_that_are_zero_there(fmt, far):
+    """A bf16 query's large channel meets keys that hold zeros: its other channels make up the whole score, and keep their bits down to 2^-32 of the large one."""
+    rng = np.random.default_rng(fmt)
+    H, Hq, D, lens = 2, 6, 64, [100, 33, 7]
+    k, v = data(rng, lens, H, D)
+    for x in k:
+        x[:, 0, 5], x[:, 1, 60] = 0, 0
+    q = rounded(rng.standard_normal((3, Hq, D)), "bf16")
+    q[:, :3, 5] = far
+    q[:, 3:, 60] = -far
+    p = Paged(rng, fmt, "bf16", lens, H, D, 16, k, v, factors=False)
+    got = call(p, q, 1, scale=0.5)
+    for b, n in enumerate(lens):
+        out, mag, span, big = attention.attend(q[b : b + 1], p.held[0][b], p.held[1][b], 0.5, [n])
+        # a query's largest value comes to 2^15 at least in fp16, the others to multiples of 2^-24 at the coarsest: off by 2^-25, 2^-40 of the largest.  A score is off by that times the sum of
+        # a key's magnitudes; in units of the bound's own error of a score, (D + 8) 2^-23 span, it is added to the span
+        cut = 2.0 ** -40 * far * np.abs(p.held[0][b]).sum(2).max() * 0.5
+        tol = attention.tolerance(out, mag, span + cut / ((D + 8) * 2.0 ** -23), big, D, n, HALF_STEP["f16"], HALF_STEP["bf16"])
+        err = np.abs(got[b : b + 1] - out)
+        assert (err <= tol).all(), (b, n, float((err / tol).max()), float(err.max()))
