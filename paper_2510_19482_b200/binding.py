@@ -443,7 +443,9 @@ def elutq_kv_bytes(fmt: int, n_pages: int, heads: int, page_size: int, head_dim:
 
 def elutq_rope_table(n_pos: int, rot_dim: int, theta: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
                      original: float = 8192.0, magnitude: float = 1.0, table=None, stream=None):
-    """Cosines and sines of positions, fp32 [n_pos, rot_dim] (allocated here when not given)."""
+    """Cosines and sines of positions, fp32 [n_pos, rot_dim] (allocated here when not given; give one with a stream that is not torch's current one)."""
+    if table is None and stream is not None:
+        _refuse("elutq_rope_table", "a stream of one's own needs a table of its own")
     torch, _, current, _ = _torch()
     d = current()
     if table is None:
