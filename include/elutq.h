@@ -562,7 +562,8 @@ int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, long long ldq,
 int elutq_attn_prefill(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
                        const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags, void* stream);
 
-/* Test entry for its bounded waits, as elutq_mx4_test_wait_expiry. */
+/* Test entry for its bounded waits, as elutq_mx4_test_wait_expiry.  wait_limit | ELUTQ_ATTN_TEST_LOADS: the loads are issued, and the products left out. */
+#define ELUTQ_ATTN_TEST_LOADS 0x80000000u
 int elutq_attn_test_wait_expiry(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
                                 const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags,
                                 unsigned wait_limit, void* stream);

@@ -31,6 +31,7 @@ KV_16, KV_E4M3, KV_NVFP4 = 0, 1, 2
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BANDS = 0, 1, 2
 ROPE_INTERLEAVED = 0x1
 ATTN_ALL_KEYS = 0x1
+ATTN_TEST_LOADS = 0x80000000
 
 
 class GemvCall(ctypes.Structure):

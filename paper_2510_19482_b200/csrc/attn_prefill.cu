@@ -53,7 +53,7 @@ struct PrefillArgs {
     int heads, group;                      // key heads; query heads of each
     int causal, type;
     float scale;                           // times log2(e)
-    int test;                              // 1: no load is issued
+    int test;                              // 1: no load is issued; 2: no product is
     uint32_t wait_limit;                   // polls (tests); a wait of a second runs out whatever this is
 };
 
@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 queue.next();
                 if (!some) break;
                 const int most = it.most();
-                if (lane == 0 && !a.test) {
+                if (lane == 0 && a.test != 1) {
                     auto load_q = [&](int i) {
                         if (it.t[i].tiles == 0) return true;
                         if (!wait_alone(bar(kBarQFree + i), (uint32_t)(used[i] & 1) ^ 1u, gave_up, limit)) return false;
@@ -457,8 +457,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 kv = __shfl_sync(0xffffffffu, kv, 0);
                 ok = __all_sync(0xffffffffu, ok);
             }
-            if (*gave_up && lane == 0) {
-                // what is on its way lands before the CTA leaves
+            if (lane == 0) {
+                // What is on its way lands before the CTA leaves, also where another role gives up only after this.  (Otherwise the results wait for these loads, too.)
                 for (int i = 0; i < 2; ++i)
                     if (used[i] > 0) poll(bar(kBarQ + i), (uint32_t)(used[i] - 1) & 1u, nullptr, 0xffffffffu);
                 for (int n = max(0, kv - kRing); n < kv; ++n) {
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 };
                 auto full = [&](int n) { return wait_alone(bar(kBarFull + n % kRing), (uint32_t)(n / kRing) & 1u, gave_up, limit); };
                 int used[2] = {0, 0}, done[2] = {0, 0};       // items that had the query tile, tiles of weights taken
-                bool ok = true;
+                bool ok = a.test != 2;
                 for (Queue queue; ok; queue.next()) {
                     ok = wait_alone(bar(kBarItem + queue.slot), queue.phase, gave_up, limit);
                     if (!ok) break;
@@ -795,8 +795,8 @@ int run_prefill(const void* q, long long ldq, const void* k, long long ldk, cons
     a.causal = (flags & ELUTQ_ATTN_ALL_KEYS) == 0;
     a.type = type;
     a.scale = scale * 1.44269504088896340736f;
-    a.test = test_limit != 0;
-    a.wait_limit = test_limit != 0 ? test_limit : 0xffffffffu;
+    a.test = test_limit == 0 ? 0 : test_limit & ELUTQ_ATTN_TEST_LOADS ? 2 : 1;
+    a.wait_limit = test_limit != 0 ? test_limit & ~ELUTQ_ATTN_TEST_LOADS : 0xffffffffu;
     const bool bf16 = type == ELUTQ_TYPE_BF16;
     CUtensorMap qm, km, vm;
     int ce = rows_map(&qm, q, total_q, n_q_heads, D, ldq, bf16);
@@ -853,6 +853,6 @@ extern "C" int elutq_attn_prefill(const void* q, long long ldq, const void* k, l
 extern "C" int elutq_attn_test_wait_expiry(const void* q, long long ldq, const void* k, long long ldk, const void* v, long long ldv, void* out, long long ldo, int type, const int* cu_q,
                                            const int* cu_k, int B, int max_q, int total_q, int total_k, int n_q_heads, int heads, int head_dim, float scale, unsigned flags,
                                            unsigned wait_limit, void* stream) {
-    if (wait_limit == 0) return ELUTQ_ERR_INVALID_ARG;
+    if ((wait_limit & ~ELUTQ_ATTN_TEST_LOADS) == 0) return ELUTQ_ERR_INVALID_ARG;
     return run_prefill(q, ldq, k, ldk, v, ldv, out, ldo, type, cu_q, cu_k, B, max_q, total_q, total_k, n_q_heads, heads, head_dim, scale, flags, wait_limit, stream);
 }

@@ -1,5 +1,7 @@
 """Attention at the limits of its types: rows whose scores vanish, values next to the largest, a channel far above the others."""
 
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -111,3 +113,23 @@ def test_a_channel_far_above_the_others_over_keys_that_are_zero_there(fmt, far):
         tol = attention.tolerance(out, mag, span + cut / ((D + 8) * 2.0 ** -23), big, D, n, HALF_STEP["f16"], HALF_STEP["bf16"])
         err = np.abs(got[b : b + 1] - out)
         assert (err <= tol).all(), (b, n, float((err / tol).max()), float(err.max()))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[1], [128], [100, 256], [600], [1300] * 5, [2000, 7] * 40])
+def test_waits_that_run_out_behind_the_last_load(D, lens):
+    """Loads are issued and no product is: the warp that loads may be through with all of its items before another role gives up.  It leaves when they have landed (a wait for a
+    load that is not on its way would take a second), and the next call works."""
+    rng = np.random.default_rng(1)
+    q, k, v = (dev(x, "bf16") for x in make(rng, [sum(lens)], [sum(lens)], 4, 2, D, "bf16"))
+    out, want, cu = torch.empty_like(q), torch.empty_like(q), ints(np.cumsum([0] + lens))
+    elutq.elutq_attn_prefill(q, k, v, want, cu, cu, max(lens))
+    assert elutq.elutq_device_status() == 0
+    begin = time.perf_counter()
+    for limit in (1, 40):
+        elutq.elutq_attn_test_wait_expiry(q, k, v, out, cu, cu, max(lens), limit | elutq.ATTN_TEST_LOADS)
+    assert elutq.elutq_device_status() == 0x7C05
+    assert time.perf_counter() - begin < 0.9
+    elutq.elutq_release_scratch()
+    elutq.elutq_attn_prefill(q, k, v, out, cu, cu, max(lens))
+    assert elutq.elutq_device_status() == 0 and torch.equal(out, want)
