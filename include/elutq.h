@@ -471,6 +471,8 @@ int elutq_mx4_test_wait_expiry(const void* x_codes, const void* x_scales, const 
  * struct lies in host memory and is read during the call only.
  *
  * Dense rows are [tokens][n][head_dim]: heads side by side, tokens ld elements apart, 16-byte aligned, ld a multiple of 8 (a merged q/k/v result can be passed in place).
+ * Results share no row with an input or another result, unless an entry says so: refused (ELUTQ_ERR_INVALID_ARG) wherever both have one ld; with different ones the first row of each is compared with
+ * the other's, and the rest is the caller's.
  * All other pointers are device memory; nothing is allocated, nothing is synchronised, every call can be captured into a graph.  As everywhere in this library, a call
  * with no token or no sequence is refused; a sequence of length 0 is not.
  */
@@ -508,7 +510,7 @@ int elutq_rope_table(float* table, int n_pos, int rot_dim, double theta, int sca
  * New tokens: queries and keys are rotated, keys and values go into the cache.
  *   q, q_out     [tokens][n_q_heads]; the rotated queries go to q_out (which may be q, with the same ld).  n_q_heads 0: none
  *   k, v         [tokens][heads]
- *   k_out        NULL, or [tokens][heads]: the rotated keys, in 16 bits (for elutq_attn_prefill); may be k
+ *   k_out        NULL, or [tokens][heads]: the rotated keys, in 16 bits (for elutq_attn_prefill); may be k, with the same ld
  *   slots        device int [tokens], distinct.  A slot outside the cache (-1): the token is not stored.  (Where two tokens name one slot, that row's contents are
  *                undefined.)
  *   rope         NULL: no rotation (positions, n_pos, rot_dim are not looked at).  Otherwise a table as of elutq_rope_table, n_pos rows of rot_dim

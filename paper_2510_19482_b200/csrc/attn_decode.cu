@@ -1067,6 +1067,8 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     if ((st = kv_rows_check(q, ldq, n_q_heads, D)) != ELUTQ_OK || (st = kv_rows_check(out, ldo, n_q_heads, D)) != ELUTQ_OK) return st;
     if (!mx4_aligned(table, 4) || !mx4_aligned(lens, 4) || !mx4_aligned(workspace, 16)) return ELUTQ_ERR_ALIGN;
     if (workspace_bytes < plan.bytes) return ELUTQ_ERR_BUFFER_TOO_SMALL;
+    const long long rows = (long long)B * new_tokens;
+    if (rows_meet({q, ldq, rows, n_q_heads}, {out, ldo, rows, n_q_heads}, D)) return ELUTQ_ERR_INVALID_ARG;
     DecodeArgs a;
     a.c = kv_view(cache);
     a.q = (const uint8_t*)q;

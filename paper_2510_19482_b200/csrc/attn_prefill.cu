@@ -782,6 +782,8 @@ int run_prefill(const void* q, long long ldq, const void* k, long long ldk, cons
     const long long blocks = ((long long)(max_q < total_q ? max_q : total_q) + kTile - 1) / kTile, pairs = (blocks * group + 1) / 2;
     const long long total_items = (((long long)total_q / kTile + B) * group / 2 + B) * heads;
     if (ldq > most_ld || ldk > most_ld || ldv > most_ld || total_q > 0x3fffffff || total_k > 0x3fffffff || total_items > 0x3fffffffLL || total_items < 0) return ELUTQ_ERR_SHAPE;
+    const Rows results = {out, ldo, total_q, n_q_heads};
+    if (rows_meet(results, {q, ldq, total_q, n_q_heads}, D) || rows_meet(results, {k, ldk, total_k, heads}, D) || rows_meet(results, {v, ldv, total_k, heads}, D)) return ELUTQ_ERR_INVALID_ARG;
     PrefillArgs a;
     a.cu_q = cu_q; a.cu_k = cu_k;
     a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v;

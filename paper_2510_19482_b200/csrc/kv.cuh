@@ -51,6 +51,30 @@ inline int kv_rows_check(const void* p, long long ld, int heads, int head_dim) {
     if (ld < (long long)heads * head_dim) return ELUTQ_ERR_SHAPE;
     return !mx4_aligned(p, 16) || ld % 8 != 0 ? ELUTQ_ERR_ALIGN : ELUTQ_OK;
 }
+// Some row of a meets some row of b: rows of `heads` heads of D values of 16 bits, ld apart.  Exact where rows are the same distance apart (parts of one buffer); otherwise the first row of each
+// is looked at with the other's rows.
+struct Rows {
+    const void* p;
+    long long ld, n;
+    int heads;
+};
+inline bool rows_meet(const Rows& a, const Rows& b, int D) {
+    auto down = [](long long x, long long by) { return x / by - (x % by < 0 ? 1 : 0); };
+    // [0, wa) meets [d + k L, d + k L + wb) for a k in [first, last]
+    auto meet = [&](long long wa, long long wb, long long d, long long L, long long first, long long last) {
+        const long long most = down(wa - d - 1, L), k = most < last ? most : last;       // the last one that begins in front of the end
+        return k >= first && d + k * L + wb > 0;
+    };
+    const long long wa = 2LL * a.heads * D, wb = 2LL * b.heads * D, d = (long long)reinterpret_cast<uintptr_t>(b.p) - (long long)reinterpret_cast<uintptr_t>(a.p);
+    auto bytes = [](long long ld) { return 2 * (ld < 1LL << 60 ? ld : 1LL << 60); };
+    const long long la = bytes(a.n > 1 ? a.ld : b.ld), lb = bytes(b.n > 1 ? b.ld : a.ld);
+    if (la == lb) return meet(wa, wb, d, la, 1 - a.n, b.n - 1);
+    return meet(wa, wb, d, lb, 0, b.n - 1) || meet(wb, wa, -d, la, 0, a.n - 1);
+}
+// ... other than by being the same rows
+inline bool rows_meet_apart(const Rows& a, const Rows& b, int D) {
+    return !(a.p == b.p && a.heads == b.heads && a.n == b.n && (a.ld == b.ld || a.n == 1)) && rows_meet(a, b, D);
+}
 
 // The status words of the prompts' attention, one a device (attn_prefill.cu): as mx4_status and mx4_clear_status.
 int attn_status(unsigned* word, cudaStream_t stream);

@@ -418,6 +418,10 @@ extern "C" int elutq_kv_write(const elutq_kv_cache* cache, const void* q, long l
     if (k_out != nullptr && (st = kv_rows_check(k_out, ldko, H, D)) != ELUTQ_OK) return st;
     if (!mx4_aligned(slots, 4) || !mx4_aligned(positions, 4) || !mx4_aligned(rope, 16)) return ELUTQ_ERR_ALIGN;
     if ((long long)n_q_heads + 2LL * H > (1 << 22) || (long long)tokens * (n_q_heads + 2LL * H) > (1LL << 34)) return ELUTQ_ERR_SHAPE;        // (blocks of a launch)
+    // in place or apart: a warp reads the rows of its token only just before it writes them
+    const Rows kr = {k, ldk, tokens, H}, vr = {v, ldv, tokens, H}, qr = {q, ldq, tokens, n_q_heads}, qo = {q_out, ldqo, tokens, n_q_heads}, ko = {k_out, ldko, tokens, H};
+    if (n_q_heads > 0 && (rows_meet_apart(qo, qr, D) || rows_meet(qo, kr, D) || rows_meet(qo, vr, D))) return ELUTQ_ERR_INVALID_ARG;
+    if (k_out != nullptr && (rows_meet_apart(ko, kr, D) || rows_meet(ko, vr, D) || (n_q_heads > 0 && (rows_meet(ko, qr, D) || rows_meet(ko, qo, D))))) return ELUTQ_ERR_INVALID_ARG;
     WriteArgs a;
     a.c = kv_view(cache);
     a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v;
@@ -441,6 +445,7 @@ extern "C" int elutq_kv_read(const elutq_kv_cache* cache, const int* table, long
     const int D = cache->head_dim, H = cache->heads;
     if ((st = kv_rows_check(k_out, ldk, H, D)) != ELUTQ_OK || (st = kv_rows_check(v_out, ldv, H, D)) != ELUTQ_OK) return st;
     if (!mx4_aligned(table, 4) || !mx4_aligned(first, 4) || !mx4_aligned(cu, 4)) return ELUTQ_ERR_ALIGN;
+    if (rows_meet({k_out, ldk, rows, H}, {v_out, ldv, rows, H}, D)) return ELUTQ_ERR_INVALID_ARG;
     ReadArgs a;
     a.c = kv_view(cache);
     a.table = table; a.first = first; a.cu = cu;

@@ -10,6 +10,7 @@ import paper_2510_19482_b200 as elutq
 from kv_util import HALF_STEP, TYPES, Paged, dev, ints, rounded
 from oracle import attention
 from test_attn_decode_gpu import call, check, data
+from test_attn_prefill_gpu import check as check_prefill
 from test_attn_prefill_gpu import make, run
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +134,29 @@ def test_waits_that_run_out_behind_the_last_load(D, lens):
     elutq.elutq_release_scratch()
     elutq.elutq_attn_prefill(q, k, v, out, cu, cu, max(lens))
     assert elutq.elutq_device_status() == 0 and torch.equal(out, want)
+
+
+def test_results_beside_their_inputs_in_one_buffer():
+    """Columns of the same rows: heads of q, k, v, of the rotated queries and keys, and of results, side by side."""
+    rng = np.random.default_rng(0)
+    Hq, H, D, n = 4, 2, 64, 70
+    p = Paged(rng, 0, "f16", [n], H, D, 16)
+    x = rounded(rng.standard_normal((n, Hq + 2 * H, D)), "f16")
+    wide = torch.zeros((n, 3 * Hq + 3 * H, D), dtype=torch.float16, device="cuda")
+    wide[:, : Hq + 2 * H] = dev(x, "f16")
+    q, k, v, q_out, k_out, out = torch.split(wide, [Hq, H, H, Hq, H, Hq], dim=1)
+    rope = elutq.elutq_rope_table(n, D)
+    elutq.elutq_kv_write(p.cache, k, v, ints(p.slots(0, np.arange(n))), q=q, q_out=q_out, k_out=k_out, positions=ints(np.arange(n)), rope=rope)
+    turned = rounded(attention.rotate(x[:, : Hq + H], rope.cpu().numpy(), np.arange(n), False), "f16")
+    cu = ints([0, n])
+    elutq.elutq_attn_prefill(q_out, k_out, v, out, cu, cu, n)
+    got = wide.double().cpu().numpy()
+    assert np.array_equal(got[:, : 2 * Hq + 3 * H], np.concatenate([x, turned], axis=1))
+    check_prefill(got[:, 2 * Hq + 3 * H :], turned[:, :Hq], turned[:, Hq:], x[:, Hq + H :], [n], [n], "f16")
+    # the last token over the cache, its result into columns of the queries' rows
+    elutq.elutq_attn_decode(p.cache, q_out[n - 1 :], out[n - 1 :], p.table_d, p.lens_d)
+    elutq.elutq_kv_read(p.cache, p.table_d, None, cu, wide[:, :H], wide[:, H : 2 * H])
+    p.held = [[turned[:, Hq:].astype(np.float64)], [x[:, Hq + H :].astype(np.float64)]]
+    got = wide.double().cpu().numpy()
+    check(got[n - 1 :, 2 * Hq + 3 * H :], p, turned[n - 1 :, :Hq], 1, D ** -0.5, Hq)
+    assert np.array_equal(got[:, : 2 * H], np.concatenate([turned[:, Hq:], x[:, Hq + H :]], axis=1))
