@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(128) kv_read_kernel(const ReadArgs a) {
     }
     const int begin = __ldg(a.cu + lo);
     if (row < begin || row >= __ldg(a.cu + lo + 1)) return;
-    const long long pos = (long long)(a.first == nullptr ? 0 : __ldg(a.first + lo)) + (row - begin);
+    const long long pos = (long long)(a.first == nullptr ? 0 : __ldg(a.first + lo)) + (row - (long long)begin);
     uint8_t* ko = a.k_out + 2 * (row * a.ldk + (long long)head * D);
     uint8_t* vo = a.v_out + 2 * (row * a.ldv + (long long)head * D);
     int page = -1, at = 0;
