@@ -37,7 +37,6 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kLead = 4;
 constexpr long long kMostTokens = 0x7fff0000LL;      // of a sequence (numbers a little behind the last one are formed)
 constexpr int kShortTokens = 128;            // of a warp
-constexpr float kNone = 3e38f;               // offset of a column that has seen no token: any score rises above it
 constexpr float kRise = 14.0f, kLag = 10.0f; // 2^(x - m + 4) in fp16, m moved when that would pass 2^14
 
 struct DecodeArgs {
@@ -47,7 +46,6 @@ struct DecodeArgs {
     long long ldq, ldo;        // elements between tokens
     const int *table, *lens;
     long long ld_table;
-    int wide;                  // pages of a sequence in the table
     int B, fresh, group;       // sequences, new tokens of each, query heads of a key head
     int rows, row_tiles;       // query rows of a key head; tiles of them
     int type;
@@ -97,18 +95,6 @@ __device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a
 __device__ __forceinline__ uint32_t transposed(uint32_t v) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
-    return d;
-}
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    uint32_t d;
-    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
@@ -1076,7 +1062,6 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     a.ldq = ldq; a.ldo = ldo;
     a.table = table; a.lens = lens;
     a.ld_table = ld_table;
-    a.wide = pages;
     a.B = B;
     a.fresh = new_tokens;
     a.group = n_q_heads / H;

@@ -35,7 +35,6 @@ constexpr int kItems = 2;                  // pairs of tiles that the roles know
 constexpr int kThreads = 384;
 // Registers of a thread: of the launch's 168 the two warpgroups of the softmax get more, the third less (2 x 208 + 80 is below 3 x 168).
 constexpr int kRowRegs = 208, kOtherRegs = 80;
-constexpr float kNone = 3e38f;               // offset of a row that has seen no key: any score rises above it
 constexpr float kBase = 4.0f, kRise = 14.0f; // 2^(x - m + 4), m moved when that would pass 2^14
 constexpr float kLarge = 4194304.0f;         // 2^22: scores beyond it leave less than half a bit behind the point in an offset
 constexpr unsigned long long kWaitNs = 1000000000ull;
@@ -51,7 +50,7 @@ struct PrefillArgs {
     long long ldq, ldk, ldv, ldo;          // elements between tokens
     int B, max_q, total_q, total_k;
     int heads, group;                      // key heads; query heads of each
-    int causal, type;
+    int causal;
     float scale;                           // times log2(e)
     int test;                              // 1: no load is issued; 2: no product is
     uint32_t wait_limit;                   // polls (tests); a wait of a second runs out whatever this is
@@ -77,21 +76,6 @@ constexpr int kTileBytes = kTile * D * 2;
 template <int D>
 constexpr int kSmem = (2 + kRing) * kTileBytes<D> + kStage + kNumBars * 8 + 16 + kItems * (int)sizeof(Item);
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
-__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
 // Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).  gave_up[1] counts what rows formed one by one have seen: the
 // time begins again while it moves.
 __device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile const uint32_t* gave_up, uint32_t limit) {
@@ -130,11 +114,6 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
     }
     __syncwarp();
     return false;
-}
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-    return e != 0;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -182,18 +161,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    uint32_t d;
-    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
 template <bool BF16>
 __device__ __forceinline__ float2 unpack(uint32_t v) {
     float y[2];
@@ -795,7 +762,6 @@ int run_prefill(const void* q, long long ldq, const void* k, long long ldk, cons
     a.heads = heads;
     a.group = group;
     a.causal = (flags & ELUTQ_ATTN_ALL_KEYS) == 0;
-    a.type = type;
     a.scale = scale * 1.44269504088896340736f;
     a.test = test_limit == 0 ? 0 : test_limit & ELUTQ_ATTN_TEST_LOADS ? 2 : 1;
     a.wait_limit = test_limit != 0 ? test_limit & ~ELUTQ_ATTN_TEST_LOADS : 0xffffffffu;

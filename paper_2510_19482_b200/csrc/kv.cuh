@@ -76,6 +76,23 @@ inline bool rows_meet_apart(const Rows& a, const Rows& b, int D) {
     return !(a.p == b.p && a.heads == b.heads && a.n == b.n && (a.ld == b.ld || a.n == 1)) && rows_meet(a, b, D);
 }
 
+// ---- softmax, for both kernels of attention -----------------------------------------------
+constexpr float kNone = 3e38f;               // offset of a row that has seen no key: any score rises above it
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two values in 16 bits, the first in the low half
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t d;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+
 // The status words of the prompts' attention, one a device (attn_prefill.cu): as mx4_status and mx4_clear_status.
 int attn_status(unsigned* word, cudaStream_t stream);
 int attn_clear_status();

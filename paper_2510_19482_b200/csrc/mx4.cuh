@@ -1,4 +1,4 @@
-// Microscaled 4-bit floating point: what the quantiser, the products and the 4-bit cache share.
+// Microscaled 4-bit floating point: what the quantiser, the products and the 4-bit cache share; barriers of the products and of the prompts' attention.
 //
 //   codes    uint8 [rows][K/2], two E2M1 values to a byte, the even column in the low half
 //   scales   uint8 [rows][K/B]: MXFP4 B = 32, E8M0 (2^(byte - 127), 255 = NaN); NVFP4 B = 16, E4M3 (sign bit clear, 127 = NaN)
@@ -102,6 +102,36 @@ __device__ __forceinline__ float quotient(float y, float s, float r) {
         if (over != 0.0f && q != 0.0f) q = __int_as_float((__float_as_int(q) - above) | 1);
     }
     return q;
+}
+
+// ---- barriers in shared memory ------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+// CLUSTER: what other CTAs of the cluster did in front of their arrivals is seen behind it
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    if constexpr (CLUSTER)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
 }
 
 }  // namespace elutq

@@ -92,13 +92,11 @@ struct Mx4Args {
 enum { kBarFull = 0, kBarEmpty = kBarFull + kMaxStages, kBarScalesFull = kBarEmpty + kMaxStages, kBarScalesEmpty = kBarScalesFull + kTurns, kBarAccFull = kBarScalesEmpty + kTurns, kBarAccFree = kBarAccFull + 2,
        kBarPartsFull = kBarAccFree + 2, kBarPartsFree, kBarDrain, kNumBars };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
 // On a barrier of another CTA (a shared::cluster address).  arrive_cluster orders all accesses in front of it for the cluster, which waits for those to global
 // memory too; arrive_remote only those to this CTA's shared memory, which is what a pair's scales need beside their proxy fence, and a pair's accumulators beside tcgen05's
 // (with the former 4096 x 28672 x 4096 takes 276 us instead of 220; an arrival that orders nothing beyond the CTA would save less than 1 % more).
@@ -108,25 +106,6 @@ __device__ __forceinline__ void arrive_remote(uint32_t bar) {
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
-}
-__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
-}
-template <bool CLUSTER>
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    if constexpr (CLUSTER)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
 }
 // Polls until the phase is over (true), something in the CTA has given up, or the time or the polls are (false).  A poll may be suspended by
 // the hardware for some tens of microseconds, so the time is what counts.
@@ -177,11 +156,6 @@ __device__ __forceinline__ bool epilogue_agrees(bool ok) {
     return all != 0;
 }
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-    return e != 0;
-}
 template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
     if constexpr (CG == 2)
