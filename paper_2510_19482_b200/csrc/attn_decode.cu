@@ -26,6 +26,7 @@
 // 4000 tokens 128 us, 98 % of the copy rate; E4M3, 64 of 4000 to 8000 137 us, 92 %; NVFP4, 64 of 4096 to 16384 165 us, 72 %, where the instructions that turn codes into 16-bit values are
 // the bound.  One sequence of 128K tokens in NVFP4 43 us, 54 %; one of up to 1000 tokens 6.5 us.
 #include <atomic>
+#include <cmath>
 
 #include "kv.cuh"
 
@@ -50,6 +51,8 @@ struct DecodeArgs {
     int rows, row_tiles;       // query rows of a key head; tiles of them
     int type;
     float scale;               // times log2(e)
+    float part;                // the same as part * 2^power, part in [0.5, 1)
+    int power;
     float* parts;
     int4* begun;               // segments that begin in a share and go on in the next ones: sequence, key head and tile of rows, worker, where its parts are (0: none).  For each
                                // segment, or, where there are more of them than shares, for each share
@@ -115,6 +118,7 @@ __device__ __forceinline__ void e2m1_pairs(uint32_t (&h)[4], uint32_t w) {
     asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }       // -126 <= e <= 127
 // 16 bytes to shared memory
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(dst), "l"(src) : "memory");
@@ -388,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
                         qf[nt][step + 1][0] = v.z; qf[nt][step + 1][1] = v.w;
                     }
             }
-            float up = 1.0f;                                  // what brings a row's scores back
+            int back = 0;                                     // the power of two that brings a row's scores back
             if (FMT != ELUTQ_KV_16 && a.type == ELUTQ_TYPE_BF16) {
                 // bf16 to fp16: the row times a power of two, its largest magnitude in [2^15, 2^16) (65280 at most).  So values down to 2^-32 of the largest keep their bits; below, they are
                 // rounded to multiples of 2^-24, 2^-39 of it.
@@ -400,8 +404,8 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 const int e = min(max((int)(top >> 7), 16), 254);          // (rows below 2^-111 and those with infinities: as near as a normal power gets)
-                const float down = __uint_as_float((uint32_t)(269 - e) << 23);
-                up = __uint_as_float((uint32_t)(e - 15) << 23);
+                const float down = power_of_two(142 - e);
+                back = e - 142;
 #pragma unroll
                 for (int k = 0; k < STEPS; ++k)
 #pragma unroll
@@ -410,11 +414,12 @@ __global__ void __launch_bounds__(kThreads, PER) attn_decode_kernel(const Decode
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                // (lane 8 t + 4 j holds column 2 t + j.  The product of the three, in an order where none leaves the range, is kept to normal numbers: a masked place is -inf times
-                // it.  Below them every score of the row vanishes, above them only the largest counts, with this factor as with the true one.)
-                const float back = __shfl_sync(0xffffffffu, up, 8 * t + 4 * j);
+                // (lane 8 t + 4 j holds column 2 t + j)
+                [[maybe_unused]] const int power = max(a.power + __shfl_sync(0xffffffffu, back, 8 * t + 4 * j), -252), half = power >> 1;
+                // Scale, factor and power of two, in an order that leaves the range only where their product does, and kept to normal numbers, as a masked place is -inf times it.
+                // (Below them every score of the row vanishes, above them only the largest counts, with this product as with the true one.)
                 if constexpr (FMT == ELUTQ_KV_16) cs[nt][j] = a.scale;
-                else cs[nt][j] = (float)fmin(fmax((double)a.scale * kf * back, 1.17549435e-38), 3.40282347e38);
+                else cs[nt][j] = fminf(fmaxf(a.part * kf * power_of_two(half) * power_of_two(power - half), 1.17549435e-38f), 3.40282347e38f);
                 const int rr = rt * NC + nt * 8 + 2 * t + j;
                 limit[nt][j] = rr < a.rows ? least + rr / a.group : len;
                 off[nt][j] = kNone;
@@ -1070,6 +1075,7 @@ extern "C" int elutq_attn_decode(const elutq_kv_cache* cache, const void* q, lon
     a.row_tiles = (a.rows + nc - 1) / nc;
     a.type = cache->type;
     a.scale = scale * 1.44269504088896340736f;
+    a.part = frexpf(a.scale, &a.power);
     a.begun = (int4*)workspace;
     a.parts = (float*)(a.begun + plan.ctas * kWarps);
     a.cap = (long long)pages * cache->page_size;
