@@ -16,15 +16,17 @@
 // softmax    One running maximum for all lanes of a column, moved only when a tile rises more than 2^10 above it (then everything is scaled): P stays below
 //            2^14, in fp16; in bf16, which has the range for it, below half of one over the number of tokens, so that sums of the largest values are finite.  Maximum, sum
 //            and result are fp32.
+//            (P goes to 16 bits because the tensor core takes it so: a weight is off by 2^-12 of itself in fp16, 2^-9 in bf16, next to a result of 16 bits.  The sum takes the weights as
+//            they were.  Against the definition in 64 bits results are off 1.0 to 1.4 times as far as with weights of fp32, most where one weight outdoes all others.)
 // codes      E4M3 and E2M1 values, also times an E4M3 block scale, are exact in fp16, so both products are fp16 ones, with q brought to fp16 by a power of two for each row.
 //            The heads' factors are multiplied into the scale and into the result.
 //
 // Masked places never reach the result, whatever they hold: scores are selected, V rows behind the sequence are zeros, and in the last tiles, where
 // the new tokens of a sequence see different lengths, every token's product is formed by itself.
 //
-// Bound: HBM (the cache), for few tokens the latency of table, keys, joining.  Measured (32 query heads, 8 key heads, dimension 128): 16 bits, 64 sequences of 2000 to
-// 4000 tokens 128 us, 98 % of the copy rate; E4M3, 64 of 4000 to 8000 137 us, 92 %; NVFP4, 64 of 4096 to 16384 165 us, 72 %, where the instructions that turn codes into 16-bit values are
-// the bound.  One sequence of 128K tokens in NVFP4 43 us, 54 %; one of up to 1000 tokens 6.5 us.
+// Bound: HBM (the cache), for few tokens the latency of table, keys, joining.  Measured (32 query heads, 8 key heads, dimension 128, us in a graph): 16 bits, 64 sequences of 2048 to
+// 4096 tokens 128, 98 % of the copy rate; E4M3, 64 of 4096 to 8192 138, 91 %; NVFP4, 64 of 4096 to 16384 166, 72 %: two warps to a scheduler, each a chain of scores, softmax
+// and products, no unit full (issue 54 %, of its stalls two thirds the wait for the instruction in front).  One sequence of 128K tokens in NVFP4 42, 55 %; one of 1000 in 16 bits 6.5.
 #include <atomic>
 #include <cmath>
 
@@ -964,7 +966,9 @@ Plan plan_of(const elutq_kv_cache* c, int pages, int B, int new_tokens, int n_q_
     const long long segments = (long long)B * c->heads * ((rows + 8 * p.nt - 1) / (8 * p.nt));
     p.split = split_of(segments, cap < kMostTokens ? cap : kMostTokens, p.ctas);
     // A round of three CTAs to an SM takes about 4/3 of one of two.  NVFP4, 8 key heads, dimension 128, us, two : three: 50 x 900 tokens (400 segments) 23.4 : 19.3, 64 x 1000 26.8 :
-    // 30.2, 256 x 300 46.3 : 40.8, 300 x 700 71.5 : 63.4.  Fewer CTAs, or shares: two (30 x 1000 14.0 : 17.8, 4 x 30000 36.1 : 40.2, 128 x 4000 88.0 : 90.9).
+    // 30.2, 256 x 300 46.3 : 40.8, 300 x 700 71.5 : 63.4.  Fewer CTAs, or shares: two (30 x 1000 14.0 : 17.8, 4 x 30000 36.1 : 40.2, 128 x 4000 88.0 : 90.9).  Dimension 64 with 12 query
+    // rows to a key head: 50 x 900 25.8 : 17.5, 64 x 1000 29.6 : 31.4, 256 x 300 58.5 : 48.3, 300 x 700 98.8 : 78.0, 30 x 1000 14.1 : 16.9; at worst, where the two are
+    // even by this count, 120 x 500 38.3 : 33.0 (two).
     if (either(c->format, c->head_dim, p.nt) && p.split == 1) {
         const long long two = device_sm_count() * 2, three = device_sm_count() * 3;
         if (4 * ((segments + three - 1) / three) < 3 * ((segments + two - 1) / two)) p.per = 3;
