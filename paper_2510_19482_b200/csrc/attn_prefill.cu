@@ -357,6 +357,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
         return it;
     };
 
+    // of the warp that loads: tiles of keys and values; items that had the query tile; a bit for each slot: its last load was announced to the tail's warp, the parity of such uses
+    int kv = 0, loaded[2] = {0, 0};
+    uint32_t tails = 0, tail_parity = 0;
     if (warp >= kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
         if (warp == kLoadWarp) {
@@ -364,8 +367,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
             Queue queue;
             Walk walk;
             walk.begin(a, gave_up + 1);
-            int kv = 0, used[2] = {0, 0};                     // tiles of keys and values; items that had the query tile
-            uint32_t tails = 0, parity = 0;                   // a bit for each slot: its last load was announced to the tail's warp; the parity of such uses
             bool ok = true;
             for (int round = 0; ok; ++round) {
                 const int n = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
@@ -407,8 +408,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                 if (lane == 0 && a.test != 1) {
                     auto load_q = [&](int i) {
                         if (it.t[i].tiles == 0) return true;
-                        if (!wait_alone(bar(kBarQFree + i), (uint32_t)(used[i] & 1) ^ 1u, gave_up, limit)) return false;
-                        ++used[i];
+                        if (!wait_alone(bar(kBarQFree + i), (uint32_t)(loaded[i] & 1) ^ 1u, gave_up, limit)) return false;
+                        ++loaded[i];
                         expect(bar(kBarQ + i), BYTES);
                         for (int s = 0; s < HALVES; ++s) tma_load(smem0 + i * BYTES + s * (kTile * 128), &qm, 64 * s, it.t[i].head, it.q0 + it.t[i].row0, bar(kBarQ + i));
                         return true;
@@ -423,24 +424,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
                         expect(bar(to), BYTES);
                         for (int s = 0; s < HALVES; ++s) tma_load(smem0 + (2 + slot) * BYTES + s * (kTile * 128), m & 1 ? &vm : &km, 64 * s, it.h, it.k0 + (m >> 1) * kTile, bar(to));
                         tails = tail ? tails | 1u << slot : tails & ~(1u << slot);
-                        parity ^= (uint32_t)tail << slot;
+                        tail_parity ^= (uint32_t)tail << slot;
                         ++kv;
                     }
                 }
                 kv = __shfl_sync(0xffffffffu, kv, 0);
                 ok = __all_sync(0xffffffffu, ok);
             }
-            if (lane == 0) {
-                // What is on its way lands before the CTA leaves, also where another role gives up only after this.  (Otherwise the results wait for these loads, too.)
-                for (int i = 0; i < 2; ++i)
-                    if (used[i] > 0) poll(bar(kBarQ + i), (uint32_t)(used[i] - 1) & 1u, nullptr, 0xffffffffu);
-                for (int n = max(0, kv - kRing); n < kv; ++n) {
-                    const int slot = n % kRing;
-                    if (tails >> slot & 1u) poll(bar(kBarTail + slot), (parity >> slot & 1u) ^ 1u, nullptr, 0xffffffffu);
-                    else poll(bar(kBarFull + slot), (uint32_t)(n / kRing) & 1u, nullptr, 0xffffffffu);
-                }
-            }
-            __syncwarp();
         } else if (warp == kTailWarp) {
             // ---- V rows behind a sequence: zeros.  Such a tile is announced to this warp, which then announces it to the MMAs --------------------------------------
             uint32_t parity = 0;                              // a bit for each slot
@@ -691,6 +681,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_prefill_kernel(const __grid_
     }
     fence_before();
     __syncthreads();
+    if (warp == kLoadWarp && lane == 0 && *gave_up) {
+        // what is on its way lands before the CTA leaves (here, as another role may give up when the loads are all issued)
+        for (int i = 0; i < 2; ++i)
+            if (loaded[i] > 0) poll(bar(kBarQ + i), (uint32_t)(loaded[i] - 1) & 1u, nullptr, 0xffffffffu);
+        for (int n = max(0, kv - kRing); n < kv; ++n) {
+            const int slot = n % kRing;
+            if (tails >> slot & 1u) poll(bar(kBarTail + slot), (tail_parity >> slot & 1u) ^ 1u, nullptr, 0xffffffffu);
+            else poll(bar(kBarFull + slot), (uint32_t)(n / kRing) & 1u, nullptr, 0xffffffffu);
+        }
+    }
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "n"(512) : "memory");
 }
 
