@@ -19,9 +19,9 @@
 //            times a V that is not finite would still be NaN, for a row in front of such a token in the same tile: rows whose result is not finite are formed again,
 //            one by one, from what they see.  So are rows whose scores pass 2^22.  Other inputs never come there.
 //
-// Bound: a tile's softmax and its hand-overs, and the power limit in long runs.  8192 tokens of 32 heads over 8 of 128 in bf16 450 us in a graph, 1.16 of the operations at the sustained
-// rate; all keys seen 973, 1.26.  Few and even items run in rounds: 1024 and 867 tokens over 3500 more are 240 items of 29 to 36 tiles for 148 SMs, so the busiest has 63 tiles and
-// the mean is 52 (125 us, 1.44; 1.19 of what the busiest SM's tiles come to).
+// Bound: a tile's softmax and its hand-overs, and the power limit in long runs.  8192 tokens of 32 heads over 8 of 128 in bf16 432 to 450 us in a graph, 1.12 to 1.16 of the operations at the
+// sustained rate; all keys seen 973, 1.26.  Few and even items run in rounds: 1024 and 867 tokens over 3500 more are 240 items of 29 to 36 tiles for 148 SMs, so the busiest has 63 tiles and
+// the mean is 52 (121 us, 1.39; 1.16 of what the busiest SM's tiles come to).
 //
 // Every wait is bounded: the thread whose wait runs out raises the device's status word, and all roles leave their loops.
 #include <atomic>
